@@ -556,6 +556,80 @@ int attn_prefill_with_prefix(hkv_pool *pool, const void *q, const int32_t *cu_q,
 size_t attn_prefill_workspace_bytes(int32_t total_q, int32_t num_q_heads);
 
 /* ------------------------------------------------------------------------------------------
+ * From a step's projections to its attention in one pass: the rows of q and k are normed per head and rotated by position, the
+ * queries go to q_out (the attention calls' q), keys and values into the pool, for all requests of a plan at once.  With
+ * x = 128 values of one head and token, in fp32:
+ *   y = x * w / sqrt(mean(x^2) + eps)  where the norm's weight w is given, else y = x;
+ *   pair i < rotary_dim / 2 is the dims (i, i + rotary_dim / 2), or (2i, 2i + 1) if interleaved; it turns by
+ *   angle = position on axis[i] * inv_freq[i] (taken in fp64, so far positions are as exact as near ones):
+ *   (a, b) -> (a cos - b sin, b cos + a sin); dims from rotary_dim on stay as they are.
+ * One rounding at the end: bf16 rows (bf16 and fp8 pools) or fp32 rows (fp32 pools); the codes and scales of an fp8 pool are taken
+ * from the unrounded keys, by the rules of kv_pool_write (a block that a request continues keeps its running scale).  Values
+ * are stored as kv_pool_write stores them.  Rows, positions and q_out are indexed by the plan's rows of q (q_rows and
+ * q_row_begin of the plan's creation apply); rows the plan does not name are neither read nor written.
+ * A row that holds a NaN or infinity gives NaN where the formula does, in that row and head only (an fp8 block whose scale it enters: in that block).
+ */
+typedef struct {
+    const void *q, *k, *v;        /* device, 16-byte aligned: row i begins at element i * stride; [num_q_heads][128], [num_kv_heads][128] elements a row */
+    int64_t q_stride, k_stride, v_stride; /* elements from row to row, whole 16-byte pieces; 0: rows without gaps */
+    void *q_out;                  /* device, 16-byte aligned, [rows][num_q_heads][128]; may be q itself where that has no gaps, else apart from q, k and v */
+    const void *q_norm, *k_norm;  /* device, 16-byte aligned, [128] of the rows' type; NULL: no norm */
+    float eps;
+    int32_t rotary_dim;           /* 0 (no rotation), 16, 32, ... 128 (else ESHAPE) */
+    int32_t interleaved;
+    const double *inv_freq;       /* device, [rotary_dim / 2]: radians per position */
+    const int32_t *positions;     /* device, [n_axes][rows], may be negative; NULL: a token's place on its request's path, 0 for the first (one axis) */
+    int64_t position_stride;      /* elements from axis to axis */
+    int32_t n_axes;               /* 1 to 4; 0 = 1.  Images and video have a place in time, height and width */
+    const int32_t *axis;          /* host, [rotary_dim / 2]: the axis each pair turns by; NULL: axis 0 */
+} hkv_qkv;
+
+/* The new tokens of a prefill plan, all requests in one launch (per 128 of them): replaces kv_pool_write and what comes in front of it.
+ * EINVAL: null / unaligned pointers, bad strides, eps, axes; a host-only plan; new tokens of two requests in the same 16-token block.
+ * Nothing is queued on error. */
+int hkv_prefill_plan_store(hkv_prefill_plan *plan, const hkv_qkv *rows, void *stream);
+/* The newest tokens_per_req tokens of every request of a decode plan (they end its last node; a growing plan: as appended so far):
+ * one token each in a generation step, a drafted run or tree in a verification step (whose positions the caller gives: a tree's tokens are
+ * not at their places in the node).  Errors as above, and as kv_pool_append: EINVAL for a page of more than one owner, and for a
+ * last node without a token. */
+int hkv_decode_plan_store(hkv_decode_plan *plan, const hkv_qkv *rows, void *stream);
+/* Growing plans: hkv_decode_plan_append and the store of the tokens it adds, row r for request r (q_rows: row q_rows[r]); for up to 256
+ * requests one launch.  Errors of both; nothing changes on error. */
+int hkv_decode_plan_append_qkv(hkv_decode_plan *plan, const int32_t *new_page_ids, const hkv_qkv *rows, void *stream);
+
+/* ------------------------------------------------------------------------------------------
+ * Weights of cached keys: what the queries of a step gave to each key, added up over rows and the query heads of its KV head, kept per
+ * slot of the pool (key_weights: device float [blocks][num_kv_heads][16], caller-owned, blocks = num_pages * page_size / 16):
+ *   key_weights[t] = decay * key_weights[t] + sum over rows r that see t of exp(scale * q_r . k_t - lse_r).
+ * Every tree node's keys are read once for all requests below it; the order of the sum is fixed (the same call gives the same
+ * bits).  A row whose lse is not a finite number adds nothing.  Keys that no request of the plan sees, and slots behind a
+ * node's last token, keep what they hold.
+ *
+ * hkv_decode_plan_track_weights: to be called once on a plan before the first attn_decode_plan_weights (it uploads the work list, blocking;
+ * a growing plan may have grown).  bf16 and fp8 pools (ESHAPE for fp32 pools).  EINVAL if a 16-token block is in the forest twice. */
+int hkv_decode_plan_track_weights(hkv_decode_plan *plan);
+/* q, lse: as attn_decode_plan_run took and gave them for this plan (lse is needed here).  decay: 0 to 1; 1 adds up, 0 replaces
+ * (key_weights is then not read).  n_new (0 .. tokens_per_req): the last n_new tokens of every request's last node are new and start
+ * from 0 (their slots may hold anything).  Calls on one key_weights must not overlap.
+ * EINVAL: null / unaligned pointers, decay or n_new out of range, no track_weights, a host-only plan. */
+int attn_decode_plan_weights(hkv_decode_plan *plan, const void *q, float scale, const float *lse, float decay, int32_t n_new, float *key_weights,
+                             void *stream);
+
+/* Eviction: of sequence i's n_tokens[i] tokens, n_keep[i] are kept per KV head (each head its own: a block's heads are apart in the
+ * pool, and attention does not ask for its keys' order): the first n_first, the newest n_recent, and of the others those
+ * with the greatest key_weights (equal ones: the earlier; NaN counts less than every number).  They move in order to new pages, slot j of
+ * the new sequence holding kept token j, with their key_weights; fp8 blocks get the scale of what they then hold and codes
+ * rounded anew.  The old pages stay as they are (shared prefixes among them may go on being used by others); slots behind the last kept
+ * token of a new block keep what they hold.
+ *   src_pages: host, ceil(n_tokens[i] / page size) ids of each sequence, one sequence after the other; dst_pages: host, ceil(n_keep[i] / page size)
+ *   ids each, all different, of one owner at most, and none of src_pages (EINVAL).  n_tokens, n_keep: host [n_seq].
+ *   key_weights: as above, read and written.  kept: device int32 [num_kv_heads][sum of n_keep], out: the old index of every kept token.
+ * EINVAL: n_keep[i] > n_tokens[i], or less than min(n_tokens[i], n_first + n_recent); a sequence of more than about a million tokens.
+ * ERANGE: page ids.  Nothing is queued on error.  Not for capture into a graph: the page lists pass through the pool's staging ring. */
+int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_pages, const int32_t *n_tokens, const int32_t *dst_pages, const int32_t *n_keep,
+                  int32_t n_first, int32_t n_recent, float *key_weights, int32_t *kept, void *stream);
+
+/* ------------------------------------------------------------------------------------------
  * Block-level prefix cache over a pool (host bookkeeping only; Section 6, "LLM Engine
  * Integration": prefixes are kept block by block, precomputed ones are pinned, blocks are evicted
  * least recently used first and a prefix never before its extensions, an evicted prefix is

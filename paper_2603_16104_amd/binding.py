@@ -36,6 +36,7 @@ EXPORTS = [
     "attn_decode_prefix_tree", "attn_decode_workspace_bytes", "hkv_prefill_plan_create", "hkv_prefill_plan_destroy",
     "hkv_prefill_plan_num_tiles", "hkv_prefill_plan_num_pieces", "hkv_prefill_plan_tiles", "hkv_prefill_plan_num_segments", "hkv_prefill_plan_segments", "attn_prefill_plan_run", "attn_prefill_plan_run_ws", "hkv_prefill_plan_workspace_bytes", "attn_prefill_with_prefix",
     "attn_prefill_workspace_bytes",
+    "hkv_prefill_plan_store", "hkv_decode_plan_store", "hkv_decode_plan_append_qkv", "hkv_decode_plan_track_weights", "attn_decode_plan_weights", "kv_pool_evict",
     "kv_cache_create", "kv_cache_destroy", "kv_cache_acquire", "kv_cache_release", "kv_cache_unpin", "kv_cache_stats",
     "trt_build", "trt_destroy", "trt_num_nodes", "trt_num_syms", "trt_num_calls", "trt_nodes", "trt_prefill_usage",
     "trt_evaluate", "trt_schedule", "trt_partition", "trt_nested", "trt_run_soft",
@@ -77,6 +78,11 @@ def lib():
         L.attn_decode_plan_run.argtypes = [p, p, f, p, p, p, n, p]
         L.attn_decode_plan_run_static.argtypes = [p, p, f, p, p, p]
         L.attn_prefill_plan_run_ws.argtypes = [p, p, f, p, p, p, n, p]
+        L.hkv_prefill_plan_store.argtypes = [p, p, p]
+        L.hkv_decode_plan_store.argtypes = [p, p, p]
+        L.hkv_decode_plan_append_qkv.argtypes = [p, p, p, p]
+        L.attn_decode_plan_weights.argtypes = [p, p, f, p, f, i, p, p]
+        L.kv_pool_evict.argtypes = [p, i, p, p, p, p, i, i, p, p, p]
         _lib = L
     return _lib
 
@@ -551,6 +557,89 @@ def attn_prefill_with_prefix(pool, q, cu_q, block_table, kv_len, num_q_heads: in
 
 def attn_prefill_workspace_bytes(total_q: int, num_q_heads: int) -> int:
     return int(lib().attn_prefill_workspace_bytes(C.c_int32(total_q), C.c_int32(num_q_heads)))
+
+
+# ----------------------------------------------------------------------------------------- around a step's attention
+class Qkv(C.Structure):
+    """hkv_qkv: the rows of a step's projections and what is done with them (build it with qkv_rows)."""
+    _fields_ = [("q", C.c_void_p), ("k", C.c_void_p), ("v", C.c_void_p), ("q_stride", C.c_int64), ("k_stride", C.c_int64), ("v_stride", C.c_int64),
+                ("q_out", C.c_void_p), ("q_norm", C.c_void_p), ("k_norm", C.c_void_p), ("eps", C.c_float), ("rotary_dim", C.c_int32),
+                ("interleaved", C.c_int32), ("inv_freq", C.c_void_p), ("positions", C.c_void_p), ("position_stride", C.c_int64), ("n_axes", C.c_int32),
+                ("axis", C.c_void_p)]
+
+
+def _row_stride(t) -> int:
+    """Elements from row to row of a [rows][heads][128] tensor whose rows are whole (raw addresses: no gaps)."""
+    if t is None or isinstance(t, int):
+        return 0
+    if t.dim() != 3 or (t.shape[0] > 1 and t.stride(0) < t.shape[1] * HEAD_DIM) or t.shape[2] != HEAD_DIM or (t.shape[0] and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != HEAD_DIM))):
+        raise ValueError("q, k and v are [rows][heads][128], the heads of a row one after the other")
+    return t.stride(0) if t.shape[0] > 1 else 0
+
+
+def qkv_rows(q, k, v, q_out, q_norm=None, k_norm=None, eps: float = 1e-6, rotary_dim: int = 0, inv_freq=None, interleaved: bool = False,
+             positions=None, axis=None, n_axes: Optional[int] = None) -> Qkv:
+    """The argument of the store calls.  q, k, v: [rows][heads][128] tensors, which may be parts of one tensor's rows; q_out: [rows][heads][128]
+    without gaps; inv_freq: float64 [rotary_dim / 2]; positions: int32 [rows], or [axes][rows] with `axis`, the axis of every pair.  May be kept
+    for as many calls as the buffers are used for; it holds no reference to them, but to `axis`."""
+    if q_out is not None and not isinstance(q_out, int) and not q_out.is_contiguous():
+        raise ValueError("q_out must be contiguous")
+    if inv_freq is not None and not isinstance(inv_freq, int) and (inv_freq.element_size() != 8 or inv_freq.numel() * 2 < rotary_dim or not inv_freq.is_contiguous()):
+        raise ValueError("inv_freq: float64 [rotary_dim / 2]")
+    stride, axes = 0, 1
+    if positions is not None and not isinstance(positions, int):
+        if positions.element_size() != 4 or positions.is_floating_point() or positions.stride(-1) != 1:
+            raise ValueError("positions: int32, the rows of an axis one after the other")
+        if positions.dim() > 1:
+            axes, stride = positions.shape[0], positions.stride(0)
+    x = Qkv(_addr(q), _addr(k), _addr(v), _row_stride(q), _row_stride(k), _row_stride(v), _addr(q_out), _addr(q_norm), _addr(k_norm), eps, rotary_dim,
+            int(interleaved), _addr(inv_freq), _addr(positions), stride, axes if n_axes is None else n_axes, None)
+    if axis is not None:
+        x._axis = _host_i32(axis)
+        if len(x._axis) * 2 < rotary_dim:
+            raise ValueError("axis: one for every pair of the rotated dimensions")
+        x.axis = x._axis.ctypes.data
+    return x
+
+
+def hkv_prefill_plan_store(plan, rows: Qkv, stream=None) -> None:
+    """Norms, rotation and store of a prefill plan's new tokens; queries to rows.q_out."""
+    _run(lib().hkv_prefill_plan_store, plan, None if rows is None else C.addressof(rows), _stream_addr(stream))
+
+
+def hkv_decode_plan_store(plan, rows: Qkv, stream=None) -> None:
+    """The same for the newest token(s) of a decode plan's requests."""
+    _run(lib().hkv_decode_plan_store, plan, None if rows is None else C.addressof(rows), _stream_addr(stream))
+
+
+def hkv_decode_plan_append_qkv(plan, new_page_ids, rows: Qkv, stream=None) -> None:
+    """hkv_decode_plan_append and the store of the tokens it adds."""
+    ids = None if new_page_ids is None else _host_i32(new_page_ids)
+    _run(lib().hkv_decode_plan_append_qkv, plan, _host_addr(ids), None if rows is None else C.addressof(rows), _stream_addr(stream))
+
+
+def hkv_decode_plan_track_weights(plan) -> None:
+    _check(lib().hkv_decode_plan_track_weights(plan))
+
+
+def attn_decode_plan_weights(plan, q, scale: float, lse, decay: float, n_new: int, key_weights, stream=None) -> None:
+    """key_weights [blocks][kv heads][16] = decay * key_weights + what the step's queries gave to each key (lse: the run's)."""
+    _run(lib().attn_decode_plan_weights, plan, _addr(q), scale, _addr(lse), decay, n_new, _addr(key_weights), _stream_addr(stream))
+
+
+def kv_pool_evict(pool, src_pages, n_tokens, dst_pages, n_keep, n_first: int, n_recent: int, key_weights, kept, stream=None) -> None:
+    """Keeps the heaviest n_keep[i] of sequence i's n_tokens[i] tokens per KV head, moved to dst_pages; src_pages and dst_pages: the
+    sequences' page ids one after the other; kept: int32 [kv heads][sum of n_keep], receives the old index of every kept token."""
+    src, dst, n, m = _host_i32(src_pages), _host_i32(dst_pages), _host_i32(n_tokens), _host_i32(n_keep)
+    if len(n) != len(m):
+        raise HkvError(EINVAL, "kv_pool_evict: n_tokens and n_keep differ in length")
+    page = kv_pool_page_size(pool)
+    for ids, count, name in ((src, n, "src_pages"), (dst, m, "dst_pages")):
+        need = int(((np.maximum(count, 0).astype(np.int64) + page - 1) // page).sum())
+        if len(ids) < need:
+            raise HkvError(EINVAL, f"kv_pool_evict: {need} page ids needed in {name}, {len(ids)} given")
+    _run(lib().kv_pool_evict, pool, len(n), _host_addr(src), _host_addr(n), _host_addr(dst), _host_addr(m), n_first, n_recent, _addr(key_weights),
+         _addr(kept), _stream_addr(stream) if len(n) > 0 else None)
 
 
 # ---------------------------------------------------------------------------------------------

@@ -1,7 +1,6 @@
 // Host side of the heliumkv C ABI: pool bookkeeping, forest validation and flattening, work
 // planning, argument checks, kernel launches.  All arithmetic on K/V/Q lives in the kernels.
-#include "../../include/heliumkv.h"
-#include "hkv_internal.h"
+#include "hkv_objects.h"
 
 #include <algorithm>
 #include <cmath>
@@ -9,15 +8,11 @@
 #include <cstdio>
 #include <cstdlib>
 #include <cstring>
-#include <deque>
 #include <functional>
 #include <new>
 #include <numeric>
 #include <string>
 #include <unordered_map>
-#include <vector>
-
-using namespace hkv;
 
 // ---------------------------------------------------------------------------------------------
 // errors
@@ -40,19 +35,7 @@ int fail(int code, const char *fmt, ...) {
 
 namespace {
 
-int fail_hip(hipError_t e, const char *what) {
-    return fail(HKV_EHIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-#define HKV_HIP(call)                                  \
-    do {                                               \
-        hipError_t e_ = (call);                        \
-        if (e_ != hipSuccess) return fail_hip(e_, #call); \
-    } while (0)
-
 size_t elem_bytes(int dtype) { return dtype == HKV_BF16 ? 2 : dtype == HKV_FP8_E4M3 ? 1 : 4; }
-
-size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 
 // What the planner needs to know of the chip: compute units, and how many workgroups of the per-node decode
 // kernel one of them holds (three with bf16 pools, two with fp8 pools: registers).  Asked of the current device;
@@ -75,123 +58,6 @@ ChipShape chip_shape() {
 }
 
 }  // namespace
-
-// ---------------------------------------------------------------------------------------------
-// opaque objects
-struct hkv_decode_plan {
-    hkv_pool *pool = nullptr;
-    int32_t n_req = 0, num_q_heads = 0, group = 0, n_parts = 0, max_parts = 1;
-    std::vector<hkv_node> key_nodes;        // the caller's forest: key of the one-shot cache
-    std::vector<int32_t> key_pages, req_leaf;
-    std::vector<hkv_node> nodes;            // the same forest in 16-token blocks (page_begin, n_pages into node_pages)
-    std::vector<int32_t> node_pages;
-    std::vector<DecodeItem> items;
-    // Items shared by kMinTileItemRows query rows or more (up to 256 / G requests each): run by the 256-row
-    // tile kernel on tile_workgroups persistent workgroups, on a stream of the plan's own next to the kernel
-    // that runs `items` (or in front of it on the caller's stream when concurrent is false).
-    std::vector<DecodeItem> tile_items;
-    int32_t tile_workgroups = 0;
-    // Small steps: whole paths instead of items, one launch (path_waves wavefronts per workgroup; 0: items)
-    std::vector<int32_t> paths;
-    int32_t path_stride = 0, n_paths = 0, path_waves = 0;
-    double paths_us = 0, items_us = 0;  // estimates of a step; paths_us = 0: paths are out of the question, items_us is not asked for
-    int32_t *d_paths = nullptr;
-    int32_t restart_tokens = kMaxSharedItemTokens;  // a stretch of a shared node's item with one reference per row
-    bool row_visibility = false;  // several query tokens per request: rows see their last node in part
-    bool concurrent = true;
-    bool fused = false;  // both kinds of items go out as one launch (no item of `items` has more than 16 rows)
-    hipStream_t side = nullptr;
-    hipEvent_t ev_fork = nullptr, ev_join = nullptr;
-    hipEvent_t ev_tile[2] = {nullptr, nullptr};  // profiling: begin/end of the tile kernel
-    std::vector<int32_t> node_req_indptr, node_req_idx, part_count;
-    // one device allocation holding items | pages | node_req_idx | part_count | tile_items
-    void *dev = nullptr;
-    DecodeItem *d_items = nullptr, *d_tile_items = nullptr;
-    int32_t n_single = 0;  // items [0, n_single) run one per workgroup, the rest four per workgroup
-    int32_t n_stages = 3;  // LDS stages of 16 KiB per workgroup of the per-node kernel
-    bool has_shared = false;  // items of `items` shared by more than 16 query rows are run by shared::body
-    int tile_form = 0;  // bf16 pools: -1 never, 1 always shared::body, 2 with tall tiles (HKV_PLAN_NARROW_TILES, _WIDE_TILES, _TALL_TILES)
-    bool fp8_matrix = false;  // fp8 pools: both products on the fp8 matrix instruction (HKV_PLAN_FP8_MATRIX)
-    hkv_decode_plan_params opt{};  // the planner's settings (0 = the library's choice)
-    int32_t *d_pages = nullptr, *d_node_req_idx = nullptr, *d_part_count = nullptr;
-    std::vector<int32_t> q_rows;  // row of q / out / lse of every row of the plan (empty: row r is row r)
-    int32_t *d_q_rows = nullptr;
-    bool profiling = false, profiled_run = false;
-    hipEvent_t ev[4] = {nullptr, nullptr, nullptr, nullptr};  // begin/end of the node kernel, begin/end of the merge
-    // several query tokens per request: n_req above counts query rows (requests x tokens_per_req)
-    int32_t tokens_per_req = 1;
-    // one allocation (d_row_mask), null when tokens_per_req == 1
-    unsigned long long *d_row_mask = nullptr;
-    int32_t *d_row_leaf = nullptr, *d_row_limit = nullptr;
-    // fp32 pools: no work items; every query row walks its own block table (one allocation: d_bt)
-    std::vector<int32_t> row_len;
-    int32_t max_pages = 0;
-    int32_t *d_bt = nullptr, *d_rows_req = nullptr, *d_rows_len = nullptr;
-    int32_t row_parts = 1;  // shares that a row's keys are cut into where the caller's workspace has room for their results
-    // growing plans (hkv_decode_plan_create_growing): every request's leaf has block slots in node_pages
-    // for reserve_tokens more tokens; grow_items holds, per request, the num_kv_heads items of the leaf's
-    // last chunk.  Items and block list are re-sent after every append through a ring of pinned buffers.
-    int32_t reserve_tokens = 0, appended = 0;
-    std::vector<int32_t> grow_items;
-    static constexpr int kGrowSlots = 4;
-    char *h_grow = nullptr;  // pinned, kGrowSlots x grow_bytes
-    char *d_grow = nullptr;  // the same memory as the device addresses it
-    int32_t *d_grow_items = nullptr;  // device copy of grow_items (up to 256 requests: updates by a small kernel)
-    size_t grow_bytes = 0;   // items + block list as laid out on the device, a multiple of 16
-    hipEvent_t grow_free[kGrowSlots] = {};
-    bool grow_in_flight[kGrowSlots] = {};
-    int grow_next = 0;
-};
-
-struct hkv_prefill_plan {
-    hkv_pool *pool = nullptr;
-    int32_t n_req = 0, num_q_heads = 0, total_q = 0;
-    int32_t key_max_pages = 0;   // row length of the caller's block table (pages)
-    int32_t max_pages = 0;       // row length of the device table (16-token blocks)
-    std::vector<int32_t> cu_q, block_table, kv_len;   // key of the one-shot cache
-    std::vector<PrefillTile> tiles;
-    std::vector<PrefillTile> pieces;  // small batches: the tiles in pieces of fewer rows, a workgroup each (empty: the tiles)
-    void *dev = nullptr;
-    PrefillTile *d_tiles = nullptr;
-    int32_t *d_block_table = nullptr;
-    int32_t *d_rows_req = nullptr, *d_rows_len = nullptr;  // fp32 pools: per new token (one allocation: d_rows_req)
-    // fp8 pools: the pages the batch reads are first dequantised into a bf16 scratch pool in the caller's
-    // workspace (page i of the scratch = src_pages[i]); the device block table then holds scratch indices.
-    std::vector<int32_t> src_pages;
-    int32_t *d_src_pages = nullptr;
-    unsigned int *d_fallback = nullptr;  // tiles that repeated with a running maximum, over all runs of the plan
-    // tiles split along their keys (empty: a workgroup per tile); the partials go to the caller's workspace
-    std::vector<PrefillSegment> segments;
-    std::vector<int32_t> seg_begin, seg_tile;  // first segment of every worker; the tile a segment was cut from
-    std::vector<PrefillSplitTile> split;
-    int32_t n_parts = 0;
-    PrefillSegment *d_segments = nullptr;
-    int32_t *d_seg_begin = nullptr;
-    PrefillSplitTile *d_split = nullptr;
-};
-
-struct hkv_pool {
-    hkv_pool_desc d{};
-    // A page of page_size = 16 * S tokens is S consecutive 16-token blocks of the buffers: block
-    // page * S + j holds tokens 16 j .. 16 j + 15 of the page.  Everything behind the entry points
-    // (work lists, kernels) deals in 16-token blocks; page ids are translated where they come in.
-    int32_t blocks_per_page = 1;
-    std::vector<int32_t> refcnt;
-    std::deque<int32_t> free_list;
-    // Staging of page ids for kv_pool_write: a ring of slots (pinned host + device, one allocation
-    // each), so that back-to-back writes on a stream do not wait for one another; a slot is reused
-    // only after the event recorded behind its last write has completed.
-    static constexpr int kMaxWritePages = 65536;
-    static constexpr int kWriteSlots = 8;
-    int32_t *h_ids = nullptr;  // pinned host, kWriteSlots x kMaxWritePages
-    int32_t *hd_ids = nullptr; // the same memory as the device addresses it (source of the copy kernel)
-    int32_t *d_ids = nullptr;  // device, same shape
-    hipEvent_t slot_free[kWriteSlots] = {};
-    bool slot_in_flight[kWriteSlots] = {};
-    int next_slot = 0;
-    hkv_decode_plan *cached_decode = nullptr;
-    hkv_prefill_plan *cached_prefill = nullptr;
-};
 
 // ---------------------------------------------------------------------------------------------
 extern "C" const char *hkv_last_error(void) { return g_err.c_str(); }
@@ -317,10 +183,6 @@ extern "C" int32_t kv_pool_refcount(const hkv_pool *pool, int32_t page_id) {
     return pool->refcnt[page_id];
 }
 
-static PoolView view_of(const hkv_pool *p) {
-    return PoolView{p->d.k_pages, p->d.v_pages, p->d.k_scale, p->d.v_scale, p->d.num_kv_heads, p->d.dtype};
-}
-
 extern "C" int kv_pool_copy_on_write(hkv_pool *pool, int32_t n, int32_t *ids, void *stream) {
     if (int rc = check_held(pool, n, ids, "kv_pool_copy_on_write")) return rc;
     std::vector<int32_t> sorted(ids, ids + n);
@@ -368,6 +230,24 @@ static int ensure_write_staging(hkv_pool *pool) {
     return HKV_OK;
 }
 
+int hkv::take_staging(hkv_pool *pool, int32_t *slot, int32_t **host, int32_t **host_on_device, int32_t **device) {
+    if (int rc = ensure_write_staging(pool)) return rc;
+    *slot = pool->next_slot;
+    pool->next_slot = (*slot + 1) % hkv_pool::kWriteSlots;
+    if (pool->slot_in_flight[*slot]) HKV_HIP(hipEventSynchronize(pool->slot_free[*slot]));  // its last use is done
+    const size_t at = (size_t)*slot * hkv_pool::kMaxWritePages;
+    *host = pool->h_ids + at;
+    *host_on_device = pool->hd_ids + at;
+    *device = pool->d_ids + at;
+    return HKV_OK;
+}
+
+int hkv::leave_staging(hkv_pool *pool, int32_t slot, hipStream_t s) {
+    HKV_HIP(hipEventRecord(pool->slot_free[slot], s));
+    pool->slot_in_flight[slot] = true;
+    return HKV_OK;
+}
+
 extern "C" int kv_pool_write(hkv_pool *pool, const int32_t *page_ids, int32_t first_slot, int32_t n_tokens,
                              const void *k_src, const void *v_src, void *stream) {
     if (!pool) return fail(HKV_EINVAL, "kv_pool_write: null pool");
@@ -397,24 +277,18 @@ extern "C" int kv_pool_write(hkv_pool *pool, const int32_t *page_ids, int32_t fi
         HKV_HIP(launch_pool_write(a, s));
         return HKV_OK;
     }
-    if (int rc = ensure_write_staging(pool)) return rc;
-    const int slot = pool->next_slot;
-    pool->next_slot = (slot + 1) % hkv_pool::kWriteSlots;
-    if (pool->slot_in_flight[slot]) HKV_HIP(hipEventSynchronize(pool->slot_free[slot]));  // its last write is done
-    int32_t *h = pool->h_ids + (size_t)slot * hkv_pool::kMaxWritePages;
-    int32_t *d = pool->d_ids + (size_t)slot * hkv_pool::kMaxWritePages;
+    int32_t slot, *h, *hd, *d;
+    if (int rc = take_staging(pool, &slot, &h, &hd, &d)) return rc;
     for (int64_t b = b0; b <= b1; ++b) h[b - b0] = page_ids[b / S] * S + (int32_t)(b % S);
     // a copy kernel on the stream reads the pinned slot (a DMA copy between kernels of one stream costs more)
-    HKV_HIP(launch_upload(pool->hd_ids + (size_t)slot * hkv_pool::kMaxWritePages, d, align_up(sizeof(int32_t) * (size_t)n_pg, 16), s));
+    HKV_HIP(launch_upload(hd, d, align_up(sizeof(int32_t) * (size_t)n_pg, 16), s));
     PoolWriteLaunch a{pool->d.k_pages, pool->d.v_pages, pool->d.k_scale, pool->d.v_scale, pool->d.num_kv_heads,
                       pool->d.dtype, d, (int32_t)n_pg, first_slot % HKV_PAGE_SIZE, n_tokens, k_src, v_src, nullptr, nullptr};
     if (pool->d.dtype == HKV_FP32)
         HKV_HIP(launch_pool_write_fp32(a, s));
     else
         HKV_HIP(launch_pool_write(a, s));
-    HKV_HIP(hipEventRecord(pool->slot_free[slot], s));
-    pool->slot_in_flight[slot] = true;
-    return HKV_OK;
+    return leave_staging(pool, slot, s);
 }
 
 extern "C" int kv_pool_append(hkv_pool *pool, const int32_t *page_ids, const int32_t *slots, int32_t n,
@@ -456,23 +330,17 @@ extern "C" int kv_pool_append(hkv_pool *pool, const int32_t *page_ids, const int
         HKV_HIP(launch_pool_append_inline(a, s));
         return HKV_OK;
     }
-    if (int rc = ensure_write_staging(pool)) return rc;
-    const int slot = pool->next_slot;
-    pool->next_slot = (slot + 1) % hkv_pool::kWriteSlots;
-    if (pool->slot_in_flight[slot]) HKV_HIP(hipEventSynchronize(pool->slot_free[slot]));
-    int32_t *h = pool->h_ids + (size_t)slot * hkv_pool::kMaxWritePages;
-    int32_t *d = pool->d_ids + (size_t)slot * hkv_pool::kMaxWritePages;
+    int32_t slot, *h, *hd, *d;
+    if (int rc = take_staging(pool, &slot, &h, &hd, &d)) return rc;
     for (int i = 0; i < n; ++i) {  // block ids, then the slots inside them
         h[i] = page_ids[i] * S + slots[i] / HKV_PAGE_SIZE;
         h[n + i] = slots[i] % HKV_PAGE_SIZE;
     }
-    HKV_HIP(launch_upload(pool->hd_ids + (size_t)slot * hkv_pool::kMaxWritePages, d, align_up(sizeof(int32_t) * 2 * (size_t)n, 16), s));
+    HKV_HIP(launch_upload(hd, d, align_up(sizeof(int32_t) * 2 * (size_t)n, 16), s));
     PoolWriteLaunch a{pool->d.k_pages, pool->d.v_pages, pool->d.k_scale, pool->d.v_scale, pool->d.num_kv_heads,
                       pool->d.dtype, d, n, 0, n, k_src, v_src, d + n, nullptr};
     HKV_HIP(launch_pool_write(a, s));
-    HKV_HIP(hipEventRecord(pool->slot_free[slot], s));
-    pool->slot_in_flight[slot] = true;
-    return HKV_OK;
+    return leave_staging(pool, slot, s);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -1436,7 +1304,8 @@ static int upload_decode_plan(hkv_decode_plan &pl) {
     size_t off_tiles = align_up(off_cnt + sizeof(int32_t) * pl.part_count.size(), 256);
     size_t off_qrows = align_up(off_tiles + sizeof(DecodeItem) * pl.tile_items.size(), 256);
     size_t off_paths = align_up(off_qrows + sizeof(int32_t) * pl.q_rows.size(), 256);
-    size_t total = align_up(off_paths + sizeof(int32_t) * pl.paths.size(), 256) + 256;
+    size_t off_store = align_up(off_paths + sizeof(int32_t) * pl.paths.size(), 256);
+    size_t total = align_up(off_store + sizeof(StoreRequest) * pl.store.size(), 256) + 256;
     HKV_HIP(hipMalloc(&pl.dev, total));
     char *base = static_cast<char *>(pl.dev);
     pl.d_items = reinterpret_cast<DecodeItem *>(base + off_items);
@@ -1445,6 +1314,7 @@ static int upload_decode_plan(hkv_decode_plan &pl) {
     pl.d_part_count = reinterpret_cast<int32_t *>(base + off_cnt);
     pl.d_tile_items = reinterpret_cast<DecodeItem *>(base + off_tiles);
     pl.d_paths = reinterpret_cast<int32_t *>(base + off_paths);
+    pl.d_store = reinterpret_cast<StoreRequest *>(base + off_store);
     pl.d_q_rows = pl.q_rows.empty() ? nullptr : reinterpret_cast<int32_t *>(base + off_qrows);
     // one host image, one copy
     std::vector<char> image(total, 0);
@@ -1458,6 +1328,7 @@ static int upload_decode_plan(hkv_decode_plan &pl) {
     put(off_tiles, pl.tile_items.data(), sizeof(DecodeItem) * pl.tile_items.size());
     put(off_qrows, pl.q_rows.data(), sizeof(int32_t) * pl.q_rows.size());
     put(off_paths, pl.paths.data(), sizeof(int32_t) * pl.paths.size());
+    put(off_store, pl.store.data(), sizeof(StoreRequest) * pl.store.size());
     HKV_HIP(hipMemcpy(pl.dev, image.data(), total, hipMemcpyHostToDevice));
     if (pl.reserve_tokens > 0 && pl.n_req <= kMaxInlineAppend && !pl.grow_items.empty() && !pl.opt.large_batch_updates) {
         HKV_HIP(hipMalloc((void **)&pl.d_grow_items, sizeof(int32_t) * pl.grow_items.size()));
@@ -1501,6 +1372,8 @@ static int build_fp32_rows(hkv_decode_plan &pl, bool upload) {
     }
     const double page_mb = 1e-6 * 2 * kBlockElems * sizeof(float) * pl.pool->d.num_kv_heads;
     pl.row_parts = row_shares(n, pl.pool->d.num_kv_heads, pl.group, pl.max_pages, page_mb * n_pages);
+    for (int r = 0; r < n; r += pl.tokens_per_req)  // (a request's rows have the same path; positions along it are places in the row's table)
+        pl.store.push_back(StoreRequest{(uint32_t)r * (uint32_t)pl.max_pages, pl.row_len[r], 0, -1});
     if (!upload || n == 0) return HKV_OK;
     std::vector<int32_t> bt((size_t)n * pl.max_pages, 0), req(n);
     for (int r = 0; r < n; ++r) {
@@ -1508,12 +1381,14 @@ static int build_fp32_rows(hkv_decode_plan &pl, bool upload) {
         req[r] = r;
     }
     const size_t b_bt = align_up(sizeof(int32_t) * bt.size(), 256), b_n = align_up(sizeof(int32_t) * n, 256);
-    HKV_HIP(hipMalloc((void **)&pl.d_bt, b_bt + 2 * b_n));
+    HKV_HIP(hipMalloc((void **)&pl.d_bt, b_bt + 2 * b_n + sizeof(StoreRequest) * pl.store.size()));
     pl.d_rows_req = reinterpret_cast<int32_t *>(reinterpret_cast<char *>(pl.d_bt) + b_bt);
     pl.d_rows_len = reinterpret_cast<int32_t *>(reinterpret_cast<char *>(pl.d_bt) + b_bt + b_n);
+    pl.d_store = reinterpret_cast<StoreRequest *>(reinterpret_cast<char *>(pl.d_bt) + b_bt + 2 * b_n);
     HKV_HIP(hipMemcpy(pl.d_bt, bt.data(), sizeof(int32_t) * bt.size(), hipMemcpyHostToDevice));
     HKV_HIP(hipMemcpy(pl.d_rows_req, req.data(), sizeof(int32_t) * n, hipMemcpyHostToDevice));
     HKV_HIP(hipMemcpy(pl.d_rows_len, pl.row_len.data(), sizeof(int32_t) * n, hipMemcpyHostToDevice));
+    HKV_HIP(hipMemcpy(pl.d_store, pl.store.data(), sizeof(StoreRequest) * pl.store.size(), hipMemcpyHostToDevice));
     return HKV_OK;
 }
 
@@ -1543,7 +1418,7 @@ static int check_plan_settings(const hkv_decode_plan_params *o) {
 static int create_decode_plan(hkv_pool *pool, const hkv_node *nodes, int32_t n_nodes, const int32_t *node_pages,
                               int32_t n_node_pages, const int32_t *req_leaf, int32_t n_req, int32_t num_q_heads,
                               uint32_t flags, int32_t reserve_tokens, const hkv_decode_plan_params *opt,
-                              hkv_decode_plan **out) {
+                              hkv_decode_plan **out, int32_t tokens_per_req = 1) {
     if (!pool || !out) return fail(HKV_EINVAL, "hkv_decode_plan_create: null argument");
     *out = nullptr;
     if (int rc = check_plan_settings(opt)) return rc;
@@ -1569,6 +1444,7 @@ static int create_decode_plan(hkv_pool *pool, const hkv_node *nodes, int32_t n_n
     if (pool->d.dtype == HKV_BF16) pl->tile_form = flags & HKV_PLAN_NARROW_TILES ? -1 : flags & HKV_PLAN_WIDE_TILES ? 1 : flags & HKV_PLAN_TALL_TILES ? 2 : 0;
     pl->pool = pool;
     pl->n_req = n_req;
+    pl->tokens_per_req = tokens_per_req;
     pl->num_q_heads = num_q_heads;
     pl->group = num_q_heads / Hkv;
     pl->fp8_matrix = pool->d.dtype == HKV_FP8_E4M3 && (flags & HKV_PLAN_FP8_MATRIX);
@@ -1657,6 +1533,13 @@ static int create_decode_plan(hkv_pool *pool, const hkv_node *nodes, int32_t n_n
         pl->key_nodes.clear();  // never the pool's cached one-shot plan
         pl->key_pages.clear();
     }
+    std::vector<int32_t> tok_start(n_nodes, 0);
+    for (int v = 0; v < n_nodes; ++v)
+        if (nodes[v].parent >= 0) tok_start[v] = tok_start[nodes[v].parent] + nodes[nodes[v].parent].n_tokens;
+    for (int r = 0; r < n_req; r += tokens_per_req) {
+        const hkv_node &leaf = pl->nodes[req_leaf[r]];
+        pl->store.push_back(StoreRequest{(uint32_t)leaf.page_begin, leaf.n_tokens, tok_start[req_leaf[r]], reserve_tokens > 0 ? pl->grow_items[(size_t)r * Hkv] : -1});
+    }
     if (!(flags & HKV_PLAN_HOST_ONLY)) {
         if (int rc = upload_decode_plan(*pl)) {
             hkv_decode_plan_destroy(pl);
@@ -1715,8 +1598,8 @@ extern "C" int hkv_decode_plan_create_growing(hkv_pool *pool, const hkv_node *no
 
 // k_src / v_src: null (the caller stores the tokens itself), or the new token of every request, stored here
 // at the end of its leaf, in the same launch as the plan's update where that runs as a kernel.
-static int plan_append(hkv_decode_plan *plan, const int32_t *new_page_ids, const void *k_src, const void *v_src,
-                       void *stream) {
+int hkv::plan_append(hkv_decode_plan *plan, const int32_t *new_page_ids, const void *k_src, const void *v_src, AppendHook *hook,
+                     void *stream) {
     if (!plan) return fail(HKV_EINVAL, "hkv_decode_plan_append: null plan");
     if (plan->reserve_tokens <= 0) return fail(HKV_EINVAL, "hkv_decode_plan_append: not a growing plan");
     if (plan->appended >= plan->reserve_tokens)
@@ -1782,6 +1665,9 @@ static int plan_append(hkv_decode_plan *plan, const int32_t *new_page_ids, const
             w.base = PoolWriteLaunch{pool->d.k_pages, pool->d.v_pages, pool->d.k_scale, pool->d.v_scale, Hkv, pool->d.dtype,
                                      nullptr, plan->n_req, 0, plan->n_req, k_src, v_src, nullptr, nullptr};
             HKV_HIP(launch_decode_step_append(w, g, s));
+        } else if (hook) {
+            HKV_HIP(hook->launch(hook->ctx, g, s));
+            hook->launched = true;
         } else {
             HKV_HIP(launch_plan_grow_inline(g, s));
         }
@@ -1805,13 +1691,13 @@ static int plan_append(hkv_decode_plan *plan, const int32_t *new_page_ids, const
 }
 
 extern "C" int hkv_decode_plan_append(hkv_decode_plan *plan, const int32_t *new_page_ids, void *stream) {
-    return plan_append(plan, new_page_ids, nullptr, nullptr, stream);
+    return plan_append(plan, new_page_ids, nullptr, nullptr, nullptr, stream);
 }
 
 extern "C" int hkv_decode_plan_append_tokens(hkv_decode_plan *plan, const int32_t *new_page_ids, const void *k_src,
                                              const void *v_src, void *stream) {
     if (!k_src || !v_src) return fail(HKV_EINVAL, "hkv_decode_plan_append_tokens: null k_src / v_src");
-    return plan_append(plan, new_page_ids, k_src, v_src, stream);
+    return plan_append(plan, new_page_ids, k_src, v_src, nullptr, stream);
 }
 
 // Plan over n_req * T query rows: the T newest tokens of every request (the last T of its leaf node) are
@@ -1831,9 +1717,8 @@ static int create_rows_plan(hkv_pool *pool, const hkv_node *nodes, int32_t n_nod
     hkv_decode_plan *pl = nullptr;
     const uint32_t rows_flags = (flags & ~kPlanRowVisibility) | ((T > 1 || masks) ? kPlanRowVisibility : 0u);
     if (int rc = create_decode_plan(pool, nodes, n_nodes, node_pages, n_node_pages, rows.data(), n_req * T, num_q_heads,
-                                    rows_flags, 0, opt, &pl))
+                                    rows_flags, 0, opt, &pl, T))
         return rc;
-    pl->tokens_per_req = T;
     if (T > 1 || masks) {
         std::vector<int32_t> lim((size_t)n_req * T);
         std::vector<unsigned long long> vis((size_t)n_req * T);
@@ -1938,6 +1823,7 @@ extern "C" int hkv_decode_plan_destroy(hkv_decode_plan *plan) {
     if (!plan) return HKV_OK;
     if (plan->dev) (void)hipFree(plan->dev);  // hipFree waits for work that may still read it
     if (plan->d_row_mask) (void)hipFree(plan->d_row_mask);
+    if (plan->d_weight_items) (void)hipFree(plan->d_weight_items);
     if (plan->d_bt) (void)hipFree(plan->d_bt);
     for (hipEvent_t e : plan->ev)
         if (e) (void)hipEventDestroy(e);
@@ -2373,6 +2259,7 @@ static int create_prefill_plan(hkv_pool *pool, const int32_t *cu_q, const int32_
     pl->total_q = n_req ? cu_q[n_req] : 0;
     pl->cu_q.assign(cu_q, cu_q + (n_req ? n_req + 1 : 0));
     pl->kv_len.assign(kv_len, kv_len + n_req);
+    if (q_row_begin) pl->q_row_begin.assign(q_row_begin, q_row_begin + n_req);
     if (n_req && max_pages) pl->block_table.assign(block_table, block_table + (size_t)n_req * max_pages);
     // the kernels index 16-token blocks: block j of page p is block p * S + j of the buffers
     const int S = pool->blocks_per_page;

@@ -179,6 +179,94 @@ struct PlanGrowInline {
     int32_t block_pos[kMaxInlineAppend];
 };
 
+// Where the newest tokens of a request of a decode plan lie: its leaf's blocks, `tokens` of them, the first at position pos0 of
+// its path.  Growing plans: the leaf's length is what item `item` says (tok_begin + n_tokens).
+struct StoreRequest {
+    uint32_t page_off;           // index of the leaf's first block in the plan's block list (fp32 pools: of the path's, in the rows' table)
+    int32_t tokens;
+    int32_t pos0;
+    int32_t item;                // -1: none
+};
+
+// Rows of a step's projections: norm and rotation of q and k, queries out, keys and values into the pool (projection_store.hip).
+struct ProjectionLaunch {
+    PoolWriteLaunch pool;        // buffers and num_kv_heads; the rest is not read
+    const void *q, *k, *v;
+    void *q_out;
+    int64_t q_stride, k_stride, v_stride;  // elements from row to row
+    const void *q_norm, *k_norm; // device [128], may be null
+    const double *inv_freq;      // device [rotary_dim / 2]
+    const int32_t *positions;    // device, may be null: [axes][rows], position_stride apart
+    int64_t position_stride;
+    uint32_t axis[4];            // axis of pair p: bits 2 * (p % 16) .. + 1 of word p / 16
+    float eps;
+    int32_t rotary_dim, interleaved, n_axes;
+    int32_t group;               // query heads of a KV head
+    const int32_t *blocks;       // device: block ids (a plan's list, or the rows of a table)
+    const int32_t *src_pages;    // device, may be null: `blocks` holds indices into this list
+    const int32_t *row_map;      // device, may be null: row of q / k / v / q_out of every row of the plan
+    // decode plans: the newest `tokens` tokens of every request
+    const StoreRequest *requests;  // device
+    const DecodeItem *items;       // device
+    int32_t tokens;
+    int32_t n_requests;
+};
+// The same for the new tokens of up to kMaxInlineRequests requests of a prefill plan: request i of the launch has the units (16-token
+// blocks it writes to) begin[i] .. begin[i + 1] - 1.
+constexpr int kMaxInlineRequests = 128;
+struct ProjectionPrefill {
+    ProjectionLaunch base;
+    int64_t table;               // offset of the first request's row in base.blocks
+    int32_t table_stride;
+    int32_t n_units;
+    int32_t begin[kMaxInlineRequests];     // (INT32_MAX behind the last)
+    int32_t row0[kMaxInlineRequests];
+    int32_t prefix[kMaxInlineRequests];
+    int32_t tokens[kMaxInlineRequests];
+};
+
+// One workgroup's keys of attn_decode_plan_weights: up to kWeightTokens tokens of a node from tok_begin on, one KV head, all rows below the node.
+constexpr int kWeightTokens = 128;
+struct KeyWeightItem {
+    int32_t page_off;            // index of the first token's block in the plan's block list
+    int32_t tok_begin;           // within the node, a multiple of 16
+    int32_t kv_head;
+    int32_t req_off;             // node->request CSR
+    int32_t n_req;
+    int32_t node;                // ~node where it is no request's last node
+    int32_t tokens;              // of the node; growing leaves: what item `item` says
+    int32_t item;
+};
+struct KeyWeightsLaunch {
+    PoolView pool;
+    const void *q;               // [rows][Hq][128] bf16
+    const float *lse;            // [rows][Hq]
+    const KeyWeightItem *items;  // device
+    const DecodeItem *plan_items;
+    const int32_t *pages, *node_req_idx, *q_rows;
+    const int32_t *row_leaf, *row_limit;
+    const unsigned long long *row_mask;
+    float *weights;              // [blocks][Hkv][16]
+    int32_t n_items, num_q_heads, tokens_per_req, n_new;
+    float scale, decay;
+};
+
+// Eviction (evict.hip).  meta (device): per sequence an EvictSequence, then the sequences' source blocks, then their new blocks.
+struct EvictSequence {
+    int32_t src, dst;            // offsets of its block ids in meta
+    int32_t tokens, keep;
+    int32_t kept;                // its first column of `kept`
+    int32_t unit;                // its first new block, counted over all sequences
+};
+struct EvictLaunch {
+    PoolWriteLaunch pool;        // buffers, num_kv_heads, dtype
+    const int32_t *meta;
+    float *weights;
+    int32_t *kept;               // [Hkv][total]
+    int64_t total;
+    int32_t n_seq, n_units, n_first, n_recent;
+};
+
 // Whole-page copies inside one pool (copy-on-write of pages that several holders share).
 constexpr int kMaxCopyPairs = 32;
 struct PoolCopyLaunch {
@@ -307,6 +395,11 @@ hipError_t launch_pool_append_inline(const PoolAppendInline &a, hipStream_t s);
 // both in one launch: workgroup (r, head) stores request r's token and lengthens the leaf's item of that head
 hipError_t launch_decode_step_append(const PoolAppendInline &w, const PlanGrowInline &g, hipStream_t s);
 hipError_t launch_plan_grow_inline(const PlanGrowInline &a, hipStream_t s);
+hipError_t launch_projection_store(const ProjectionLaunch &a, hipStream_t s);
+hipError_t launch_projection_store(const ProjectionPrefill &a, hipStream_t s);
+hipError_t launch_projection_append(const ProjectionLaunch &a, const PlanGrowInline &g, hipStream_t s);
+hipError_t launch_key_weights(const KeyWeightsLaunch &a, hipStream_t s);
+hipError_t launch_evict(const EvictLaunch &a, hipStream_t s);
 hipError_t launch_pool_copy(const PoolCopyLaunch &a, hipStream_t s);
 hipError_t launch_pool_dequant(const PoolDequantLaunch &a, hipStream_t s);
 // Once per device (later calls only read the result), with that device current and outside graph capture:
