@@ -22,7 +22,13 @@ __device__ __forceinline__ uint32_t quant4(float a, float b, float c, float d, f
     return (uint32_t)p;
 }
 
-// The same codes for bf16 values x and a scale of amax / 448 of such values, |x| <= amax, from the scale's reciprocal
+// Four codes under an old scale, rounded again under a new one: value * old / scale.
+__device__ __forceinline__ uint32_t requant4(uint32_t w, float old, float scale) {
+    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
+    return quant4(lo[0] * old, lo[1] * old, hi[0] * old, hi[1] * old, scale);
+}
+
+// Codes as quant4's for bf16 values x and a scale of amax / 448 of such values, |x| <= amax, from the scale's reciprocal
 // (correctly rounded): product, remainder, correction.  For every such pair with a scale in [2^-60, 2^60] (5.3e8 pairs, all
 // of them tried) the quotient equals the division's bit for bit wherever it is at least 2^-11 in magnitude; below 2^-10
 // both round to zero with the sign of x.  Four instructions instead of about ten, two of them slow ones.
@@ -130,15 +136,11 @@ __device__ __forceinline__ void store_block(const PoolWriteLaunch &a, const int 
             return c;
         };
         const bool k_grew = append && ksc > sOld[0], v_grew = append && vsc > sOld[1];
-        auto reencode4 = [](uint32_t w, float old, float sc) {  // four codes: value * old / sc, rounded again
-            const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)w, true);
-            return quant4(lo[0] * old, lo[1] * old, hi[0] * old, hi[1] * old, sc);
-        };
         if (k_grew && slot < s_lo) {
             uint8_t *kdst = static_cast<uint8_t *>(a.k_pages) + blk + (d0 >> 6) * (kPage * 64) + slot * 64 + (d0 & 63);
             u32x2 c = *reinterpret_cast<u32x2 *>(kdst);
-            c[0] = reencode4(c[0], sOld[0], ksc);
-            c[1] = reencode4(c[1], sOld[0], ksc);
+            c[0] = requant4(c[0], sOld[0], ksc);
+            c[1] = requant4(c[1], sOld[0], ksc);
             *reinterpret_cast<u32x2 *>(kdst) = c;
         }
         if (valid) {
@@ -158,8 +160,8 @@ __device__ __forceinline__ void store_block(const PoolWriteLaunch &a, const int 
             u32x2 r = {0u, 0u};  // the earlier codes of these eight slots, re-encoded if the scale grew
             if (v_grew && half * 8 < s_lo) {
                 r = *reinterpret_cast<u32x2 *>(vdst);
-                r[0] = reencode4(r[0], sOld[1], vsc);
-                r[1] = reencode4(r[1], sOld[1], vsc);
+                r[0] = requant4(r[0], sOld[1], vsc);
+                r[1] = requant4(r[1], sOld[1], vsc);
             }
             for (int j = 0; j < 8; ++j) {
                 const int sl = half * 8 + j;

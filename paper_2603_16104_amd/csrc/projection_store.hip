@@ -49,52 +49,60 @@ __device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
     return u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(x[4], x[5]), pack_bf16(x[6], x[7])};
 }
 
+// (By value: a choice between variables, or of an array's element, goes through memory, LDS whose place the wavefront then reads from the
+// dispatch packet in host memory: 14 us a launch.)
+__device__ __forceinline__ int choose(uint32_t i, int a, int b, int c, int d) { return i < 2 ? (i == 0 ? +a : +b) : (i == 2 ? +c : +d); }
+
+// Cosine and sine of N pairs from p0 on (a multiple of N) of the row's angles.
+template <int DT, int N>
+__device__ __forceinline__ void angles(const ProjectionLaunch &a, int p0, int64_t row, int pos, float (&co)[N], float (&si)[N]) {
+    double freq[N];
+#pragma unroll
+    for (int e = 0; e < N; ++e) freq[e] = a.inv_freq[p0 + e];
+    int on0 = pos, on1 = pos, on2 = pos, on3 = pos;
+    if (a.positions) {
+        on0 = a.positions[row];
+        if (a.n_axes > 1) on1 = a.positions[a.position_stride + row];
+        if (a.n_axes > 2) on2 = a.positions[2 * a.position_stride + row];
+        if (a.n_axes > 3) on3 = a.positions[3 * a.position_stride + row];
+    }
+    const uint32_t axes = (p0 < 32 ? (p0 < 16 ? a.axis[0] : a.axis[1]) : (p0 < 48 ? a.axis[2] : a.axis[3])) >> (2 * (p0 & 15));
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const int place = a.n_axes == 1 ? on0 : choose(axes >> (2 * e) & 3u, on0, on1, on2, on3);
+        const double turns = (double)place * (freq[e] * 0.15915494309189533577);
+        const float part = (float)(turns - __builtin_rint(turns));
+        if constexpr (DT == 2) {
+            sincospif(2.0f * part, &si[e], &co[e]);
+        } else {  // off by 1.25e-7 at most (2^24 parts tried): results keep 8 bits
+            si[e] = __builtin_amdgcn_sinf(part);
+            co[e] = __builtin_amdgcn_cosf(part);
+        }
+    }
+}
+
 // What a lane's dims 8 c .. 8 c + 7 turn by: z = x * cos + (the pair's other value) * sin, sin with the sign of the place in the pair.
 struct Turn {
     float cos[8], sin[8];
     bool on;
 };
-template <int DT>
-__device__ __forceinline__ void turn_of(const ProjectionLaunch &a, int c, int64_t row, int pos, Turn &t) {
+// From a row's table of cosines and sines, [2][64] in LDS.
+__device__ __forceinline__ void turn_of(const ProjectionLaunch &a, const float *table, int c, Turn &t) {
     t.on = 8 * c < a.rotary_dim;
     if (!t.on) return;
-    const int half = a.rotary_dim >> 1;
-    const bool second = 8 * c >= half;
-    const int p0 = a.interleaved ? 4 * c : 8 * c - (second ? half : 0);
-    int p[4] = {pos, pos, pos, pos};
-    if (a.positions) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-            if (i < a.n_axes) p[i] = a.positions[i * a.position_stride + row];
-    }
-    const uint32_t axes = (p0 < 32 ? (p0 < 16 ? a.axis[0] : a.axis[1]) : (p0 < 48 ? a.axis[2] : a.axis[3])) >> (2 * (p0 & 15));
-    auto angle = [&](int e, float &co, float &si) {
-        const uint32_t ax = axes >> (2 * e) & 3u;
-        const double place = (double)(ax < 2 ? (ax == 0 ? p[0] : p[1]) : (ax == 2 ? p[2] : p[3]));
-        const double turns = place * (a.inv_freq[p0 + e] * 0.15915494309189533577);
-        const float part = (float)(turns - __builtin_rint(turns));
-        if constexpr (DT == 2) {
-            sincospif(2.0f * part, &si, &co);
-        } else {  // good to 2^-19 or so of a result that keeps 8 bits and fewer
-            si = __builtin_amdgcn_sinf(part);
-            co = __builtin_amdgcn_cosf(part);
-        }
-    };
+    const float4 *co = reinterpret_cast<const float4 *>(table), *si = co + 16;
     if (a.interleaved) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            float co, si;
-            angle(e, co, si);
-            t.cos[2 * e] = t.cos[2 * e + 1] = co;
-            t.sin[2 * e] = -si;
-            t.sin[2 * e + 1] = si;
-        }
+        const float4 x = co[c], y = si[c];
+        t.cos[0] = t.cos[1] = x.x, t.cos[2] = t.cos[3] = x.y, t.cos[4] = t.cos[5] = x.z, t.cos[6] = t.cos[7] = x.w;
+        t.sin[0] = -y.x, t.sin[1] = y.x, t.sin[2] = -y.y, t.sin[3] = y.y, t.sin[4] = -y.z, t.sin[5] = y.z, t.sin[6] = -y.w, t.sin[7] = y.w;
     } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            angle(e, t.cos[e], t.sin[e]);
-            if (!second) t.sin[e] = -t.sin[e];
-        }
+        const bool second = 16 * c >= a.rotary_dim;
+        const int p = 2 * c - (second ? a.rotary_dim >> 3 : 0);
+        const float s = second ? 1.0f : -1.0f;
+        const float4 x0 = co[p], x1 = co[p + 1], y0 = si[p], y1 = si[p + 1];
+        t.cos[0] = x0.x, t.cos[1] = x0.y, t.cos[2] = x0.z, t.cos[3] = x0.w, t.cos[4] = x1.x, t.cos[5] = x1.y, t.cos[6] = x1.z, t.cos[7] = x1.w;
+        t.sin[0] = s * y0.x, t.sin[1] = s * y0.y, t.sin[2] = s * y0.z, t.sin[3] = s * y0.w;
+        t.sin[4] = s * y1.x, t.sin[5] = s * y1.y, t.sin[6] = s * y1.z, t.sin[7] = s * y1.w;
     }
 }
 
@@ -105,13 +113,20 @@ __device__ __forceinline__ float row16_sum(float v) {
     return v + dpp<kRor8>(v);
 }
 
+__device__ __forceinline__ float row16_max(float v) {
+    v = fmaxf(v, dpp<kQuadXor1>(v));
+    v = fmaxf(v, dpp<kQuadXor2>(v));
+    v = fmaxf(v, dpp<kRor4>(v));
+    return fmaxf(v, dpp<kRor8>(v));
+}
+
 // Norm and rotation of one row.  All 16 lanes of a row take part.
 __device__ __forceinline__ void norm_and_turn(const ProjectionLaunch &a, int c, bool normed, const float (&w)[8], const Turn &t, float (&x)[8]) {
     if (normed) {
         float sq = 0.f;
 #pragma unroll
         for (int j = 0; j < 8; ++j) sq = __builtin_fmaf(x[j], x[j], sq);
-        const float inv = 1.0f / __builtin_sqrtf(row16_sum(sq) * (1.0f / kHeadDim) + a.eps);
+        const float inv = __builtin_amdgcn_rsqf(row16_sum(sq) * (1.0f / kHeadDim) + a.eps);
 #pragma unroll
         for (int j = 0; j < 8; ++j) x[j] = x[j] * inv * w[j];
     }
@@ -176,67 +191,169 @@ __device__ __forceinline__ void put_block(const ProjectionLaunch &a, const Unit 
 // One KV head of one block with up to 16 tokens: thread row = slot.
 template <int DT>
 __device__ __forceinline__ void store_tokens(const ProjectionLaunch &a, const Unit &u, int h) {
+    __shared__ __align__(16) float sTurn[kPage][2 * 64 + 4];
     const int slot = threadIdx.x >> 4, c = threadIdx.x & 15;
     const bool valid = slot >= u.lo && slot < u.hi;
+    constexpr int kAhead = 4;  // query rows on their way
+    int64_t row = u.row + max(0, min(slot, u.hi - 1) - u.lo);
+    if (a.row_map) row = a.row_map[row];
     float k[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     Row<DT> v{};
     if (valid) {
-        int64_t row = u.row + slot - u.lo;
-        if (a.row_map) row = a.row_map[row];
         const Row<DT> kr = load_row<DT>(a.k, a.k_stride, row, h, c);
         v = load_row<DT>(a.v, a.v_stride, row, h, c);
-        Row<DT> q = load_row<DT>(a.q, a.q_stride, row, h * a.group, c);
-        float qw[8] = {}, kwt[8] = {};
+        Row<DT> q[kAhead];
+#pragma unroll
+        for (int j = 0; j < kAhead; ++j)
+            if (j < a.group) q[j] = load_row<DT>(a.q, a.q_stride, row, h * a.group + j, c);
+        float qw[8] = {}, kw[8] = {};
         load_weight<DT>(a.q_norm, c, qw);
-        load_weight<DT>(a.k_norm, c, kwt);
+        load_weight<DT>(a.k_norm, c, kw);
+        // four angles a lane; the row's lanes, of one wavefront, bring theirs together
+        if (8 * c < a.rotary_dim) {
+            float co[4], si[4];
+            angles<DT, 4>(a, 4 * c, row, u.pos + slot - u.lo, co, si);
+            *reinterpret_cast<float4 *>(&sTurn[slot][4 * c]) = make_float4(co[0], co[1], co[2], co[3]);
+            *reinterpret_cast<float4 *>(&sTurn[slot][64 + 4 * c]) = make_float4(si[0], si[1], si[2], si[3]);
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         Turn t;
-        turn_of<DT>(a, c, row, u.pos + slot - u.lo, t);
+        turn_of(a, sTurn[slot], c, t);
         values<DT>(kr, k);
-        norm_and_turn(a, c, a.k_norm != nullptr, kwt, t, k);
-        for (int j = 0; j < a.group; ++j) {
-            float x[8];
-            values<DT>(q, x);
-            if (j + 1 < a.group) q = load_row<DT>(a.q, a.q_stride, row, h * a.group + j + 1, c);
-            norm_and_turn(a, c, a.q_norm != nullptr, qw, t, x);
-            put_query<DT>(a, row, h * a.group + j, c, x);
+        norm_and_turn(a, c, a.k_norm != nullptr, kw, t, k);
+        for (int j0 = 0; j0 < a.group; j0 += kAhead) {
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) {
+                const int head = j0 + j;
+                if (head >= a.group) break;
+                float x[8];
+                values<DT>(q[j], x);
+                if (head + kAhead < a.group) q[j] = load_row<DT>(a.q, a.q_stride, row, h * a.group + head + kAhead, c);
+                norm_and_turn(a, c, a.q_norm != nullptr, qw, t, x);
+                put_query<DT>(a, row, h * a.group + head, c, x);
+            }
         }
     }
     put_block<DT>(a, u, h, valid, k, v);
 }
 
+// K and V of one token, by the 16 lanes of its thread row; all threads of the workgroup call.  fp8 blocks that are continued: as
+// store_block, but the scales are found without the other wavefronts, and the workgroup comes together only to round earlier codes again.
+template <int DT>
+__device__ __forceinline__ void put_token(const ProjectionLaunch &a, const Unit &u, int h, bool valid, const float (&k)[8], const Row<DT> &v) {
+    const int tid = threadIdx.x, c = tid & 15, d = 8 * c;
+    const size_t blk = ((size_t)u.block * a.pool.num_kv_heads + h) * kBlockElems;
+    if constexpr (DT == 0) {
+        if (!valid) return;
+        *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.pool.k_pages) + blk + (d >> 5) * 512 + u.lo * 32 + (d & 31)) = pack8(k);
+        uint16_t *vd = static_cast<uint16_t *>(a.pool.v_pages) + blk + d * kPage + u.lo;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) vd[j * kPage] = (uint16_t)(v.w[0][j >> 1] >> (16 * (j & 1)));
+    } else if constexpr (DT == 1) {
+        __shared__ float sScales[4];  // K's and V's old scale, and new
+        const size_t at = (size_t)u.block * a.pool.num_kv_heads + h;
+        uint8_t *kb = static_cast<uint8_t *>(a.pool.k_pages) + blk, *vb = static_cast<uint8_t *>(a.pool.v_pages) + blk;
+        if (valid) {
+            float vf[8], am[2] = {0.f, 0.f}, old[2] = {0.f, 0.f}, sc[2];
+            unpack_bf16(v.w[0], vf);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                am[0] = fmaxf(am[0], fabsf(k[j]));
+                am[1] = fmaxf(am[1], fabsf(vf[j]));
+            }
+            if (u.lo > 0) {
+                old[0] = a.pool.k_scale[at];
+                old[1] = a.pool.v_scale[at];
+            }
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+                const float m = row16_max(am[i]);
+                const float cand = m > 0.f ? m / 448.0f : 0.f;
+                sc[i] = u.lo > 0 && old[i] >= cand ? old[i] : cand;  // an unset (NaN) old scale gives cand
+                if (!(sc[i] > 0.f)) sc[i] = 1.0f;
+            }
+            if (c == 0) {
+                a.pool.k_scale[at] = sc[0];
+                a.pool.v_scale[at] = sc[1];
+                sScales[0] = old[0];
+                sScales[1] = old[1];
+                sScales[2] = sc[0];
+                sScales[3] = sc[1];
+            }
+            *reinterpret_cast<u32x2 *>(kb + (d >> 6) * 1024 + u.lo * 64 + (d & 63)) = u32x2{quant4(k[0], k[1], k[2], k[3], sc[0]), quant4(k[4], k[5], k[6], k[7], sc[0])};
+            const u32x2 vc = {quant4(vf[0], vf[1], vf[2], vf[3], sc[1]), quant4(vf[4], vf[5], vf[6], vf[7], sc[1])};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) vb[(d + j) * kPage + u.lo] = (uint8_t)(vc[j >> 2] >> (8 * (j & 3)));
+        }
+        if (u.lo == 0) return;
+        __syncthreads();
+        const float ko = sScales[0], vo = sScales[1], ks = sScales[2], vs = sScales[3];
+        const int slot = tid >> 4;
+        if (ks > ko && slot < u.lo) {
+            u32x2 *p = reinterpret_cast<u32x2 *>(kb + (d >> 6) * 1024 + slot * 64 + (d & 63));
+            const u32x2 w = *p;
+            *p = u32x2{requant4(w[0], ko, ks), requant4(w[1], ko, ks)};
+        }
+        const int s0 = 8 * (tid & 1);
+        if (vs > vo && s0 < u.lo) {  // eight slots of a dimension
+            uint8_t *p = vb + (tid >> 1) * kPage + s0;
+            u32x2 w = *reinterpret_cast<const u32x2 *>(p);
+            w[0] = requant4(w[0], vo, vs);
+            w[1] = requant4(w[1], vo, vs);
+            if (s0 + 8 <= u.lo)
+                *reinterpret_cast<u32x2 *>(p) = w;
+            else
+                for (int j = 0; s0 + j < u.lo; ++j) p[j] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
+        }
+    } else {
+        put_block<DT>(a, u, h, valid, k, v);
+    }
+}
+
 // One KV head of one token: thread row u.lo takes K and V, the others a query head each (the 16th, too, is K's row's).
 template <int DT>
 __device__ __forceinline__ void store_token(const ProjectionLaunch &a, const Unit &u, int h) {
+    __shared__ __align__(16) float sTurn[2 * 64];
     const int g = threadIdx.x >> 4, c = threadIdx.x & 15;
     const bool valid = g == u.lo;
     const int j = (g - u.lo - 1) & 15;
     const int64_t row = a.row_map ? a.row_map[u.row] : u.row;
     float k[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    Row<DT> v{};
+    Row<DT> kr{}, v{}, q{};
+    float w[8] = {}, kw[8] = {};
+    if (valid) {
+        kr = load_row<DT>(a.k, a.k_stride, row, h, c);
+        v = load_row<DT>(a.v, a.v_stride, row, h, c);
+        load_weight<DT>(a.k_norm, c, kw);
+    }
+    if (j < a.group) {
+        q = load_row<DT>(a.q, a.q_stride, row, h * a.group + j, c);
+        load_weight<DT>(a.q_norm, c, w);
+    }
+    if ((int)threadIdx.x < a.rotary_dim / 2) {  // an angle a lane, for all heads
+        float co[1], si[1];
+        angles<DT, 1>(a, threadIdx.x, row, u.pos, co, si);
+        sTurn[threadIdx.x] = co[0];
+        sTurn[64 + threadIdx.x] = si[0];
+    }
+    __syncthreads();
     if (valid || j < a.group) {
-        Row<DT> r{}, q{};
-        if (valid) {
-            r = load_row<DT>(a.k, a.k_stride, row, h, c);
-            v = load_row<DT>(a.v, a.v_stride, row, h, c);
-        }
-        if (j < a.group) q = load_row<DT>(a.q, a.q_stride, row, h * a.group + j, c);
-        float w[8] = {};
         Turn t;
-        turn_of<DT>(a, c, row, u.pos, t);
+        turn_of(a, sTurn, c, t);
         if (j < a.group) {
             float x[8];
-            load_weight<DT>(a.q_norm, c, w);
             values<DT>(q, x);
             norm_and_turn(a, c, a.q_norm != nullptr, w, t, x);
             put_query<DT>(a, row, h * a.group + j, c, x);
         }
         if (valid) {
-            load_weight<DT>(a.k_norm, c, w);
-            values<DT>(r, k);
-            norm_and_turn(a, c, a.k_norm != nullptr, w, t, k);
+            values<DT>(kr, k);
+            norm_and_turn(a, c, a.k_norm != nullptr, kw, t, k);
         }
     }
-    put_block<DT>(a, u, h, valid, k, v);
+    put_token<DT>(a, u, h, valid, k, v);
 }
 
 // The newest tokens of a decode plan's requests.  grid: (requests x blocks that the tokens of one can span, KV heads)
