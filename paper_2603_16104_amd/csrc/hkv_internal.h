@@ -225,11 +225,13 @@ struct ProjectionPrefill {
     int32_t tokens[kMaxInlineRequests];
 };
 
-// One workgroup's keys of attn_decode_plan_weights: up to kWeightTokens tokens of a node from tok_begin on, one KV head, all rows below the node.
-constexpr int kWeightTokens = 128;
+// Keys of attn_decode_plan_weights: up to `length` tokens of a node from tok_begin on, one KV head, all rows below the node.  A workgroup's items are
+// kWeightWaves in a row: one for each wavefront, or, of a node of more than 16 rows, one for all of them, listed so many times.
+constexpr int kMaxWeightTokens = 1024, kWeightWaves = 8;
 struct KeyWeightItem {
     int32_t page_off;            // index of the first token's block in the plan's block list
-    int32_t tok_begin;           // within the node, a multiple of 16
+    int32_t tok_begin;           // within the node, a multiple of 32
+    int32_t length;              // at most kMaxWeightTokens; a multiple of 32, for more than 16 rows 32, 64, 128 or a multiple of 256; 0: nothing
     int32_t kv_head;
     int32_t req_off;             // node->request CSR
     int32_t n_req;

@@ -219,22 +219,56 @@ extern "C" int hkv_decode_plan_track_weights(hkv_decode_plan *plan) {
         last[plan->req_leaf[r]] = 1;
         if (plan->reserve_tokens > 0) grows[plan->req_leaf[r]] = r;
     }
-    // the nodes of many rows first: their workgroups take longest
+    auto rows = [&](int v) { return (int64_t)(plan->node_req_indptr[v + 1] - plan->node_req_indptr[v]) * plan->group; };
+    auto room = [&](int v) { return (int64_t)plan->nodes[v].n_tokens + (grows[v] >= 0 ? plan->reserve_tokens - plan->appended : 0); };
+    // Tokens of an item: for nodes of up to 16 rows as many as make 4096 items, a wavefront each (what the chip holds); the others' work goes by tiles
+    // of 16 rows.
+    int64_t keys = 0, work = 0;
+    for (int v = 0; v < n_nodes; ++v) (rows(v) > 16 ? work : keys) += room(v) * Hkv * (rows(v) > 16 ? (rows(v) + 15) / 16 : rows(v) > 0);
+    const int64_t few_length = std::clamp<int64_t>((keys / 4096 + 31) / 32 * 32, 32, kMaxWeightTokens);
+    // Nodes of many rows get up to 384 workgroups between them (512 are on the chip at once), fewer where the others' keys take most of the time: a
+    // workgroup of theirs takes one of two places of its compute unit.  64 requests' step (2048 shared tokens, 0.7 x 512 own) 16.5 us with 64 of
+    // them, 19.3 with 512; 32 queries' look back at 4 x 6400 tokens 20.8 with 384, 23.4 with 256 and 512.
+    const double many_us = 0.12 / 1024 / 32 * (double)work, few_us = (double)keys * (plan->pool->d.dtype == HKV_BF16 ? 256 : 128) / 5.5e6;
+    const int64_t shares = work > 0 ? std::clamp<int64_t>((int64_t)(384 * many_us / (many_us + few_us)), 64, 384) : 1;
+    auto length_of = [&](int v) -> int64_t {
+        if (rows(v) <= 16) return few_length;
+        const int64_t tokens = work / shares / ((rows(v) + 15) / 16);
+        return tokens < 64 ? 32 : tokens < 128 ? 64 : tokens < 256 ? 128 : std::min<int64_t>(tokens / 256 * 256, kMaxWeightTokens);
+    };
+    std::vector<KeyWeightItem> of[2];  // of nodes of up to 16 rows, of others
     std::vector<int32_t> order(n_nodes);
     std::iota(order.begin(), order.end(), 0);
-    auto requests = [&](int v) { return plan->node_req_indptr[v + 1] - plan->node_req_indptr[v]; };
-    std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return requests(a) > requests(b); });
-    std::vector<KeyWeightItem> items;
+    std::stable_sort(order.begin(), order.end(), [&](int a, int b) { return rows(a) > rows(b); });
     for (int v : order) {
-        if (requests(v) == 0) continue;
+        if (rows(v) == 0) continue;
         const hkv_node &nd = plan->nodes[v];
-        const int64_t room = (int64_t)nd.n_tokens + (grows[v] >= 0 ? plan->reserve_tokens - plan->appended : 0);
-        for (int64_t t = 0; t < room; t += kWeightTokens)
+        const int64_t length = length_of(v);
+        for (int64_t t = 0; t < room(v); t += length)
             for (int h = 0; h < Hkv; ++h)
-                items.push_back(KeyWeightItem{nd.page_begin + (int32_t)(t / HKV_PAGE_SIZE), (int32_t)t, h, plan->node_req_indptr[v], requests(v), last[v] ? v : ~v,
-                                              nd.n_tokens, grows[v] >= 0 ? plan->grow_items[(size_t)grows[v] * Hkv + h] : -1});
+                of[rows(v) > 16].push_back(KeyWeightItem{nd.page_begin + (int32_t)(t / HKV_PAGE_SIZE), (int32_t)t, (int32_t)length, h, plan->node_req_indptr[v],
+                                                         plan->node_req_indptr[v + 1] - plan->node_req_indptr[v], last[v] ? v : ~v, nd.n_tokens,
+                                                         grows[v] >= 0 ? plan->grow_items[(size_t)grows[v] * Hkv + h] : -1});
     }
-    if (items.size() > INT_MAX / 256) return fail(HKV_EINVAL, "%s: too many keys", who);
+    // The two kinds side by side, so that one computes while the other reads; those of many rows, which take longer, in the first three quarters.
+    // In groups that go round all XCDs (workgroup i runs on XCD i % 8) and all heads, so that every XCD gets its part of both; and in no regular
+    // order (the multiples of the golden ratio), since an XCD deals its workgroups out to its four shader engines in turn: every fourth group
+    // of many rows and they all ran on a quarter of the chip, 249 us instead of 110 for 16 prompts of 8192 tokens x 256 rows.
+    const int of_wave = kWeightWaves, workgroups[2] = {((int)of[0].size() + of_wave - 1) / of_wave, (int)of[1].size()};
+    of[0].resize((size_t)workgroups[0] * of_wave, KeyWeightItem{});
+    const int group[2] = {8, std::lcm(8, Hkv)}, n_all = workgroups[0] + workgroups[1];
+    const double share = n_all ? 4.0 / 3.0 * workgroups[1] * group[0] / (workgroups[1] * group[0] + (double)workgroups[0] * group[1]) : 0.0;
+    std::vector<KeyWeightItem> items;
+    items.reserve((size_t)n_all * of_wave);
+    int at[2] = {0, 0};
+    for (int64_t i = 1; at[0] + at[1] < n_all; ++i) {
+        const double x = (double)i * 0.6180339887498949;
+        int k = x - std::floor(x) < share;
+        if (at[k] == workgroups[k]) k = !k;
+        for (const int end = std::min(at[k] + group[k], workgroups[k]); at[k] < end; ++at[k])
+            for (int w = 0; w < of_wave; ++w) items.push_back(k ? of[1][at[1]] : of[0][(size_t)at[0] * of_wave + w]);
+    }
+    if (items.size() > INT_MAX / 64) return fail(HKV_EINVAL, "%s: too many keys", who);
     if (plan->dev && !items.empty()) {
         KeyWeightItem *d = nullptr;
         HKV_HIP(hipMalloc((void **)&d, sizeof(KeyWeightItem) * items.size()));

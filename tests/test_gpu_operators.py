@@ -407,6 +407,12 @@ WEIGHTS = [  # dtype, heads, page, parents, tokens, last nodes, tokens per reque
     (hkv.FP8_E4M3, (8, 2), 16, [-1, 0, 0, 0], [300, 17, 1, 129], [1, 2, 3], 1, 1.0, 1),
     (hkv.FP8_E4M3, (10, 2), 32, [-1, 0, 0], [33, 31, 200], [1, 2], 21, 0.0, 21),
     (hkv.FP8_E4M3, (8, 1), 16, [-1] + [0] * 40, [260] + [20] * 40, list(range(1, 41)), 1, 0.9, 1),
+    # a workgroup's keys are 64, 128, 256 and 512 of one long node, its rows less and more than it holds at a time; then wavefronts of 96 keys
+    (hkv.BF16, (24, 8), 16, [-1], [4003], [0], 8, 1.0, 3),
+    (hkv.FP8_E4M3, (24, 8), 32, [-1], [7001], [0], 8, 0.5, 0),
+    (hkv.BF16, (24, 8), 64, [-1], [13001], [0], 6, 0.0, 6),
+    (hkv.FP8_E4M3, (8, 2), 16, [-1] + [0] * 80, [40001] + [16] * 80, list(range(1, 81)), 1, 1.0, 1),
+    (hkv.BF16, (8, 8), 16, [-1, 0], [35000, 12345], [1], 2, 0.9, 1),
 ]
 
 
@@ -486,6 +492,36 @@ def test_rows_without_a_finite_lse_add_nothing(dtype):
     want = key_weights(pool.values()[0], weight_nodes(parent, tokens, blocks, leaves, 1), q64, l64, SCALE, heads, np.zeros(w.shape), 1.0, 1, 1)
     got = w.cpu().double().numpy()
     assert np.isfinite(got).all() and (np.abs(got - want) <= WEIGHT_TOL * want).all()
+    hkv.hkv_decode_plan_destroy(plan)
+    pool.close()
+
+
+@pytest.mark.parametrize("n_req", [2, 12])
+def test_a_key_that_is_no_number_gets_nothing(n_req):
+    """Drafted tokens of a tree: a NaN or infinite key spoils the rows that see it and no other key's sum."""
+    hq, heads, T, n = 4, 1, 3, 20
+    pool = Pool(2 * n_req, heads, hkv.BF16)
+    nodes = [(-1, 2 * r, 2, n) for r in range(n_req)]
+    masks = np.tile(np.asarray([1, 3, 5], dtype=np.uint64), n_req)       # two tokens under the first
+    plan = hkv.hkv_decode_plan_create_tree(pool.handle, nodes, np.arange(2 * n_req), np.arange(n_req), T, masks, hq)
+    k = pool.k.view(2 * n_req, 4, 16, 32)
+    k[1, 0, 2, 7] = float("nan")                                         # request 0's drafted token 1, seen by itself alone
+    k[3, 0, 3, 0] = float("inf")                                         # request 1's drafted token 2
+    q = torch.randn(n_req * T, hq, 128, device="cuda").to(torch.bfloat16)
+    out, lse = torch.empty_like(q), torch.empty(n_req * T, hq, device="cuda")
+    ws = torch.empty(hkv.hkv_decode_plan_workspace_bytes(plan) + 256, dtype=torch.uint8, device="cuda")
+    hkv.attn_decode_plan_run(plan, q, SCALE, out, lse, ws, ws.numel())
+    lse[1] = float("nan")
+    lse[T + 2] = float("inf")
+    w = torch.zeros(2 * n_req, heads, 16, device="cuda")
+    hkv.hkv_decode_plan_track_weights(plan)
+    hkv.attn_decode_plan_weights(plan, q, SCALE, lse, 1.0, 3, w)
+    torch.cuda.synchronize()
+    got = w.cpu().double().numpy()[:, 0].reshape(n_req, 32)[:, :n]
+    assert np.isfinite(got).all() and got[0, 18] == 0 and got[1, 19] == 0
+    gave = np.full(n_req, float(T * hq))
+    gave[:2] -= hq                                                       # the spoilt rows
+    assert np.abs(got.sum(1) - gave).max() <= 1e-3 * T * hq
     hkv.hkv_decode_plan_destroy(plan)
     pool.close()
 
