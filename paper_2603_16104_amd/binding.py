@@ -633,11 +633,12 @@ def kv_pool_evict(pool, src_pages, n_tokens, dst_pages, n_keep, n_first: int, n_
     src, dst, n, m = _host_i32(src_pages), _host_i32(dst_pages), _host_i32(n_tokens), _host_i32(n_keep)
     if len(n) != len(m):
         raise HkvError(EINVAL, "kv_pool_evict: n_tokens and n_keep differ in length")
-    page = kv_pool_page_size(pool)
-    for ids, count, name in ((src, n, "src_pages"), (dst, m, "dst_pages")):
-        need = int(((np.maximum(count, 0).astype(np.int64) + page - 1) // page).sum())
-        if len(ids) < need:
-            raise HkvError(EINVAL, f"kv_pool_evict: {need} page ids needed in {name}, {len(ids)} given")
+    page = lib().kv_pool_page_size(pool)
+    if page > 0:  # (a null pool is the library's to refuse)
+        for ids, count, name in ((src, n, "src_pages"), (dst, m, "dst_pages")):
+            need = sum(-(-c // page) for c in count.tolist()) if len(count) <= 32 else int((-(-count.astype(np.int64) // page)).sum())
+            if len(ids) < need:
+                raise HkvError(EINVAL, f"kv_pool_evict: {need} page ids needed in {name}, {len(ids)} given")
     _run(lib().kv_pool_evict, pool, len(n), _host_addr(src), _host_addr(n), _host_addr(dst), _host_addr(m), n_first, n_recent, _addr(key_weights),
          _addr(kept), _stream_addr(stream) if len(n) > 0 else None)
 

@@ -1,18 +1,24 @@
 // Eviction: per sequence and KV head the heaviest tokens are chosen and moved, in order, to other blocks (kv_pool_evict).
 //
-// Choosing: the weights as integers in the order of the numbers, the k-th largest by its bits from the top (four histograms of 256
-// bins), then the tokens above it and as many of its equals as are left, lowest index first, written in order by counts over wavefronts.
-// One workgroup per (sequence, head); bound by the chain of its passes.
-// Moving: one workgroup per (new block, head); 16 tokens come from 16 places.  K's dimensions lie in runs of 64 bytes a token, V's are
-// 16 tokens wide, so that V is read in whole blocks however few of their tokens are kept.  fp8 blocks get the scale of what they
-// hold now and are rounded again, as a block written anew.
+// Choosing: the weights as integers in the order of the numbers, kept in registers; the k-th largest is found from its highest bits down by three
+// histograms of 11 bits in LDS.  Then the tokens above it and as many of its equals as are left, lowest index first, written in order
+// by counts over wavefronts.  One workgroup per (sequence, head); bound by the chain of its steps.
+// Moving: one wavefront per (new block, head); 16 tokens come from 16 places.  K's dimensions lie in runs of 64 bytes a token, V's are
+// 16 tokens wide, so that V is read in whole blocks however few of their tokens are kept.  A lane takes all 16 tokens of two of V's dimensions: its
+// 32 loads are on their way together, neighbouring lanes read neighbouring dimensions, and what it holds goes out as it lies in the
+// block.  fp8 blocks get the scale of what they hold now and are rounded again, as a block written anew.
+#include <type_traits>
+
 #include "pool_block.h"
 
 namespace hkv {
 
 namespace {
 
-constexpr int kChooseThreads = 1024, kChooseWaves = kChooseThreads / 64;
+constexpr int kChooseThreads = 1024, kChooseWaves = kChooseThreads / 64, kMaxRounds = 32;  // a round: a token a thread
+
+__device__ __forceinline__ const int32_t *meta_of(const EvictLaunch &a) { return a.meta; }
+__device__ __forceinline__ const int32_t *meta_of(const EvictInline &a) { return a.list; }
 
 // Order of the weights as integers: NaN below every number, both zeros equal.
 __device__ __forceinline__ uint32_t key_of(float w) {
@@ -21,204 +27,299 @@ __device__ __forceinline__ uint32_t key_of(float w) {
     return u >> 31 ? ~u : u | 0x80000000u;
 }
 
-__global__ __launch_bounds__(kChooseThreads) void evict_choose_kernel(EvictLaunch a) {
-    const EvictSequence q = reinterpret_cast<const EvictSequence *>(a.meta)[blockIdx.x];
-    const int h = blockIdx.y, Hkv = a.pool.num_kv_heads, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+// N: keys a thread keeps in registers (0: more tokens than that, the weights are read again for every step).
+template <int N, class Args>
+__global__ __launch_bounds__(kChooseThreads) void evict_choose_kernel(Args a) {
+    const int32_t *const meta = meta_of(a);
+    const EvictSequence q = reinterpret_cast<const EvictSequence *>(meta)[blockIdx.x];
+    const int h = blockIdx.y, Hkv = a.pool.num_kv_heads, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     int32_t *kept = a.kept + (size_t)h * a.total + q.kept;
     if (q.keep >= q.tokens) {
         for (int t = tid; t < q.tokens; t += kChooseThreads) kept[t] = t;
         return;
     }
-    __shared__ int sBins[kChooseWaves][256];
-    __shared__ int sCount[2][kChooseWaves];
-    __shared__ uint32_t sPrefix;
-    __shared__ int sLeft;
+    __shared__ int sBins[2 * kChooseThreads];
+    __shared__ int sWave[kChooseWaves];
+    __shared__ int sPick[2];  // the digit of the last one chosen, and how many there are above it with the same digits before
+    __shared__ int sRank[2][kMaxRounds * kChooseWaves + 1];  // of the wavefronts of a round: what is sure to stay, and equals of the last one
     const int begin = a.n_first, end = q.tokens - a.n_recent;  // those in between are chosen from
-    auto key_at = [&](int t) { return key_of(a.weights[((size_t)a.meta[q.src + (t >> 4)] * Hkv + h) * kPage + (t & 15)]); };
-
-    // the key of the last one chosen, and how many of its equals are chosen
-    uint32_t prefix = 0;
-    int left = q.keep - a.n_first - a.n_recent;
+    const int left = q.keep - a.n_first - a.n_recent, rounds = (q.tokens + kChooseThreads - 1) / kChooseThreads;
+    auto chosen_from = [&](int t) { return t >= begin && t < end; };
+    auto block_at = [&](int t) { return meta[q.src + (min(t, q.tokens - 1) >> 4)]; };
+    auto weight_at = [&](int t, int block) { return a.weights[((size_t)block * Hkv + h) * kPage + (min(t, q.tokens - 1) & 15)]; };
+    auto key_at = [&](int t, float w) { return chosen_from(t) ? key_of(w) : 0u; };  // 0: not chosen from (or no number)
+    uint32_t keys[N > 0 ? N : 1];
+    if constexpr (N > 0) {  // (all loads at once)
+        int block[N];
+        float w[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) block[i] = block_at(i * kChooseThreads + tid);
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[i] = weight_at(i * kChooseThreads + tid, block[i]);
+#pragma unroll
+        for (int i = 0; i < N; ++i) keys[i] = key_at(i * kChooseThreads + tid, w[i]);
+    }
+    auto each = [&](int from, int to, auto &&f) {  // f(round, key of this thread's token), for some rounds or, in registers, all
+        if constexpr (N > 0) {
+#pragma unroll
+            for (int i = 0; i < N; ++i)
+                if (i < rounds) f(i, keys[i]);
+        } else {
+            constexpr int kAtOnce = 8;
+            for (int i0 = from; i0 < to; i0 += kAtOnce) {
+                int block[kAtOnce];
+                float w[kAtOnce];
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i) block[i] = block_at((i0 + i) * kChooseThreads + tid);
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i) w[i] = weight_at((i0 + i) * kChooseThreads + tid, block[i]);
+#pragma unroll
+                for (int i = 0; i < kAtOnce; ++i)
+                    if (i0 + i < to) f(i0 + i, key_at((i0 + i) * kChooseThreads + tid, w[i]));
+            }
+        }
+    };
+    // `last`: the key of the last one chosen (0: there are not so many numbers), and how many are above it.
+    uint32_t last = 0;
+    int above = 0;
     if (left > 0)
-        for (int shift = 24; shift >= 0; shift -= 8) {
-            for (int i = tid; i < kChooseWaves * 256; i += kChooseThreads) (&sBins[0][0])[i] = 0;
+        for (int shift = 21;; shift = shift == 21 ? 10 : 0) {
+            const int bits = shift > 0 ? 11 : 10, top = 2 * kChooseThreads - 1 - 2 * tid;  // this thread's bins: top, top - 1
+            sBins[top] = sBins[top - 1] = 0;
             __syncthreads();
-            for (int t = begin + tid; t < end; t += kChooseThreads) {
-                const uint32_t k = key_at(t);
-                if (shift == 24 || (k ^ prefix) >> (shift + 8) == 0) atomicAdd(&sBins[wave][k >> shift & 255], 1);
+            each(0, rounds, [&](int, uint32_t k) {
+                if (k != 0 && (shift == 21 || k >> (shift + bits) == last >> (shift + bits))) atomicAdd(&sBins[k >> shift & ((1u << bits) - 1)], 1);
+            });
+            __syncthreads();
+            const int n0 = sBins[top], n1 = sBins[top - 1];
+            int x = n0 + n1;
+            for (int d = 1; d < 64; d <<= 1) {
+                const int y = __shfl_up(x, d);
+                if (lane >= d) x += y;
+            }
+            if (lane == 63) sWave[wave] = x;
+            __syncthreads();
+            int total = 0;
+            x -= n0 + n1;
+#pragma unroll
+            for (int w = 0; w < kChooseWaves; ++w) {
+                if (w < wave) x += sWave[w];
+                total += sWave[w];
+            }
+            const int want = left - above;
+            if (x < want && want <= x + n0) {
+                sPick[0] = top;
+                sPick[1] = x;
+            } else if (x + n0 < want && want <= x + n0 + n1) {
+                sPick[0] = top - 1;
+                sPick[1] = x + n0;
             }
             __syncthreads();
-            if (tid < 256) {
-                int n = 0;
-                for (int w = 0; w < kChooseWaves; ++w) n += sBins[w][tid];
-                sBins[0][tid] = n;
+            if (total < want) {  // (the first time only) no number is the last one
+                above = total;
+                break;
             }
-            __syncthreads();
-            if (wave == 0) {  // lane l: bins 255 - 4 l .. 252 - 4 l
-                int n[4], total = 0;
-                for (int i = 0; i < 4; ++i) total += n[i] = sBins[0][255 - 4 * lane - i];
-                int above = total;
-                for (int d = 1; d < 64; d <<= 1) {
-                    const int x = __shfl_up(above, d);
-                    if (lane >= d) above += x;
-                }
-                above -= total;
-                for (int i = 0; i < 4; ++i) {
-                    if (above < left && left <= above + n[i]) {
-                        sPrefix = prefix | (uint32_t)(255 - 4 * lane - i) << shift;
-                        sLeft = left - above;
-                    }
-                    above += n[i];
-                }
-            }
-            __syncthreads();
-            prefix = sPrefix;
-            left = sLeft;
+            last |= (uint32_t)sPick[0] << shift;
+            above += sPick[1];
+            if (shift == 0) break;
             __syncthreads();
         }
+    const int equals = left - above;  // that are kept
 
-    int base = 0, equal_base = 0;
-    for (int t0 = 0; t0 < q.tokens; t0 += kChooseThreads) {
-        const int t = t0 + tid;
-        const bool free = t >= begin && t < end;
-        const uint32_t k = free && q.keep > a.n_first + a.n_recent ? key_at(t) : 0u;
-        const bool same = free && left > 0 && k == prefix;
-        const uint64_t equals = __ballot(same);
-        if (lane == 0) sCount[0][wave] = __popcll(equals);
+    // Places: by round, wavefront and lane.
+    int base[2] = {0, 0};
+    for (int r0 = 0; r0 < rounds; r0 += kMaxRounds) {
+        auto sure = [&](int i, uint32_t k) {
+            const int t = i * kChooseThreads + tid;
+            return t < q.tokens && (!chosen_from(t) || (left > 0 && k > last));
+        };
+        auto same = [&](int i, uint32_t k) { return left > 0 && chosen_from(i * kChooseThreads + tid) && k == last; };
+        const int r1 = min(rounds, r0 + kMaxRounds), n_ranks = (r1 - r0) * kChooseWaves;
+        each(r0, r1, [&](int i, uint32_t k) {
+            const uint64_t s = __ballot(sure(i, k)), e = __ballot(same(i, k));
+            if (lane == 0) {
+                sRank[0][(i - r0) * kChooseWaves + wave] = __popcll(s);
+                sRank[1][(i - r0) * kChooseWaves + wave] = __popcll(e);
+            }
+        });
         __syncthreads();
-        int rank = equal_base + __popcll(equals & ((1ull << lane) - 1)), all = 0;
-        for (int w = 0; w < kChooseWaves; ++w) {
-            if (w < wave) rank += sCount[0][w];
-            all += sCount[0][w];
+        if (wave < 2) {  // running sums: of what is sure (wavefront 0) and of equals (1)
+            int run = base[wave];
+            for (int j = 0; j < n_ranks; j += 64) {
+                const int n = j + lane < n_ranks ? sRank[wave][j + lane] : 0;
+                int x = n;
+                for (int d = 1; d < 64; d <<= 1) {
+                    const int y = __shfl_up(x, d);
+                    if (lane >= d) x += y;
+                }
+                if (j + lane < n_ranks) sRank[wave][j + lane] = run + x - n;
+                run += __shfl(x, 63);
+            }
+            if (lane == 0) sRank[wave][n_ranks] = run;
         }
-        equal_base += all;
-        const bool keep = t < q.tokens && (!free || (left > 0 && (k > prefix || (same && rank < left))));
-        const uint64_t keeps = __ballot(keep);
-        if (lane == 0) sCount[1][wave] = __popcll(keeps);
         __syncthreads();
-        int at = base + __popcll(keeps & ((1ull << lane) - 1));
-        all = 0;
-        for (int w = 0; w < kChooseWaves; ++w) {
-            if (w < wave) at += sCount[1][w];
-            all += sCount[1][w];
-        }
-        base += all;
-        if (keep && at < q.keep) kept[at] = t;
+        each(r0, r1, [&](int i, uint32_t k) {
+            const bool is_sure = sure(i, k), is_same = same(i, k);
+            const uint64_t s = __ballot(is_sure), e = __ballot(is_same), below = (1ull << lane) - 1;
+            const int j = (i - r0) * kChooseWaves + wave, rank = sRank[1][j] + __popcll(e & below);
+            const int at = sRank[0][j] + __popcll(s & below) + min(equals, rank);
+            if (is_sure || (is_same && rank < equals)) kept[at] = i * kChooseThreads + tid;
+        });
+        base[0] = sRank[0][n_ranks];
+        base[1] = sRank[1][n_ranks];
+        __syncthreads();
     }
 }
 
-template <int DT>
-__global__ __launch_bounds__(256) void evict_move_kernel(EvictLaunch a) {
-    const int x = blockIdx.x, h = blockIdx.y, Hkv = a.pool.num_kv_heads, tid = threadIdx.x, lane = tid & 63;
-    const EvictSequence *seq = reinterpret_cast<const EvictSequence *>(a.meta);
+// Wavefronts go by head first: the blocks that neighbouring new blocks take tokens from are the same, and with 8 heads mostly on one XCD.
+template <int DT, class Args>
+__global__ __launch_bounds__(256) void evict_move_kernel(Args a) {
+    using Elem = std::conditional_t<DT == 0, uint16_t, std::conditional_t<DT == 1, uint8_t, float>>;
+    const int32_t *const meta = meta_of(a);
+    const int Hkv = a.pool.num_kv_heads, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int x = blockIdx.x / Hkv * 4 + wave, h = blockIdx.x % Hkv;
+    if (x >= a.n_units) return;
+    const EvictSequence *seq = reinterpret_cast<const EvictSequence *>(meta);
     int i = -1;  // the last sequence that begins at or before the block
     for (int s = 0; s < a.n_seq; s += 64) i += __popcll(__ballot(s + lane < a.n_seq && seq[min(s + lane, a.n_seq - 1)].unit <= x));
     const EvictSequence q = seq[i];
-    const int j0 = (x - q.unit) * kPage, n = min(kPage, q.keep - j0), to = a.meta[q.dst + (x - q.unit)];
-    const int slot = tid >> 4, c = tid & 15, d0 = 8 * c;
-    const bool valid = slot < n;
-    size_t from = 0;
-    int fs = 0;
-    if (valid) {
-        const int t = a.kept[(size_t)h * a.total + q.kept + j0 + slot];
-        from = (size_t)a.meta[q.src + (t >> 4)] * Hkv + h;
-        fs = t & 15;
-        if (c == 0) a.weights[((size_t)to * Hkv + h) * kPage + slot] = a.weights[from * kPage + fs];
+    const int j0 = (x - q.unit) * kPage, n = min(kPage, q.keep - j0), to = meta[q.dst + (x - q.unit)];
+    const int64_t out = (int64_t)to * Hkv + h;
+    // lane s (and s + 16, ...) knows token s: its old block and slot; behind the last token: that one again
+    const int token = a.kept[(size_t)h * a.total + q.kept + j0 + min(lane & 15, n - 1)];
+    const int block = meta[q.src + (token >> 4)];
+    if (lane < n) a.weights[out * kPage + lane] = a.weights[((int64_t)block * Hkv + h) * kPage + (token & 15)];
+    Elem *const kb = static_cast<Elem *>(a.pool.k_pages), *const vb = static_cast<Elem *>(a.pool.v_pages);
+    constexpr int C = 64 / sizeof(Elem), kChunks = kHeadDim / C;  // K: dimensions of a 64-byte piece
+    // K: lane (token lane / 4, 16 bytes of it) of every piece
+    const int kt = lane >> 2, k_block = __builtin_amdgcn_ds_bpermute(4 * kt, block), k_slot = __builtin_amdgcn_ds_bpermute(4 * kt, token) & 15;
+    const int64_t k_from = (int64_t)k_block * Hkv + h;
+    const char *ks = reinterpret_cast<const char *>(kb + k_from * kBlockElems) + 64 * k_slot + 16 * (lane & 3);
+    u32x4 kw[kChunks];
+#pragma unroll
+    for (int c = 0; c < kChunks; ++c) kw[c] = ld16(ks + 1024 * c);
+    Elem v[2][kPage];
+    float vs[kPage];
+#pragma unroll
+    for (int s = 0; s < kPage; ++s) {
+        const int64_t from = (int64_t)__builtin_amdgcn_readlane(block, s) * Hkv + h;
+        const Elem *p = vb + from * kBlockElems + (__builtin_amdgcn_readlane(token, s) & 15);
+        v[0][s] = p[lane * kPage];
+        v[1][s] = p[(lane + 64) * kPage];
+        if constexpr (DT == 1) vs[s] = a.pool.v_scale[from];
     }
-    const size_t src = from * kBlockElems, blk = ((size_t)to * Hkv + h) * kBlockElems;
-    if constexpr (DT == 0) {
-        u32x4 kw = {0u, 0u, 0u, 0u}, vw = {0u, 0u, 0u, 0u};
-        if (valid) {
-            kw = ld16(static_cast<const uint16_t *>(a.pool.k_pages) + src + (d0 >> 5) * 512 + fs * 32 + (d0 & 31));
-            const uint16_t *v = static_cast<const uint16_t *>(a.pool.v_pages) + src + d0 * kPage + fs;
+    u32x4 vw[2][kPage * sizeof(Elem) / 16];  // what goes out: two dimensions, 16 slots each
+    if constexpr (DT == 1) {
+        const float kscale = a.pool.k_scale[k_from];
+        float kf[kChunks][16], ka = 0.f, va = 0.f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) vw[j] = (uint32_t)v[2 * j * kPage] | (uint32_t)v[(2 * j + 1) * kPage] << 16;
-        }
-        const float none[8] = {};
-        store_block<0>(a.pool, to, h, valid, kw, none, vw, 0, n);
-    } else if constexpr (DT == 1) {
-        __shared__ uint32_t sV[kPage][kHeadDim / 4 + 1];
-        __shared__ float sRed[2][4];
-        float kf[8] = {}, vf[8] = {}, ka = 0.f, va = 0.f;
-        if (valid) {
-            const float ks = a.pool.k_scale[from], vs = a.pool.v_scale[from];
-            const u32x2 kw = *reinterpret_cast<const u32x2 *>(static_cast<const uint8_t *>(a.pool.k_pages) + src + (d0 >> 6) * 1024 + fs * 64 + (d0 & 63));
-            const uint8_t *v = static_cast<const uint8_t *>(a.pool.v_pages) + src + d0 * kPage + fs;
-            u32x2 vw = {0u, 0u};
+        for (int c = 0; c < kChunks; ++c)
 #pragma unroll
-            for (int j = 0; j < 8; ++j) vw[j >> 2] |= (uint32_t)v[j * kPage] << (8 * (j & 3));
+            for (int j = 0; j < 4; ++j) {
+                const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)kw[c][j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)kw[c][j], true);
+                kf[c][4 * j] = lo[0] * kscale, kf[c][4 * j + 1] = lo[1] * kscale, kf[c][4 * j + 2] = hi[0] * kscale, kf[c][4 * j + 3] = hi[1] * kscale;
 #pragma unroll
-            for (int j = 0; j < 2; ++j) {
-                const auto k0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)kw[j], false), k1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)kw[j], true);
-                const auto v0 = __builtin_amdgcn_cvt_pk_f32_fp8((int)vw[j], false), v1 = __builtin_amdgcn_cvt_pk_f32_fp8((int)vw[j], true);
-                kf[4 * j] = k0[0] * ks, kf[4 * j + 1] = k0[1] * ks, kf[4 * j + 2] = k1[0] * ks, kf[4 * j + 3] = k1[1] * ks;
-                vf[4 * j] = v0[0] * vs, vf[4 * j + 1] = v0[1] * vs, vf[4 * j + 2] = v1[0] * vs, vf[4 * j + 3] = v1[1] * vs;
+                for (int e = 0; e < 4; ++e) ka = fmaxf(ka, fabsf(kf[c][4 * j + e]));
             }
+        float vf[2][kPage];
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                ka = fmaxf(ka, fabsf(kf[j]));
-                va = fmaxf(va, fabsf(vf[j]));
-            }
+        for (int s = 0; s < kPage; ++s) {
+            const auto c = __builtin_amdgcn_cvt_pk_f32_fp8((int)v[0][s] | (int)v[1][s] << 8, false);
+            vf[0][s] = c[0] * vs[s];
+            vf[1][s] = c[1] * vs[s];
+            va = fmaxf(va, fmaxf(fabsf(vf[0][s]), fabsf(vf[1][s])));
         }
-        ka = wave_max(ka);
+        ka = wave_max(ka);  // (tokens taken again behind the last one do not change it)
         va = wave_max(va);
+        const float kscale1 = ka > 0.f ? ka / 448.0f : 1.0f, vscale1 = va > 0.f ? va / 448.0f : 1.0f;
         if (lane == 0) {
-            sRed[0][tid >> 6] = ka;
-            sRed[1][tid >> 6] = va;
+            a.pool.k_scale[out] = kscale1;
+            a.pool.v_scale[out] = vscale1;
         }
-        __syncthreads();
-        ka = fmaxf(fmaxf(sRed[0][0], sRed[0][1]), fmaxf(sRed[0][2], sRed[0][3]));
-        va = fmaxf(fmaxf(sRed[1][0], sRed[1][1]), fmaxf(sRed[1][2], sRed[1][3]));
-        const float ks = ka > 0.f ? ka / 448.0f : 1.0f, vs = va > 0.f ? va / 448.0f : 1.0f;
-        if (tid == 0) {
-            a.pool.k_scale[(size_t)to * Hkv + h] = ks;
-            a.pool.v_scale[(size_t)to * Hkv + h] = vs;
-        }
-        if (valid) {
-            *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(a.pool.k_pages) + blk + (d0 >> 6) * 1024 + slot * 64 + (d0 & 63)) =
-                u32x2{quant4(kf[0], kf[1], kf[2], kf[3], ks), quant4(kf[4], kf[5], kf[6], kf[7], ks)};
-            sV[slot][2 * c] = quant4(vf[0], vf[1], vf[2], vf[3], vs);
-            sV[slot][2 * c + 1] = quant4(vf[4], vf[5], vf[6], vf[7], vs);
-        }
-        __syncthreads();
-        // thread (dim, half): eight slots of a dimension
-        const int d = tid >> 1, s0 = 8 * (tid & 1), sh = 8 * (d & 3);
-        uint8_t *vd = static_cast<uint8_t *>(a.pool.v_pages) + blk + d * kPage + s0;
-        if (s0 + 8 <= n) {
-            u32x2 w = {0u, 0u};
+        const float ki = 1.0f / kscale1, vi = 1.0f / vscale1;
+        auto encode = [&](auto &&four) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) w[j >> 2] |= (sV[s0 + j][d >> 2] >> sh & 255u) << (8 * (j & 3));
-            *reinterpret_cast<u32x2 *>(vd) = w;
+            for (int j = 0; j < 4; ++j) {
+#pragma unroll
+                for (int c = 0; c < kChunks; ++c) kw[c][j] = four(kf[c] + 4 * j, kscale1, ki);
+#pragma unroll
+                for (int d = 0; d < 2; ++d) vw[d][0][j] = four(vf[d] + 4 * j, vscale1, vi);
+            }
+        };
+        const float least = fminf(kscale1, vscale1), most = fmaxf(kscale1, vscale1);
+        if (__builtin_amdgcn_readfirstlane(least >= 0x1p-60f && most <= 0x1p60f)) {
+            // by the reciprocal and a correction, a third of the division's instructions; the quotient is the division's but for its last bit now and then
+            encode([](const float *x, float sc, float inv) { return quant4_by(x[0], x[1], x[2], x[3], sc, inv); });
         } else {
-            for (int j = 0; s0 + j < n; ++j) vd[j] = (uint8_t)(sV[s0 + j][d >> 2] >> sh);
+            encode([](const float *x, float sc, float) { return quant4(x[0], x[1], x[2], x[3], sc); });
         }
-    } else if (valid) {
-        const float *k = static_cast<const float *>(a.pool.k_pages) + src + (d0 >> 4) * 256 + fs * 16 + (d0 & 15);
-        const float *v = static_cast<const float *>(a.pool.v_pages) + src + d0 * kPage + fs;
-        float *kd = static_cast<float *>(a.pool.k_pages) + blk + (d0 >> 4) * 256 + slot * 16 + (d0 & 15);
-        float *vd = static_cast<float *>(a.pool.v_pages) + blk + d0 * kPage + slot;
+    } else {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            kd[j] = k[j];
-            vd[j * kPage] = v[j * kPage];
+        for (int d = 0; d < 2; ++d)
+#pragma unroll
+            for (int j = 0; j < (int)(kPage * sizeof(Elem) / 4); ++j) {
+                if constexpr (DT == 0)
+                    vw[d][j >> 2][j & 3] = (uint32_t)v[d][2 * j] | (uint32_t)v[d][2 * j + 1] << 16;
+                else
+                    vw[d][j >> 2][j & 3] = __float_as_uint(v[d][j]);
+            }
+    }
+    if (kt < n) {
+        char *kd = reinterpret_cast<char *>(kb + out * kBlockElems) + 64 * kt + 16 * (lane & 3);
+#pragma unroll
+        for (int c = 0; c < kChunks; ++c) *reinterpret_cast<u32x4 *>(kd + 1024 * c) = kw[c];
+    }
+#pragma unroll
+    for (int d = 0; d < 2; ++d) {
+        Elem *vd = vb + out * kBlockElems + (lane + 64 * d) * kPage;
+        if (n == kPage) {
+#pragma unroll
+            for (int j = 0; j < (int)(kPage * sizeof(Elem) / 16); ++j) reinterpret_cast<u32x4 *>(vd)[j] = vw[d][j];
+        } else {
+            constexpr int E = sizeof(Elem);
+#pragma unroll
+            for (int s = 0; s < kPage; ++s)
+                if (s < n) {
+                    const uint32_t w = vw[d][s * E / 16][s * E / 4 % 4] >> (8 * (s * E % 4));
+                    if constexpr (DT == 2)
+                        vd[s] = __uint_as_float(w);
+                    else
+                        vd[s] = (Elem)w;
+                }
         }
     }
 }
 
 }  // namespace
 
-hipError_t launch_evict(const EvictLaunch &a, hipStream_t s) {
-    if (a.n_units <= 0) return hipSuccess;
-    hipLaunchKernelGGL(evict_choose_kernel, dim3(a.n_seq, a.pool.num_kv_heads), dim3(kChooseThreads), 0, s, a);
-    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
-    const dim3 grid(a.n_units, a.pool.num_kv_heads), block(256);
-    if (a.pool.dtype == 0)
-        hipLaunchKernelGGL(evict_move_kernel<0>, grid, block, 0, s, a);
-    else if (a.pool.dtype == 1)
-        hipLaunchKernelGGL(evict_move_kernel<1>, grid, block, 0, s, a);
+namespace {
+template <class Args>
+hipError_t go(const Args &a, hipStream_t s) {
+    const int Hkv = a.pool.num_kv_heads, rounds = (a.most_tokens + kChooseThreads - 1) / kChooseThreads;
+    auto choose = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3(a.n_seq, Hkv), dim3(kChooseThreads), 0, s, a); };
+    if (rounds <= 2)
+        choose(evict_choose_kernel<2, Args>);
+    else if (rounds <= 4)
+        choose(evict_choose_kernel<4, Args>);
+    else if (rounds <= 8)
+        choose(evict_choose_kernel<8, Args>);
+    else if (rounds <= 16)
+        choose(evict_choose_kernel<16, Args>);
     else
-        hipLaunchKernelGGL(evict_move_kernel<2>, grid, block, 0, s, a);
+        choose(evict_choose_kernel<0, Args>);
+    if (hipError_t e = hipGetLastError(); e != hipSuccess) return e;
+    auto move = [&](auto kernel) { hipLaunchKernelGGL(kernel, dim3((unsigned)((a.n_units + 3) / 4) * Hkv), dim3(256), 0, s, a); };
+    if (a.pool.dtype == 0)
+        move(evict_move_kernel<0, Args>);
+    else if (a.pool.dtype == 1)
+        move(evict_move_kernel<1, Args>);
+    else
+        move(evict_move_kernel<2, Args>);
     return hipGetLastError();
 }
+}  // namespace
+
+hipError_t launch_evict(const EvictLaunch &a, hipStream_t s) { return a.n_units <= 0 ? hipSuccess : go(a, s); }
+hipError_t launch_evict(const EvictInline &a, hipStream_t s) { return a.n_units <= 0 ? hipSuccess : go(a, s); }
 
 }  // namespace hkv

@@ -267,7 +267,14 @@ struct EvictLaunch {
     int32_t *kept;               // [Hkv][total]
     int64_t total;
     int32_t n_seq, n_units, n_first, n_recent;
+    int32_t most_tokens;         // of a sequence
 };
+// The same with what is short enough in the arguments instead of at `meta`.
+constexpr int kMaxInlineEvict = 960;
+struct EvictInline : EvictLaunch {
+    int32_t list[kMaxInlineEvict];
+};
+static_assert(sizeof(EvictInline) <= 4096, "kernel argument segment");
 
 // Whole-page copies inside one pool (copy-on-write of pages that several holders share).
 constexpr int kMaxCopyPairs = 32;
@@ -402,6 +409,7 @@ hipError_t launch_projection_store(const ProjectionPrefill &a, hipStream_t s);
 hipError_t launch_projection_append(const ProjectionLaunch &a, const PlanGrowInline &g, hipStream_t s);
 hipError_t launch_key_weights(const KeyWeightsLaunch &a, hipStream_t s);
 hipError_t launch_evict(const EvictLaunch &a, hipStream_t s);
+hipError_t launch_evict(const EvictInline &a, hipStream_t s);
 hipError_t launch_pool_copy(const PoolCopyLaunch &a, hipStream_t s);
 hipError_t launch_pool_dequant(const PoolDequantLaunch &a, hipStream_t s);
 // Once per device (later calls only read the result), with that device current and outside graph capture:

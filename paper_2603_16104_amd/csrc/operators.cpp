@@ -328,7 +328,7 @@ extern "C" int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_p
     if (total == 0) return HKV_OK;
     if (!src_pages || !dst_pages || !key_weights || !kept) return fail(HKV_EINVAL, "%s: null argument", who);
     if (!aligned16(key_weights) || (reinterpret_cast<uintptr_t>(kept) & 3)) return fail(HKV_EINVAL, "%s: key_weights must be 16-byte aligned, kept 4-byte", who);
-    if (total > INT_MAX) return fail(HKV_EINVAL, "%s: too many tokens", who);
+    if (total > INT_MAX || total / 16 * pool->d.num_kv_heads > INT_MAX / 256) return fail(HKV_EINVAL, "%s: too many tokens", who);
     for (int64_t i = 0; i < src; ++i)
         if (src_pages[i] < 0 || src_pages[i] >= pool->d.num_pages)
             return fail(HKV_ERANGE, "%s: page id %d (entry %lld of src_pages) outside pool of %d pages", who, src_pages[i], (long long)i, pool->d.num_pages);
@@ -349,7 +349,7 @@ extern "C" int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_p
     for (int64_t i = 0; i < src; ++i)
         if (pool->mark[src_pages[i]] == pool->mark_now) return fail(HKV_EINVAL, "%s: page %d is read and written", who, src_pages[i]);
 
-    EvictLaunch a{};
+    EvictInline a{};
     a.pool = PoolWriteLaunch{pool->d.k_pages, pool->d.v_pages, pool->d.k_scale, pool->d.v_scale, pool->d.num_kv_heads, pool->d.dtype, nullptr, 0, 0, 0, nullptr, nullptr, nullptr, nullptr};
     a.weights = key_weights;
     a.kept = kept;
@@ -364,8 +364,11 @@ extern "C" int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_p
         int64_t ints = 0;
         int i1 = i0;
         while (i1 < n_seq && ints + ints_of(i1) <= hkv_pool::kMaxWritePages) ints += ints_of(i1++);
-        int32_t slot, *hm, *hdm, *dm;
-        if (int rc = take_staging(pool, &slot, &hm, &hdm, &dm)) return rc;
+        // what the kernels index with: in their arguments where it fits (2.2 us of a call less), else through the ring
+        const bool in_arguments = ints <= kMaxInlineEvict;
+        int32_t slot = 0, *hm = a.list, *hdm = nullptr, *dm = nullptr;
+        if (!in_arguments)
+            if (int rc = take_staging(pool, &slot, &hm, &hdm, &dm)) return rc;
         int32_t at = (i1 - i0) * kRecord, unit = 0;
         for (int i = i0; i < i1; ++i) {
             const int nb = (n_tokens[i] + 15) / 16, mb = (n_keep[i] + 15) / 16;
@@ -382,9 +385,14 @@ extern "C" int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_p
         a.meta = dm;
         a.n_seq = i1 - i0;
         a.n_units = unit;
-        HKV_HIP(launch_upload(hdm, dm, align_up(sizeof(int32_t) * (size_t)at, 16), s));
-        HKV_HIP(launch_evict(a, s));
-        if (int rc = leave_staging(pool, slot, s)) return rc;
+        a.most_tokens = *std::max_element(n_tokens + i0, n_tokens + i1);
+        if (in_arguments) {
+            HKV_HIP(launch_evict(a, s));
+        } else {
+            HKV_HIP(launch_upload(hdm, dm, align_up(sizeof(int32_t) * (size_t)at, 16), s));
+            HKV_HIP(launch_evict(static_cast<const EvictLaunch &>(a), s));
+            if (int rc = leave_staging(pool, slot, s)) return rc;
+        }
         i0 = i1;
     }
     return HKV_OK;
