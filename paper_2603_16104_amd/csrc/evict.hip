@@ -20,11 +20,16 @@ constexpr int kChooseThreads = 1024, kChooseWaves = kChooseThreads / 64, kMaxRou
 __device__ __forceinline__ const int32_t *meta_of(const EvictLaunch &a) { return a.meta; }
 __device__ __forceinline__ const int32_t *meta_of(const EvictInline &a) { return a.list; }
 
-// Order of the weights as integers: NaN below every number, both zeros equal.
+// Order of the weights as integers: both zeros equal, NaN below every number (no number has a key of kNaN or less, or kStays).
+constexpr uint32_t kOutside = 0, kNaN = 1, kStays = 0xFFFFFFFFu;  // behind the last token; no number; among the first or the newest
 __device__ __forceinline__ uint32_t key_of(float w) {
     const uint32_t u = __float_as_uint(w + 0.0f);
-    if ((u & 0x7FFFFFFFu) > 0x7F800000u) return 0u;
+    if ((u & 0x7FFFFFFFu) > 0x7F800000u) return kNaN;
     return u >> 31 ? ~u : u | 0x80000000u;
+}
+
+__device__ __forceinline__ int ones_below(uint64_t ones) {  // how many lanes below this one have a one
+    return __builtin_amdgcn_mbcnt_hi((uint32_t)(ones >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)ones, 0));
 }
 
 // N: keys a thread keeps in registers (0: more tokens than that, the weights are read again for every step).
@@ -40,14 +45,13 @@ __global__ __launch_bounds__(kChooseThreads) void evict_choose_kernel(Args a) {
     }
     __shared__ int sBins[2 * kChooseThreads];
     __shared__ int sWave[kChooseWaves];
-    __shared__ int sPick[2];  // the digit of the last one chosen, and how many there are above it with the same digits before
-    __shared__ int sRank[2][kMaxRounds * kChooseWaves + 1];  // of the wavefronts of a round: what is sure to stay, and equals of the last one
+    __shared__ int sPick[3];  // the digit of the last one chosen, how many there are above it with the same digits before, and how many like it
+    __shared__ int sRank[2][kMaxRounds * kChooseWaves + 1];  // by round and wavefront: tokens that are sure to stay, and equals of the last one
     const int begin = a.n_first, end = q.tokens - a.n_recent;  // those in between are chosen from
-    const int left = q.keep - a.n_first - a.n_recent, rounds = (q.tokens + kChooseThreads - 1) / kChooseThreads;
-    auto chosen_from = [&](int t) { return t >= begin && t < end; };
+    const int rounds = (q.tokens + kChooseThreads - 1) / kChooseThreads;
     auto block_at = [&](int t) { return meta[q.src + (min(t, q.tokens - 1) >> 4)]; };
     auto weight_at = [&](int t, int block) { return a.weights[((size_t)block * Hkv + h) * kPage + (min(t, q.tokens - 1) & 15)]; };
-    auto key_at = [&](int t, float w) { return chosen_from(t) ? key_of(w) : 0u; };  // 0: not chosen from (or no number)
+    auto key_at = [&](int t, float w) { return t >= q.tokens ? kOutside : t < begin || t >= end ? kStays : key_of(w); };
     uint32_t keys[N > 0 ? N : 1];
     if constexpr (N > 0) {  // (all loads at once)
         int block[N];
@@ -79,16 +83,17 @@ __global__ __launch_bounds__(kChooseThreads) void evict_choose_kernel(Args a) {
             }
         }
     };
-    // `last`: the key of the last one chosen (0: there are not so many numbers), and how many are above it.
-    uint32_t last = 0;
-    int above = 0;
-    if (left > 0)
+    // `last`: the key of the last one kept; `equals`: how many tokens of that key are kept, of `alike`.
+    uint32_t last = kStays;
+    int above = a.n_first + a.n_recent, alike = 0;
+    if (above < q.keep) {
+        last = 0;
         for (int shift = 21;; shift = shift == 21 ? 10 : 0) {
             const int bits = shift > 0 ? 11 : 10, top = 2 * kChooseThreads - 1 - 2 * tid;  // this thread's bins: top, top - 1
             sBins[top] = sBins[top - 1] = 0;
             __syncthreads();
             each(0, rounds, [&](int, uint32_t k) {
-                if (k != 0 && (shift == 21 || k >> (shift + bits) == last >> (shift + bits))) atomicAdd(&sBins[k >> shift & ((1u << bits) - 1)], 1);
+                if (shift == 21 ? k != kStays : k >> (shift + bits) == last >> (shift + bits)) atomicAdd(&sBins[k >> shift & ((1u << bits) - 1)], 1);
             });
             __syncthreads();
             const int n0 = sBins[top], n1 = sBins[top - 1];
@@ -99,51 +104,47 @@ __global__ __launch_bounds__(kChooseThreads) void evict_choose_kernel(Args a) {
             }
             if (lane == 63) sWave[wave] = x;
             __syncthreads();
-            int total = 0;
             x -= n0 + n1;
 #pragma unroll
-            for (int w = 0; w < kChooseWaves; ++w) {
+            for (int w = 0; w < kChooseWaves; ++w)
                 if (w < wave) x += sWave[w];
-                total += sWave[w];
-            }
-            const int want = left - above;
+            const int want = q.keep - above;  // (fewer than there are tokens)
             if (x < want && want <= x + n0) {
                 sPick[0] = top;
                 sPick[1] = x;
+                sPick[2] = n0;
             } else if (x + n0 < want && want <= x + n0 + n1) {
                 sPick[0] = top - 1;
                 sPick[1] = x + n0;
+                sPick[2] = n1;
             }
             __syncthreads();
-            if (total < want) {  // (the first time only) no number is the last one
-                above = total;
-                break;
-            }
             last |= (uint32_t)sPick[0] << shift;
             above += sPick[1];
+            alike = sPick[2];
             if (shift == 0) break;
-            __syncthreads();
         }
-    const int equals = left - above;  // that are kept
+    }
+    const int equals = last == kStays ? 0 : q.keep - above;
+    const bool ties = equals < alike;  // (seldom: then the lowest indexes among the equals are found too)
+    const uint32_t least = ties ? last + 1 : last;  // tokens of at least this key are sure to stay
 
     // Places: by round, wavefront and lane.
+    uint64_t stay[N > 0 ? N : 1];
     int base[2] = {0, 0};
     for (int r0 = 0; r0 < rounds; r0 += kMaxRounds) {
-        auto sure = [&](int i, uint32_t k) {
-            const int t = i * kChooseThreads + tid;
-            return t < q.tokens && (!chosen_from(t) || (left > 0 && k > last));
-        };
-        auto same = [&](int i, uint32_t k) { return left > 0 && chosen_from(i * kChooseThreads + tid) && k == last; };
         const int r1 = min(rounds, r0 + kMaxRounds), n_ranks = (r1 - r0) * kChooseWaves;
         each(r0, r1, [&](int i, uint32_t k) {
-            const uint64_t s = __ballot(sure(i, k)), e = __ballot(same(i, k));
+            const uint64_t s = __ballot(k >= least);
+            if constexpr (N > 0) stay[i] = s;
+            const int e = ties ? __popcll(__ballot(k == last)) : 0;
             if (lane == 0) {
                 sRank[0][(i - r0) * kChooseWaves + wave] = __popcll(s);
-                sRank[1][(i - r0) * kChooseWaves + wave] = __popcll(e);
+                sRank[1][(i - r0) * kChooseWaves + wave] = e;
             }
         });
         __syncthreads();
-        if (wave < 2) {  // running sums: of what is sure (wavefront 0) and of equals (1)
+        if (wave < (ties ? 2 : 1)) {  // running sums: of what is sure (wavefront 0) and of equals (1)
             int run = base[wave];
             for (int j = 0; j < n_ranks; j += 64) {
                 const int n = j + lane < n_ranks ? sRank[wave][j + lane] : 0;
@@ -159,11 +160,20 @@ __global__ __launch_bounds__(kChooseThreads) void evict_choose_kernel(Args a) {
         }
         __syncthreads();
         each(r0, r1, [&](int i, uint32_t k) {
-            const bool is_sure = sure(i, k), is_same = same(i, k);
-            const uint64_t s = __ballot(is_sure), e = __ballot(is_same), below = (1ull << lane) - 1;
-            const int j = (i - r0) * kChooseWaves + wave, rank = sRank[1][j] + __popcll(e & below);
-            const int at = sRank[0][j] + __popcll(s & below) + min(equals, rank);
-            if (is_sure || (is_same && rank < equals)) kept[at] = i * kChooseThreads + tid;
+            uint64_t s;
+            if constexpr (N > 0)
+                s = stay[i];
+            else
+                s = __ballot(k >= least);
+            const int j = (i - r0) * kChooseWaves + wave;
+            int at = sRank[0][j] + ones_below(s);
+            bool stays = k >= least;
+            if (ties) {
+                const int rank = sRank[1][j] + ones_below(__ballot(k == last));
+                at += min(equals, rank);
+                stays |= k == last && rank < equals;
+            }
+            if (stays) kept[at] = i * kChooseThreads + tid;
         });
         base[0] = sRank[0][n_ranks];
         base[1] = sRank[1][n_ranks];

@@ -161,6 +161,7 @@ extern "C" int hkv_decode_plan_store(hkv_decode_plan *plan, const hkv_qkv *rows,
     }
     if (look) plan->store_blocks = all_different(blocks);
     if (plan->store_blocks < 0) return fail(HKV_EINVAL, "%s: newest tokens of two requests go to the same 16-token block", who);
+    if ((int64_t)n * (plan->tokens_per_req / HKV_PAGE_SIZE + 2) > INT_MAX / 256) return fail(HKV_EINVAL, "%s: too many requests", who);
     decode_places(plan, a);
     HKV_HIP(launch_projection_store(a, static_cast<hipStream_t>(stream)));
     return HKV_OK;
@@ -312,6 +313,7 @@ extern "C" int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_p
     if (n_seq < 0 || n_first < 0 || n_recent < 0) return fail(HKV_EINVAL, "%s: n_seq %d, n_first %d, n_recent %d", who, n_seq, n_first, n_recent);
     if (n_seq == 0) return HKV_OK;
     if (!n_tokens || !n_keep) return fail(HKV_EINVAL, "%s: null n_tokens or n_keep", who);
+    if (pool->d.num_kv_heads > 1024) return fail(HKV_ESHAPE, "%s: %d KV heads (1024 at most)", who, pool->d.num_kv_heads);
     const int P = pool->d.page_size, S = pool->blocks_per_page;
     int64_t src = 0, dst = 0, total = 0;
     for (int i = 0; i < n_seq; ++i) {
@@ -328,7 +330,7 @@ extern "C" int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_p
     if (total == 0) return HKV_OK;
     if (!src_pages || !dst_pages || !key_weights || !kept) return fail(HKV_EINVAL, "%s: null argument", who);
     if (!aligned16(key_weights) || (reinterpret_cast<uintptr_t>(kept) & 3)) return fail(HKV_EINVAL, "%s: key_weights must be 16-byte aligned, kept 4-byte", who);
-    if (total > INT_MAX || total / 16 * pool->d.num_kv_heads > INT_MAX / 256) return fail(HKV_EINVAL, "%s: too many tokens", who);
+    if (total > INT_MAX) return fail(HKV_EINVAL, "%s: too many tokens", who);
     for (int64_t i = 0; i < src; ++i)
         if (src_pages[i] < 0 || src_pages[i] >= pool->d.num_pages)
             return fail(HKV_ERANGE, "%s: page id %d (entry %lld of src_pages) outside pool of %d pages", who, src_pages[i], (long long)i, pool->d.num_pages);
