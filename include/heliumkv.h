@@ -567,7 +567,8 @@ size_t attn_prefill_workspace_bytes(int32_t total_q, int32_t num_q_heads);
  * from the unrounded keys, by the rules of kv_pool_write (a block that a request continues keeps its running scale).  Values
  * are stored as kv_pool_write stores them.  Rows, positions and q_out are indexed by the plan's rows of q (q_rows and
  * q_row_begin of the plan's creation apply); rows the plan does not name are neither read nor written.
- * A row that holds a NaN or infinity gives NaN where the formula does, in that row and head only (an fp8 block whose scale it enters: in that block).
+ * A row that holds a NaN or infinity gives what the formula does, in that row and head only; in the codes of fp8 pools, as kv_pool_write,
+ * a NaN is held as the lowest value of its block and head, and an infinity is the scale of all of it.
  */
 typedef struct {
     const void *q, *k, *v;        /* device, 16-byte aligned: row i begins at element i * stride; [num_q_heads][128], [num_kv_heads][128] elements a row */
@@ -586,7 +587,7 @@ typedef struct {
 
 /* The new tokens of a prefill plan, all requests in one launch (per 128 of them): replaces kv_pool_write and what comes in front of it.
  * EINVAL: null / unaligned pointers, bad strides, eps, axes; a host-only plan; new tokens of two requests in the same 16-token block.
- * Nothing is queued on error. */
+ * ENOMEM: no host memory.  Nothing is queued on error. */
 int hkv_prefill_plan_store(hkv_prefill_plan *plan, const hkv_qkv *rows, void *stream);
 /* The newest tokens_per_req tokens of every request of a decode plan (they end its last node; a growing plan: as appended so far):
  * one token each in a generation step, a drafted run or tree in a verification step (whose positions the caller gives: a tree's tokens are
@@ -625,7 +626,8 @@ int attn_decode_plan_weights(hkv_decode_plan *plan, const void *q, float scale, 
  *   ids each, all different, of one owner at most, and none of src_pages (EINVAL).  n_tokens, n_keep: host [n_seq].
  *   key_weights: as above, read and written.  kept: device int32 [num_kv_heads][sum of n_keep], out: the old index of every kept token.
  * EINVAL: n_keep[i] > n_tokens[i], or less than min(n_tokens[i], n_first + n_recent); a sequence of more than about a million tokens.
- * ERANGE: page ids.  Nothing is queued on error.  Not for capture into a graph: the page lists pass through the pool's staging ring. */
+ * ERANGE: page ids.  ESHAPE: more than 1024 KV heads.  Nothing is queued on error.  Not for capture into a graph (EINVAL): longer page lists
+ * pass through the pool's staging ring. */
 int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_pages, const int32_t *n_tokens, const int32_t *dst_pages, const int32_t *n_keep,
                   int32_t n_first, int32_t n_recent, float *key_weights, int32_t *kept, void *stream);
 

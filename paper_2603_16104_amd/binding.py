@@ -569,12 +569,12 @@ class Qkv(C.Structure):
 
 
 def _row_stride(t) -> int:
-    """Elements from row to row of a [rows][heads][128] tensor whose rows are whole (raw addresses: no gaps)."""
+    """Elements from row to row of a [rows][heads][128] tensor whose rows are whole (raw addresses: no gaps, 0)."""
     if t is None or isinstance(t, int):
         return 0
     if t.dim() != 3 or (t.shape[0] > 1 and t.stride(0) < t.shape[1] * HEAD_DIM) or t.shape[2] != HEAD_DIM or (t.shape[0] and (t.stride(2) != 1 or (t.shape[1] > 1 and t.stride(1) != HEAD_DIM))):
         raise ValueError("q, k and v are [rows][heads][128], the heads of a row one after the other")
-    return t.stride(0) if t.shape[0] > 1 else 0
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1] * HEAD_DIM  # (fewer heads than the plan's are refused by it)
 
 
 def qkv_rows(q, k, v, q_out, q_norm=None, k_norm=None, eps: float = 1e-6, rotary_dim: int = 0, inv_freq=None, interleaved: bool = False,
@@ -584,6 +584,13 @@ def qkv_rows(q, k, v, q_out, q_norm=None, k_norm=None, eps: float = 1e-6, rotary
     for as many calls as the buffers are used for; it holds no reference to them, but to `axis`."""
     if q_out is not None and not isinstance(q_out, int) and not q_out.is_contiguous():
         raise ValueError("q_out must be contiguous")
+    given = [t for t in (q, k, v, q_out, q_norm, k_norm) if t is not None and not isinstance(t, int)]
+    if any(t.dtype != given[0].dtype for t in given):
+        raise ValueError("q, k, v, q_out and the norms' weights are of one type")
+    if not any(t is None or isinstance(t, int) for t in (q, q_out)) and (q.shape[1:] != q_out.shape[1:] or q.shape[0] > q_out.shape[0]):
+        raise ValueError("q_out: [rows][heads][128] for all rows of q")
+    if any(t is not None and not isinstance(t, int) and (t.numel() != HEAD_DIM or not t.is_contiguous()) for t in (q_norm, k_norm)):
+        raise ValueError("q_norm, k_norm: [128]")
     if inv_freq is not None and not isinstance(inv_freq, int) and (inv_freq.element_size() != 8 or inv_freq.numel() * 2 < rotary_dim or not inv_freq.is_contiguous()):
         raise ValueError("inv_freq: float64 [rotary_dim / 2]")
     stride, axes = 0, 1

@@ -6,7 +6,7 @@
 #include <climits>
 #include <cmath>
 #include <cstring>
-#include <new>
+#include <exception>
 #include <numeric>
 
 namespace {
@@ -71,7 +71,7 @@ int all_different(std::vector<int32_t> &v) {
 
 // ---------------------------------------------------------------------------------------------
 // projections
-extern "C" int hkv_prefill_plan_store(hkv_prefill_plan *plan, const hkv_qkv *rows, void *stream) {
+extern "C" int hkv_prefill_plan_store(hkv_prefill_plan *plan, const hkv_qkv *rows, void *stream) try {
     const char *who = "hkv_prefill_plan_store";
     if (!plan) return fail(HKV_EINVAL, "%s: null plan", who);
     if (plan->tiles.empty()) return HKV_OK;
@@ -88,6 +88,8 @@ extern "C" int hkv_prefill_plan_store(hkv_prefill_plan *plan, const hkv_qkv *row
     if (plan->store_blocks == 0) {
         std::vector<int32_t> blocks;
         for (int r = 0; r < plan->n_req; ++r)
+            if (units_of(r) > INT_MAX / 256) return fail(HKV_EINVAL, "%s: request %d brings too many tokens", who, r);  // (a launch keeps below 2^31 threads)
+        for (int r = 0; r < plan->n_req; ++r)
             for (int b = (plan->kv_len[r] - tokens_of(r)) / HKV_PAGE_SIZE, e = b + units_of(r); b < e; ++b)
                 blocks.push_back(plan->block_table[(size_t)r * plan->key_max_pages + (size_t)b * HKV_PAGE_SIZE / P] * S + b % S);
         plan->store_blocks = all_different(blocks);
@@ -102,10 +104,7 @@ extern "C" int hkv_prefill_plan_store(hkv_prefill_plan *plan, const hkv_qkv *row
         int i = 0;
         for (; i < kMaxInlineRequests && r < plan->n_req; ++i, ++r) {
             const int64_t units = units_of(r);
-            if (p.n_units + units > INT_MAX / 256) {  // (a launch keeps below 2^31 threads)
-                if (i == 0) return fail(HKV_EINVAL, "%s: request %d brings too many tokens", who, r);
-                break;
-            }
+            if (p.n_units + units > INT_MAX / 256) break;
             p.begin[i] = p.n_units;
             p.row0[i] = plan->q_row_begin.empty() ? plan->cu_q[r] : plan->q_row_begin[r];
             p.tokens[i] = tokens_of(r);
@@ -116,6 +115,8 @@ extern "C" int hkv_prefill_plan_store(hkv_prefill_plan *plan, const hkv_qkv *row
         HKV_HIP(launch_projection_store(p, static_cast<hipStream_t>(stream)));
     }
     return HKV_OK;
+} catch (const std::exception &) {  // (no memory for a list)
+    return fail(HKV_ENOMEM, "hkv_prefill_plan_store: out of host memory");
 }
 
 static bool on_device(const hkv_decode_plan *plan) { return plan->pool->d.dtype == HKV_FP32 ? plan->d_bt != nullptr : plan->dev != nullptr; }
@@ -136,7 +137,7 @@ static void newest_blocks(const hkv_decode_plan *plan, int r, int *b, int *e) {
     *e = (leaf.n_tokens + HKV_PAGE_SIZE - 1) / HKV_PAGE_SIZE;
 }
 
-extern "C" int hkv_decode_plan_store(hkv_decode_plan *plan, const hkv_qkv *rows, void *stream) {
+extern "C" int hkv_decode_plan_store(hkv_decode_plan *plan, const hkv_qkv *rows, void *stream) try {
     const char *who = "hkv_decode_plan_store";
     if (!plan) return fail(HKV_EINVAL, "%s: null plan", who);
     if (plan->n_req == 0) return HKV_OK;
@@ -165,9 +166,11 @@ extern "C" int hkv_decode_plan_store(hkv_decode_plan *plan, const hkv_qkv *rows,
     decode_places(plan, a);
     HKV_HIP(launch_projection_store(a, static_cast<hipStream_t>(stream)));
     return HKV_OK;
+} catch (const std::exception &) {  // (no memory for a list)
+    return fail(HKV_ENOMEM, "hkv_decode_plan_store: out of host memory");
 }
 
-extern "C" int hkv_decode_plan_append_qkv(hkv_decode_plan *plan, const int32_t *new_page_ids, const hkv_qkv *rows, void *stream) {
+extern "C" int hkv_decode_plan_append_qkv(hkv_decode_plan *plan, const int32_t *new_page_ids, const hkv_qkv *rows, void *stream) try {
     const char *who = "hkv_decode_plan_append_qkv";
     if (!plan) return fail(HKV_EINVAL, "%s: null plan", who);
     if (plan->reserve_tokens <= 0) return fail(HKV_EINVAL, "%s: not a growing plan", who);
@@ -183,11 +186,13 @@ extern "C" int hkv_decode_plan_append_qkv(hkv_decode_plan *plan, const int32_t *
     std::vector<int32_t> blocks(plan->n_req);
     for (int r = 0; r < plan->n_req; ++r) {
         const hkv_node &leaf = plan->nodes[plan->req_leaf[r]];
-        int32_t page = plan->node_pages[leaf.page_begin + leaf.n_pages - 1] / S;
+        int32_t page;
         if (leaf.n_tokens % P == 0) {
             if (!new_page_ids || new_page_ids[r] < 0 || new_page_ids[r] >= pool->d.num_pages) return plan_append(plan, new_page_ids, nullptr, nullptr, nullptr, stream);
             page = new_page_ids[r];
             opens = true;
+        } else {
+            page = plan->node_pages[leaf.page_begin + leaf.n_pages - 1] / S;
         }
         if (pool->refcnt[page] > 1) return fail(HKV_EINVAL, "%s: page %d (request %d) has %d owners: kv_pool_copy_on_write first", who, page, r, pool->refcnt[page]);
         blocks[r] = page * S + leaf.n_tokens % P / HKV_PAGE_SIZE;
@@ -199,11 +204,13 @@ extern "C" int hkv_decode_plan_append_qkv(hkv_decode_plan *plan, const int32_t *
     plan->store_blocks = 1;
     if (!hook.launched) HKV_HIP(launch_projection_store(a, static_cast<hipStream_t>(stream)));  // behind the update of the plan's lists
     return HKV_OK;
+} catch (const std::exception &) {  // (no memory for a list)
+    return fail(HKV_ENOMEM, "hkv_decode_plan_append_qkv: out of host memory");
 }
 
 // ---------------------------------------------------------------------------------------------
 // weights of cached keys
-extern "C" int hkv_decode_plan_track_weights(hkv_decode_plan *plan) {
+extern "C" int hkv_decode_plan_track_weights(hkv_decode_plan *plan) try {
     const char *who = "hkv_decode_plan_track_weights";
     if (!plan) return fail(HKV_EINVAL, "%s: null plan", who);
     if (plan->pool->d.dtype == HKV_FP32) return fail(HKV_ESHAPE, "%s: bf16 and fp8 pools only", who);
@@ -282,6 +289,8 @@ extern "C" int hkv_decode_plan_track_weights(hkv_decode_plan *plan) {
     plan->weight_items.swap(items);
     plan->tracks_weights = true;
     return HKV_OK;
+} catch (const std::exception &) {  // (no memory for a list)
+    return fail(HKV_ENOMEM, "hkv_decode_plan_track_weights: out of host memory");
 }
 
 extern "C" int attn_decode_plan_weights(hkv_decode_plan *plan, const void *q, float scale, const float *lse, float decay, int32_t n_new,
@@ -307,7 +316,7 @@ extern "C" int attn_decode_plan_weights(hkv_decode_plan *plan, const void *q, fl
 // ---------------------------------------------------------------------------------------------
 // eviction
 extern "C" int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_pages, const int32_t *n_tokens, const int32_t *dst_pages, const int32_t *n_keep,
-                             int32_t n_first, int32_t n_recent, float *key_weights, int32_t *kept, void *stream) {
+                             int32_t n_first, int32_t n_recent, float *key_weights, int32_t *kept, void *stream) try {
     const char *who = "kv_pool_evict";
     if (!pool) return fail(HKV_EINVAL, "%s: null pool", who);
     if (n_seq < 0 || n_first < 0 || n_recent < 0) return fail(HKV_EINVAL, "%s: n_seq %d, n_first %d, n_recent %d", who, n_seq, n_first, n_recent);
@@ -351,6 +360,9 @@ extern "C" int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_p
     for (int64_t i = 0; i < src; ++i)
         if (pool->mark[src_pages[i]] == pool->mark_now) return fail(HKV_EINVAL, "%s: page %d is read and written", who, src_pages[i]);
 
+    hipStream_t s = static_cast<hipStream_t>(stream);
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;  // (a replay would need slots of the ring as they are now)
+    if (hipStreamIsCapturing(s, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone) return fail(HKV_EINVAL, "%s: not for capture into a graph", who);
     EvictInline a{};
     a.pool = PoolWriteLaunch{pool->d.k_pages, pool->d.v_pages, pool->d.k_scale, pool->d.v_scale, pool->d.num_kv_heads, pool->d.dtype, nullptr, 0, 0, 0, nullptr, nullptr, nullptr, nullptr};
     a.weights = key_weights;
@@ -358,7 +370,6 @@ extern "C" int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_p
     a.total = total;
     a.n_first = n_first;
     a.n_recent = n_recent;
-    hipStream_t s = static_cast<hipStream_t>(stream);
     constexpr int kRecord = sizeof(EvictSequence) / sizeof(int32_t);
     int64_t kept_at = 0, sp = 0, dp = 0;
     for (int i0 = 0; i0 < n_seq;) {  // as many sequences at once as a slot of the staging ring describes
@@ -398,4 +409,6 @@ extern "C" int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_p
         i0 = i1;
     }
     return HKV_OK;
+} catch (const std::exception &) {  // (no memory for a list)
+    return fail(HKV_ENOMEM, "kv_pool_evict: out of host memory");
 }

@@ -31,7 +31,9 @@ __device__ __forceinline__ uint32_t requant4(uint32_t w, float old, float scale)
 // Codes as quant4's for bf16 values x and a scale of amax / 448 of such values, |x| <= amax, from the scale's reciprocal
 // (correctly rounded): product, remainder, correction.  For every such pair with a scale in [2^-60, 2^60] (5.3e8 pairs, all
 // of them tried) the quotient equals the division's bit for bit wherever it is at least 2^-11 in magnitude; below 2^-10
-// both round to zero with the sign of x.  Four instructions instead of about ten, two of them slow ones.
+// both round to zero with the sign of x.  Four instructions instead of about ten, two of them slow ones.  For other values (keys before
+// their rounding to bf16, codes times a scale) the quotient is the division's but for its last bit now and then, and a code another one only where the quotient
+// lies between two of them to within that bit.
 __device__ __forceinline__ uint32_t quant4_by(float a, float b, float c, float d, float scale, float inv) {
     auto q = [scale, inv](float x) {
         const float y = x * inv;

@@ -603,6 +603,10 @@ EVICT = [  # dtype, kv heads, page, tokens, keep, first, recent, weights
     (hkv.FP8_E4M3, 2, 16, [100, 17, 1], [37, 17, 1], 1, 0, "plain"),
     (hkv.FP8_E4M3, 2, 64, [1000, 200], [333, 65], 2, 16, "ties"),
     (hkv.FP32, 2, 16, [100, 17, 40], [37, 17, 20], 0, 5, "odd"),
+    # around the lengths at which a thread holds another number of weights, or none
+    (hkv.BF16, 1, 16, [2048, 4096, 8192, 8193], [1025, 4095, 4000, 8000], 1, 1024, "ties"),
+    (hkv.FP8_E4M3, 1, 64, [16384, 16385, 40000], [16000, 3000, 2000], 5, 1500, "plain"),
+    (hkv.BF16, 1, 16, [40000], [17000], 0, 0, "zeros"),
 ]
 
 
@@ -658,6 +662,26 @@ def test_eviction(case):
     for i in range(2):
         assert np.array_equal(after[i][untouched], before[i][untouched]), "slots that no kept token goes to"
     assert np.array_equal(now[untouched], was[untouched], equal_nan=True)
+    pool.close()
+
+
+def test_eviction_is_refused_while_a_graph_is_captured():
+    """... and the capture goes on."""
+    pool = Pool(8, 1, hkv.BF16)
+    w, kept = torch.rand(8, 1, 16, device="cuda"), torch.full((1, 10), -1, dtype=torch.int32, device="cuda")
+    x = torch.zeros(4, device="cuda")
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        with pytest.raises(hkv.HkvError) as e:
+            hkv.kv_pool_evict(pool.handle, [0, 1], [20], [2], [10], 0, 0, w, kept)
+        x += 1
+    assert e.value.code == hkv.EINVAL
+    for i in range(3):
+        graph.replay()
+    torch.cuda.synchronize()
+    assert (x == 3).all() and (kept == -1).all()
+    hkv.kv_pool_evict(pool.handle, [0, 1], [20], [2], [10], 0, 0, w, kept)
+    assert np.array_equal(kept.cpu().numpy()[0], evicted(w.cpu().numpy()[:, 0], np.arange(2), 20, 10, 0, 0))
     pool.close()
 
 
@@ -742,6 +766,23 @@ def test_a_prompt_is_stored_judged_and_shrunk(dtype):
         hkv.hkv_decode_plan_destroy(p)
     hkv.hkv_prefill_plan_destroy(plan)
     pool.close()
+
+
+def test_an_8_bit_pool_holds_what_is_no_number_as_its_writer_does():
+    pools = [Pool(3, 2, hkv.FP8_E4M3, seed=5) for _ in range(2)]
+    x = Rows(40, 2, 2, hkv.FP8_E4M3, 6, norm=False, rotary=0, fused=False)
+    bad = (float("nan"), float("inf"), -float("inf"))
+    for i, b in enumerate(bad):
+        x.k[16 * i + 3, 0, 7 * i], x.v[16 * i + 4, 1, 9 * i] = b, b
+    plan = hkv.hkv_prefill_plan_create(pools[0].handle, [0, 40], [[2, 0, 1]], [40], 2)
+    hkv.hkv_prefill_plan_store(plan, x.arg)
+    hkv.kv_pool_write(pools[1].handle, [2, 0, 1], 0, 40, x.k, x.v)
+    torch.cuda.synchronize()
+    for a, b in zip(*((p.k.view(torch.uint8), p.v.view(torch.uint8), p.k_scale.view(torch.int32), p.v_scale.view(torch.int32)) for p in pools)):
+        assert torch.equal(a, b)
+    hkv.hkv_prefill_plan_destroy(plan)
+    for p in pools:
+        p.close()
 
 
 def test_captured_and_on_other_streams():

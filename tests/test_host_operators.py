@@ -98,8 +98,9 @@ def test_rows_are_checked_by_shape():
     q, k, v = (x.unflatten(1, (-1, 128)) for x in t.split([1024, 256, 256], dim=1))
     x = hkv.qkv_rows(q, k, v, torch.zeros(4, 8, 128, dtype=torch.bfloat16))
     assert (x.q_stride, x.k_stride, x.v_stride, x.n_axes) == (1536, 1536, 1536, 1)
-    out = torch.zeros(4, 8, 128)
+    out = torch.zeros(4, 8, 128, dtype=torch.bfloat16)
     for bad in (dict(q=q.transpose(0, 1)), dict(k=k[:1].expand(4, -1, -1)), dict(q=q[:, ::2]), dict(q=t), dict(q_out=out[:, ::2]), dict(inv_freq=torch.zeros(64)),
+                dict(q_out=out.float()), dict(q_out=out[:, :4].contiguous()), dict(q_norm=torch.zeros(128)), dict(k_norm=out[0, 0, :64]), dict(v=v.float()),
                 dict(inv_freq=torch.zeros(32, dtype=torch.float64)), dict(positions=torch.zeros(4, dtype=torch.int64)),
                 dict(positions=torch.zeros(4)), dict(axis=[0] * 63)):
         with pytest.raises(ValueError):
@@ -107,6 +108,13 @@ def test_rows_are_checked_by_shape():
     p = torch.zeros(3, 8, dtype=torch.int32)[:, :4]
     x = hkv.qkv_rows(q, k, v, out, positions=p, axis=np.arange(64) % 3, rotary_dim=128, inv_freq=torch.zeros(64, dtype=torch.float64))
     assert x.n_axes == 3 and x.position_stride == 8 and C.cast(x.axis, C.POINTER(C.c_int32))[2] == 2
+
+
+def test_a_single_row_has_the_plans_heads(prefill):
+    import torch
+    q, k = torch.zeros(1, 8, 128, dtype=torch.bfloat16), torch.zeros(1, 2, 128, dtype=torch.bfloat16)
+    for q_, k_ in ((q[:, :4], k), (q, k[:, :1])):
+        assert code(hkv.hkv_prefill_plan_store, prefill, hkv.qkv_rows(q_, k_, k, q_.clone()), 0) == hkv.EINVAL and "stride" in hkv.last_error()
 
 
 def test_weights_refusals():
