@@ -225,6 +225,14 @@ struct ProjectionPrefill {
     int32_t tokens[kMaxInlineRequests];
 };
 
+// The same for the new token of every request of a growing plan, in the launch that applies the plan's update (PlanGrowInline): `length` is what
+// their leaves held before.
+struct ProjectionAppend {
+    ProjectionLaunch base;
+    int32_t length[kMaxInlineAppend];
+};
+static_assert(sizeof(ProjectionAppend) + sizeof(PlanGrowInline) <= 4096, "kernel argument segment");
+
 // Keys of attn_decode_plan_weights: up to `length` tokens of a node from tok_begin on, one KV head, all rows below the node.  A workgroup's items are
 // kWeightWaves in a row: one for each wavefront, or, of a node of more than 16 rows, one for all of them, listed so many times.
 constexpr int kMaxWeightTokens = 1024, kWeightWaves = 8;
@@ -406,7 +414,7 @@ hipError_t launch_decode_step_append(const PoolAppendInline &w, const PlanGrowIn
 hipError_t launch_plan_grow_inline(const PlanGrowInline &a, hipStream_t s);
 hipError_t launch_projection_store(const ProjectionLaunch &a, hipStream_t s);
 hipError_t launch_projection_store(const ProjectionPrefill &a, hipStream_t s);
-hipError_t launch_projection_append(const ProjectionLaunch &a, const PlanGrowInline &g, hipStream_t s);
+hipError_t launch_projection_append(const ProjectionAppend &a, const PlanGrowInline &g, hipStream_t s);
 hipError_t launch_key_weights(const KeyWeightsLaunch &a, hipStream_t s);
 hipError_t launch_evict(const EvictLaunch &a, hipStream_t s);
 hipError_t launch_evict(const EvictInline &a, hipStream_t s);

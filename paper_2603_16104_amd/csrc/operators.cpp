@@ -162,7 +162,8 @@ extern "C" int hkv_decode_plan_store(hkv_decode_plan *plan, const hkv_qkv *rows,
     }
     if (look) plan->store_blocks = all_different(blocks);
     if (plan->store_blocks < 0) return fail(HKV_EINVAL, "%s: newest tokens of two requests go to the same 16-token block", who);
-    if ((int64_t)n * (plan->tokens_per_req / HKV_PAGE_SIZE + 2) > INT_MAX / 256) return fail(HKV_EINVAL, "%s: too many requests", who);
+    const int64_t parts = plan->tokens_per_req > 1 ? plan->tokens_per_req / HKV_PAGE_SIZE + 2 : (plan->num_q_heads + pool->d.num_kv_heads + 15) / 16;
+    if (n * parts > INT_MAX / 256) return fail(HKV_EINVAL, "%s: too many requests", who);
     decode_places(plan, a);
     HKV_HIP(launch_projection_store(a, static_cast<hipStream_t>(stream)));
     return HKV_OK;
@@ -174,7 +175,8 @@ extern "C" int hkv_decode_plan_append_qkv(hkv_decode_plan *plan, const int32_t *
     const char *who = "hkv_decode_plan_append_qkv";
     if (!plan) return fail(HKV_EINVAL, "%s: null plan", who);
     if (plan->reserve_tokens <= 0) return fail(HKV_EINVAL, "%s: not a growing plan", who);
-    ProjectionLaunch a{};
+    ProjectionAppend p{};
+    ProjectionLaunch &a = p.base;
     if (plan->n_req > 0) {
         if (int rc = projection_of(plan->pool, plan->num_q_heads, rows, a, who)) return rc;
         if (!plan->dev) return fail(HKV_EINVAL, "%s: plan was built host-only", who);
@@ -195,11 +197,12 @@ extern "C" int hkv_decode_plan_append_qkv(hkv_decode_plan *plan, const int32_t *
             page = plan->node_pages[leaf.page_begin + leaf.n_pages - 1] / S;
         }
         if (pool->refcnt[page] > 1) return fail(HKV_EINVAL, "%s: page %d (request %d) has %d owners: kv_pool_copy_on_write first", who, page, r, pool->refcnt[page]);
+        if (r < kMaxInlineAppend) p.length[r] = leaf.n_tokens;
         blocks[r] = page * S + leaf.n_tokens % P / HKV_PAGE_SIZE;
     }
     if (opens && all_different(blocks) < 0) return fail(HKV_EINVAL, "%s: new tokens of two requests go to the same 16-token block", who);
     decode_places(plan, a);
-    AppendHook hook{[](void *ctx, const PlanGrowInline &g, hipStream_t s) { return launch_projection_append(*static_cast<ProjectionLaunch *>(ctx), g, s); }, &a, false};
+    AppendHook hook{[](void *ctx, const PlanGrowInline &g, hipStream_t s) { return launch_projection_append(*static_cast<ProjectionAppend *>(ctx), g, s); }, &p, false};
     if (int rc = plan_append(plan, new_page_ids, nullptr, nullptr, &hook, stream)) return rc;
     plan->store_blocks = 1;
     if (!hook.launched) HKV_HIP(launch_projection_store(a, static_cast<hipStream_t>(stream)));  // behind the update of the plan's lists

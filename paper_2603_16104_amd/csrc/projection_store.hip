@@ -10,7 +10,7 @@
 // the lane eight further (whole heads: one vector instruction, else through the LDS crossbar), interleaved pairs lie in one lane.
 // A workgroup takes one 16-token block of one KV head: a thread row per token, K, V and then the query heads of the group, so that the
 // angles are taken once for all of them, and the fp8 scale of the block is the workgroup's own.  Where a request brings a
-// single token the 16 thread rows take its K / V and its query heads side by side.
+// single token the 16 thread rows take 16 of its heads' rows.
 #include "pool_block.h"
 
 namespace hkv {
@@ -53,24 +53,37 @@ __device__ __forceinline__ u32x4 pack8(const float (&x)[8]) {
 // dispatch packet in host memory: 14 us a launch.)
 __device__ __forceinline__ int choose(uint32_t i, int a, int b, int c, int d) { return i < 2 ? (i == 0 ? +a : +b) : (i == 2 ? +c : +d); }
 
-// Cosine and sine of N pairs from p0 on (a multiple of N) of the row's angles.
-template <int DT, int N>
-__device__ __forceinline__ void angles(const ProjectionLaunch &a, int p0, int64_t row, int pos, float (&co)[N], float (&si)[N]) {
+// What N pairs from p0 on (a multiple of N) turn by: radians per position, and the row's places on the axes (not where the caller gives none).
+template <int N>
+struct Angles {
     double freq[N];
+    int on0, on1, on2, on3;
+};
+template <int N>
+__device__ __forceinline__ Angles<N> load_angles(const ProjectionLaunch &a, const double *inv_freq, int p0, int64_t row) {
+    Angles<N> x{};
 #pragma unroll
-    for (int e = 0; e < N; ++e) freq[e] = a.inv_freq[p0 + e];
-    int on0 = pos, on1 = pos, on2 = pos, on3 = pos;
+    for (int e = 0; e < N; ++e) x.freq[e] = inv_freq[p0 + e];
     if (a.positions) {
-        on0 = a.positions[row];
-        if (a.n_axes > 1) on1 = a.positions[a.position_stride + row];
-        if (a.n_axes > 2) on2 = a.positions[2 * a.position_stride + row];
-        if (a.n_axes > 3) on3 = a.positions[3 * a.position_stride + row];
+        x.on0 = a.positions[row];
+        if (a.n_axes > 1) x.on1 = a.positions[a.position_stride + row];
+        if (a.n_axes > 2) x.on2 = a.positions[2 * a.position_stride + row];
+        if (a.n_axes > 3) x.on3 = a.positions[3 * a.position_stride + row];
     }
-    const uint32_t axes = (p0 < 32 ? (p0 < 16 ? a.axis[0] : a.axis[1]) : (p0 < 48 ? a.axis[2] : a.axis[3])) >> (2 * (p0 & 15));
+    return x;
+}
+// Their cosines and sines; pos: the place of a row without places of its own.
+template <int DT, int N>
+__device__ __forceinline__ void angles(const ProjectionLaunch &a, int p0, const Angles<N> &x, int pos, float (&co)[N], float (&si)[N]) {
+    const int on0 = a.positions ? x.on0 : pos;
+    uint32_t axes = 0;  // (as above)
+#pragma unroll
+    for (int j = 0; j < 4; ++j) axes |= p0 >> 4 == j ? a.axis[j] : 0u;
+    axes >>= 2 * (p0 & 15);
 #pragma unroll
     for (int e = 0; e < N; ++e) {
-        const int place = a.n_axes == 1 ? on0 : choose(axes >> (2 * e) & 3u, on0, on1, on2, on3);
-        const double turns = (double)place * (freq[e] * 0.15915494309189533577);
+        const int place = a.n_axes == 1 ? on0 : choose(axes >> (2 * e) & 3u, on0, x.on1, x.on2, x.on3);
+        const double turns = (double)place * (x.freq[e] * 0.15915494309189533577);
         const float part = (float)(turns - __builtin_rint(turns));
         if constexpr (DT == 2) {
             sincospif(2.0f * part, &si[e], &co[e]);
@@ -151,11 +164,6 @@ __device__ __forceinline__ void norm_and_turn(const ProjectionLaunch &a, int c, 
 }
 
 template <int DT>
-__device__ __forceinline__ void load_weight(const void *w, int c, float (&x)[8]) {
-    if (w) values<DT>(load_row<DT>(w, 0, 0, 0, c), x);
-}
-
-template <int DT>
 __device__ __forceinline__ void put_query(const ProjectionLaunch &a, int64_t row, int head, int c, const float (&x)[8]) {
     const int64_t at = (row * (a.pool.num_kv_heads * a.group) + head) * kHeadDim + 8 * c;
     if constexpr (DT == 2) {
@@ -197,22 +205,26 @@ __device__ __forceinline__ void store_tokens(const ProjectionLaunch &a, const Un
     constexpr int kAhead = 4;  // query rows on their way
     int64_t row = u.row + max(0, min(slot, u.hi - 1) - u.lo);
     if (a.row_map) row = a.row_map[row];
+    // All loads at once, by all lanes and of what there is, if only a row again: a wait at the end of a branch would hold up those behind it.
+    const Row<DT> kr = load_row<DT>(a.k, a.k_stride, row, h, c), vr = load_row<DT>(a.v, a.v_stride, row, h, c);
+    Row<DT> q[kAhead];
+#pragma unroll
+    for (int j = 0; j < kAhead; ++j) q[j] = load_row<DT>(a.q, a.q_stride, row, h * a.group + min(j, a.group - 1), c);
+    const Row<DT> qn = load_row<DT>(a.q_norm ? a.q_norm : a.q, 0, 0, 0, c), kn = load_row<DT>(a.k_norm ? a.k_norm : a.q, 0, 0, 0, c);
+    const bool turns = 8 * c < a.rotary_dim;
+    const int p0 = turns ? 4 * c : 0;
+    const Angles<4> angle = load_angles<4>(a, a.rotary_dim > 0 ? a.inv_freq : static_cast<const double *>(a.q), p0, row);
     float k[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     Row<DT> v{};
     if (valid) {
-        const Row<DT> kr = load_row<DT>(a.k, a.k_stride, row, h, c);
-        v = load_row<DT>(a.v, a.v_stride, row, h, c);
-        Row<DT> q[kAhead];
-#pragma unroll
-        for (int j = 0; j < kAhead; ++j)
-            if (j < a.group) q[j] = load_row<DT>(a.q, a.q_stride, row, h * a.group + j, c);
-        float qw[8] = {}, kw[8] = {};
-        load_weight<DT>(a.q_norm, c, qw);
-        load_weight<DT>(a.k_norm, c, kw);
+        v = vr;
+        float qw[8], kw[8];
+        values<DT>(qn, qw);
+        values<DT>(kn, kw);
         // four angles a lane; the row's lanes, of one wavefront, bring theirs together
-        if (8 * c < a.rotary_dim) {
+        if (turns) {
             float co[4], si[4];
-            angles<DT, 4>(a, 4 * c, row, u.pos + slot - u.lo, co, si);
+            angles<DT, 4>(a, p0, angle, u.pos + slot - u.lo, co, si);
             *reinterpret_cast<float4 *>(&sTurn[slot][4 * c]) = make_float4(co[0], co[1], co[2], co[3]);
             *reinterpret_cast<float4 *>(&sTurn[slot][64 + 4 * c]) = make_float4(si[0], si[1], si[2], si[3]);
         }
@@ -239,143 +251,170 @@ __device__ __forceinline__ void store_tokens(const ProjectionLaunch &a, const Un
     put_block<DT>(a, u, h, valid, k, v);
 }
 
-// K and V of one token, by the 16 lanes of its thread row; all threads of the workgroup call.  fp8 blocks that are continued: as
-// store_block, but the scales are found without the other wavefronts, and the workgroup comes together only to round earlier codes again.
-template <int DT>
-__device__ __forceinline__ void put_token(const ProjectionLaunch &a, const Unit &u, int h, bool valid, const float (&k)[8], const Row<DT> &v) {
-    const int tid = threadIdx.x, c = tid & 15, d = 8 * c;
-    const size_t blk = ((size_t)u.block * a.pool.num_kv_heads + h) * kBlockElems;
-    if constexpr (DT == 0) {
-        if (!valid) return;
-        *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.pool.k_pages) + blk + (d >> 5) * 512 + u.lo * 32 + (d & 31)) = pack8(k);
-        uint16_t *vd = static_cast<uint16_t *>(a.pool.v_pages) + blk + d * kPage + u.lo;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) vd[j * kPage] = (uint16_t)(v.w[0][j >> 1] >> (16 * (j & 1)));
-    } else if constexpr (DT == 1) {
-        __shared__ float sScales[4];  // K's and V's old scale, and new
-        const size_t at = (size_t)u.block * a.pool.num_kv_heads + h;
-        uint8_t *kb = static_cast<uint8_t *>(a.pool.k_pages) + blk, *vb = static_cast<uint8_t *>(a.pool.v_pages) + blk;
-        if (valid) {
-            float vf[8], am[2] = {0.f, 0.f}, old[2] = {0.f, 0.f}, sc[2];
-            unpack_bf16(v.w[0], vf);
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                am[0] = fmaxf(am[0], fabsf(k[j]));
-                am[1] = fmaxf(am[1], fabsf(vf[j]));
-            }
-            if (u.lo > 0) {
-                old[0] = a.pool.k_scale[at];
-                old[1] = a.pool.v_scale[at];
-            }
+// Codes of earlier tokens (slots below lo) of an fp8 block and head under scales that have grown, by a whole wavefront; `vc`: the lanes from lane
+// `at` on, sixteen, hold V's codes of the new token, which goes to slot lo with them (K's is stored apart).
+__device__ __forceinline__ void round_again(const ProjectionLaunch &a, int64_t blk, int lo, int at, u32x2 vc, float ko, float ks, float vo, float vs) {
+    const int lane = threadIdx.x & 63;
+    if (ks > ko) {
+        u32x4 *p = reinterpret_cast<u32x4 *>(static_cast<uint8_t *>(a.pool.k_pages) + blk) + lane;  // 16 bytes of token lane / 4
+        if (lane >> 2 < lo) {
+            u32x4 w[2] = {p[0], p[64]};
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
-                const float m = row16_max(am[i]);
-                const float cand = m > 0.f ? m / 448.0f : 0.f;
-                sc[i] = u.lo > 0 && old[i] >= cand ? old[i] : cand;  // an unset (NaN) old scale gives cand
-                if (!(sc[i] > 0.f)) sc[i] = 1.0f;
-            }
-            if (c == 0) {
-                a.pool.k_scale[at] = sc[0];
-                a.pool.v_scale[at] = sc[1];
-                sScales[0] = old[0];
-                sScales[1] = old[1];
-                sScales[2] = sc[0];
-                sScales[3] = sc[1];
-            }
-            *reinterpret_cast<u32x2 *>(kb + (d >> 6) * 1024 + u.lo * 64 + (d & 63)) = u32x2{quant4(k[0], k[1], k[2], k[3], sc[0]), quant4(k[4], k[5], k[6], k[7], sc[0])};
-            const u32x2 vc = {quant4(vf[0], vf[1], vf[2], vf[3], sc[1]), quant4(vf[4], vf[5], vf[6], vf[7], sc[1])};
 #pragma unroll
-            for (int j = 0; j < 8; ++j) vb[(d + j) * kPage + u.lo] = (uint8_t)(vc[j >> 2] >> (8 * (j & 3)));
+                for (int j = 0; j < 4; ++j) w[i][j] = requant4(w[i][j], ko, ks);
+                p[64 * i] = w[i];
+            }
         }
-        if (u.lo == 0) return;
-        __syncthreads();
-        const float ko = sScales[0], vo = sScales[1], ks = sScales[2], vs = sScales[3];
-        const int slot = tid >> 4;
-        if (ks > ko && slot < u.lo) {
-            u32x2 *p = reinterpret_cast<u32x2 *>(kb + (d >> 6) * 1024 + slot * 64 + (d & 63));
-            const u32x2 w = *p;
-            *p = u32x2{requant4(w[0], ko, ks), requant4(w[1], ko, ks)};
+    }
+    if (vs > vo) {
+        u32x4 *p = reinterpret_cast<u32x4 *>(static_cast<uint8_t *>(a.pool.v_pages) + blk) + lane;  // dimension `lane`, all tokens
+        u32x4 w[2] = {p[0], p[64]};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int from = 4 * (at + 8 * i + (lane >> 3));
+            const uint32_t c0 = __builtin_amdgcn_ds_bpermute(from, vc[0]), c1 = __builtin_amdgcn_ds_bpermute(from, vc[1]);
+            const uint32_t code = (lane & 4 ? c1 : c0) >> (8 * (lane & 3)) & 0xFFu;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int n = min(max(lo - 4 * j, 0), 4);  // earlier tokens among the word's
+                const uint32_t earlier = n == 4 ? 0xFFFFFFFFu : (1u << (8 * n)) - 1, own = lo >> 2 == j ? 0xFFu << (8 * (lo & 3)) : 0u;
+                w[i][j] = (requant4(w[i][j], vo, vs) & earlier) | (code << (8 * (lo & 3)) & own) | (w[i][j] & ~(earlier | own));
+            }
+            p[64 * i] = w[i];
         }
-        const int s0 = 8 * (tid & 1);
-        if (vs > vo && s0 < u.lo) {  // eight slots of a dimension
-            uint8_t *p = vb + (tid >> 1) * kPage + s0;
-            u32x2 w = *reinterpret_cast<const u32x2 *>(p);
-            w[0] = requant4(w[0], vo, vs);
-            w[1] = requant4(w[1], vo, vs);
-            if (s0 + 8 <= u.lo)
-                *reinterpret_cast<u32x2 *>(p) = w;
-            else
-                for (int j = 0; s0 + j < u.lo; ++j) p[j] = (uint8_t)(w[j >> 2] >> (8 * (j & 3)));
-        }
-    } else {
-        put_block<DT>(a, u, h, valid, k, v);
     }
 }
 
-// One KV head of one token: thread row u.lo takes K and V, the others a query head each (the 16th, too, is K's row's).
-template <int DT>
-__device__ __forceinline__ void store_token(const ProjectionLaunch &a, const Unit &u, int h) {
+__host__ __device__ inline int token_parts(const ProjectionLaunch &a) { return (a.pool.num_kv_heads * (a.group + 1) + 15) / 16; }
+
+// One token, row `token` of the rows: 16 of its heads' rows, K's (with V's) first, then the queries'.  All threads of the workgroup call.  `place` finds the
+// token's Unit, by a chain of loads that goes on beside those of the rows.
+template <int DT, class Place>
+__device__ __forceinline__ void store_token(const ProjectionLaunch &a, int64_t token, int part, Place &&place) {
     __shared__ __align__(16) float sTurn[2 * 64];
-    const int g = threadIdx.x >> 4, c = threadIdx.x & 15;
-    const bool valid = g == u.lo;
-    const int j = (g - u.lo - 1) & 15;
-    const int64_t row = a.row_map ? a.row_map[u.row] : u.row;
-    float k[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    Row<DT> kr{}, v{}, q{};
-    float w[8] = {}, kw[8] = {};
-    if (valid) {
-        kr = load_row<DT>(a.k, a.k_stride, row, h, c);
-        v = load_row<DT>(a.v, a.v_stride, row, h, c);
-        load_weight<DT>(a.k_norm, c, kw);
+    const int Hkv = a.pool.num_kv_heads, Hq = Hkv * a.group, c = threadIdx.x & 15, d = 8 * c, i = 16 * part + ((int)threadIdx.x >> 4);
+    const bool is_k = i < Hkv, is_q = !is_k && i - Hkv < Hq, has_angle = (int)threadIdx.x < a.rotary_dim / 2;
+    const int head = is_k ? i : min(i - Hkv, Hq - 1);
+    const int64_t row = a.row_map ? a.row_map[token] : token;
+    // All loads at once, by all lanes and of what there is, if only the row itself again: a wait at the end of a branch would hold up those behind
+    // it.  (Places, not a choice of the arguments: that would be read from memory first, by lane.)
+    constexpr int E = DT == 2 ? 4 : 2;
+    const char *const k_row = static_cast<const char *>(a.k) + row * a.k_stride * E, *const q_row = static_cast<const char *>(a.q) + row * a.q_stride * E;
+    const char *const mine = (is_k ? k_row : q_row) + (head * kHeadDim + d) * E;
+    const char *const k_norm = a.k_norm ? static_cast<const char *>(a.k_norm) + 0 : k_row, *const q_norm = a.q_norm ? static_cast<const char *>(a.q_norm) + 0 : q_row;
+    const bool normed = is_k ? k_norm != k_row : q_norm != q_row;
+    const Row<DT> r = load_row<DT>(mine, 0, 0, 0, 0), wr = load_row<DT>(is_k ? k_norm : q_norm, 0, 0, 0, c);
+    Row<DT> v{};
+    if (16 * part < Hkv) v = load_row<DT>(a.v, a.v_stride, row, min(head, Hkv - 1), c);
+    const Angles<1> angle = load_angles<1>(a, a.rotary_dim > 0 ? a.inv_freq : reinterpret_cast<const double *>(k_row), max(0, min((int)threadIdx.x, a.rotary_dim / 2 - 1)), row);
+    const Unit u = place();
+    const int64_t at = (int64_t)u.block * Hkv + head;
+    float old[2] = {0.f, 0.f}, w[8], x[8];
+    if (DT == 1 && 16 * part < Hkv && u.lo > 0) {
+        const int64_t s = (int64_t)u.block * Hkv + min(head, Hkv - 1);
+        old[0] = a.pool.k_scale[s];
+        old[1] = a.pool.v_scale[s];
     }
-    if (j < a.group) {
-        q = load_row<DT>(a.q, a.q_stride, row, h * a.group + j, c);
-        load_weight<DT>(a.q_norm, c, w);
-    }
-    if ((int)threadIdx.x < a.rotary_dim / 2) {  // an angle a lane, for all heads
+    if (has_angle) {  // an angle a lane, for all heads
         float co[1], si[1];
-        angles<DT, 1>(a, threadIdx.x, row, u.pos, co, si);
+        angles<DT, 1>(a, threadIdx.x, angle, u.pos, co, si);
         sTurn[threadIdx.x] = co[0];
         sTurn[64 + threadIdx.x] = si[0];
     }
     __syncthreads();
-    if (valid || j < a.group) {
+    if (is_k || is_q) {
         Turn t;
         turn_of(a, sTurn, c, t);
-        if (j < a.group) {
-            float x[8];
-            values<DT>(q, x);
-            norm_and_turn(a, c, a.q_norm != nullptr, w, t, x);
-            put_query<DT>(a, row, h * a.group + j, c, x);
+        values<DT>(r, x);
+        values<DT>(wr, w);
+        norm_and_turn(a, c, normed, w, t, x);
+    }
+    if (is_q) put_query<DT>(a, row, head, c, x);
+    const int64_t blk = at * kBlockElems;
+    if constexpr (DT == 0) {
+        if (!is_k) return;
+        *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.pool.k_pages) + blk + (d >> 5) * 512 + u.lo * 32 + (d & 31)) = pack8(x);
+        uint16_t *vd = static_cast<uint16_t *>(a.pool.v_pages) + blk + d * kPage + u.lo;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) vd[j * kPage] = (uint16_t)(v.w[0][j >> 1] >> (16 * (j & 1)));
+    } else if constexpr (DT == 1) {
+        // the block's running scales, as store_block finds them
+        float vf[8], sc[2] = {0.f, 0.f};
+        u32x2 vc = {0u, 0u};
+        bool grown = false;
+        if (is_k) {
+            float am[2] = {0.f, 0.f};
+            unpack_bf16(v.w[0], vf);
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                am[0] = fmaxf(am[0], fabsf(x[j]));
+                am[1] = fmaxf(am[1], fabsf(vf[j]));
+            }
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+                const float m = row16_max(am[s]);
+                const float cand = m > 0.f ? m / 448.0f : 0.f;
+                sc[s] = u.lo > 0 && old[s] >= cand ? old[s] : cand;  // an unset (NaN) old scale gives cand
+                if (!(sc[s] > 0.f)) sc[s] = 1.0f;
+            }
+            if (c == 0) {
+                a.pool.k_scale[at] = sc[0];
+                a.pool.v_scale[at] = sc[1];
+            }
+            *reinterpret_cast<u32x2 *>(static_cast<uint8_t *>(a.pool.k_pages) + blk + (d >> 6) * 1024 + u.lo * 64 + (d & 63)) =
+                u32x2{quant4(x[0], x[1], x[2], x[3], sc[0]), quant4(x[4], x[5], x[6], x[7], sc[0])};
+            vc = u32x2{quant4(vf[0], vf[1], vf[2], vf[3], sc[1]), quant4(vf[4], vf[5], vf[6], vf[7], sc[1])};
+            if (!(u.lo > 0 && sc[1] > old[1])) {
+                uint8_t *vd = static_cast<uint8_t *>(a.pool.v_pages) + blk + d * kPage + u.lo;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) vd[j * kPage] = (uint8_t)(vc[j >> 2] >> (8 * (j & 3)));
+            }
+            grown = u.lo > 0 && (sc[0] > old[0] || sc[1] > old[1]);
         }
-        if (valid) {
-            values<DT>(kr, k);
-            norm_and_turn(a, c, a.k_norm != nullptr, kw, t, k);
+        // rounding again takes the whole wavefront, a head at a time
+        for (uint64_t rest = __ballot(c == 0 && grown); rest; rest &= rest - 1) {
+            const int l = __builtin_ctzll(rest);
+            auto of = [&](float f) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(f), l)); };
+            round_again(a, ((int64_t)u.block * Hkv + __builtin_amdgcn_readlane(head, l)) * kBlockElems, u.lo, l, vc, of(old[0]), of(sc[0]), of(old[1]), of(sc[1]));
+        }
+    } else {
+        if (!is_k) return;
+        float *kd = static_cast<float *>(a.pool.k_pages) + blk + (d >> 4) * 256 + u.lo * 16 + (d & 15);
+        float *vd = static_cast<float *>(a.pool.v_pages) + blk + d * kPage + u.lo;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            kd[j] = x[j];
+            vd[j * kPage] = __uint_as_float(v.w[j >> 2][j & 3]);
         }
     }
-    put_token<DT>(a, u, h, valid, k, v);
 }
 
-// The newest tokens of a decode plan's requests.  grid: (requests x blocks that the tokens of one can span, KV heads)
+// The newest tokens of a decode plan's requests.  grid: (requests x blocks that the tokens of one can span, KV heads); a single token each: requests x
+// sixteens of its rows
 template <int DT, bool ONE>
 __global__ __launch_bounds__(256) void projection_decode_kernel(ProjectionLaunch a) {
-    const int spans = ONE ? 1 : (a.tokens + kPage - 2) / kPage + 1;
-    const int r = blockIdx.x / spans, i = blockIdx.x % spans;
-    const StoreRequest s = a.requests[r];
-    int n = s.tokens;
-    if (s.item >= 0) n = a.items[s.item].tok_begin + a.items[s.item].n_tokens;
-    const int first = n - a.tokens, b = first / kPage + i;
-    if (b * kPage >= n) return;
-    Unit u;
-    u.block = a.blocks[s.page_off + (uint32_t)b];
-    u.lo = max(first - b * kPage, 0);
-    u.hi = min(n - b * kPage, kPage);
-    u.row = (int64_t)r * a.tokens + (b * kPage + u.lo - first);
-    u.pos = s.pos0 + b * kPage + u.lo;
-    if constexpr (ONE)
-        store_token<DT>(a, u, blockIdx.y);
-    else
-        store_tokens<DT>(a, u, blockIdx.y);
+    const int parts = ONE ? token_parts(a) : (a.tokens + kPage - 2) / kPage + 1;
+    const int r = blockIdx.x / parts, part = blockIdx.x % parts;
+    auto place = [&](int i) {  // block i of those that the newest tokens can lie in (hi <= lo: they do not reach it)
+        const StoreRequest s = a.requests[r];
+        int n = s.tokens;
+        if (s.item >= 0) n = a.items[s.item].tok_begin + a.items[s.item].n_tokens;
+        const int first = n - a.tokens, b = first / kPage + i;
+        Unit u;
+        u.lo = max(first - b * kPage, 0);
+        u.hi = min(n - b * kPage, kPage);
+        u.block = a.blocks[s.page_off + (uint32_t)(u.hi > u.lo ? b : first / kPage)];
+        u.row = (int64_t)r * a.tokens + (b * kPage + u.lo - first);
+        u.pos = s.pos0 + b * kPage + u.lo;
+        return u;
+    };
+    if constexpr (ONE) {
+        store_token<DT>(a, r, part, [&] { return place(0); });
+    } else {
+        const Unit u = place(part);
+        if (u.hi > u.lo) store_tokens<DT>(a, u, blockIdx.y);
+    }
 }
 
 // The new tokens of a prefill plan's requests.  grid: (blocks they go to, KV heads)
@@ -395,32 +434,29 @@ __global__ __launch_bounds__(256) void projection_prefill_kernel(ProjectionPrefi
     store_tokens<DT>(p.base, u, blockIdx.y);
 }
 
-// A growing plan's step: workgroup (r, head) stores request r's new token and lengthens the item of that head in its leaf.
+// A growing plan's step: a request's new token, and the items of its leaf get longer.  (The leaf's length comes by value: other workgroups may have
+// lengthened its items already.)
 template <int DT>
-__global__ __launch_bounds__(256) void projection_append_kernel(ProjectionLaunch a, PlanGrowInline g) {
-    const int r = blockIdx.x, h = blockIdx.y;
-    const StoreRequest s = a.requests[r];
-    DecodeItem *item = g.items + g.grow_items[r * a.pool.num_kv_heads + h];
-    const int n = item->tok_begin + item->n_tokens, fresh = g.new_block[r];  // tokens in front of the new one
-    Unit u;
-    u.block = fresh >= 0 ? fresh : a.blocks[s.page_off + (uint32_t)(n / kPage)];
-    u.lo = n % kPage;
-    u.hi = u.lo + 1;
-    u.row = r;
-    u.pos = s.pos0 + n;
-    store_token<DT>(a, u, h);
-    __syncthreads();  // every wavefront has read the item
-    if (threadIdx.x == 0) item->n_tokens += 1;
-    if (threadIdx.x == 1 && h == 0 && fresh >= 0) g.pages[g.block_pos[r]] = fresh;
+__global__ __launch_bounds__(256) void projection_append_kernel(ProjectionAppend p, PlanGrowInline g) {
+    const ProjectionLaunch &a = p.base;
+    const int parts = token_parts(a), r = blockIdx.x / parts, part = blockIdx.x % parts, Hkv = a.pool.num_kv_heads;
+    const int n = p.length[r], fresh = g.new_block[r];
+    store_token<DT>(a, r, part, [&] {
+        const StoreRequest s = a.requests[r];
+        return Unit{fresh >= 0 ? fresh : a.blocks[s.page_off + (uint32_t)(n / kPage)], n % kPage, n % kPage + 1, r, s.pos0 + n};
+    });
+    const int h = 16 * part + (int)threadIdx.x;
+    if (threadIdx.x < 16 && h < Hkv) g.items[g.grow_items[r * Hkv + h]].n_tokens += 1;
+    if (threadIdx.x == 16 && part == 0 && fresh >= 0) g.pages[g.block_pos[r]] = fresh;
 }
 
 }  // namespace
 
 hipError_t launch_projection_store(const ProjectionLaunch &a, hipStream_t s) {
-    const int spans = a.tokens == 1 ? 1 : (a.tokens + kPage - 2) / kPage + 1;
-    const dim3 grid((unsigned)(a.n_requests * spans), a.pool.num_kv_heads), block(256);
     if (a.n_requests <= 0) return hipSuccess;
-    auto go = [&](auto one, auto many) { hipLaunchKernelGGL(a.tokens == 1 ? one : many, grid, block, 0, s, a); };
+    const bool single = a.tokens == 1;
+    const dim3 grid((unsigned)(a.n_requests * (single ? token_parts(a) : (a.tokens + kPage - 2) / kPage + 1)), single ? 1 : a.pool.num_kv_heads), block(256);
+    auto go = [&](auto one, auto many) { hipLaunchKernelGGL(single ? one : many, grid, block, 0, s, a); };
     if (a.pool.dtype == 0)
         go(projection_decode_kernel<0, true>, projection_decode_kernel<0, false>);
     else if (a.pool.dtype == 1)
@@ -442,10 +478,10 @@ hipError_t launch_projection_store(const ProjectionPrefill &a, hipStream_t s) {
     return hipGetLastError();
 }
 
-hipError_t launch_projection_append(const ProjectionLaunch &a, const PlanGrowInline &g, hipStream_t s) {
-    if (a.n_requests <= 0) return hipSuccess;
-    const dim3 grid(a.n_requests, a.pool.num_kv_heads), block(256);
-    if (a.pool.dtype == 0)
+hipError_t launch_projection_append(const ProjectionAppend &a, const PlanGrowInline &g, hipStream_t s) {
+    if (a.base.n_requests <= 0) return hipSuccess;
+    const dim3 grid((unsigned)(a.base.n_requests * token_parts(a.base))), block(256);
+    if (a.base.pool.dtype == 0)
         hipLaunchKernelGGL(projection_append_kernel<0>, grid, block, 0, s, a, g);
     else
         hipLaunchKernelGGL(projection_append_kernel<1>, grid, block, 0, s, a, g);

@@ -102,12 +102,16 @@ static void grow(const PlanGrowInline &g) {
     for (int r = 0; r < g.n_req; ++r)
         if (g.new_block[r] >= 0) g.pages[g.block_pos[r]] = g.new_block[r];
 }
-hipError_t launch_projection_append(const ProjectionLaunch &a, const PlanGrowInline &g, hipStream_t) {
+hipError_t launch_projection_append(const ProjectionAppend &p, const PlanGrowInline &g, hipStream_t) {
     ++store_launches;
+    const ProjectionLaunch &a = p.base;
     for (int r = 0; r < a.n_requests; ++r) {
         const StoreRequest s = a.requests[r];
-        const DecodeItem &item = g.items[g.grow_items[r * a.pool.num_kv_heads]];
-        const int n = item.tok_begin + item.n_tokens;
+        const int n = p.length[r];
+        for (int h = 0; h < a.pool.num_kv_heads; ++h) {
+            const DecodeItem &item = g.items[g.grow_items[r * a.pool.num_kv_heads + h]];
+            CHECK(item.tok_begin + item.n_tokens == n && item.kv_head == h);
+        }
         put_unit(a, g.new_block[r] >= 0 ? g.new_block[r] : a.blocks[s.page_off + (uint32_t)(n / 16)], n % 16, n % 16 + 1, r, s.pos0 + n);
     }
     grow(g);
