@@ -8,9 +8,9 @@
 // loads are on their way together, neighbouring lanes read neighbouring dimensions, and what it holds goes out as it lies in the
 // block.  fp8 blocks get the scale of what they hold now and are rounded again, as a block written anew.
 //
-// Bound by memory and, in 8 bits, as much by the rounding's instructions.  8 KV heads, MI355X: the choice of 2048 of 8190 tokens takes 11 us, their move (bf16)
-// 9 us; 32 sequences of 4096 tokens that keep 1000 each (fp8) 10 us and 52 us, 150 MB of HBM traffic at 2.9 TB/s; 15 of 5907 that keep 2923 57 us in fp8, 119 us in
-// bf16 (3.8 TB/s).
+// The choice is bound by the chain of its steps: 2048 of 8190 tokens, 8 heads, 11 us (loads 3, a digit 1.3, places 2; digits of two bits by ballots
+// took 36).  The move is bound by memory, V's whole blocks included: 32 sequences of 4096 tokens that keep 1000 (8 heads, fp8) 52 us, 235 MB of HBM traffic
+// at 4.5 TB/s; 15 of 5907 that keep 2923 57 us, in bf16 119 us, 452 MB at 3.8 TB/s.
 #include <type_traits>
 
 #include "pool_block.h"

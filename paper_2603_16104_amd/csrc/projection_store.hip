@@ -10,7 +10,12 @@
 // the lane eight further (whole heads: one vector instruction, else through the LDS crossbar), interleaved pairs lie in one lane.
 // A workgroup takes one 16-token block of one KV head: a thread row per token, K, V and then the query heads of the group, so that the
 // angles are taken once for all of them, and the fp8 scale of the block is the workgroup's own.  Where a request brings a
-// single token the 16 thread rows take 16 of its heads' rows.
+// single token the 16 thread rows take 16 of its heads' rows (512 requests x 72 rows, fp8: 9.7 us; a workgroup per KV head, most of whose thread
+// rows had nothing to do, 12.6).
+//
+// Many tokens are bound by memory: 29 000 tokens of 32 + 8 heads, 708 MB, 153 us, 4.6 TB/s.  Few tokens are bound by latency: a launch, the loads of the rows
+// beside those that find the block, angles, stores: 64 requests 3.9 us, four 2.6.  V's part of a block is 16 tokens wide, so that a single token
+// costs a write of 32 bytes (fp8: 16) for every dimension of its V: 17 MB for the 512 requests, whose keys and values are 1 MB.
 #include "pool_block.h"
 
 namespace hkv {
