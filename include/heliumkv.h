@@ -607,7 +607,7 @@ int hkv_decode_plan_append_qkv(hkv_decode_plan *plan, const int32_t *new_page_id
  * node's last token, keep what they hold.
  *
  * hkv_decode_plan_track_weights: to be called once on a plan before the first attn_decode_plan_weights (it uploads the work list, blocking;
- * a growing plan may have grown).  bf16 and fp8 pools (ESHAPE for fp32 pools).  EINVAL if a 16-token block is in the forest twice. */
+ * a growing plan may have grown).  EINVAL if a 16-token block is in the forest twice. */
 int hkv_decode_plan_track_weights(hkv_decode_plan *plan);
 /* q, lse: as attn_decode_plan_run took and gave them for this plan (lse is needed here).  decay: 0 to 1; 1 adds up, 0 replaces
  * (key_weights is then not read).  n_new (0 .. tokens_per_req): the last n_new tokens of every request's last node are new and start

@@ -236,6 +236,7 @@ static_assert(sizeof(ProjectionAppend) + sizeof(PlanGrowInline) <= 4096, "kernel
 // Keys of attn_decode_plan_weights: up to `length` tokens of a node from tok_begin on, one KV head, all rows below the node.  A workgroup's items are
 // kWeightWaves in a row: one for each wavefront, or, of a node of more than 16 rows, one for all of them, listed so many times.
 constexpr int kMaxWeightTokens = 1024, kWeightWaves = 8;
+constexpr int kFp32Waves = 4;  // fp32 pools: an item is a workgroup's, a multiple of 128 tokens
 struct KeyWeightItem {
     int32_t page_off;            // index of the first token's block in the plan's block list
     int32_t tok_begin;           // within the node, a multiple of 32
@@ -249,7 +250,7 @@ struct KeyWeightItem {
 };
 struct KeyWeightsLaunch {
     PoolView pool;
-    const void *q;               // [rows][Hq][128] bf16
+    const void *q;               // [rows][Hq][128] bf16 (fp32 pools: fp32)
     const float *lse;            // [rows][Hq]
     const KeyWeightItem *items;  // device
     const DecodeItem *plan_items;

@@ -12,6 +12,10 @@
 //   the wavefronts walk over the keys; more rows are taken in turns over the same keys.  Where there are few keys, a workgroup has 32, 64 or
 //   128 of them and several wavefronts share the rows of a pair of blocks.
 //
+// fp32 pools: the same with the matrix instruction of that type, 16 times slower, so that its time is what counts beyond some 16 rows
+// (64 requests over 2048 shared and 512 own tokens 44 us, their attention 92; 16 requests over 4096 own tokens 47 us, 5.8 TB/s.  A key a lane with a row's dimensions by
+// scalar loads, without matrix instructions: 109 and 45).
+//
 // MI355X, 8 KV heads: 16 prompts x 8192 tokens x 256 rows alone 107 us (0.64 PFLOP/s; 48 vector instructions a step of 16 x 32, 8 of them exponentials); 1024 requests'
 // own 2048 tokens alone (fp8) 394 us, 5.45 TB/s of keys beside their weights; both kinds (512 requests), 1.29 GB, 273 us.  Rows and keys the other way round (queries as
 // columns, a shuffle a row for every sum) took 607 us there, tiles of 32 rows whose exponentials wait for their products 311.
@@ -330,11 +334,106 @@ __global__ __launch_bounds__(kThreads, 4) void key_weights_kernel(KeyWeightsLaun
         many_rows<DT>(a, it, b, n_node, G, rows);
 }
 
+// ---- fp32 pools
+struct Rows32 {
+    float q[16][kHeadDim + 4];
+    float lse2[16];
+    int limit[16];
+    unsigned long long mask[16];
+};
+// Workgroup: an item.  A wavefront holds a pair of blocks; the rows come by in tiles of 16, through LDS, the next tile's on their way meanwhile.
+__global__ __launch_bounds__(64 * kFp32Waves) void key_weights_fp32_kernel(KeyWeightsLaunch a) {
+    static_assert(kFp32Waves == 4, "16 threads a row");
+    __shared__ __align__(16) Rows32 s;
+    const KeyWeightItem it = a.items[blockIdx.x];
+    const int tid = threadIdx.x, lane = tid & 63, wave = wave_index(), g = lane >> 4, G = a.num_q_heads / a.pool.num_kv_heads;
+    const int n_rows = it.n_req * G, row_tiles = (n_rows + 15) / 16;
+    Blocks b;
+    b.n = (min(it.length, it.tokens - it.tok_begin) + kPage - 1) / kPage;
+    b.id = a.pages[it.page_off + min(lane, b.n - 1)];
+    b.scale = 1.f;
+    const float c = a.scale * kLog2e;
+    // 16 threads bring a row: its place, two pieces of it, what is known of it
+    auto row_of = [&](int rt, int *row) { return row_place(a, it, 16 * rt + (tid >> 4), G, row); };
+    u32x4 w[2];
+    QueryRow info;
+    auto fetch = [&](int64_t q, int row) {
+        const float *p = static_cast<const float *>(a.q) + q + 8 * (tid & 15);
+        w[0] = ld16(p);
+        w[1] = ld16(p + 4);
+        info = row_at(a, it, q, row);
+    };
+    for (int first = 0; first < (b.n + 1) / 2; first += kFp32Waves) {
+        const int tile = first + wave, t0 = it.tok_begin + 32 * tile;
+        f32x4 k[2][8];  // dims 16 i + 4 g .. + 3 of a key, which are steps 4 i .. 4 i + 3 of the product
+        float old = 0.f, sum[2] = {0.f, 0.f};
+        if (a.decay != 0.f) old = a.weights[weight_place(a, it, b, tile)];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+            const float *p = static_cast<const float *>(a.pool.k_pages) + place(a, it, b, 2 * tile + j) * kBlockElems + (lane & 15) * 16 + 4 * g;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) k[j][i] = *reinterpret_cast<const f32x4 *>(p + 256 * i);
+        }
+        const bool staged = row_tiles == 1 && first > 0, partial = a.row_leaf && it.node >= 0 && t0 + 32 > it.tokens - a.tokens_per_req;
+        int next_row;
+        int64_t next_q = 0;
+        if (!staged) {
+            next_q = row_of(0, &next_row);
+            fetch(next_q, next_row);
+            next_q = row_of(1, &next_row);
+        }
+        for (int rt = 0; rt < row_tiles; ++rt) {
+            if (!staged) {
+                __syncthreads();  // the tile before has been read
+                const bool counts = info.lse2 < INFINITY;
+                float *p = s.q[tid >> 4] + 8 * (tid & 15);
+                *reinterpret_cast<u32x4 *>(p) = counts ? w[0] : u32x4{0u, 0u, 0u, 0u};
+                *reinterpret_cast<u32x4 *>(p + 4) = counts ? w[1] : u32x4{0u, 0u, 0u, 0u};
+                if ((tid & 15) == 0) {
+                    s.lse2[tid >> 4] = info.lse2;
+                    s.limit[tid >> 4] = info.limit;
+                    s.mask[tid >> 4] = info.mask;
+                }
+                __syncthreads();
+                if (rt + 1 < row_tiles) {
+                    fetch(next_q, next_row);
+                    next_q = row_of(rt + 2, &next_row);
+                }
+            }
+            f32x4 x[2] = {{0.f, 0.f, 0.f, 0.f}, {0.f, 0.f, 0.f, 0.f}};
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const f32x4 q = *reinterpret_cast<const f32x4 *>(s.q[lane & 15] + 16 * i + 4 * g);
+#pragma unroll
+                for (int e = 0; e < 4; ++e)
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) x[j] = __builtin_amdgcn_mfma_f32_16x16x4f32(q[e], k[j][i][e], x[j], 0, 0, 0);
+            }
+            const float4 l = *reinterpret_cast<const float4 *>(s.lse2 + 4 * g);  // the result's rows 4 g .. 4 g + 3
+#pragma unroll
+            for (int j = 0; j < 2; ++j) {
+                float p[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    p[i] = fast_exp2(__builtin_fmaf(x[j][i], c, -(i == 0 ? l.x : i == 1 ? l.y : i == 2 ? l.z : l.w)));
+                    if (partial && !sees(s.limit[4 * g + i], s.mask[4 * g + i], t0 + 16 * j + (lane & 15))) p[i] = 0.f;
+                }
+                sum[j] += (p[0] + p[1]) + (p[2] + p[3]);
+            }
+        }
+        sum[0] = rows_sum(sum[0]);
+        sum[1] = rows_sum(sum[1]);
+        put_weight(a, it, b, tile, it.tokens, true, old, lane & 16 ? sum[1] : sum[0]);
+    }
+}
+
 }  // namespace
 
 hipError_t launch_key_weights(const KeyWeightsLaunch &a, hipStream_t s) {
     if (a.n_items <= 0) return hipSuccess;
-    if (a.pool.dtype == 0)
+    if (a.pool.dtype == 2)
+        hipLaunchKernelGGL(key_weights_fp32_kernel, dim3(a.n_items), dim3(64 * kFp32Waves), 0, s, a);
+    else if (a.pool.dtype == 0)
         hipLaunchKernelGGL(key_weights_kernel<0>, dim3(a.n_items / kWaves), dim3(kThreads), 0, s, a);
     else
         hipLaunchKernelGGL(key_weights_kernel<1>, dim3(a.n_items / kWaves), dim3(kThreads), 0, s, a);

@@ -221,10 +221,71 @@ extern "C" int hkv_decode_plan_append_qkv(hkv_decode_plan *plan, const int32_t *
 
 // ---------------------------------------------------------------------------------------------
 // weights of cached keys
+// fp32 pools: the work list, and the lists that the kernel reads beside it, which plans over them do not have on the device.
+static int track_fp32(hkv_decode_plan *plan) {
+    const char *who = "hkv_decode_plan_track_weights";
+    const int Hkv = plan->pool->d.num_kv_heads, n_nodes = (int)plan->nodes.size(), T = plan->tokens_per_req, n = plan->n_req;
+    std::vector<char> last(n_nodes, 0);
+    for (int r = 0; r < n; ++r) last[plan->req_leaf[r]] = 1;
+    auto requests = [&](int v) { return plan->node_req_indptr[v + 1] - plan->node_req_indptr[v]; };
+    // nodes of a single tile of rows: as many tokens as make 1024 workgroups, which load their rows once; others: a step of 128, since it loads all rows
+    int64_t keys = 0;
+    for (int v = 0; v < n_nodes; ++v)
+        if (requests(v) > 0) keys += (int64_t)plan->nodes[v].n_tokens * Hkv;
+    const int alone = (int)std::clamp<int64_t>(keys / 1024 / 128 * 128, 128, kMaxWeightTokens);
+    std::vector<KeyWeightItem> items;
+    for (int v = 0; v < n_nodes; ++v) {
+        const hkv_node &nd = plan->nodes[v];
+        const int length = (int64_t)requests(v) * plan->group > 16 ? 128 : alone;
+        for (int64_t t = 0; requests(v) > 0 && t < nd.n_tokens; t += length)
+            for (int h = 0; h < Hkv; ++h)
+                items.push_back(KeyWeightItem{nd.page_begin + (int32_t)(t / HKV_PAGE_SIZE), (int32_t)t, length, h, plan->node_req_indptr[v], requests(v), last[v] ? v : ~v,
+                                              nd.n_tokens, -1});
+    }
+    if (items.size() > INT_MAX / (64 * kFp32Waves)) return fail(HKV_EINVAL, "%s: too many keys", who);
+    if (plan->d_bt && !items.empty()) {
+        std::vector<int32_t> lists(plan->node_pages);
+        lists.insert(lists.end(), plan->node_req_idx.begin(), plan->node_req_idx.end());
+        const size_t bytes = sizeof(KeyWeightItem) * items.size();
+        std::vector<unsigned long long> masks;  // then the rows' last nodes and limits: query token t of a request sees all but the T - 1 - t newest keys
+        std::vector<int32_t> rows;
+        for (int r = 0; T > 1 && r < n; ++r) {
+            masks.push_back((2ull << (r % T)) - 1);
+            rows.push_back(plan->req_leaf[r]);
+        }
+        for (int r = 0; T > 1 && r < n; ++r) rows.push_back(plan->nodes[plan->req_leaf[r]].n_tokens - T);
+        char *d = nullptr;
+        void *visible = nullptr;
+        hipError_t e = hipMalloc((void **)&d, bytes + sizeof(int32_t) * lists.size());
+        if (e == hipSuccess) e = hipMemcpy(d, items.data(), bytes, hipMemcpyHostToDevice);
+        if (e == hipSuccess) e = hipMemcpy(d + bytes, lists.data(), sizeof(int32_t) * lists.size(), hipMemcpyHostToDevice);
+        if (T > 1) {
+            if (e == hipSuccess) e = hipMalloc(&visible, n * (sizeof(unsigned long long) + 2 * sizeof(int32_t)));
+            if (e == hipSuccess) e = hipMemcpy(visible, masks.data(), sizeof(unsigned long long) * n, hipMemcpyHostToDevice);
+            if (e == hipSuccess) e = hipMemcpy(static_cast<unsigned long long *>(visible) + n, rows.data(), 2 * sizeof(int32_t) * n, hipMemcpyHostToDevice);
+        }
+        if (e != hipSuccess) {
+            if (d) (void)hipFree(d);
+            if (visible) (void)hipFree(visible);
+            return fail_hip(e, who);
+        }
+        plan->d_weight_items = reinterpret_cast<KeyWeightItem *>(d);
+        plan->d_pages = reinterpret_cast<int32_t *>(d + bytes);
+        plan->d_node_req_idx = plan->d_pages + plan->node_pages.size();
+        if (T > 1) {
+            plan->d_row_mask = static_cast<unsigned long long *>(visible);
+            plan->d_row_leaf = reinterpret_cast<int32_t *>(plan->d_row_mask + n);
+            plan->d_row_limit = plan->d_row_leaf + n;
+        }
+    }
+    plan->weight_items.swap(items);
+    plan->tracks_weights = true;
+    return HKV_OK;
+}
+
 extern "C" int hkv_decode_plan_track_weights(hkv_decode_plan *plan) try {
     const char *who = "hkv_decode_plan_track_weights";
     if (!plan) return fail(HKV_EINVAL, "%s: null plan", who);
-    if (plan->pool->d.dtype == HKV_FP32) return fail(HKV_ESHAPE, "%s: bf16 and fp8 pools only", who);
     if (plan->tracks_weights) return HKV_OK;
     const int Hkv = plan->pool->d.num_kv_heads, n_nodes = (int)plan->nodes.size();
     std::vector<int32_t> blocks;
@@ -232,6 +293,7 @@ extern "C" int hkv_decode_plan_track_weights(hkv_decode_plan *plan) try {
         if (plan->node_req_indptr[v + 1] > plan->node_req_indptr[v])
             blocks.insert(blocks.end(), plan->node_pages.begin() + plan->nodes[v].page_begin, plan->node_pages.begin() + plan->nodes[v].page_begin + plan->nodes[v].n_pages);
     if (all_different(blocks) < 0) return fail(HKV_EINVAL, "%s: a 16-token block is in the forest twice", who);
+    if (plan->pool->d.dtype == HKV_FP32) return track_fp32(plan);
     std::vector<char> last(n_nodes, 0);
     std::vector<int32_t> grows(n_nodes, -1);
     for (int r = 0; r < plan->n_req; ++r) {
@@ -308,7 +370,6 @@ extern "C" int attn_decode_plan_weights(hkv_decode_plan *plan, const void *q, fl
                                         float *key_weights, void *stream) {
     const char *who = "attn_decode_plan_weights";
     if (!plan) return fail(HKV_EINVAL, "%s: null plan", who);
-    if (plan->pool->d.dtype == HKV_FP32) return fail(HKV_ESHAPE, "%s: bf16 and fp8 pools only", who);
     if (!plan->tracks_weights) return fail(HKV_EINVAL, "%s: hkv_decode_plan_track_weights has not been called", who);
     if (plan->n_req == 0) return HKV_OK;
     if (!q || !lse || !key_weights) return fail(HKV_EINVAL, "%s: null q, lse or key_weights", who);
@@ -316,7 +377,7 @@ extern "C" int attn_decode_plan_weights(hkv_decode_plan *plan, const void *q, fl
         return fail(HKV_EINVAL, "%s: q and key_weights must be 16-byte aligned, lse 4-byte", who);
     if (!(decay >= 0.f && decay <= 1.f)) return fail(HKV_EINVAL, "%s: decay %g (0 to 1)", who, (double)decay);
     if (n_new < 0 || n_new > plan->tokens_per_req) return fail(HKV_EINVAL, "%s: n_new %d (0 to the %d query tokens of a request)", who, n_new, plan->tokens_per_req);
-    if (!plan->dev) return fail(HKV_EINVAL, "%s: plan was built host-only", who);
+    if (!on_device(plan)) return fail(HKV_EINVAL, "%s: plan was built host-only", who);
     const KeyWeightsLaunch a{view_of(plan->pool), q, lse, plan->d_weight_items, plan->d_items, plan->d_pages, plan->d_node_req_idx, plan->d_q_rows,
                              plan->d_row_leaf, plan->d_row_limit, plan->d_row_mask, key_weights, (int32_t)plan->weight_items.size(), plan->num_q_heads,
                              plan->tokens_per_req, n_new, scale, decay};

@@ -119,8 +119,21 @@ hipError_t launch_projection_append(const ProjectionAppend &p, const PlanGrowInl
 }
 hipError_t launch_key_weights(const KeyWeightsLaunch &a, hipStream_t) {
     ++weights_launches;
-    CHECK(a.n_items % kWeightWaves == 0);
     const int G = a.num_q_heads / a.pool.num_kv_heads;
+    if (a.pool.dtype == HKV_FP32) {
+        for (int x = 0; x < a.n_items; ++x) {
+            const KeyWeightItem &it = a.items[x];
+            CHECK(it.length % 128 == 0 && it.length <= kMaxWeightTokens && (it.n_req * G <= 16 || it.length == 128) && it.tok_begin < it.tokens);
+            for (int j = 0; j < it.n_req; ++j) {
+                const int row = a.node_req_idx[it.req_off + j];
+                CHECK(row >= 0 && (!a.row_leaf || (a.row_leaf[row] >= 0 && a.row_limit[row] >= 0 && (a.row_mask[row] & 1))));
+            }
+            for (int t = it.tok_begin; t < std::min(it.tok_begin + it.length, it.tokens); ++t)
+                keys_seen.push_back({((int64_t)a.pages[it.page_off + (t - it.tok_begin) / 16] * a.pool.num_kv_heads + it.kv_head) * 16 + t % 16, it.n_req});
+        }
+        return hipSuccess;
+    }
+    CHECK(a.n_items % kWeightWaves == 0);
     for (int x = 0; x < a.n_items; ++x) {
         const KeyWeightItem &it = a.items[x];
         const bool many = it.n_req * G > 16;
@@ -273,7 +286,7 @@ static void decode_plans(std::mt19937 &rng) {
     for (int trial = 0; trial < 120; ++trial) {
         const int dtype = trial % 5 == 4 ? HKV_FP32 : trial & 1 ? HKV_FP8_E4M3 : HKV_BF16, P = 16 << pick(rng, 4), S = P / 16, heads = 1 + pick(rng, 9), group = 1 + pick(rng, 16);
         const bool growing = dtype != HKV_FP32 && trial % 3 == 1;
-        const int T = growing || dtype == HKV_FP32 ? 1 : pick(rng, 3) ? 1 : 1 + pick(rng, 40);
+        const int T = growing ? 1 : pick(rng, 3) ? 1 : 1 + pick(rng, dtype == HKV_FP32 ? 16 : 40);
         const int n = trial < 8 ? 257 + pick(rng, 60) : 1 + pick(rng, 40), reserve = growing ? 1 + pick(rng, 3 * P) : 0;
         std::vector<hkv_node> nodes;
         std::vector<int32_t> pages, leaf;
@@ -355,12 +368,8 @@ static void decode_plans(std::mt19937 &rng) {
         for (int step = 0;; ++step) {
             CHECK(hkv_decode_plan_store(plan, &x, nullptr) == HKV_OK);
             CHECK(same(taken(), newest()));
-            if (dtype != HKV_FP32) {
-                if (step == track) CHECK(hkv_decode_plan_track_weights(plan) == HKV_OK);
-                if (step >= track && step % 4 == track % 4) weights();
-            } else {
-                CHECK(hkv_decode_plan_track_weights(plan) == HKV_ESHAPE);
-            }
+            if (step == track) CHECK(hkv_decode_plan_track_weights(plan) == HKV_OK);
+            if (step >= track && step % 4 == track % 4) weights();
             if (step == steps) break;
             std::vector<int32_t> ids(n, -1);
             for (int r = 0; r < n; ++r) {

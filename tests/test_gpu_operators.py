@@ -413,11 +413,17 @@ WEIGHTS = [  # dtype, heads, page, parents, tokens, last nodes, tokens per reque
     (hkv.BF16, (24, 8), 64, [-1], [13001], [0], 6, 0.0, 6),
     (hkv.FP8_E4M3, (8, 2), 16, [-1] + [0] * 80, [40001] + [16] * 80, list(range(1, 81)), 1, 1.0, 1),
     (hkv.BF16, (8, 8), 16, [-1, 0], [35000, 12345], [1], 2, 0.9, 1),
+    # fp32 pools: 4 partial sums of 32 products, each with a rounding, and 3 more: 35 * 2^-24 of the sum of |products| (below 40) in the exponent, the rest as above
+    (hkv.FP32, (8, 2), 16, [-1, 0, 0, 0], [304, 17, 1, 129], [1, 2, 3], 1, 1.0, 1),
+    (hkv.FP32, (16, 1), 32, [-1, 0, 1, 1, 0], [32, 64, 5, 0, 128], [2, 3, 4, 4, 1], 1, 0.5, 0),
+    (hkv.FP32, (6, 2), 64, [-1, 0, 0], [64, 64, 270], [1, 2], 9, 0.0, 9),
+    (hkv.FP32, (1, 1), 16, [-1], [1], [0], 1, 1.0, 1),
+    (hkv.FP32, (8, 2), 16, [-1] + [0] * 40, [2000] + [20] * 40, list(range(1, 41)), 1, 0.9, 1),
 ]
 
 
-@pytest.mark.parametrize("mapped", [False, True])
-@pytest.mark.parametrize("case", range(len(WEIGHTS)))
+# (plans over fp32 pools have no rows of their own)
+@pytest.mark.parametrize("case, mapped", [(c, m) for c in range(len(WEIGHTS)) for m in (False, True) if not m or WEIGHTS[c][0] != hkv.FP32])
 def test_weights_of_cached_keys(case, mapped):
     dtype, (hq, heads), page, parent, tokens, leaves, T, decay, n_new = WEIGHTS[case]
     nodes, pages, blocks, _ = forest(parent, tokens, page, case)
@@ -435,7 +441,7 @@ def test_weights_of_cached_keys(case, mapped):
     plan = hkv.hkv_decode_plan_create_ex(pool.handle, nodes, pages, leaves, hq, tokens_per_req=T, visible=masks, q_rows=row_of if mapped else None)
     g = torch.Generator(device="cuda")
     g.manual_seed(case)
-    q = (2 * torch.randn(n + 3, hq, 128, device="cuda", generator=g)).to(torch.bfloat16)
+    q = (2 * torch.randn(n + 3, hq, 128, device="cuda", generator=g)).to(torch.float32 if dtype == hkv.FP32 else torch.bfloat16)
     q64 = q.float().cpu().double().numpy()[row_of]
     kv = pool.values()[0]
     lse64 = path_lse(kv, parent, tokens, blocks, leaves, q64, T, heads, masks)
@@ -765,6 +771,36 @@ def test_a_prompt_is_stored_judged_and_shrunk(dtype):
     for p in (window, grown):
         hkv.hkv_decode_plan_destroy(p)
     hkv.hkv_prefill_plan_destroy(plan)
+    pool.close()
+
+
+@pytest.mark.parametrize("dtype", [hkv.BF16, hkv.FP8_E4M3, hkv.FP32])
+def test_the_attentions_own_lse_and_then_eviction(dtype):
+    """Every row of a step gives away 1 in all, whatever the pool's type; what is kept weighs at least what is dropped."""
+    hq, heads, T = 8, 2, 2
+    nodes, pages, blocks, _ = forest([-1, 0, 0, 0], [160, 70, 33, 2], 16, 4)
+    pool = Pool(len(pages) + 8, heads, dtype, seed=9)
+    plan = hkv.hkv_decode_plan_create_ex(pool.handle, nodes, pages, [1, 2, 3], hq, tokens_per_req=T)
+    g = torch.Generator(device="cuda")
+    g.manual_seed(1)
+    q = (2 * torch.randn(3 * T, hq, 128, device="cuda", generator=g)).to(torch.float32 if dtype == hkv.FP32 else torch.bfloat16)
+    out, lse = torch.empty_like(q), torch.empty(3 * T, hq, device="cuda")
+    ws = torch.empty(hkv.hkv_decode_plan_workspace_bytes(plan) + 256, dtype=torch.uint8, device="cuda")
+    w = torch.full((pool.blocks, heads, 16), float("nan"), device="cuda")
+    hkv.attn_decode_plan_run(plan, q, SCALE, out, lse, ws, ws.numel())
+    hkv.hkv_decode_plan_track_weights(plan)
+    hkv.attn_decode_plan_weights(plan, q, SCALE, lse, 0.0, T, w)
+    got = w.cpu().double().numpy()
+    live = ~np.isnan(got)
+    assert live.sum() == (160 + 70 + 33 + 2) * heads
+    assert abs(got[live].sum() - 3 * T * hq) <= 1e-3 * 3 * T * hq    # (lse as the attention rounds it)
+    kept = torch.empty(heads, 40, dtype=torch.int32, device="cuda")
+    free = np.setdiff1d(np.arange(len(pages) + 8), pages)[:3]
+    hkv.kv_pool_evict(pool.handle, pages[:10], [160], free, [40], 2, 5, w, kept)
+    k = kept.cpu().numpy()
+    for h in range(heads):
+        assert np.array_equal(k[h], evicted(got[:, h].astype(np.float32), blocks[0], 160, 40, 2, 5))
+    hkv.hkv_decode_plan_destroy(plan)
     pool.close()
 
 

@@ -136,9 +136,12 @@ def test_weights_refusals():
     hkv.kv_pool_destroy(pool)
     pool = fake_pool(dtype=hkv.FP32)
     plan = decode_plan(pool)
-    assert code(hkv.hkv_decode_plan_track_weights, plan) == hkv.ESHAPE
-    assert code(run, p=plan) == hkv.ESHAPE
-    hkv.hkv_decode_plan_destroy(plan)
+    hkv.hkv_decode_plan_track_weights(plan)
+    assert code(run, p=plan) == hkv.EINVAL and "host-only" in hkv.last_error()
+    twice = decode_plan(pool, pages=(0, 1, 2, 3, 1))
+    assert code(hkv.hkv_decode_plan_track_weights, twice) == hkv.EINVAL and "twice" in hkv.last_error()
+    for p in (plan, twice):
+        hkv.hkv_decode_plan_destroy(p)
     hkv.kv_pool_destroy(pool)
 
 
