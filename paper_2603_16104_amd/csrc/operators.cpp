@@ -170,8 +170,8 @@ extern "C" int hkv_decode_plan_store(hkv_decode_plan *plan, const hkv_qkv *rows,
     }
     if (look) plan->store_blocks = all_different(blocks);
     if (plan->store_blocks < 0) return fail(HKV_EINVAL, "%s: newest tokens of two requests go to the same 16-token block", who);
-    const int64_t parts = plan->tokens_per_req > 1 ? plan->tokens_per_req / HKV_PAGE_SIZE + 2 : (plan->num_q_heads + pool->d.num_kv_heads + 15) / 16;
-    if (n * parts > INT_MAX / 256) return fail(HKV_EINVAL, "%s: too many requests", who);
+    const int64_t T = plan->tokens_per_req, Hkv = pool->d.num_kv_heads;  // (a launch keeps below 2^31 threads, whatever it goes by)
+    if (n * ((T / HKV_PAGE_SIZE + 2) * Hkv + T * ((plan->num_q_heads + Hkv) / 16 + 1)) > INT_MAX / 256) return fail(HKV_EINVAL, "%s: too many requests", who);
     decode_places(plan, a);
     HKV_HIP(launch_projection_store(a, static_cast<hipStream_t>(stream)));
     return HKV_OK;

@@ -9,9 +9,9 @@
 // 16 lanes hold a row, eight dimensions each: the sum of squares is four steps across them, the other half of a split pair comes from
 // the lane eight further (whole heads: one vector instruction, else through the LDS crossbar), interleaved pairs lie in one lane.
 // A workgroup takes one 16-token block of one KV head: a thread row per token, K, V and then the query heads of the group, so that the
-// angles are taken once for all of them, and the fp8 scale of the block is the workgroup's own.  Where a request brings a
-// single token the 16 thread rows take 16 of its heads' rows (512 requests x 72 rows, fp8: 9.7 us; a workgroup per KV head, most of whose thread
-// rows had nothing to do, 12.6).
+// angles are taken once for all of them, and the fp8 scale of the block is the workgroup's own.  Where a request brings one or two tokens, the 16 thread rows take 16
+// of a token's heads (512 requests x 72 rows, fp8: 9.7 us; a workgroup per KV head, most of whose thread rows had nothing to do, 12.6), and up to 24 tokens, its queries
+// go that way and its keys and values by blocks.
 //
 // Many tokens are bound by memory: 29 000 tokens of 32 + 8 heads, 708 MB, 153 us, 4.6 TB/s.  Few tokens are bound by latency: a launch, the loads of the rows
 // beside those that find the block, angles, stores: 64 requests 3.9 us, four 2.6.  V's part of a block is 16 tokens wide, so that a single token
@@ -201,8 +201,8 @@ __device__ __forceinline__ void put_block(const ProjectionLaunch &a, const Unit 
     }
 }
 
-// One KV head of one block with up to 16 tokens: thread row = slot.
-template <int DT>
+// One KV head of one block with up to 16 tokens: thread row = slot.  Q: with the query heads of its group.
+template <int DT, bool Q = true>
 __device__ __forceinline__ void store_tokens(const ProjectionLaunch &a, const Unit &u, int h) {
     __shared__ __align__(16) float sTurn[kPage][2 * 64 + 4];
     const int slot = threadIdx.x >> 4, c = threadIdx.x & 15;
@@ -213,8 +213,9 @@ __device__ __forceinline__ void store_tokens(const ProjectionLaunch &a, const Un
     // All loads at once, by all lanes and of what there is, if only a row again: a wait at the end of a branch would hold up those behind it.
     const Row<DT> kr = load_row<DT>(a.k, a.k_stride, row, h, c), vr = load_row<DT>(a.v, a.v_stride, row, h, c);
     Row<DT> q[kAhead];
+    if constexpr (Q)
 #pragma unroll
-    for (int j = 0; j < kAhead; ++j) q[j] = load_row<DT>(a.q, a.q_stride, row, h * a.group + min(j, a.group - 1), c);
+        for (int j = 0; j < kAhead; ++j) q[j] = load_row<DT>(a.q, a.q_stride, row, h * a.group + min(j, a.group - 1), c);
     const Row<DT> qn = load_row<DT>(a.q_norm ? a.q_norm : a.q, 0, 0, 0, c), kn = load_row<DT>(a.k_norm ? a.k_norm : a.q, 0, 0, 0, c);
     const bool turns = 8 * c < a.rotary_dim;
     const int p0 = turns ? 4 * c : 0;
@@ -240,7 +241,7 @@ __device__ __forceinline__ void store_tokens(const ProjectionLaunch &a, const Un
         turn_of(a, sTurn[slot], c, t);
         values<DT>(kr, k);
         norm_and_turn(a, c, a.k_norm != nullptr, kw, t, k);
-        for (int j0 = 0; j0 < a.group; j0 += kAhead) {
+        for (int j0 = 0; Q && j0 < a.group; j0 += kAhead) {
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
                 const int head = j0 + j;
@@ -293,12 +294,12 @@ __device__ __forceinline__ void round_again(const ProjectionLaunch &a, int64_t b
 
 __host__ __device__ inline int token_parts(const ProjectionLaunch &a) { return (a.pool.num_kv_heads * (a.group + 1) + 15) / 16; }
 
-// One token, row `token` of the rows: 16 of its heads' rows, K's (with V's) first, then the queries'.  All threads of the workgroup call.  `place` finds the
+// One token, row `token` of the rows: 16 of its heads' rows, from row `from` on, K's (with V's) first, then the queries'.  All threads of the workgroup call.  `place` finds the
 // token's Unit, by a chain of loads that goes on beside those of the rows.
 template <int DT, class Place>
-__device__ __forceinline__ void store_token(const ProjectionLaunch &a, int64_t token, int part, Place &&place) {
+__device__ __forceinline__ void store_token(const ProjectionLaunch &a, int64_t token, int from, Place &&place) {
     __shared__ __align__(16) float sTurn[2 * 64];
-    const int Hkv = a.pool.num_kv_heads, Hq = Hkv * a.group, c = threadIdx.x & 15, d = 8 * c, i = 16 * part + ((int)threadIdx.x >> 4);
+    const int Hkv = a.pool.num_kv_heads, Hq = Hkv * a.group, c = threadIdx.x & 15, d = 8 * c, i = from + ((int)threadIdx.x >> 4);
     const bool is_k = i < Hkv, is_q = !is_k && i - Hkv < Hq, has_angle = (int)threadIdx.x < a.rotary_dim / 2;
     const int head = is_k ? i : min(i - Hkv, Hq - 1);
     const int64_t row = a.row_map ? a.row_map[token] : token;
@@ -311,12 +312,12 @@ __device__ __forceinline__ void store_token(const ProjectionLaunch &a, int64_t t
     const bool normed = is_k ? k_norm != k_row : q_norm != q_row;
     const Row<DT> r = load_row<DT>(mine, 0, 0, 0, 0), wr = load_row<DT>(is_k ? k_norm : q_norm, 0, 0, 0, c);
     Row<DT> v{};
-    if (16 * part < Hkv) v = load_row<DT>(a.v, a.v_stride, row, min(head, Hkv - 1), c);
+    if (from < Hkv) v = load_row<DT>(a.v, a.v_stride, row, min(head, Hkv - 1), c);
     const Angles<1> angle = load_angles<1>(a, a.rotary_dim > 0 ? a.inv_freq : reinterpret_cast<const double *>(k_row), max(0, min((int)threadIdx.x, a.rotary_dim / 2 - 1)), row);
     const Unit u = place();
     const int64_t at = (int64_t)u.block * Hkv + head;
     float old[2] = {0.f, 0.f}, w[8], x[8];
-    if (DT == 1 && 16 * part < Hkv && u.lo > 0) {
+    if (DT == 1 && from < Hkv && u.lo > 0) {
         const int64_t s = (int64_t)u.block * Hkv + min(head, Hkv - 1);
         old[0] = a.pool.k_scale[s];
         old[1] = a.pool.v_scale[s];
@@ -395,30 +396,35 @@ __device__ __forceinline__ void store_token(const ProjectionLaunch &a, int64_t t
     }
 }
 
-// The newest tokens of a decode plan's requests.  grid: (requests x blocks that the tokens of one can span, KV heads); a single token each: requests x
-// sixteens of its rows
-template <int DT, bool ONE>
+// The newest tokens of a decode plan's requests.  By tokens: a workgroup takes 16 rows of heads of one token.  By blocks: a block that the tokens of
+// a request can span, and a KV head with its queries.  Both: keys and values by blocks (an fp8 block's scale is of all its new tokens), the queries by tokens.
+enum class By { kTokens, kBlocks, kBoth };
+__host__ __device__ inline int spans(const ProjectionLaunch &a) { return (a.tokens + kPage - 2) / kPage + 1; }
+template <int DT, By BY>
 __global__ __launch_bounds__(256) void projection_decode_kernel(ProjectionLaunch a) {
-    const int parts = ONE ? token_parts(a) : (a.tokens + kPage - 2) / kPage + 1;
-    const int r = blockIdx.x / parts, part = blockIdx.x % parts;
-    auto place = [&](int i) {  // block i of those that the newest tokens can lie in (hi <= lo: they do not reach it)
-        const StoreRequest s = a.requests[r];
+    const int Hkv = a.pool.num_kv_heads, n_blocks = a.n_requests * spans(a) * Hkv;  // (kBoth: workgroups that go by blocks, first)
+    // position of the first of the request's newest tokens in its last node
+    auto newest = [&](const StoreRequest &s) {
         int n = s.tokens;
         if (s.item >= 0) n = a.items[s.item].tok_begin + a.items[s.item].n_tokens;
-        const int first = n - a.tokens, b = first / kPage + i;
-        Unit u;
-        u.lo = max(first - b * kPage, 0);
-        u.hi = min(n - b * kPage, kPage);
-        u.block = a.blocks[s.page_off + (uint32_t)(u.hi > u.lo ? b : first / kPage)];
-        u.row = (int64_t)r * a.tokens + (b * kPage + u.lo - first);
-        u.pos = s.pos0 + b * kPage + u.lo;
-        return u;
+        return n - a.tokens;
     };
-    if constexpr (ONE) {
-        store_token<DT>(a, r, part, [&] { return place(0); });
+    if (BY == By::kTokens || (BY == By::kBoth && (int)blockIdx.x >= n_blocks)) {
+        const int from = BY == By::kBoth ? Hkv : 0, parts = (Hkv * (a.group + 1) - from + 15) / 16, i = blockIdx.x - (BY == By::kBoth ? n_blocks : 0);
+        const int x = i / parts, part = i % parts;
+        store_token<DT>(a, x, from + 16 * part, [&] {
+            const int r = x / a.tokens;
+            const StoreRequest s = a.requests[r];
+            const int t = newest(s) + (x - r * a.tokens);
+            return Unit{a.blocks[s.page_off + (uint32_t)(t / kPage)], t % kPage, t % kPage + 1, x, s.pos0 + t};
+        });
     } else {
-        const Unit u = place(part);
-        if (u.hi > u.lo) store_tokens<DT>(a, u, blockIdx.y);
+        const int unit = blockIdx.x / Hkv, h = blockIdx.x % Hkv, r = unit / spans(a), part = unit % spans(a);
+        const StoreRequest s = a.requests[r];
+        const int first = newest(s), b = first / kPage + part, lo = max(first - b * kPage, 0);
+        if (b * kPage >= first + a.tokens) return;
+        const Unit u{a.blocks[s.page_off + (uint32_t)b], lo, min(first + a.tokens - b * kPage, kPage), (int64_t)r * a.tokens + (b * kPage + lo - first), s.pos0 + b * kPage + lo};
+        store_tokens<DT, BY != By::kBoth>(a, u, h);
     }
 }
 
@@ -446,7 +452,7 @@ __global__ __launch_bounds__(256) void projection_append_kernel(ProjectionAppend
     const ProjectionLaunch &a = p.base;
     const int parts = token_parts(a), r = blockIdx.x / parts, part = blockIdx.x % parts, Hkv = a.pool.num_kv_heads;
     const int n = p.length[r], fresh = g.new_block[r];
-    store_token<DT>(a, r, part, [&] {
+    store_token<DT>(a, r, 16 * part, [&] {
         const StoreRequest s = a.requests[r];
         return Unit{fresh >= 0 ? fresh : a.blocks[s.page_off + (uint32_t)(n / kPage)], n % kPage, n % kPage + 1, r, s.pos0 + n};
     });
@@ -459,15 +465,18 @@ __global__ __launch_bounds__(256) void projection_append_kernel(ProjectionAppend
 
 hipError_t launch_projection_store(const ProjectionLaunch &a, hipStream_t s) {
     if (a.n_requests <= 0) return hipSuccess;
-    const bool single = a.tokens == 1;
-    const dim3 grid((unsigned)(a.n_requests * (single ? token_parts(a) : (a.tokens + kPage - 2) / kPage + 1)), single ? 1 : a.pool.num_kv_heads), block(256);
-    auto go = [&](auto one, auto many) { hipLaunchKernelGGL(single ? one : many, grid, block, 0, s, a); };
+    // us, 32 + 8 heads, by tokens / blocks / both.  bf16, 64 requests of 2 new tokens: 4.4 / 6.1 / 4.4, of 4: 5.9 / 6.9 / 4.8, 8: 8.5 / 7.8 / 6.0, 16: 12.6 / 9.1 / 8.3, 32: 20 / 11.7 / 11.5,
+    // 64: 42 / 21.4 / 22.3; 300 requests of 2: 9.7 / 19.2 / 13.1, of 4: 16.0 / 20.3 / 15.5.  fp8, 64 requests of 2: - / 8.1 / 6.5, of 16: - / 10.0 / 9.1, of 64: - / 20.9 / 22.9.
+    const By by = a.tokens == 1 || (a.tokens == 2 && a.pool.dtype != 1) ? By::kTokens : a.tokens <= 24 ? By::kBoth : By::kBlocks;
+    const int heads = a.pool.num_kv_heads, blocks = a.n_requests * spans(a) * heads, tokens = a.n_requests * a.tokens;
+    const dim3 grid(by == By::kTokens ? tokens * token_parts(a) : by == By::kBlocks ? blocks : blocks + tokens * ((heads * a.group + 15) / 16)), block(256);
+    auto go = [&](auto tokens, auto blocks, auto both) { hipLaunchKernelGGL(by == By::kTokens ? tokens : by == By::kBlocks ? blocks : both, grid, block, 0, s, a); };
     if (a.pool.dtype == 0)
-        go(projection_decode_kernel<0, true>, projection_decode_kernel<0, false>);
+        go(projection_decode_kernel<0, By::kTokens>, projection_decode_kernel<0, By::kBlocks>, projection_decode_kernel<0, By::kBoth>);
     else if (a.pool.dtype == 1)
-        go(projection_decode_kernel<1, true>, projection_decode_kernel<1, false>);
-    else
-        go(projection_decode_kernel<2, true>, projection_decode_kernel<2, false>);
+        go(projection_decode_kernel<1, By::kTokens>, projection_decode_kernel<1, By::kBlocks>, projection_decode_kernel<1, By::kBoth>);
+    else  // (no more than 16 query tokens, so never by blocks alone)
+        go(projection_decode_kernel<2, By::kTokens>, projection_decode_kernel<2, By::kBoth>, projection_decode_kernel<2, By::kBoth>);
     return hipGetLastError();
 }
 

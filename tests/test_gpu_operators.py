@@ -239,6 +239,19 @@ DECODE = [  # dtype, heads, page, parents, tokens, last nodes, tokens per reques
     (hkv.FP8_E4M3, (8, 2), 32, [-1, 0, 0], [33, 31, 18], [2, 1], 18, dict(big=4.0)),
     (hkv.FP32, (8, 2), 16, [-1, 0, 0], [32, 17, 3], [1, 2], 1, dict()),
     (hkv.FP32, (4, 1), 32, [-1, 0, 0], [32, 17, 40], [1, 2], 16, dict(interleaved=True, norm=False)),
+    # around the numbers of tokens at which rows are dealt out another way; heads that do not fill the last sixteen of rows; more than one sixteen of K's rows
+    (hkv.BF16, (5, 5), 16, [-1, 0, 0], [20, 2, 33], [1, 2], 2, dict(fused=False, in_place=True)),
+    (hkv.BF16, (14, 7), 16, [-1, 0, 0], [20, 3, 33], [1, 2], 3, dict(fused=False, in_place=True, rotary=64)),
+    (hkv.BF16, (20, 20), 32, [-1, 0, 0], [20, 17, 33], [1, 2], 1, dict(rotary=0)),
+    (hkv.BF16, (8, 2), 16, [-1, 0], [20, 40], [1], 24, dict(interleaved=True, rotary=96)),
+    (hkv.BF16, (8, 2), 16, [-1, 0], [20, 41], [1], 25, dict()),
+    (hkv.FP8_E4M3, (20, 20), 16, [-1, 0, 0], [20, 31, 16], [1, 2], 1, dict(big=20.0)),
+    (hkv.FP8_E4M3, (9, 3), 16, [-1, 0, 0], [20, 2, 33], [1, 2], 2, dict(fused=False, in_place=True, big=5.0)),
+    (hkv.FP8_E4M3, (6, 2), 64, [-1, 0], [20, 50], [1], 24, dict(axes=4, norm=False)),
+    (hkv.FP8_E4M3, (6, 2), 16, [-1, 0], [20, 70], [1], 64, dict(big=2.0)),
+    (hkv.FP32, (20, 20), 16, [-1, 0, 0], [32, 17, 40], [1, 2], 1, dict(rotary=48)),
+    (hkv.FP32, (6, 2), 16, [-1, 0, 0], [32, 17, 40], [1, 2], 2, dict(fused=False, in_place=True)),
+    (hkv.FP32, (6, 2), 16, [-1, 0, 0], [32, 17, 40], [1, 2], 7, dict(axes=2)),
 ]
 
 
