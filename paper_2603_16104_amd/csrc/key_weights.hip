@@ -17,7 +17,7 @@
 // scalar loads, without matrix instructions: 109 and 45).
 //
 // MI355X, 8 KV heads: 16 prompts x 8192 tokens x 256 rows alone 107 us (0.64 PFLOP/s; 48 vector instructions a step of 16 x 32, 8 of them exponentials); 1024 requests'
-// own 2048 tokens alone (fp8) 394 us, 5.45 TB/s of keys beside their weights; both kinds (512 requests), 1.29 GB, 273 us.  Rows and keys the other way round (queries as
+// own 2048 tokens alone (fp8) 375 to 440 us, 4.9 to 5.7 TB/s of keys beside their weights; both kinds (512 requests), 1.29 GB, 273 us.  Rows and keys the other way round (queries as
 // columns, a shuffle a row for every sum) took 607 us there, tiles of 32 rows whose exponentials wait for their products 311.
 #include <climits>
 #include <type_traits>
