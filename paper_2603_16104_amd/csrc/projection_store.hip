@@ -22,6 +22,11 @@ namespace hkv {
 
 namespace {
 
+// Prefill plans of up to kFewUnits blocks x KV heads: queries by workgroups of their own, kHeadsApart heads each, since there is room beside the others and a
+// workgroup's chain gets shorter.  us with 1 / 2 / 4 heads / together (32 + 8 heads, bf16): 100 tokens 4.4 / 4.4 / 4.6 / 5.1, 700 6.2 / 6.2 / 6.4 / 6.9, 1500 10.2 / 9.1 / 9.3 / 9.9,
+// 3000 16 / 14.6 / 15.3 / 14.4, 16000 105 / 90 / 88 / 87.
+constexpr int kHeadsApart = 2, kFewUnits = 1024;
+
 struct Unit {
     int block, lo, hi;  // slots lo .. hi - 1 of this block of the pool ...
     int64_t row;        // ... are the rows from this one on (before row_map)
@@ -201,9 +206,9 @@ __device__ __forceinline__ void put_block(const ProjectionLaunch &a, const Unit 
     }
 }
 
-// One KV head of one block with up to 16 tokens: thread row = slot.  Q: with the query heads of its group.
-template <int DT, bool Q = true>
-__device__ __forceinline__ void store_tokens(const ProjectionLaunch &a, const Unit &u, int h) {
+// Keys and values (KV) of one KV head h of one block with up to 16 tokens, and n query heads from head q0 on (Q): thread row = slot.
+template <int DT, bool KV, bool Q>
+__device__ __forceinline__ void store_tokens(const ProjectionLaunch &a, const Unit &u, int h, int q0, int n) {
     __shared__ __align__(16) float sTurn[kPage][2 * 64 + 4];
     const int slot = threadIdx.x >> 4, c = threadIdx.x & 15;
     const bool valid = slot >= u.lo && slot < u.hi;
@@ -211,11 +216,14 @@ __device__ __forceinline__ void store_tokens(const ProjectionLaunch &a, const Un
     int64_t row = u.row + max(0, min(slot, u.hi - 1) - u.lo);
     if (a.row_map) row = a.row_map[row];
     // All loads at once, by all lanes and of what there is, if only a row again: a wait at the end of a branch would hold up those behind it.
-    const Row<DT> kr = load_row<DT>(a.k, a.k_stride, row, h, c), vr = load_row<DT>(a.v, a.v_stride, row, h, c);
-    Row<DT> q[kAhead];
+    Row<DT> kr{}, vr{}, q[kAhead];
+    if constexpr (KV) {
+        kr = load_row<DT>(a.k, a.k_stride, row, h, c);
+        vr = load_row<DT>(a.v, a.v_stride, row, h, c);
+    }
     if constexpr (Q)
 #pragma unroll
-        for (int j = 0; j < kAhead; ++j) q[j] = load_row<DT>(a.q, a.q_stride, row, h * a.group + min(j, a.group - 1), c);
+        for (int j = 0; j < kAhead; ++j) q[j] = load_row<DT>(a.q, a.q_stride, row, q0 + min(j, n - 1), c);
     const Row<DT> qn = load_row<DT>(a.q_norm ? a.q_norm : a.q, 0, 0, 0, c), kn = load_row<DT>(a.k_norm ? a.k_norm : a.q, 0, 0, 0, c);
     const bool turns = 8 * c < a.rotary_dim;
     const int p0 = turns ? 4 * c : 0;
@@ -239,22 +247,24 @@ __device__ __forceinline__ void store_tokens(const ProjectionLaunch &a, const Un
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
         Turn t;
         turn_of(a, sTurn[slot], c, t);
-        values<DT>(kr, k);
-        norm_and_turn(a, c, a.k_norm != nullptr, kw, t, k);
-        for (int j0 = 0; Q && j0 < a.group; j0 += kAhead) {
+        if constexpr (KV) {
+            values<DT>(kr, k);
+            norm_and_turn(a, c, a.k_norm != nullptr, kw, t, k);
+        }
+        for (int j0 = 0; Q && j0 < n; j0 += kAhead) {
 #pragma unroll
             for (int j = 0; j < kAhead; ++j) {
-                const int head = j0 + j;
-                if (head >= a.group) break;
+                const int i = j0 + j;
+                if (i >= n) break;
                 float x[8];
                 values<DT>(q[j], x);
-                if (head + kAhead < a.group) q[j] = load_row<DT>(a.q, a.q_stride, row, h * a.group + head + kAhead, c);
+                if (i + kAhead < n) q[j] = load_row<DT>(a.q, a.q_stride, row, q0 + i + kAhead, c);
                 norm_and_turn(a, c, a.q_norm != nullptr, qw, t, x);
-                put_query<DT>(a, row, h * a.group + head, c, x);
+                put_query<DT>(a, row, q0 + i, c, x);
             }
         }
     }
-    put_block<DT>(a, u, h, valid, k, v);
+    if constexpr (KV) put_block<DT>(a, u, h, valid, k, v);
 }
 
 // Codes of earlier tokens (slots below lo) of an fp8 block and head under scales that have grown, by a whole wavefront; `vc`: the lanes from lane
@@ -424,12 +434,12 @@ __global__ __launch_bounds__(256) void projection_decode_kernel(ProjectionLaunch
         const int first = newest(s), b = first / kPage + part, lo = max(first - b * kPage, 0);
         if (b * kPage >= first + a.tokens) return;
         const Unit u{a.blocks[s.page_off + (uint32_t)b], lo, min(first + a.tokens - b * kPage, kPage), (int64_t)r * a.tokens + (b * kPage + lo - first), s.pos0 + b * kPage + lo};
-        store_tokens<DT, BY != By::kBoth>(a, u, h);
+        store_tokens<DT, true, BY != By::kBoth>(a, u, h, h * a.group, a.group);
     }
 }
 
-// The new tokens of a prefill plan's requests.  grid: (blocks they go to, KV heads)
-template <int DT>
+// The new tokens of a prefill plan's requests.  grid: (blocks they go to, KV heads), or queries APART: (blocks, KV heads and then kHeadsApart query heads each)
+template <int DT, bool APART>
 __global__ __launch_bounds__(256) void projection_prefill_kernel(ProjectionPrefill p) {
     const int x = blockIdx.x, lane = threadIdx.x & 63;
     static_assert(kMaxInlineRequests == 128, "two entries a lane");
@@ -442,7 +452,13 @@ __global__ __launch_bounds__(256) void projection_prefill_kernel(ProjectionPrefi
     u.hi = min(end - b * kPage, kPage);
     u.pos = b * kPage + u.lo;
     u.row = (int64_t)p.row0[i] + u.pos - prefix;
-    store_tokens<DT>(p.base, u, blockIdx.y);
+    const int h = blockIdx.y, Hkv = p.base.pool.num_kv_heads, q0 = (h - Hkv) * kHeadsApart;
+    if constexpr (!APART)
+        store_tokens<DT, true, true>(p.base, u, h, h * p.base.group, p.base.group);
+    else if (h < Hkv)
+        store_tokens<DT, true, false>(p.base, u, h, 0, 0);
+    else
+        store_tokens<DT, false, true>(p.base, u, 0, q0, min(kHeadsApart, Hkv * p.base.group - q0));
 }
 
 // A growing plan's step: a request's new token, and the items of its leaf get longer.  (The leaf's length comes by value: other workgroups may have
@@ -482,13 +498,16 @@ hipError_t launch_projection_store(const ProjectionLaunch &a, hipStream_t s) {
 
 hipError_t launch_projection_store(const ProjectionPrefill &a, hipStream_t s) {
     if (a.n_units <= 0) return hipSuccess;
-    const dim3 grid(a.n_units, a.base.pool.num_kv_heads), block(256);
+    const int Hkv = a.base.pool.num_kv_heads;
+    const bool apart = (int64_t)a.n_units * Hkv <= kFewUnits;
+    const dim3 grid(a.n_units, apart ? Hkv + (Hkv * a.base.group + kHeadsApart - 1) / kHeadsApart : Hkv), block(256);
+    auto go = [&](auto together, auto apart_) { hipLaunchKernelGGL(apart ? apart_ : together, grid, block, 0, s, a); };
     if (a.base.pool.dtype == 0)
-        hipLaunchKernelGGL(projection_prefill_kernel<0>, grid, block, 0, s, a);
+        go(projection_prefill_kernel<0, false>, projection_prefill_kernel<0, true>);
     else if (a.base.pool.dtype == 1)
-        hipLaunchKernelGGL(projection_prefill_kernel<1>, grid, block, 0, s, a);
+        go(projection_prefill_kernel<1, false>, projection_prefill_kernel<1, true>);
     else
-        hipLaunchKernelGGL(projection_prefill_kernel<2>, grid, block, 0, s, a);
+        go(projection_prefill_kernel<2, false>, projection_prefill_kernel<2, true>);
     return hipGetLastError();
 }
 

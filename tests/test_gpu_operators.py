@@ -91,6 +91,10 @@ STORE = [  # dtype, (q heads, kv heads), page size, (prefix, new) of the request
     (hkv.FP8_E4M3, (3, 3), 64, [(21, 60)], dict(rotary=112, big=30.0)),
     (hkv.FP32, (8, 2), 16, [(0, 1), (32, 33), (16, 0), (48, 16)], dict(fused=False, in_place=True)),
     (hkv.FP32, (5, 1), 32, [(5, 40)], dict(norm=False, interleaved=True, rotary=32, axes=2)),
+    # more blocks x heads than go with queries apart
+    (hkv.BF16, (15, 5), 16, [(20, 2000), (0, 1700), (3, 1)], dict(fused=False, in_place=True)),
+    (hkv.FP8_E4M3, (14, 7), 32, [(20, 2000), (0, 700), (3, 1)], dict(rotary=64)),
+    (hkv.FP32, (6, 6), 16, [(20, 2000), (0, 1700), (3, 1)], dict(interleaved=True)),
 ]
 
 
