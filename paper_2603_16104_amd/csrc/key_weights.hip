@@ -41,13 +41,13 @@ struct QueryRow {
     int limit;                // of the node's tokens: it sees those before `limit` and, of the 64 from there on, those whose bit of `mask` is set
     unsigned long long mask;
 };
-// The row's place alone, and its row of the plan (-1: there is none) ...
+// The row's place alone, and its row of the plan (-1: there is none; the place is then the first row's) ...
 __device__ __forceinline__ int64_t row_place(const KeyWeightsLaunch &a, const KeyWeightItem &it, int r, int G, int *row) {
-    *row = -1;
-    if (r >= it.n_req * G) return 0;
-    const int j = (int)((uint32_t)r / (uint32_t)G);
-    *row = a.node_req_idx[it.req_off + j];
-    return ((int64_t)(a.q_rows ? a.q_rows[*row] : *row) * a.num_q_heads + it.kv_head * G + (r - j * G)) * kHeadDim;
+    const bool there = r < it.n_req * G;
+    r = there ? r : 0;
+    const int j = (int)((uint32_t)r / (uint32_t)G), own = a.node_req_idx[it.req_off + j];
+    *row = there ? own : -1;
+    return ((int64_t)(a.q_rows ? a.q_rows[own] : own) * a.num_q_heads + it.kv_head * G + (r - j * G)) * kHeadDim;
 }
 // ... and what else there is to know.
 __device__ __forceinline__ QueryRow row_at(const KeyWeightsLaunch &a, const KeyWeightItem &it, int64_t q, int row) {

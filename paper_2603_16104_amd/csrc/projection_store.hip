@@ -224,10 +224,11 @@ __device__ __forceinline__ void store_tokens(const ProjectionLaunch &a, const Un
     if constexpr (Q)
 #pragma unroll
         for (int j = 0; j < kAhead; ++j) q[j] = load_row<DT>(a.q, a.q_stride, row, q0 + min(j, n - 1), c);
-    const Row<DT> qn = load_row<DT>(a.q_norm ? a.q_norm : a.q, 0, 0, 0, c), kn = load_row<DT>(a.k_norm ? a.k_norm : a.q, 0, 0, 0, c);
+    const char *const mine = static_cast<const char *>(a.q) + row * a.q_stride * (DT == 2 ? 4 : 2);  // (for what there is none of)
+    const Row<DT> qn = load_row<DT>(a.q_norm ? static_cast<const char *>(a.q_norm) + 0 : mine, 0, 0, 0, c), kn = load_row<DT>(a.k_norm ? static_cast<const char *>(a.k_norm) + 0 : mine, 0, 0, 0, c);
     const bool turns = 8 * c < a.rotary_dim;
     const int p0 = turns ? 4 * c : 0;
-    const Angles<4> angle = load_angles<4>(a, a.rotary_dim > 0 ? a.inv_freq : static_cast<const double *>(a.q), p0, row);
+    const Angles<4> angle = load_angles<4>(a, a.rotary_dim > 0 ? a.inv_freq + 0 : reinterpret_cast<const double *>(mine), p0, row);
     float k[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
     Row<DT> v{};
     if (valid) {
