@@ -192,7 +192,6 @@ extern "C" int hkv_decode_plan_append_qkv(hkv_decode_plan *plan, const int32_t *
     // the places of the new tokens: blocks of their own, in pages of one owner (what plan_append refuses is refused there, before anything changes)
     const hkv_pool *pool = plan->pool;
     const int P = pool->d.page_size, S = pool->blocks_per_page;
-    bool opens = plan->store_blocks == 0;
     std::vector<int32_t> blocks(plan->n_req);
     for (int r = 0; r < plan->n_req; ++r) {
         const hkv_node &leaf = plan->nodes[plan->req_leaf[r]];
@@ -200,7 +199,6 @@ extern "C" int hkv_decode_plan_append_qkv(hkv_decode_plan *plan, const int32_t *
         if (leaf.n_tokens % P == 0) {
             if (!new_page_ids || new_page_ids[r] < 0 || new_page_ids[r] >= pool->d.num_pages) return plan_append(plan, new_page_ids, nullptr, nullptr, nullptr, stream);
             page = new_page_ids[r];
-            opens = true;
         } else {
             page = plan->node_pages[leaf.page_begin + leaf.n_pages - 1] / S;
         }
@@ -208,11 +206,11 @@ extern "C" int hkv_decode_plan_append_qkv(hkv_decode_plan *plan, const int32_t *
         if (r < kMaxInlineAppend) p.length[r] = leaf.n_tokens;
         blocks[r] = page * S + leaf.n_tokens % P / HKV_PAGE_SIZE;
     }
-    if (opens && all_different(blocks) < 0) return fail(HKV_EINVAL, "%s: new tokens of two requests go to the same 16-token block", who);
+    // (looked at in every call: what an earlier one found says nothing of leaves that other calls have lengthened, or that have reached the next block of their page)
+    if (all_different(blocks) < 0) return fail(HKV_EINVAL, "%s: new tokens of two requests go to the same 16-token block", who);
     decode_places(plan, a);
     AppendHook hook{[](void *ctx, const PlanGrowInline &g, hipStream_t s) { return launch_projection_append(*static_cast<ProjectionAppend *>(ctx), g, s); }, &p, false};
     if (int rc = plan_append(plan, new_page_ids, nullptr, nullptr, &hook, stream)) return rc;
-    plan->store_blocks = 1;
     if (!hook.launched) HKV_HIP(launch_projection_store(a, static_cast<hipStream_t>(stream)));  // behind the update of the plan's lists
     return HKV_OK;
 } catch (const std::exception &) {  // (no memory for a list)

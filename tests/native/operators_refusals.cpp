@@ -1,0 +1,69 @@
+// What the calls around a step's attention refuse in the middle of a plan's life, after other calls on it: the stubs of
+// operators_check.cpp (no GPU, no HIP library), programs of its own.  Exit status 0 = clean.
+#define main operators_check_main
+#include "operators_check.cpp"
+#undef main
+
+static hkv_decode_plan *growing_plan(hkv_pool *pool, const std::vector<hkv_node> &nodes, const std::vector<int32_t> &pages, int reserve) {
+    std::vector<int32_t> leaf(nodes.size());
+    for (size_t i = 0; i < leaf.size(); ++i) leaf[i] = (int32_t)i;
+    hkv_decode_plan *plan = nullptr;
+    CHECK(hkv_decode_plan_create_growing(pool, nodes.data(), (int32_t)nodes.size(), pages.data(), (int32_t)pages.size(), leaf.data(), (int32_t)leaf.size(), 4, reserve,
+                                         0, &plan) == HKV_OK);
+    return plan;
+}
+
+// Two requests' new tokens in one block, by ways on which an earlier call has looked at the blocks already.
+static void appends_to_one_block() {
+    const hkv_qkv x = make_rows();
+    for (int dtype : {HKV_BF16, HKV_FP8_E4M3}) {
+        hkv_pool *pool = make_pool(16, 16, 2, dtype);
+        // a store that is refused, then the append
+        hkv_decode_plan *plan = growing_plan(pool, {{-1, 0, 1, 5}, {-1, 0, 1, 5}}, {1}, 40);
+        for (int i = 0; i < 2; ++i) {
+            CHECK(hkv_decode_plan_store(plan, &x, nullptr) == HKV_EINVAL && stored.empty());
+            CHECK(hkv_decode_plan_append_qkv(plan, nullptr, &x, nullptr) == HKV_EINVAL && stored.empty());
+        }
+        CHECK(hkv_decode_plan_destroy(plan) == HKV_OK);
+        // appends that store, then one that only lengthens and opens one page for both, then another that stores
+        plan = growing_plan(pool, {{-1, 0, 1, 15}, {-1, 1, 1, 15}}, {0, 5}, 40);
+        const int32_t twice[2] = {7, 7};
+        CHECK(hkv_decode_plan_append_qkv(plan, nullptr, &x, nullptr) == HKV_OK);
+        CHECK(same(taken(), {Put{0, 15, 0, 15}, Put{5, 15, 1, 15}}));
+        CHECK(hkv_decode_plan_append(plan, twice, nullptr) == HKV_OK);
+        CHECK(hkv_decode_plan_append_qkv(plan, nullptr, &x, nullptr) == HKV_EINVAL && stored.empty());
+        CHECK(hkv_decode_plan_store(plan, &x, nullptr) == HKV_EINVAL && stored.empty());
+        CHECK(hkv_decode_plan_destroy(plan) == HKV_OK);
+        CHECK(kv_pool_destroy(pool) == HKV_OK);
+        // leaves in one page of several blocks: a leaf reaches the block of the other
+        pool = make_pool(16, 64, 2, dtype);
+        plan = growing_plan(pool, {{-1, 0, 1, 15}, {-1, 0, 1, 20}}, {2}, 40);
+        CHECK(hkv_decode_plan_append_qkv(plan, nullptr, &x, nullptr) == HKV_OK);
+        CHECK(same(taken(), {Put{8, 15, 0, 15}, Put{9, 4, 1, 20}}));
+        CHECK(hkv_decode_plan_append_qkv(plan, nullptr, &x, nullptr) == HKV_EINVAL && stored.empty());
+        CHECK(hkv_decode_plan_destroy(plan) == HKV_OK);
+        // what is refused changes nothing: with pages of their own it goes on where it was
+        plan = growing_plan(pool, {{-1, 0, 1, 64}, {-1, 1, 1, 64}}, {2, 3}, 40);
+        const int32_t own[2] = {4, 5};
+        for (int i = 0; i < 3; ++i) CHECK(hkv_decode_plan_append_qkv(plan, twice, &x, nullptr) == HKV_EINVAL && stored.empty());
+        CHECK(hkv_decode_plan_append_qkv(plan, own, &x, nullptr) == HKV_OK);
+        CHECK(same(taken(), {Put{16, 0, 0, 64}, Put{20, 0, 1, 64}}));
+        CHECK(hkv_decode_plan_destroy(plan) == HKV_OK);
+        CHECK(kv_pool_destroy(pool) == HKV_OK);
+    }
+}
+
+int main(int argc, char **argv) {
+    const struct {
+        const char *name;
+        void (*run)();
+    } programs[] = {{"appends_to_one_block", appends_to_one_block}};
+    int ran = 0;
+    for (const auto &p : programs)
+        if (argc < 2 || !std::strcmp(argv[1], p.name)) {
+            p.run();
+            ++ran;
+        }
+    std::printf("operators_refusals: %d programs, %d failed checks\n", ran, failures);
+    return failures || !ran ? 1 : 0;
+}
