@@ -586,7 +586,9 @@ typedef struct {
 } hkv_qkv;
 
 /* The new tokens of a prefill plan, all requests in one launch (per 128 of them): replaces kv_pool_write and what comes in front of it.
- * EINVAL: null / unaligned pointers, bad strides, eps, axes; a host-only plan; new tokens of two requests in the same 16-token block.
+ * EINVAL: null / unaligned pointers, bad strides, eps, axes; a host-only plan; new tokens of two requests in the same 16-token block; new
+ * tokens behind earlier ones in a page of more than one owner (as it is at the call; kv_pool_copy_on_write first, and a plan over the page it gives).  Pages that
+ * the call begins may have several: a prompt is stored once for all who hold it.
  * ENOMEM: no host memory.  Nothing is queued on error. */
 int hkv_prefill_plan_store(hkv_prefill_plan *plan, const hkv_qkv *rows, void *stream);
 /* The newest tokens_per_req tokens of every request of a decode plan (they end its last node; a growing plan: as appended so far):

@@ -103,6 +103,13 @@ extern "C" int hkv_prefill_plan_store(hkv_prefill_plan *plan, const hkv_qkv *row
         plan->store_blocks = all_different(blocks);
     }
     if (plan->store_blocks < 0) return fail(HKV_EINVAL, "%s: new tokens of two requests go to the same 16-token block", who);
+    for (int r = 0; r < plan->n_req; ++r) {  // (in every call: owners come and go)
+        const int prefix = plan->kv_len[r] - tokens_of(r);
+        if (tokens_of(r) == 0 || prefix % P == 0) continue;
+        const int32_t page = plan->block_table[(size_t)r * plan->key_max_pages + prefix / P];
+        if (pool->refcnt[page] > 1)
+            return fail(HKV_EINVAL, "%s: page %d, which request %d continues, has %d owners: kv_pool_copy_on_write first", who, page, r, pool->refcnt[page]);
+    }
     p.base.blocks = plan->d_block_table;
     p.base.src_pages = pool->d.dtype == HKV_FP8_E4M3 ? plan->d_src_pages : nullptr;
     p.table_stride = plan->max_pages;

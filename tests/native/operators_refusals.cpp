@@ -53,11 +53,40 @@ static void appends_to_one_block() {
     }
 }
 
+// A prompt's new tokens behind earlier ones in a page that somebody else holds, too; pages that the call begins may have any number of holders.
+static void prompts_into_shared_pages() {
+    const hkv_qkv x = make_rows();
+    for (int page : {16, 64})
+        for (int dtype : {HKV_BF16, HKV_FP8_E4M3, HKV_FP32}) {
+            hkv_pool *pool = make_pool(8, page, 2, dtype);
+            int32_t ids[4];
+            CHECK(kv_pool_alloc(pool, 4, ids) == HKV_OK);
+            // request 0 goes on inside page ids[1], request 1 begins with it whole pages of its own
+            const int inside = page == 16 ? page + 7 : page + 32;  // (of larger pages: where a block of it begins)
+            const int32_t cu[3] = {0, 5, 5 + page + 3}, table[4] = {ids[0], ids[1], ids[2], ids[3]}, kv[2] = {inside + 5, page + 3};
+            hkv_prefill_plan *plan = nullptr;
+            CHECK(hkv_prefill_plan_create(pool, cu, table, 2, kv, 2, 4, 0, &plan) == HKV_OK);
+            CHECK(hkv_prefill_plan_store(plan, &x, nullptr) == HKV_OK);
+            const std::vector<Put> all = taken();
+            CHECK(all.size() == (size_t)cu[2]);
+            CHECK(kv_pool_retain(pool, 1, ids + 1) == HKV_OK);
+            for (int again = 0; again < 2; ++again) CHECK(hkv_prefill_plan_store(plan, &x, nullptr) == HKV_EINVAL && stored.empty());
+            CHECK(kv_pool_release(pool, 1, ids + 1) == HKV_OK);
+            CHECK(hkv_prefill_plan_store(plan, &x, nullptr) == HKV_OK);
+            CHECK(same(taken(), all));
+            for (int i : {0, 2, 3}) CHECK(kv_pool_retain(pool, 1, ids + i) == HKV_OK);  // a prefix that is only read, a prompt stored once for two
+            CHECK(hkv_prefill_plan_store(plan, &x, nullptr) == HKV_OK);
+            CHECK(same(taken(), all));
+            CHECK(hkv_prefill_plan_destroy(plan) == HKV_OK);
+            CHECK(kv_pool_destroy(pool) == HKV_OK);
+        }
+}
+
 int main(int argc, char **argv) {
     const struct {
         const char *name;
         void (*run)();
-    } programs[] = {{"appends_to_one_block", appends_to_one_block}};
+    } programs[] = {{"appends_to_one_block", appends_to_one_block}, {"prompts_into_shared_pages", prompts_into_shared_pages}};
     int ran = 0;
     for (const auto &p : programs)
         if (argc < 2 || !std::strcmp(argv[1], p.name)) {
