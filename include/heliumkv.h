@@ -597,7 +597,8 @@ int hkv_prefill_plan_store(hkv_prefill_plan *plan, const hkv_qkv *rows, void *st
  * last node without a token. */
 int hkv_decode_plan_store(hkv_decode_plan *plan, const hkv_qkv *rows, void *stream);
 /* Growing plans: hkv_decode_plan_append and the store of the tokens it adds, row r for request r (q_rows: row q_rows[r]); for up to 256
- * requests one launch.  Errors of both; nothing changes on error. */
+ * requests one launch.  Errors of both; nothing changes on error.  Not for capture into a graph (EINVAL): the plan's lengths change with
+ * every append, and a replay would not change them.  hkv_decode_plan_store may be captured, and follows the lengths. */
 int hkv_decode_plan_append_qkv(hkv_decode_plan *plan, const int32_t *new_page_ids, const hkv_qkv *rows, void *stream);
 
 /* ------------------------------------------------------------------------------------------

@@ -13,6 +13,11 @@ namespace {
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
+bool is_capturing(hipStream_t s) {
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    return hipStreamIsCapturing(s, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone;
+}
+
 // The call's rows, checked, as the kernels take them.
 int projection_of(const hkv_pool *pool, int num_q_heads, const hkv_qkv *x, ProjectionLaunch &a, const char *who) {
     if (!x) return fail(HKV_EINVAL, "%s: null rows", who);
@@ -195,6 +200,8 @@ extern "C" int hkv_decode_plan_append_qkv(hkv_decode_plan *plan, const int32_t *
     if (plan->n_req > 0) {
         if (int rc = projection_of(plan->pool, plan->num_q_heads, rows, a, who)) return rc;
         if (!plan->dev) return fail(HKV_EINVAL, "%s: plan was built host-only", who);
+        // a replay would store to the same slots and lengthen the items again, of which the host's lengths know nothing
+        if (is_capturing(static_cast<hipStream_t>(stream))) return fail(HKV_EINVAL, "%s: not for capture into a graph", who);
     }
     // the places of the new tokens: blocks of their own, in pages of one owner (what plan_append refuses is refused there, before anything changes)
     const hkv_pool *pool = plan->pool;
@@ -438,8 +445,7 @@ extern "C" int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_p
         if (pool->mark[src_pages[i]] == pool->mark_now) return fail(HKV_EINVAL, "%s: page %d is read and written", who, src_pages[i]);
 
     hipStream_t s = static_cast<hipStream_t>(stream);
-    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;  // (a replay would need slots of the ring as they are now)
-    if (hipStreamIsCapturing(s, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone) return fail(HKV_EINVAL, "%s: not for capture into a graph", who);
+    if (is_capturing(s)) return fail(HKV_EINVAL, "%s: not for capture into a graph", who);  // (a replay would need slots of the ring as they are now)
     EvictInline a{};
     a.pool = PoolWriteLaunch{pool->d.k_pages, pool->d.v_pages, pool->d.k_scale, pool->d.v_scale, pool->d.num_kv_heads, pool->d.dtype, nullptr, 0, 0, 0, nullptr, nullptr, nullptr, nullptr};
     a.weights = key_weights;

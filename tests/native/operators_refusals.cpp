@@ -82,11 +82,41 @@ static void prompts_into_shared_pages() {
         }
 }
 
+// An append cannot be captured (its places travel by value, the lengths that a replay would change again are the host's): nothing changes.
+static void appends_under_capture() {
+    const hkv_qkv x = make_rows();
+    for (int requests : {2, 300}) {  // (the update in arguments, and through the plan's buffers)
+        hkv_pool *pool = make_pool(2 * requests, 16, 2, HKV_BF16);
+        std::vector<hkv_node> nodes;
+        std::vector<int32_t> pages, fresh;
+        for (int r = 0; r < requests; ++r) {
+            nodes.push_back(hkv_node{-1, r, 1, 16 - r % 2});
+            pages.push_back(r);
+            fresh.push_back(requests + r);
+        }
+        hkv_decode_plan *plan = growing_plan(pool, nodes, pages, 3);
+        for (auto status : {hipStreamCaptureStatusActive, hipStreamCaptureStatusInvalidated}) {
+            capturing = status;
+            CHECK(hkv_decode_plan_append_qkv(plan, fresh.data(), &x, nullptr) == HKV_EINVAL && stored.empty());
+            CHECK(hkv_decode_plan_append_qkv(plan, nullptr, &x, nullptr) == HKV_EINVAL && stored.empty());
+        }
+        CHECK(hkv_decode_plan_store(plan, &x, nullptr) == HKV_OK);  // (which may be captured)
+        for (const Put &p : taken()) CHECK(p.block < requests && p.slot == 15 - p.row % 2);
+        capturing = hipStreamCaptureStatusNone;
+        for (int i = 0; i < 3; ++i) CHECK(hkv_decode_plan_append_qkv(plan, fresh.data(), &x, nullptr) == HKV_OK);
+        stored.clear();
+        CHECK(hkv_decode_plan_append_qkv(plan, fresh.data(), &x, nullptr) == HKV_ENOMEM);
+        CHECK(hkv_decode_plan_destroy(plan) == HKV_OK);
+        CHECK(kv_pool_destroy(pool) == HKV_OK);
+    }
+}
+
 int main(int argc, char **argv) {
     const struct {
         const char *name;
         void (*run)();
-    } programs[] = {{"appends_to_one_block", appends_to_one_block}, {"prompts_into_shared_pages", prompts_into_shared_pages}};
+    } programs[] = {{"appends_to_one_block", appends_to_one_block}, {"prompts_into_shared_pages", prompts_into_shared_pages},
+                    {"appends_under_capture", appends_under_capture}};
     int ran = 0;
     for (const auto &p : programs)
         if (argc < 2 || !std::strcmp(argv[1], p.name)) {

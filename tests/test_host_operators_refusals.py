@@ -19,7 +19,7 @@ def program(tmp_path_factory):
     return exe
 
 
-@pytest.mark.parametrize("name", ["appends_to_one_block", "prompts_into_shared_pages"])
+@pytest.mark.parametrize("name", ["appends_to_one_block", "prompts_into_shared_pages", "appends_under_capture"])
 def test_refusals_after_other_calls(program, name):
     r = subprocess.run([program, name], capture_output=True, text=True, timeout=300, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=0"))
     out = r.stdout + r.stderr
