@@ -580,7 +580,7 @@ typedef struct {
     int32_t interleaved;
     const double *inv_freq;       /* device, [rotary_dim / 2]: radians per position */
     const int32_t *positions;     /* device, [n_axes][rows], may be negative; NULL: a token's place on its request's path, 0 for the first (one axis) */
-    int64_t position_stride;      /* elements from axis to axis */
+    int64_t position_stride;      /* elements from axis to axis; more than 0 where there are several */
     int32_t n_axes;               /* 1 to 4; 0 = 1.  Images and video have a place in time, height and width */
     const int32_t *axis;          /* host, [rotary_dim / 2]: the axis each pair turns by; NULL: axis 0 */
 } hkv_qkv;

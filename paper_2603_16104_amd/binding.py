@@ -599,13 +599,16 @@ def qkv_rows(q, k, v, q_out, q_norm=None, k_norm=None, eps: float = 1e-6, rotary
             raise ValueError("positions: int32, the rows of an axis one after the other")
         if positions.dim() > 1:
             axes, stride = positions.shape[0], positions.stride(0)
+    if axis is not None:
+        axis = _host_i32(axis)
+        if len(axis) * 2 < rotary_dim:
+            raise ValueError("axis: one for every pair of the rotated dimensions")
+        if axes > 1 and stride == 0 and n_axes in (None, axes) and (axis >= 0).all() and (axis < axes).all():
+            axes, n_axes, axis = 1, None, None  # (one row of places, expanded: every axis is the same)
     x = Qkv(_addr(q), _addr(k), _addr(v), _row_stride(q), _row_stride(k), _row_stride(v), _addr(q_out), _addr(q_norm), _addr(k_norm), eps, rotary_dim,
             int(interleaved), _addr(inv_freq), _addr(positions), stride, axes if n_axes is None else n_axes, None)
     if axis is not None:
-        x._axis = _host_i32(axis)
-        if len(x._axis) * 2 < rotary_dim:
-            raise ValueError("axis: one for every pair of the rotated dimensions")
-        x.axis = x._axis.ctypes.data
+        x._axis, x.axis = axis, axis.ctypes.data
     return x
 
 

@@ -42,7 +42,7 @@ int projection_of(const hkv_pool *pool, int num_q_heads, const hkv_qkv *x, Proje
         return fail(HKV_EINVAL, "%s: inv_freq must be non-null and 8-byte aligned", who);
     if (x->positions && (reinterpret_cast<uintptr_t>(x->positions) & 3)) return fail(HKV_EINVAL, "%s: positions must be 4-byte aligned", who);
     if (n_axes > 1 && (!x->positions || !x->axis)) return fail(HKV_EINVAL, "%s: several axes need positions and the axis of every pair", who);
-    if (x->position_stride < 0) return fail(HKV_EINVAL, "%s: position_stride %lld", who, (long long)x->position_stride);
+    if (x->position_stride < (n_axes > 1)) return fail(HKV_EINVAL, "%s: position_stride %lld of %d axes", who, (long long)x->position_stride, n_axes);
     if (x->axis)
         for (int p = 0; p < x->rotary_dim / 2; ++p) {
             if (x->axis[p] < 0 || x->axis[p] >= n_axes) return fail(HKV_EINVAL, "%s: pair %d has axis %d of %d", who, p, x->axis[p], n_axes);

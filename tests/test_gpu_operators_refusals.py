@@ -41,3 +41,17 @@ def test_an_append_is_refused_while_a_graph_is_captured(n_req):
         hkv.hkv_decode_plan_destroy(p)
     for p in twins:
         p.close()
+
+
+def test_places_expanded_over_the_axes_turn_as_when_written_out():
+    pool = Pool(2, 2, hkv.BF16)
+    plan = hkv.hkv_prefill_plan_create(pool.handle, [0, 20], [[1, 0]], [20], 4)
+    line, axis = torch.arange(100, 120, dtype=torch.int32, device="cuda"), np.arange(64) % 3
+    x, results = Rows(20, 4, 2, hkv.BF16, 3, norm=False), []
+    for places in (line.expand(3, 20), line.repeat(3, 1)):
+        hkv.hkv_prefill_plan_store(plan, hkv.qkv_rows(x.q, x.k, x.v, x.q_out, rotary_dim=128, inv_freq=x.inv_freq, positions=places, axis=axis))
+        torch.cuda.synchronize()
+        results.append((x.q_out.clone(), pool.k.clone()))
+    assert all(torch.equal(a, b) for a, b in zip(*results)) and not torch.isnan(results[0][0]).any()
+    hkv.hkv_prefill_plan_destroy(plan)
+    pool.close()

@@ -1,11 +1,17 @@
 """What the calls around a step's attention refuse in the middle of a plan's life, in a native program built with AddressSanitizer +
-UndefinedBehaviorSanitizer over the host code (no GPU, no HIP library: tests/native/operators_refusals.cpp)."""
+UndefinedBehaviorSanitizer over the host code (no GPU, no HIP library: tests/native/operators_refusals.cpp); and of rows that do not belong together."""
 import os
 import shutil
 import subprocess
 
+import numpy as np
 import pytest
 
+from paper_2603_16104_amd import binding as hkv
+
+from test_host_library import fake_pool
+
+A = 0x100000
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
@@ -25,3 +31,40 @@ def test_refusals_after_other_calls(program, name):
     out = r.stdout + r.stderr
     assert r.returncode == 0 and "1 programs, 0 failed checks" in out, out[-4000:]
     assert "AddressSanitizer" not in out and "runtime error" not in out and "LeakSanitizer" not in out, out[-4000:]
+
+
+# ---- rows of the stores (addresses are never dereferenced here)
+def store_code(x):
+    pool = fake_pool()
+    plan = hkv.hkv_prefill_plan_create(pool, [0, 5, 9], [[0, 1], [2, 3]], [20, 9], 8, hkv.PLAN_HOST_ONLY)
+    try:
+        with pytest.raises(hkv.HkvError) as e:
+            hkv.hkv_prefill_plan_store(plan, x, 0)
+        return e.value.code, hkv.last_error()
+    finally:
+        hkv.hkv_prefill_plan_destroy(plan)
+        hkv.kv_pool_destroy(pool)
+
+
+def test_several_axes_need_a_stride():
+    x = hkv.qkv_rows(A, A, A, 2 * A, rotary_dim=128, inv_freq=A, positions=A, n_axes=3, axis=[0, 1, 2, 1] * 16)
+    for stride, text in ((0, "position_stride"), (-9, "position_stride"), (9, "host-only")):
+        x.position_stride = stride
+        code, error = store_code(x)
+        assert code == hkv.EINVAL and text in error
+    x.n_axes, x.axis, x.position_stride = 1, None, 0     # (one axis: there is nothing to step over)
+    assert "host-only" in store_code(x)[1]
+
+
+def test_places_expanded_over_the_axes_are_one_axis():
+    import torch
+    q = torch.zeros(4, 8, 128, dtype=torch.bfloat16)
+    how = dict(q=q, k=q[:, :2].contiguous(), v=q[:, :2].contiguous(), q_out=q, rotary_dim=128, inv_freq=torch.zeros(64, dtype=torch.float64), axis=np.arange(64) % 3)
+    line = torch.arange(4, dtype=torch.int32)
+    x = hkv.qkv_rows(positions=line.expand(3, 4), **how)
+    assert x.n_axes == 1 and x.axis is None and x.positions == line.data_ptr()
+    assert "host-only" in store_code(x)[1]
+    x = hkv.qkv_rows(positions=line.repeat(3, 1), **how)
+    assert x.n_axes == 3 and x.axis is not None and x.position_stride == 4
+    for bad in (dict(axis=np.arange(64) % 4), dict(axis=None)):   # what is wrong without them stays wrong
+        assert store_code(hkv.qkv_rows(positions=line.expand(3, 4), **{**how, **bad}))[0] == hkv.EINVAL
