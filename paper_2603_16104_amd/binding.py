@@ -580,7 +580,7 @@ def _row_stride(t) -> int:
 def qkv_rows(q, k, v, q_out, q_norm=None, k_norm=None, eps: float = 1e-6, rotary_dim: int = 0, inv_freq=None, interleaved: bool = False,
              positions=None, axis=None, n_axes: Optional[int] = None) -> Qkv:
     """The argument of the store calls.  q, k, v: [rows][heads][128] tensors, which may be parts of one tensor's rows; q_out: [rows][heads][128]
-    without gaps; inv_freq: float64 [rotary_dim / 2]; positions: int32 [rows], or [axes][rows] with `axis`, the axis of every pair.  May be kept
+    without gaps; k, v and positions for all rows of q; inv_freq: float64 [rotary_dim / 2]; positions: int32 [rows], or [axes][rows] with `axis`, the axis of every pair.  May be kept
     for as many calls as the buffers are used for; it holds no reference to them, but to `axis`."""
     if q_out is not None and not isinstance(q_out, int) and not q_out.is_contiguous():
         raise ValueError("q_out must be contiguous")
@@ -593,12 +593,17 @@ def qkv_rows(q, k, v, q_out, q_norm=None, k_norm=None, eps: float = 1e-6, rotary
         raise ValueError("q_norm, k_norm: [128]")
     if inv_freq is not None and not isinstance(inv_freq, int) and (inv_freq.element_size() != 8 or inv_freq.numel() * 2 < rotary_dim or not inv_freq.is_contiguous()):
         raise ValueError("inv_freq: float64 [rotary_dim / 2]")
-    stride, axes = 0, 1
+    rows, stride, axes = 0 if q is None or isinstance(q, int) else q.shape[0], 0, 1
+    if any(t is not None and not isinstance(t, int) and t.shape[0] < rows for t in (k, v)):
+        raise ValueError("k and v: [rows][heads][128] for all rows of q")
     if positions is not None and not isinstance(positions, int):
-        if positions.element_size() != 4 or positions.is_floating_point() or positions.stride(-1) != 1:
+        places = positions[:1] if positions.dim() > 1 else positions
+        if positions.element_size() != 4 or positions.is_floating_point() or positions.dim() == 0 or not places.is_contiguous():
             raise ValueError("positions: int32, the rows of an axis one after the other")
         if positions.dim() > 1:
             axes, stride = positions.shape[0], positions.stride(0)
+        if positions.numel() < axes * rows or (n_axes or 1) > axes:
+            raise ValueError("positions: int32 [rows], or [axes][rows], for all rows of q and all axes")
     if axis is not None:
         axis = _host_i32(axis)
         if len(axis) * 2 < rotary_dim:

@@ -68,3 +68,19 @@ def test_places_expanded_over_the_axes_are_one_axis():
     assert x.n_axes == 3 and x.axis is not None and x.position_stride == 4
     for bad in (dict(axis=np.arange(64) % 4), dict(axis=None)):   # what is wrong without them stays wrong
         assert store_code(hkv.qkv_rows(positions=line.expand(3, 4), **{**how, **bad}))[0] == hkv.EINVAL
+
+
+def test_rows_that_are_fewer_than_the_queries_are_refused():
+    import torch
+    q, k = torch.zeros(6, 8, 128, dtype=torch.bfloat16), torch.zeros(9, 2, 128, dtype=torch.bfloat16)
+    how = dict(q=q, k=k, v=k, q_out=q, rotary_dim=128, inv_freq=torch.zeros(64, dtype=torch.float64))
+    grid = torch.zeros(3, 6, dtype=torch.int32)
+    three = dict(positions=grid, axis=np.arange(64) % 3)
+    for ok in (dict(), dict(k=k[:6]), dict(positions=grid[0]), three, dict(positions=torch.zeros(3, 7, dtype=torch.int32), axis=np.arange(64) % 2, n_axes=2),
+               dict(positions=torch.zeros(3, 2, 3, dtype=torch.int32), axis=np.arange(64) % 3), dict(k=A, v=A, positions=A)):
+        hkv.qkv_rows(**{**how, **ok})
+    for bad in (dict(k=k[:5]), dict(v=k[:5]), dict(k=k[:0]), dict(positions=grid[0, :5]), dict(positions=grid[:, :5], axis=np.arange(64) % 3),
+                {**three, "n_axes": 4}, dict(positions=grid[0], axis=np.arange(64) % 3, n_axes=3), dict(positions=grid[:, :5].expand(3, 5), n_axes=1),
+                dict(positions=grid[0, 0]), dict(positions=torch.zeros(12, dtype=torch.int32)[::2])):
+        with pytest.raises(ValueError):
+            hkv.qkv_rows(**{**how, **bad})
