@@ -591,7 +591,7 @@ def qkv_rows(q, k, v, q_out, q_norm=None, k_norm=None, eps: float = 1e-6, rotary
         raise ValueError("q_out: [rows][heads][128] for all rows of q")
     if any(t is not None and not isinstance(t, int) and (t.numel() != HEAD_DIM or not t.is_contiguous()) for t in (q_norm, k_norm)):
         raise ValueError("q_norm, k_norm: [128]")
-    if inv_freq is not None and not isinstance(inv_freq, int) and (inv_freq.element_size() != 8 or inv_freq.numel() * 2 < rotary_dim or not inv_freq.is_contiguous()):
+    if inv_freq is not None and not isinstance(inv_freq, int) and (inv_freq.element_size() != 8 or not inv_freq.is_floating_point() or inv_freq.numel() * 2 < rotary_dim or not inv_freq.is_contiguous()):
         raise ValueError("inv_freq: float64 [rotary_dim / 2]")
     rows, stride, axes = 0 if q is None or isinstance(q, int) else q.shape[0], 0, 1
     if any(t is not None and not isinstance(t, int) and t.shape[0] < rows for t in (k, v)):

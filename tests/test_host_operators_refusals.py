@@ -84,3 +84,13 @@ def test_rows_that_are_fewer_than_the_queries_are_refused():
                 dict(positions=grid[0, 0]), dict(positions=torch.zeros(12, dtype=torch.int32)[::2])):
         with pytest.raises(ValueError):
             hkv.qkv_rows(**{**how, **bad})
+
+
+def test_frequencies_are_float64():
+    import torch
+    q = torch.zeros(6, 8, 128, dtype=torch.bfloat16)
+    how = dict(q=q, k=q, v=q, q_out=q, rotary_dim=128)
+    hkv.qkv_rows(inv_freq=torch.zeros(64, dtype=torch.float64), **how)
+    for wide in (torch.int64, torch.complex64):
+        with pytest.raises(ValueError):
+            hkv.qkv_rows(inv_freq=torch.zeros(64, dtype=wide), **how)
