@@ -579,7 +579,8 @@ typedef struct {
     int32_t rotary_dim;           /* 0 (no rotation), 16, 32, ... 128 (else ESHAPE) */
     int32_t interleaved;
     const double *inv_freq;       /* device, [rotary_dim / 2]: radians per position */
-    const int32_t *positions;     /* device, [n_axes][rows], may be negative; NULL: a token's place on its request's path, 0 for the first (one axis) */
+    const int32_t *positions;     /* device, [n_axes][rows], may be negative; NULL: a token's place on its request's path, 0 for the first (one axis),
+                                     which is not its position where tokens before it are gone (kv_pool_evict) or hold several places: give them there */
     int64_t position_stride;      /* elements from axis to axis; more than 0 where there are several */
     int32_t n_axes;               /* 1 to 4; 0 = 1.  Images and video have a place in time, height and width */
     const int32_t *axis;          /* host, [rotary_dim / 2]: the axis each pair turns by; NULL: axis 0 */
@@ -606,8 +607,10 @@ int hkv_decode_plan_append_qkv(hkv_decode_plan *plan, const int32_t *new_page_id
  * slot of the pool (key_weights: device float [blocks][num_kv_heads][16], caller-owned, blocks = num_pages * page_size / 16):
  *   key_weights[t] = decay * key_weights[t] + sum over rows r that see t of exp(scale * q_r . k_t - lse_r).
  * Every tree node's keys are read once for all requests below it; the order of the sum is fixed (the same call gives the same
- * bits).  A row whose lse is not a finite number adds nothing.  Keys that no request of the plan sees, and slots behind a
- * node's last token, keep what they hold.
+ * bits).  A row whose lse is not a finite number adds nothing.  Keys on no request's path, and slots behind a
+ * node's last token, keep what they hold.  Nothing else writes key_weights but kv_pool_evict: a page that a sequence takes holds the sums of
+ * whoever had it before, so the caller clears a page's weights when it is taken (or passes decay 0 in the first step that sees it; the newest
+ * tokens' own slots are n_new's to clear), and a page that kv_pool_copy_on_write gives has none of the old page's: they are the caller's to copy.
  *
  * hkv_decode_plan_track_weights: to be called once on a plan before the first attn_decode_plan_weights (it uploads the work list, blocking;
  * a growing plan may have grown).  EINVAL if a 16-token block is in the forest twice. */
@@ -623,7 +626,8 @@ int attn_decode_plan_weights(hkv_decode_plan *plan, const void *q, float scale, 
  * pool, and attention does not ask for its keys' order): the first n_first, the newest n_recent, and of the others those
  * with the greatest key_weights (equal ones: the earlier; NaN counts less than every number).  They move in order to new pages, slot j of
  * the new sequence holding kept token j, with their key_weights; fp8 blocks get the scale of what they then hold and codes
- * rounded anew.  The old pages stay as they are (shared prefixes among them may go on being used by others); slots behind the last kept
+ * rounded anew.  Keys stay rotated as they are, by their old positions: tokens that follow go on counting from n_tokens[i], which
+ * the stores then have to be told (hkv_qkv.positions), since a plan over the new pages has only n_keep[i] places.  The old pages stay as they are (shared prefixes among them may go on being used by others); slots behind the last kept
  * token of a new block keep what they hold.
  *   src_pages: host, ceil(n_tokens[i] / page size) ids of each sequence, one sequence after the other; dst_pages: host, ceil(n_keep[i] / page size)
  *   ids each, all different, of one owner at most, and none of src_pages (EINVAL).  n_tokens, n_keep: host [n_seq].
