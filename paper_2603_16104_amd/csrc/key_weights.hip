@@ -13,8 +13,8 @@
 //   128 of them and several wavefronts share the rows of a pair of blocks.
 //
 // fp32 pools: the same with the matrix instruction of that type, 16 times slower, so that its time is what counts beyond some 16 rows
-// (64 requests over 2048 shared and 512 own tokens 44 us, their attention 92; 16 requests over 4096 own tokens 47 us, 5.8 TB/s.  A key a lane with a row's dimensions by
-// scalar loads, without matrix instructions: 109 and 45).
+// (64 requests over 2048 shared and 512 own tokens 44 us, their attention 92; 16 requests over 4096 own tokens 47 us; both the same inputs again and again.  A key a lane with a row's
+// dimensions by scalar loads, without matrix instructions: 109 and 45.  Over three sets of inputs in turn, which no cache holds, 16 x 4096 tokens take 62 us, 4.4 TB/s).
 //
 // MI355X, 8 KV heads: 16 prompts x 8192 tokens x 256 rows alone 107 us (0.64 PFLOP/s; 48 vector instructions a step of 16 x 32, 8 of them exponentials); 1024 requests'
 // own 2048 tokens alone (fp8) 375 to 440 us, 4.9 to 5.7 TB/s of keys beside their weights; both kinds (512 requests), 1.29 GB, 273 us.  Rows and keys the other way round (queries as

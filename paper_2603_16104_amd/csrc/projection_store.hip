@@ -10,12 +10,13 @@
 // the lane eight further (whole heads: one vector instruction, else through the LDS crossbar), interleaved pairs lie in one lane.
 // A workgroup takes one 16-token block of one KV head: a thread row per token, K, V and then the query heads of the group, so that the
 // angles are taken once for all of them, and the fp8 scale of the block is the workgroup's own.  Where a request brings one or two tokens, the 16 thread rows take 16
-// of a token's heads (512 requests x 72 rows, fp8: 9.7 us; a workgroup per KV head, most of whose thread rows had nothing to do, 12.6), and up to 24 tokens, its queries
+// of a token's heads (512 requests x 72 rows, fp8: 9.7 to 10.6 us; a workgroup per KV head, most of whose thread rows had nothing to do, 12.6), and up to 24 tokens, its queries
 // go that way and its keys and values by blocks.
 //
-// Many tokens are bound by memory: 29 000 tokens of 32 + 8 heads, 708 MB, 153 us, 4.6 TB/s.  Few tokens are bound by latency: a launch, the loads of the rows
+// Many tokens are bound by memory: 29 000 tokens of 32 + 8 heads, 708 MB, 154 us, 4.6 TB/s (fp8: 649 MB, 143; fp32, whose V leaves as single floats 64 bytes apart: 1417 MB,
+// 350 us, 4.0 TB/s).  Few tokens are bound by latency: a launch, the loads of the rows
 // beside those that find the block, angles, stores: 64 requests 3.9 us, four 2.6.  V's part of a block is 16 tokens wide, so that a single token
-// costs a write of 32 bytes (fp8: 16) for every dimension of its V: 17 MB for the 512 requests, whose keys and values are 1 MB.
+// costs a write of 32 bytes (fp8: 16) for every dimension of its V: 8 MB for the 512 requests, whose keys and values are 1 MB, beside 8 MB of queries.
 #include "pool_block.h"
 
 namespace hkv {
@@ -94,10 +95,10 @@ __device__ __forceinline__ void angles(const ProjectionLaunch &a, int p0, const 
     for (int e = 0; e < N; ++e) {
         const int place = a.n_axes == 1 ? on0 : choose(axes >> (2 * e) & 3u, on0, x.on1, x.on2, x.on3);
         const double turns = (double)place * (x.freq[e] * 0.15915494309189533577);
-        const float part = (float)(turns - __builtin_rint(turns));
+        const float part = (float)(turns - __builtin_rint(turns));  // (off by 2^-26 of a turn, 9.4e-8 of the radius)
         if constexpr (DT == 2) {
             sincospif(2.0f * part, &si[e], &co[e]);
-        } else {  // off by 1.25e-7 at most (2^24 parts tried): results keep 8 bits
+        } else {  // off by 1.25e-7 at most (2^24 parts tried): bf16 results keep 8 bits, codes 4
             si[e] = __builtin_amdgcn_sinf(part);
             co[e] = __builtin_amdgcn_cosf(part);
         }
