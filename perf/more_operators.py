@@ -443,7 +443,7 @@ def _own(s, op):
         hkv.attn_decode_plan_run(s.plan, s.q, SCALE, s.out, s.lse, s.ws, s.ws_bytes, s.stream)
         return {"out": s.out, "lse": s.lse}
     if op == "prefill":
-        hkv.attn_prefill_plan_run_ws(s.plan, s.q, SCALE, s.out, s.lse, s.ws, s.ws_bytes, s.stream)
+        hkv.attn_prefill_plan_run(s.plan, s.q, SCALE, s.out, s.lse, s.stream, s.ws, s.ws_bytes)
         return {"out": s.out, "lse": s.lse}
     if op == "cold":
         hkv.kv_pool_copy_pages(s.other, s.mid, s.pool, s.src, s.tokens, s.stream)
