@@ -50,6 +50,11 @@
  *   fp8 pools (OCP e4m3, no infinities, max 448) carry k_scale and v_scale, float
  *   [num_pages * S][num_kv_heads] (one scale per 16-token block and head); the stored value is
  *   code * scale.
+ *   fp4 pools (OCP e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) hold two codes a byte, the even dimension in the lower half, and
+ *   one scale byte b per token, KV head and 32 dimensions, that stands for 2^(b - 127), 1 <= b <= 252; the stored value is code * scale.
+ *     K block: 1024 bytes, dims d, d + 1 of slot t at byte (t % 4) * 256 + (t / 4) * 64 + d / 2.
+ *     V block: 1024 bytes, the same at byte (t / 4) * 256 + (d / 8) * 16 + (t % 4) * 4 + d % 8 / 2.
+ *     k_scale, v_scale: uint8_t [num_pages * S][num_kv_heads][4][16], entry (d / 32, t) (passed as float *).
  *   Slots past the end of a sequence and unreferenced pages may hold anything, NaN included.
  */
 #ifndef HELIUMKV_H
@@ -84,8 +89,12 @@ enum {
  * cuts their keys into shares where it is given one), and results agree with exact attention to about 1e-6 (the bound asked
  * of fp32 inputs is 1e-4).
  * fp32 block format: K in 64-byte chunks of 16 floats ((d/16)*256 + slot*16 + d%16), V
- * dimension-major (d*16 + slot). */
-enum { HKV_BF16 = 0, HKV_FP8_E4M3 = 1, HKV_FP32 = 2 };
+ * dimension-major (d*16 + slot).
+ * fp4 pools hold a token in 136 bytes per KV head (bf16 512, fp8 256): bf16 sources, q and out, as bf16 pools; attention over
+ * one equals attention over a bf16 pool that holds the same values (code * scale is a bf16 number) up to the order of sums.  Their decode plans
+ * know the settings leaf_chunk, shared_chunk and max_rows of the planner's, and run all nodes as items of up to 64 query
+ * rows (no tiles, no whole paths); prefill widens the batch's pages into workspace first, as over fp8 pools. */
+enum { HKV_BF16 = 0, HKV_FP8_E4M3 = 1, HKV_FP32 = 2, HKV_FP4_E2M1 = 3 };
 
 typedef struct hkv_pool hkv_pool;
 typedef struct hkv_decode_plan hkv_decode_plan;
@@ -104,10 +113,11 @@ typedef struct {
     int32_t page_size;    /* 16, 32, 64 or 128 tokens */
     int32_t num_kv_heads;
     int32_t head_dim;     /* must be 128 */
-    int32_t dtype;        /* HKV_BF16, HKV_FP8_E4M3 or HKV_FP32 */
+    int32_t dtype;        /* HKV_BF16, HKV_FP8_E4M3, HKV_FP32 or HKV_FP4_E2M1 */
     void *k_pages;        /* device, num_pages*(page_size/16)*num_kv_heads*2048 elements, format above */
     void *v_pages;        /* device, same size */
-    float *k_scale;       /* device, [num_pages*(page_size/16)][num_kv_heads]; fp8 pools only, else NULL */
+    float *k_scale;       /* device, [num_pages*(page_size/16)][num_kv_heads]; fp8 pools and, as bytes (format above), 16-byte
+                             aligned, fp4 pools; else NULL */
     float *v_scale;       /* device, same */
     const int32_t *free_order; /* host, optional permutation of 0..num_pages-1: the order in
                                   which kv_pool_alloc hands pages out; NULL = ascending */
@@ -115,7 +125,7 @@ typedef struct {
 
 /* Creates the host-side pool object.  Borrows the device pointers; copies free_order.
  * EINVAL: null desc/out or buffers, num_pages <= 0, free_order not a permutation.
- * ESHAPE: page_size not 16/32/64/128, head_dim != 128, dtype not storable, scales missing for fp8. */
+ * ESHAPE: page_size not 16/32/64/128, head_dim != 128, dtype not storable, scales missing for fp8 or fp4. */
 int kv_pool_create(const hkv_pool_desc *desc, hkv_pool **out);
 
 /* Frees host metadata and any cached plan.  Waits for the device to be idle first if a cached
@@ -171,6 +181,9 @@ int32_t kv_pool_refcount(const hkv_pool *pool, int32_t page_id);
  * RNE(value(code) * scale / scale') (a second rounding of those tokens); the scale never
  * shrinks.  Those slots of such a block must have been written before.  Slots not written keep
  * their contents.  n_tokens == 0 is a no-op.
+ * fp4 pools: each 32 neighbouring dimensions of a token get the scale 2^e, e = floor(log2(amax)) - 2 over them, at least -126 and
+ * at most 125, and code = round-to-nearest-even(x / 2^e), saturated to +-6 (an infinity too; a NaN is held as 6 or -6 times the
+ * scale of the others); no other token's bytes change.
  * EINVAL / ERANGE / ESHAPE as above; the ids are checked before anything is queued. */
 int kv_pool_write(hkv_pool *pool, const int32_t *page_ids, int32_t first_slot, int32_t n_tokens,
                   const void *k_src, const void *v_src, void *stream);
@@ -179,10 +192,10 @@ int kv_pool_write(hkv_pool *pool, const int32_t *page_ids, int32_t first_slot, i
  * of k_src / v_src, device, [n][num_kv_heads][128] bf16) goes to slot slots[i] (0 .. page size - 1)
  * of page page_ids[i]; page_ids and slots are host arrays of n entries (n <= 32768).  Same
  * arithmetic as kv_pool_write with n_tokens = 1 (fp8: the block's running scale, re-encoding of
- * its earlier codes if the scale grows).  No two tokens of one call may go to the same 16-token
+ * its earlier codes if the scale grows; fp4: the token's own scales).  No two tokens of one call may go to the same 16-token
  * block, and no token to a page that has more than one owner (kv_pool_refcount > 1: such a page is
  * shared, kv_pool_copy_on_write gives the writer its own): EINVAL, checked before anything is queued.
- * bf16 and fp8 pools (ESHAPE for fp32 pools: use kv_pool_write). */
+ * bf16, fp8 and fp4 pools (ESHAPE for fp32 pools: use kv_pool_write). */
 int kv_pool_append(hkv_pool *pool, const int32_t *page_ids, const int32_t *slots, int32_t n,
                    const void *k_src, const void *v_src, void *stream);
 
@@ -530,17 +543,17 @@ int hkv_prefill_plan_segments(const hkv_prefill_plan *plan, int32_t *segments_ou
  * [cu_q[n_req]][num_q_heads] float or NULL. */
 int attn_prefill_plan_run(hkv_prefill_plan *plan, const void *q, float scale, void *out, float *lse_out,
                           void *stream);
-/* fp8 pools: the matrix-core kernel reads bf16, so the pages the batch reads (each once, however
- * many requests share it) are first dequantised (code * scale, rounded to bf16) into a scratch pool
+/* fp8 and fp4 pools: the matrix-core kernel reads bf16, so the pages the batch reads (each once, however
+ * many requests share it) are first dequantised (code * scale, rounded to bf16; fp4: exact) into a scratch pool
  * in the caller's workspace (8 KiB per distinct page and KV head), 256-byte aligned device memory.  The pre-pass
  * moves 3 bytes per cached element against 512 flop per (query, key) pair: well below 1 % of the
  * kernel at the sizes prefill runs at.
- * bf16 and fp8 pools: a plan that splits its tiles keeps their partial results in the workspace too, behind those pages (133 KB
+ * bf16, fp8 and fp4 pools: a plan that splits its tiles keeps their partial results in the workspace too, behind those pages (133 KB
  * per partial, 140 MB at most).  hkv_prefill_plan_workspace_bytes is what both take together, 0 where neither is needed;
  * with less (the pages alone, or none for a bf16 pool) the tiles stay whole, which is slower but gives the same
  * results up to the order of the sums.  The workspace is scratch and belongs to one run at a time: runs on different
  * streams take one each.  attn_prefill_plan_run is the same call without a workspace.
- * EINVAL (fp8 pool and no / unaligned workspace), ENOMEM (too small for an fp8 pool's pages). */
+ * EINVAL (fp8 or fp4 pool and no / unaligned workspace), ENOMEM (too small for such a pool's pages). */
 size_t hkv_prefill_plan_workspace_bytes(const hkv_prefill_plan *plan);
 int attn_prefill_plan_run_ws(hkv_prefill_plan *plan, const void *q, float scale, void *out, float *lse_out,
                              void *workspace, size_t workspace_bytes, void *stream);
@@ -569,6 +582,7 @@ size_t attn_prefill_workspace_bytes(int32_t total_q, int32_t num_q_heads);
  * q_row_begin of the plan's creation apply); rows the plan does not name are neither read nor written.
  * A row that holds a NaN or infinity gives what the formula does, in that row and head only; in the codes of fp8 pools, as kv_pool_write,
  * a NaN is held as the lowest value of its block and head, and an infinity is the scale of all of it.
+ * bf16, fp8 and fp32 pools (ESHAPE for fp4 pools, here, of hkv_decode_plan_track_weights and of kv_pool_evict).
  */
 typedef struct {
     const void *q, *k, *v;        /* device, 16-byte aligned: row i begins at element i * stride; [num_q_heads][128], [num_kv_heads][128] elements a row */

@@ -14,6 +14,8 @@
 #include <string>
 #include <unordered_map>
 
+#include "four_bit_plan.h"
+
 // ---------------------------------------------------------------------------------------------
 // errors
 namespace {
@@ -73,13 +75,18 @@ extern "C" int kv_pool_create(const hkv_pool_desc *desc, hkv_pool **out) {
                     desc->page_size, desc->head_dim);
     if ((int64_t)desc->num_pages * (desc->page_size / HKV_PAGE_SIZE) > INT32_MAX)
         return fail(HKV_EINVAL, "kv_pool_create: too many 16-token blocks");
-    if (desc->dtype != HKV_BF16 && desc->dtype != HKV_FP8_E4M3 && desc->dtype != HKV_FP32)
-        return fail(HKV_ESHAPE, "kv_pool_create: pool dtype %d (bf16, fp8 e4m3 or fp32)", desc->dtype);
+    if (desc->dtype != HKV_BF16 && desc->dtype != HKV_FP8_E4M3 && desc->dtype != HKV_FP32 && desc->dtype != HKV_FP4_E2M1)
+        return fail(HKV_ESHAPE, "kv_pool_create: pool dtype %d (bf16, fp8 e4m3, fp32 or fp4 e2m1)", desc->dtype);
     if (desc->num_pages <= 0 || desc->num_kv_heads <= 0)
         return fail(HKV_EINVAL, "kv_pool_create: num_pages and num_kv_heads must be positive");
     if (!desc->k_pages || !desc->v_pages) return fail(HKV_EINVAL, "kv_pool_create: null page buffer");
     if (desc->dtype == HKV_FP8_E4M3 && (!desc->k_scale || !desc->v_scale))
         return fail(HKV_ESHAPE, "kv_pool_create: fp8 pools need k_scale and v_scale");
+    if (desc->dtype == HKV_FP4_E2M1) {
+        if (!desc->k_scale || !desc->v_scale) return fail(HKV_ESHAPE, "kv_pool_create: fp4 pools need k_scale and v_scale");
+        if ((reinterpret_cast<uintptr_t>(desc->k_scale) | reinterpret_cast<uintptr_t>(desc->v_scale)) & 15)
+            return fail(HKV_EINVAL, "kv_pool_create: the scales of an fp4 pool must be 16-byte aligned");
+    }
     if ((reinterpret_cast<uintptr_t>(desc->k_pages) | reinterpret_cast<uintptr_t>(desc->v_pages)) & 15)
         return fail(HKV_EINVAL, "kv_pool_create: page buffers must be 16-byte aligned");
     hkv_pool *p = new (std::nothrow) hkv_pool;
@@ -1510,10 +1517,14 @@ static int create_decode_plan(hkv_pool *pool, const hkv_node *nodes, int32_t n_n
         *out = pl;
         return HKV_OK;
     }
-    RowsByLeaf by_leaf;
-    estimate_paths(*pl, by_leaf);
-    plan_items(*pl);
-    plan_paths(*pl, by_leaf);
+    if (pool->d.dtype == HKV_FP4_E2M1) {
+        plan_four_bit(*pl, chip_shape().n_cu);
+    } else {
+        RowsByLeaf by_leaf;
+        estimate_paths(*pl, by_leaf);
+        plan_items(*pl);
+        plan_paths(*pl, by_leaf);
+    }
     if (reserve_tokens > 0) {  // the items that grow with each request: the leaf's last chunk, one per KV head
         pl->grow_items.assign((size_t)n_req * Hkv, -1);
         for (int r = 0; r < n_req; ++r) {
@@ -2107,6 +2118,9 @@ extern "C" size_t attn_decode_workspace_bytes(hkv_pool *pool, const hkv_node *no
     return hkv_decode_plan_workspace_bytes(pl);
 }
 
+// Pools whose pages prefill reads as bf16, from a scratch pool in the caller's workspace.
+static bool reads_scratch(const hkv_pool *pool) { return pool->d.dtype == HKV_FP8_E4M3 || pool->d.dtype == HKV_FP4_E2M1; }
+
 // ---------------------------------------------------------------------------------------------
 // prefill planning
 // cu_q: request r's new tokens are rows cu_q[r] .. cu_q[r + 1] - 1 of q / out / lse.  q_row_begin (may be null):
@@ -2417,9 +2431,9 @@ static int create_prefill_plan(hkv_pool *pool, const int32_t *cu_q, const int32_
             of_all_heads(taken, pl->pieces);
         }
     }
-    // fp8 pools: number the pages this batch reads (first use first) and point the device table at them
+    // fp8 and fp4 pools: number the pages this batch reads (first use first) and point the device table at them
     std::vector<int32_t> remapped;
-    if (pool->d.dtype == HKV_FP8_E4M3) {
+    if (reads_scratch(pool)) {
         std::unordered_map<int32_t, int32_t> index;
         remapped.assign(blocks.size(), 0);
         for (int r = 0; r < n_req; ++r) {
@@ -2436,7 +2450,7 @@ static int create_prefill_plan(hkv_pool *pool, const int32_t *cu_q, const int32_
             }
         }
     }
-    const std::vector<int32_t> &dev_table = pool->d.dtype == HKV_FP8_E4M3 ? remapped : blocks;
+    const std::vector<int32_t> &dev_table = reads_scratch(pool) ? remapped : blocks;
     const std::vector<PrefillTile> &run_tiles = pl->pieces.empty() ? pl->tiles : pl->pieces;
     if (!(flags & HKV_PLAN_HOST_ONLY) && !run_tiles.empty()) {
         size_t off_bt = align_up(sizeof(PrefillTile) * run_tiles.size(), 256);
@@ -2570,7 +2584,7 @@ extern "C" int hkv_prefill_plan_segments(const hkv_prefill_plan *plan, int32_t *
     return HKV_OK;
 }
 
-// The workspace: fp8 pools first the batch's pages as bf16 (K, then V), then the partials of split tiles and their flags.
+// The workspace: fp8 and fp4 pools first the batch's pages as bf16 (K, then V), then the partials of split tiles and their flags.
 static size_t prefill_pages_bytes(const hkv_prefill_plan *plan) {
     return 2 * plan->src_pages.size() * (size_t)plan->pool->d.num_kv_heads * HKV_PAGE_SIZE * HKV_HEAD_DIM * sizeof(uint16_t);
 }
@@ -2600,10 +2614,11 @@ extern "C" int attn_prefill_plan_run_ws(hkv_prefill_plan *plan, const void *q, f
         return HKV_OK;
     }
     PoolView view = view_of(plan->pool);
-    if (plan->pool->d.dtype == HKV_FP8_E4M3) {  // dequantise the pages of this batch, then read the scratch pool
+    if (reads_scratch(plan->pool)) {  // widen the pages of this batch, then read the scratch pool
         const size_t need = prefill_pages_bytes(plan);
         if (!workspace || (reinterpret_cast<uintptr_t>(workspace) & 255))
-            return fail(HKV_EINVAL, "attn_prefill_plan_run: an fp8 pool needs a 256-byte aligned workspace of %zu bytes", need);
+            return fail(HKV_EINVAL, "attn_prefill_plan_run: an %s pool needs a 256-byte aligned workspace of %zu bytes",
+                        plan->pool->d.dtype == HKV_FP8_E4M3 ? "fp8" : "fp4", need);
         if (workspace_bytes < need)
             return fail(HKV_ENOMEM, "attn_prefill_plan_run: workspace has %zu bytes, %zu needed", workspace_bytes, need);
         void *k_dst = workspace, *v_dst = static_cast<char *>(workspace) + need / 2;
@@ -2614,7 +2629,7 @@ extern "C" int attn_prefill_plan_run_ws(hkv_prefill_plan *plan, const void *q, f
     PrefillLaunch a{view, q, plan->d_tiles, plan->d_block_table, out, lse_out,
                     (int32_t)(plan->pieces.empty() ? plan->tiles : plan->pieces).size(), plan->num_q_heads, scale, plan->d_fallback,
                     plan->d_segments, plan->d_seg_begin, plan->d_split, nullptr, nullptr, 0, 0};
-    // Split tiles need room for their partials; a caller that brings none, or only an fp8 pool's pages, gets whole tiles.
+    // Split tiles need room for their partials; a caller that brings none, or only an fp8 or fp4 pool's pages, gets whole tiles.
     // The room is the caller's, so that runs on different streams (of the one-shot form's cached plan too) share nothing.
     if (plan->d_segments && workspace && (reinterpret_cast<uintptr_t>(workspace) & 255) == 0 &&
         workspace_bytes >= hkv_prefill_plan_workspace_bytes(plan)) {

@@ -113,6 +113,7 @@ hipError_t prepare_decode_device(void **static_ws) {
 // their difference is the kernel's duration without the gap to its neighbours in the queue.
 hipError_t launch_decode(const DecodeLaunch &a, hipStream_t s, hipEvent_t ev_begin, hipEvent_t ev_end) {
     if (a.n_items <= 0) return hipSuccess;
+    if (a.pool.dtype == kDtypeFp4) return launch_four_decode(a, s, ev_begin, ev_end);
     if (a.n_stages < kMinStages || a.n_stages > kMaxStages) return hipErrorInvalidValue;
     if (a.has_shared && !a.fp8_matrix && a.n_stages < 4) return hipErrorInvalidValue;  // shared::body's ring
     if (hipError_t e = prepare_decode_device(nullptr); e != hipSuccess) return e;

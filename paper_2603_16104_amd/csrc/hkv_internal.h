@@ -11,6 +11,7 @@ namespace hkv {
 constexpr int kPage = 16;
 constexpr int kHeadDim = 128;
 constexpr int kBlockElems = kPage * kHeadDim;  // elements of one (page, head) K or V block
+constexpr int kDtypeFp4 = 3;                   // PoolView::dtype etc. of 4-bit pools (HKV_FP4_E2M1)
 
 // One decode workgroup: the tokens [tok_begin, tok_begin + n_tokens) of one tree node, one KV
 // head, applied to n_req of the requests below the node (n_req * G query rows, at most 64; in bf16 plans with tall tiles 128).
@@ -295,10 +296,10 @@ struct PoolCopyLaunch {
     int32_t dst[kMaxCopyPairs];
 };
 
-// fp8 pages -> bf16 pages of a scratch pool (page i of the scratch = src_pages[i] of the pool), so that
-// the matrix-core prefill kernel can read an fp8 pool.
+// fp8 or fp4 pages -> bf16 pages of a scratch pool (page i of the scratch = src_pages[i] of the pool), so that
+// the matrix-core prefill kernel can read such a pool.
 struct PoolDequantLaunch {
-    PoolView pool;               // the fp8 pool
+    PoolView pool;               // the fp8 or fp4 pool
     const int32_t *src_pages;    // device [n_pages]
     int32_t n_pages;
     void *k_dst;                 // device, n_pages * num_kv_heads * 2048 bf16, bf16 block format
@@ -421,6 +422,12 @@ hipError_t launch_evict(const EvictLaunch &a, hipStream_t s);
 hipError_t launch_evict(const EvictInline &a, hipStream_t s);
 hipError_t launch_pool_copy(const PoolCopyLaunch &a, hipStream_t s);
 hipError_t launch_pool_dequant(const PoolDequantLaunch &a, hipStream_t s);
+// 4-bit pools (four_bit.hip, four_bit_decode.hip); the scales' pointers address bytes there.  The launches above go on to these where the pool is one.
+hipError_t launch_four_write(const PoolWriteLaunch &a, hipStream_t s);
+hipError_t launch_four_append(const PoolAppendInline &a, hipStream_t s);
+hipError_t launch_four_step_append(const PoolAppendInline &w, const PlanGrowInline &g, hipStream_t s);
+hipError_t launch_four_widen(const PoolDequantLaunch &a, hipStream_t s);
+hipError_t launch_four_decode(const DecodeLaunch &a, hipStream_t s, hipEvent_t ev_begin = nullptr, hipEvent_t ev_end = nullptr);
 // Once per device (later calls only read the result), with that device current and outside graph capture:
 // allows the decode kernels their LDS and looks up the device's static workspace (kStaticWorkspaceBytes
 // bytes, 256-byte aligned), returned through static_ws unless that is null.  Safe from several threads.

@@ -94,7 +94,7 @@ struct hkv_prefill_plan {
     PrefillTile *d_tiles = nullptr;
     int32_t *d_block_table = nullptr;
     int32_t *d_rows_req = nullptr, *d_rows_len = nullptr;  // fp32 pools: per new token (one allocation: d_rows_req)
-    // fp8 pools: the pages the batch reads are first dequantised into a bf16 scratch pool in the caller's
+    // fp8 and fp4 pools: the pages the batch reads are first dequantised into a bf16 scratch pool in the caller's
     // workspace (page i of the scratch = src_pages[i]); the device block table then holds scratch indices.
     std::vector<int32_t> src_pages;
     int32_t *d_src_pages = nullptr;

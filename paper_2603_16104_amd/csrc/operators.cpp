@@ -22,6 +22,7 @@ bool is_capturing(hipStream_t s) {
 int projection_of(const hkv_pool *pool, int num_q_heads, const hkv_qkv *x, ProjectionLaunch &a, const char *who) {
     if (!x) return fail(HKV_EINVAL, "%s: null rows", who);
     if (!x->q || !x->k || !x->v || !x->q_out) return fail(HKV_EINVAL, "%s: null q, k, v or q_out", who);
+    if (pool->d.dtype == HKV_FP4_E2M1) return fail(HKV_ESHAPE, "%s: not over fp4 pools (kv_pool_write, kv_pool_append)", who);
     if (!aligned16(x->q) || !aligned16(x->k) || !aligned16(x->v) || !aligned16(x->q_out) || !aligned16(x->q_norm) || !aligned16(x->k_norm))
         return fail(HKV_EINVAL, "%s: q, k, v, q_out and the norms' weights must be 16-byte aligned", who);
     const int Hkv = pool->d.num_kv_heads, per16 = pool->d.dtype == HKV_FP32 ? 4 : 8;
@@ -298,6 +299,7 @@ static int track_fp32(hkv_decode_plan *plan) {
 extern "C" int hkv_decode_plan_track_weights(hkv_decode_plan *plan) try {
     const char *who = "hkv_decode_plan_track_weights";
     if (!plan) return fail(HKV_EINVAL, "%s: null plan", who);
+    if (plan->pool->d.dtype == HKV_FP4_E2M1) return fail(HKV_ESHAPE, "%s: not over fp4 pools", who);
     if (plan->tracks_weights) return HKV_OK;
     const int Hkv = plan->pool->d.num_kv_heads, n_nodes = (int)plan->nodes.size();
     std::vector<int32_t> blocks;
@@ -403,6 +405,7 @@ extern "C" int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_p
                              int32_t n_first, int32_t n_recent, float *key_weights, int32_t *kept, void *stream) try {
     const char *who = "kv_pool_evict";
     if (!pool) return fail(HKV_EINVAL, "%s: null pool", who);
+    if (pool->d.dtype == HKV_FP4_E2M1) return fail(HKV_ESHAPE, "%s: not over fp4 pools", who);
     if (n_seq < 0 || n_first < 0 || n_recent < 0) return fail(HKV_EINVAL, "%s: n_seq %d, n_first %d, n_recent %d", who, n_seq, n_first, n_recent);
     if (n_seq == 0) return HKV_OK;
     if (!n_tokens || !n_keep) return fail(HKV_EINVAL, "%s: null n_tokens or n_keep", who);

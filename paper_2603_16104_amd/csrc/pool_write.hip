@@ -156,18 +156,19 @@ __global__ __launch_bounds__(256) void pool_append_inline_kernel(PoolAppendInlin
 }
 
 // One workgroup per (pair, K or V): copies the page's blocks of all KV heads, 16 bytes per thread and
-// step, and (fp8 pools) the page's scales.  Source and destination pages are distinct.
+// step, and (fp8 and fp4 pools) the page's scales.  Source and destination pages are distinct.
 __global__ __launch_bounds__(256) void pool_copy_kernel(PoolCopyLaunch a) {
     const int pair = blockIdx.x, which = blockIdx.y;
-    const int elem = a.pool.dtype == 0 ? 2 : a.pool.dtype == 1 ? 1 : 4;
-    const size_t page_bytes = (size_t)a.blocks_per_page * a.pool.num_kv_heads * kBlockElems * elem;
+    const int bits = a.pool.dtype == 0 ? 16 : a.pool.dtype == 1 ? 8 : a.pool.dtype == kDtypeFp4 ? 4 : 32;
+    const size_t page_bytes = (size_t)a.blocks_per_page * a.pool.num_kv_heads * (kBlockElems / 8) * bits;
     const char *base = static_cast<const char *>(which ? a.pool.v_pages : a.pool.k_pages);
     const uint4 *src = reinterpret_cast<const uint4 *>(base + (size_t)a.src[pair] * page_bytes);
     uint4 *dst = reinterpret_cast<uint4 *>(const_cast<char *>(base) + (size_t)a.dst[pair] * page_bytes);
     for (size_t i = threadIdx.x; i < page_bytes / 16; i += 256) dst[i] = src[i];
-    if (a.pool.dtype == 1) {
+    if (a.pool.dtype == 1 || a.pool.dtype == kDtypeFp4) {
         float *sc = const_cast<float *>(which ? a.pool.v_scale : a.pool.k_scale);
-        const int per_page = a.blocks_per_page * a.pool.num_kv_heads;  // one scale per 16-token block and head
+        // one scale per 16-token block and head; 4-bit pools 64 bytes of them
+        const int per_page = a.blocks_per_page * a.pool.num_kv_heads * (a.pool.dtype == kDtypeFp4 ? 16 : 1);
         for (int h = threadIdx.x; h < per_page; h += 256)
             sc[(size_t)a.dst[pair] * per_page + h] = sc[(size_t)a.src[pair] * per_page + h];
     }
@@ -231,6 +232,7 @@ __global__ __launch_bounds__(256) void decode_step_append_kernel(PoolAppendInlin
 
 hipError_t launch_decode_step_append(const PoolAppendInline &w, const PlanGrowInline &g, hipStream_t s) {
     if (w.base.n_pages <= 0) return hipSuccess;
+    if (w.base.dtype == kDtypeFp4) return launch_four_step_append(w, g, s);
     dim3 grid(w.base.n_pages, w.base.num_kv_heads), block(256);
     if (w.base.dtype == 0)
         hipLaunchKernelGGL(decode_step_append_kernel<0>, grid, block, 0, s, w, g);
@@ -248,6 +250,7 @@ hipError_t launch_plan_grow_inline(const PlanGrowInline &a, hipStream_t s) {
 
 hipError_t launch_pool_dequant(const PoolDequantLaunch &a, hipStream_t s) {
     if (a.n_pages <= 0) return hipSuccess;
+    if (a.pool.dtype == kDtypeFp4) return launch_four_widen(a, s);
     hipLaunchKernelGGL(pool_dequant_kernel, dim3(a.n_pages, a.pool.num_kv_heads), dim3(256), 0, s, a);
     return hipGetLastError();
 }
@@ -269,6 +272,7 @@ hipError_t launch_pool_copy(const PoolCopyLaunch &a, hipStream_t s) {
 
 hipError_t launch_pool_append_inline(const PoolAppendInline &a, hipStream_t s) {
     if (a.base.n_pages <= 0) return hipSuccess;
+    if (a.base.dtype == kDtypeFp4) return launch_four_append(a, s);
     dim3 grid(a.base.n_pages, a.base.num_kv_heads), block(256);
     if (a.base.dtype == 0)
         hipLaunchKernelGGL(pool_append_inline_kernel<0>, grid, block, 0, s, a);
@@ -279,6 +283,7 @@ hipError_t launch_pool_append_inline(const PoolAppendInline &a, hipStream_t s) {
 
 hipError_t launch_pool_write(const PoolWriteLaunch &a, hipStream_t s) {
     if (a.n_pages <= 0) return hipSuccess;
+    if (a.dtype == kDtypeFp4) return launch_four_write(a, s);
     // A wavefront per K or V of a block takes longer alone than the four of a workgroup together; from 400 blocks x heads on that no
     // longer counts (fp8, device time of a write, workgroup per block and head / this: 8 heads, 320 tokens 2.80 / 2.99 us, 500 3.10 /
     // 3.33, 1000 3.51 / 3.26, 4096 5.89 / 5.08; 2 heads, 2000 tokens 2.88 / 3.06, 4096 3.20 / 3.22, 8192 3.99 / 3.72; 1 head, half

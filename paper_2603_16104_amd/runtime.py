@@ -11,7 +11,8 @@ from . import binding as hkv
 from . import workloads as wl
 
 # bf16 bit patterns travel as int16 tensors (full torch support); 0x7FC0 is a bf16 NaN, 0x7F the e4m3 NaN
-_ELEM = {hkv.BF16: (torch.int16, 0x7FC0), hkv.FP8_E4M3: (torch.uint8, 0x7F), hkv.FP32: (torch.float32, float("nan"))}
+_ELEM = {hkv.BF16: (torch.int16, 0x7FC0), hkv.FP8_E4M3: (torch.uint8, 0x7F), hkv.FP32: (torch.float32, float("nan")),
+         hkv.FP4_E2M1: (torch.uint8, 0x77)}   # (two codes a byte; there is no NaN code, the scales poison)
 
 
 class DevicePool:
@@ -21,7 +22,7 @@ class DevicePool:
                  free_order: Optional[np.ndarray] = None, poison: bool = True, page_size: int = hkv.PAGE_SIZE):
         self.num_pages, self.num_kv_heads, self.dtype, self.page_size = num_pages, num_kv_heads, dtype, page_size
         tdt, nan_bits = _ELEM[dtype]
-        n = num_pages * num_kv_heads * page_size * hkv.HEAD_DIM
+        n = num_pages * num_kv_heads * page_size * hkv.HEAD_DIM // (2 if dtype == hkv.FP4_E2M1 else 1)
         fill = nan_bits if poison else 0
         self.k = torch.full((n,), fill, dtype=tdt, device=device)
         self.v = torch.full((n,), fill, dtype=tdt, device=device)
@@ -31,6 +32,9 @@ class DevicePool:
             n_sc = num_pages * (page_size // hkv.PAGE_SIZE) * num_kv_heads   # one scale per 16-token block and head
             self.k_scale = torch.full((n_sc,), sv, dtype=torch.float32, device=device)
             self.v_scale = torch.full((n_sc,), sv, dtype=torch.float32, device=device)
+        elif dtype == hkv.FP4_E2M1:   # one per token, head and 32 dims; 255 stands for no number
+            n_sc = num_pages * page_size * num_kv_heads * 4
+            self.k_scale, self.v_scale = (torch.full((n_sc,), 255 if poison else 127, dtype=torch.uint8, device=device) for _ in range(2))
         self.handle = hkv.kv_pool_create(num_pages, num_kv_heads, dtype, self.k, self.v, self.k_scale, self.v_scale,
                                          free_order, page_size=page_size)
 
