@@ -157,6 +157,41 @@ int kv_pool_release(hkv_pool *pool, int32_t n, const int32_t *ids /* host */);
  * free than copies are needed; nothing changes on these errors. */
 int kv_pool_copy_on_write(hkv_pool *pool, int32_t n, int32_t *ids /* host, in/out */, void *stream);
 
+/* Copies pages within a pool or from one pool to another of the same page size and number of KV heads (else ESHAPE), of the same type or
+ * not: prompts that no call waits for go from a bf16 to an fp4 pool, and come back when one hits them.  Page src_ids[i] of src goes to page
+ * dst_ids[i] of dst on `stream`; n_tokens[i] (host, 0 .. page size; NULL: the page size) of its slots count.
+ * Same type: whole 16-token blocks up to the last token, scales with them.  Other type: the tokens' values (code * scale) by the rules of
+ * kv_pool_write, a block at a time as one written from its slot 0 (bf16: round to nearest even; fp8: one scale for the block's tokens; fp4: as
+ * there; fp32: as they are), from the values in fp32, not from a bf16 rounding of them; slots behind the last token keep what they hold.
+ *   src_ids, dst_ids: host, n entries.  dst_ids all different, of one owner at most, and, within one pool, none of src_ids (EINVAL).
+ * References do not change, and key_weights are the caller's to copy.  ERANGE: page ids.  Nothing is queued on error.  Not for capture into a graph
+ * (EINVAL): longer lists pass through the target pool's staging ring.  The pools' buffers may be on one device only, the current one. */
+int kv_pool_copy_pages(hkv_pool *dst, const int32_t *dst_ids, hkv_pool *src, const int32_t *src_ids, int32_t n, const int32_t *n_tokens, void *stream);
+
+/* Forks sequences: fork j begins as sequence parent[j] (host, n_out entries, in any order, a sequence any number of times) and goes on by itself.  It shares
+ * every full page of its sequence (one reference more) and gets a page of its own for a last page that is not full: the next free one
+ * (in the order of the forks), to which the 16-token blocks in use are copied on `stream`, all in one launch.
+ *   pages: host, ceil(n_tokens[i] / page size) ids of each sequence, one sequence after the other.  out_pages: host, the same of each fork.
+ * release != 0: the sequences end here, and their references (one per listing) are dropped, as a step of a beam search replaces its beams
+ * by others: a sequence that no fork continues is gone (its pages return to the free list, in the order listed), and one that owns its last page
+ * alone hands that to its first fork without a copy.  release == 0: the sequences stay as they are.
+ * A copied page has no key_weights of the old one's: they are the caller's to copy.
+ * ERANGE: page ids, parents.  EINVAL: pages that are not allocated, or listed more often than held (release).  ENOMEM: fewer free pages than copies.  Nothing
+ * changes on error.  Not for capture into a graph where something is copied (EINVAL): a replay would take the same pages. */
+int kv_pool_fork(hkv_pool *pool, int32_t n_seq, const int32_t *pages, const int32_t *n_tokens, int32_t n_out, const int32_t *parent, int32_t release,
+                 int32_t *out_pages, void *stream);
+
+/* Compaction: the n_live pages in use move to ids 0 .. n_live - 1, so that the end of the page buffers is free (to be handed back, or to another pool).
+ * Pages below n_live stay; the others go to the free ids there, in ascending order, with their contents (on `stream`, one launch per 21845 16-token
+ * blocks) and references; then the free ids n_live .. follow in ascending order.  new_ids: host [num_pages], out: the new id of every page in use, -1 for a free one.
+ * Prefix caches over the pool follow by themselves.  Everything else that holds page ids is the caller's to renumber: page lists and
+ * block tables (plans are made anew), rows of key_weights.  Work queued before on other streams that reads or writes pages has to be ordered in front.
+ * Returns the number of pages that moved, or a negative error code.  EINVAL: null arguments, a stream under capture.  Nothing changes on error. */
+int32_t kv_pool_compact(hkv_pool *pool, int32_t *new_ids, void *stream);
+
+/* Number of pages of the pool, or a negative error code. */
+int32_t kv_pool_num_pages(const hkv_pool *pool);
+
 /* Number of free pages, or a negative error code. */
 int32_t kv_pool_num_free(const hkv_pool *pool);
 

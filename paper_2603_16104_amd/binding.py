@@ -24,7 +24,7 @@ PAGE_SIZE, HEAD_DIM = 16, 128
 
 EXPORTS = [
     "hkv_last_error", "kv_pool_create", "kv_pool_destroy", "kv_pool_alloc", "kv_pool_retain", "kv_pool_release", "kv_pool_copy_on_write",
-    "kv_pool_num_free", "kv_pool_page_size", "kv_pool_refcount", "kv_pool_write", "kv_pool_append", "prefix_tree_flatten",
+    "kv_pool_copy_pages", "kv_pool_fork", "kv_pool_compact", "kv_pool_num_pages", "kv_pool_num_free", "kv_pool_page_size", "kv_pool_refcount", "kv_pool_write", "kv_pool_append", "prefix_tree_flatten",
     "hkv_decode_plan_create_growing", "hkv_decode_plan_append", "hkv_decode_plan_append_tokens",
     "prefix_tree_flatten_paged", "prefix_tree_prefill_usage",
     "lse_merge", "hkv_decode_plan_create", "hkv_decode_plan_create_multi", "hkv_decode_plan_create_tree", "hkv_decode_plan_create_ex", "hkv_prefill_plan_create_rows", "hkv_prefill_plan_fallback_tiles", "hkv_decode_plan_destroy", "hkv_decode_plan_workspace_bytes",
@@ -82,6 +82,9 @@ def lib():
         L.hkv_decode_plan_store.argtypes = [p, p, p]
         L.hkv_decode_plan_append_qkv.argtypes = [p, p, p, p]
         L.attn_decode_plan_weights.argtypes = [p, p, f, p, f, i, p, p]
+        L.kv_pool_copy_pages.argtypes = [p, p, p, p, i, p, p]
+        L.kv_pool_fork.argtypes = [p, i, p, p, i, p, i, p, p]
+        L.kv_pool_compact.argtypes = [p, p, p]
         L.kv_pool_evict.argtypes = [p, i, p, p, p, p, i, i, p, p, p]
         _lib = L
     return _lib
@@ -197,6 +200,37 @@ def kv_pool_copy_on_write(pool, ids, stream=None) -> np.ndarray:
     ids = _host_i32(ids).copy()
     _check(lib().kv_pool_copy_on_write(pool, C.c_int32(len(ids)), _hp(ids), _stream(stream)))
     return ids
+
+
+def kv_pool_copy_pages(dst_pool, dst_ids, src_pool, src_ids, n_tokens=None, stream=None) -> None:
+    """Pages src_ids of one pool to pages dst_ids of another or the same; n_tokens: tokens of each page that count (None: all)."""
+    dst_ids, src_ids = _host_i32(dst_ids), _host_i32(src_ids)
+    n_tokens = None if n_tokens is None else _host_i32(n_tokens)
+    if len(dst_ids) != len(src_ids) or (n_tokens is not None and len(n_tokens) != len(dst_ids)):
+        raise HkvError(EINVAL, "kv_pool_copy_pages: lists of different length")
+    _run(lib().kv_pool_copy_pages, dst_pool, _host_addr(dst_ids), src_pool, _host_addr(src_ids), len(dst_ids), _host_addr(n_tokens),
+         _stream_addr(stream) if len(dst_ids) else None)
+
+
+def kv_pool_fork(pool, pages, n_tokens, parent, release: bool = False, stream=None) -> np.ndarray:
+    """pages: the sequences' page lists, one after the other; returns those of the forks, fork j of sequence parent[j]."""
+    pages, n_tokens, parent = _host_i32(pages), _host_i32(n_tokens), _host_i32(parent)
+    page = kv_pool_page_size(pool)
+    count = -(-n_tokens.astype(np.int64) // page)
+    if (n_tokens >= 0).all() and len(pages) != count.sum():
+        raise HkvError(EINVAL, f"kv_pool_fork: {count.sum()} page ids needed, {len(pages)} given")
+    known = len(parent) > 0 and len(n_tokens) > 0 and 0 <= parent.min() and parent.max() < len(n_tokens)
+    out = np.empty(int(count[parent].sum()) if known else 0, dtype=np.int32)
+    _run(lib().kv_pool_fork, pool, len(n_tokens), _host_addr(pages), _host_addr(n_tokens), len(parent), _host_addr(parent), int(release),
+         _host_addr(out), _stream_addr(stream))
+    return out
+
+
+def kv_pool_compact(pool, stream=None) -> np.ndarray:
+    """Moves the pages in use to the front of the pool; returns the new id of every page (-1: free)."""
+    new_ids = np.empty(_check(lib().kv_pool_num_pages(pool)), dtype=np.int32)
+    _run(lib().kv_pool_compact, pool, _host_addr(new_ids), _stream_addr(stream))
+    return new_ids
 
 
 def kv_pool_num_free(pool) -> int:

@@ -9,7 +9,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libheliumkv.so")
 SOURCES = ["api.cpp", "operators.cpp", "decode.hip", "merge.hip", "pool_write.hip", "projection_store.hip", "key_weights.hip", "evict.hip", "prefill.hip",
-           "rows_fp32.hip", "four_bit.hip", "four_bit_decode.hip", "trt.cpp", "cache.cpp"]
+           "rows_fp32.hip", "four_bit.hip", "four_bit_decode.hip", "page_copy.hip", "pages.cpp", "trt.cpp", "cache.cpp"]
 HEADERS = ["hkv_internal.h", "hkv_objects.h", "hkv_device.h", "pool_block.h", "four_bit.h", "four_bit_plan.h", "rows_body.h", "shared_body.h", "tall_body.h", "tile_body.h", os.path.join("..", "..", "include", "heliumkv.h")]
 
 # Packed-FP32 VALU forms are switched off for every kernel in this library.

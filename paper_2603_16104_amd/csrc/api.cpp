@@ -162,13 +162,10 @@ extern "C" int kv_pool_retain(hkv_pool *pool, int32_t n, const int32_t *ids) {
 
 extern "C" int kv_pool_release(hkv_pool *pool, int32_t n, const int32_t *ids) {
     if (int rc = check_held(pool, n, ids, "kv_pool_release")) return rc;
-    std::vector<int32_t> sorted(ids, ids + n);  // a page may occur several times: count per page
-    std::sort(sorted.begin(), sorted.end());
-    for (int i = 0, run = 0; i < n; ++i) {
-        run = (i > 0 && sorted[i] == sorted[i - 1]) ? run + 1 : 1;
-        if (run > pool->refcnt[sorted[i]])
-            return fail(HKV_EINVAL, "kv_pool_release: page %d released more often than it is held", sorted[i]);
-    }
+    int held = 0;  // a page may occur several times: every listing is counted, then the counts are as they were again
+    while (held < n && pool->refcnt[ids[held]] > 0) --pool->refcnt[ids[held++]];
+    for (int i = 0; i < held; ++i) ++pool->refcnt[ids[i]];
+    if (held < n) return fail(HKV_EINVAL, "kv_pool_release: page %d released more often than it is held", ids[held]);
     for (int i = 0; i < n; ++i)
         if (--pool->refcnt[ids[i]] == 0) pool->free_list.push_back(ids[i]);
     return HKV_OK;
@@ -177,6 +174,11 @@ extern "C" int kv_pool_release(hkv_pool *pool, int32_t n, const int32_t *ids) {
 extern "C" int32_t kv_pool_num_free(const hkv_pool *pool) {
     if (!pool) return fail(HKV_EINVAL, "kv_pool_num_free: null pool");
     return (int32_t)pool->free_list.size();
+}
+
+extern "C" int32_t kv_pool_num_pages(const hkv_pool *pool) {
+    if (!pool) return fail(HKV_EINVAL, "kv_pool_num_pages: null pool");
+    return pool->d.num_pages;
 }
 
 extern "C" int32_t kv_pool_page_size(const hkv_pool *pool) {

@@ -17,12 +17,9 @@
 #include <unordered_map>
 #include <vector>
 
-#include "../../include/heliumkv.h"
+#include <algorithm>
 
-namespace hkv {
-int fail(int code, const char *fmt, ...);
-}
-using hkv::fail;
+#include "hkv_objects.h"
 
 namespace {
 
@@ -94,6 +91,24 @@ struct hkv_cache {
             add(b);
         }
     }
+    // kv_pool_compact: the same blocks under their pages' new ids, held aside until the pages move
+    std::unordered_map<int32_t, Block *> moved_by_page;
+    std::unordered_map<int32_t, int> moved_private;
+    std::set<std::pair<int64_t, int32_t>> moved_evictable;
+    void prepare(const int32_t *new_ids) {
+        moved_by_page.clear();
+        moved_private.clear();
+        moved_evictable.clear();
+        for (const auto &kv : by_page) moved_by_page[new_ids[kv.first]] = kv.second;
+        for (const auto &kv : private_pages) moved_private[new_ids[kv.first]] = kv.second;
+        for (const auto &e : evictable) moved_evictable.insert({e.first, new_ids[e.second]});
+    }
+    void commit() {
+        by_page.swap(moved_by_page);
+        private_pages.swap(moved_private);
+        evictable.swap(moved_evictable);
+        for (auto &kv : by_page) kv.second->page = kv.first;
+    }
     void free_tree(Block *b) {
         for (auto &kv : b->children) {
             free_tree(kv.second);
@@ -109,12 +124,20 @@ extern "C" int kv_cache_create(hkv_pool *pool, hkv_cache **out) {
     if (!c) return fail(HKV_ENOMEM, "kv_cache_create: out of host memory");
     c->pool = pool;
     c->block = kv_pool_page_size(pool);
+    try {
+        pool->followers.push_back({c, [](void *p, const int32_t *ids) { static_cast<hkv_cache *>(p)->prepare(ids); }, [](void *p) { static_cast<hkv_cache *>(p)->commit(); }});
+    } catch (const std::exception &) {
+        delete c;
+        return fail(HKV_ENOMEM, "kv_cache_create: out of host memory");
+    }
     *out = c;
     return HKV_OK;
 }
 
 extern "C" int kv_cache_destroy(hkv_cache *c) {
     if (!c) return HKV_OK;
+    auto &followers = c->pool->followers;
+    followers.erase(std::remove_if(followers.begin(), followers.end(), [c](const hkv_pool::Follower &f) { return f.object == c; }), followers.end());
     for (auto &kv : c->by_page) (void)kv_pool_release(c->pool, 1, &kv.first);
     for (auto &kv : c->private_pages) (void)kv_pool_release(c->pool, 1, &kv.first);
     c->free_tree(&c->root);

@@ -296,6 +296,20 @@ struct PoolCopyLaunch {
     int32_t dst[kMaxCopyPairs];
 };
 
+// Copies of 16-token blocks between pools of the same heads (page_copy.hip): entry i of the list is {source block, target block, tokens of it}.
+struct PageCopyLaunch {
+    PoolView src, dst;
+    const int32_t *list;         // device
+    int32_t n;
+    int32_t bits, scale_words;   // of an element; of a block's scales and head (set by the launch)
+};
+// The same with a list that is short enough in the arguments.
+constexpr int kMaxInlineCopies = 320;
+struct PageCopyInline : PageCopyLaunch {
+    int32_t entries[3 * kMaxInlineCopies];
+};
+static_assert(sizeof(PageCopyInline) <= 4096, "kernel argument segment");
+
 // fp8 or fp4 pages -> bf16 pages of a scratch pool (page i of the scratch = src_pages[i] of the pool), so that
 // the matrix-core prefill kernel can read such a pool.
 struct PoolDequantLaunch {
@@ -421,6 +435,8 @@ hipError_t launch_key_weights(const KeyWeightsLaunch &a, hipStream_t s);
 hipError_t launch_evict(const EvictLaunch &a, hipStream_t s);
 hipError_t launch_evict(const EvictInline &a, hipStream_t s);
 hipError_t launch_pool_copy(const PoolCopyLaunch &a, hipStream_t s);
+hipError_t launch_page_copy(const PageCopyLaunch &a, hipStream_t s);
+hipError_t launch_page_copy(const PageCopyInline &a, hipStream_t s);
 hipError_t launch_pool_dequant(const PoolDequantLaunch &a, hipStream_t s);
 // 4-bit pools (four_bit.hip, four_bit_decode.hip); the scales' pointers address bytes there.  The launches above go on to these where the pool is one.
 hipError_t launch_four_write(const PoolWriteLaunch &a, hipStream_t s);

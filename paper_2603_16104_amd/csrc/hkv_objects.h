@@ -128,7 +128,14 @@ struct hkv_pool {
     hipEvent_t slot_free[kWriteSlots] = {};
     bool slot_in_flight[kWriteSlots] = {};
     int next_slot = 0;
-    std::vector<uint32_t> mark;  // kv_pool_evict: pages marked in the present call (mark[id] == mark_now)
+    // What else holds page ids of the pool and follows kv_pool_compact (prefix caches): prepare may throw, commit does not.
+    struct Follower {
+        void *object;
+        void (*prepare)(void *object, const int32_t *new_ids);
+        void (*commit)(void *object);
+    };
+    std::vector<Follower> followers;
+    std::vector<uint32_t> mark;  // kv_pool_evict, kv_pool_copy_pages: pages marked in the present call (mark[id] == mark_now)
     uint32_t mark_now = 0;
     hkv_decode_plan *cached_decode = nullptr;
     hkv_prefill_plan *cached_prefill = nullptr;
