@@ -19,7 +19,7 @@ namespace four {
 constexpr int kCodeBytes = kBlockElems / 2, kScaleBytes = kPage * kHeadDim / 32;  // of a block and head
 
 // 2^(b - 127) of scale byte `i` of a word (b is 1 .. 252 in what the writers leave).
-__device__ __forceinline__ float scale_of(uint32_t w, int i) { return __uint_as_float(((w >> (8 * i)) & 0xFFu) << 23); }
+__device__ __forceinline__ float scale_of(uint32_t w, int i) { return __uint_as_float(__builtin_amdgcn_ubfe(w, 8 * i, 8) << 23); }
 
 // Codes 2 B, 2 B + 1 of a word times a scale, as two bf16 (exact).
 template <int B>

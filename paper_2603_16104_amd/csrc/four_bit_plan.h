@@ -9,7 +9,7 @@
 // a partial per row; the chunks of a node take the same places in the partial lists of all requests below it (as in the other pools' plans).
 static void plan_four_bit(hkv_decode_plan &pl, int n_cu) {
     const int G = pl.group, Hkv = pl.pool->d.num_kv_heads, n_nodes = (int)pl.nodes.size();
-    const int max_rows = pl.opt.max_rows ? pl.opt.max_rows : 64, max_req = std::max(1, max_rows / G);
+    const int max_rows = pl.opt.max_rows ? pl.opt.max_rows : 128, max_req = std::max(1, max_rows / G);
     auto requests = [&](int v) { return pl.node_req_indptr[v + 1] - pl.node_req_indptr[v]; };
     int64_t work = 0;  // blocks times row groups and heads
     for (int v = 0; v < n_nodes; ++v)

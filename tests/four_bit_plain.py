@@ -80,8 +80,9 @@ def of_sequence(values, pages, page_size, n):
 
 
 def attention(q, k, v, scale, seen):
-    """q [heads of q][128], k and v [n][kv heads][128], seen [n] of truth values: out, lse, and what tolerances are made of: sum of p |v| per dim, and the largest
-    sum of |q k| scale."""
+    """q [heads of q][128], k and v [n][kv heads][128], seen [n] of truth values: out, lse, and what tolerances are made of: sum of p |v| per dim, and how far a
+    score may be off: 130 roundings of 2^-24 of the largest sum of |q k| scale, and 2^-17 of the row's largest element for those below 2^-9 of it (decode
+    splits a row of q into two terms of 4 bits each above the smallest step of 2^-9, the row's largest brought into [128, 256))."""
     hq, hk = q.shape[0], k.shape[1]
     out, weight, lse, size = np.zeros((hq, 128)), np.zeros((hq, 128)), np.full(hq, -math.inf), np.zeros(hq)
     if not seen.any():
@@ -89,7 +90,8 @@ def attention(q, k, v, scale, seen):
     for h in range(hq):
         kk, vv = k[seen][:, h // (hq // hk)], v[seen][:, h // (hq // hk)]
         x = kk @ q[h] * scale
-        size[h] = (np.abs(kk) @ np.abs(q[h])).max() * abs(scale)
+        far = np.where(np.abs(q[h]) < 2.0 ** -9 * np.abs(q[h]).max(), 2.0 ** -17 * np.abs(q[h]).max(), 0)
+        size[h] = ((np.abs(kk) @ np.abs(q[h])) * 130 * STEP["fp32"] + np.abs(kk) @ far).max() * abs(scale)
         lse[h] = x.max() + math.log(np.exp(x - x.max()).sum())
         p = np.exp(x - lse[h])
         out[h], weight[h] = p @ vv, p @ np.abs(vv)
@@ -98,9 +100,9 @@ def attention(q, k, v, scale, seen):
 
 def check_rows(out, lse, ref, tile=False):
     """Rows of a kernel against attention()'s.  out: a probability is rounded to bf16 (half a step of 2^-8, into the sum of p |v|), the partial to 11 bits of the
-    row's largest, the result to bf16; scores of size S are off by up to 130 roundings of 2^-24 S in the worst case, which p and lse carry."""
+    row's largest, the result to bf16; what a score is off by, p and lse carry, and some 160 roundings of sums and exponentials (1e-5)."""
     o, x, w, size = ref
-    off = 130 * STEP["fp32"] * size + 1e-5
+    off = size + 1e-5
     tol = (2.0 ** -8 + 2 * off[..., None]) * w + 2.0 ** -11 * w.max(-1, keepdims=True)
     tol = tol + 2.0 ** -8 * (np.abs(o) + tol) + 1e-30
     assert (np.abs(out - o) <= tol).all(), float((np.abs(out - o) / tol).max())
