@@ -13,6 +13,7 @@
 // share of P^T is made of, so probabilities stay where they are.  Widened values are exact (two significant bits, a power of two).
 #include <hip/hip_ext.h>
 
+#include <climits>
 #include <type_traits>
 
 #include "four_bit.h"
@@ -90,238 +91,325 @@ __device__ __forceinline__ void split_row(RowTile &x, const u32x4 (&w)[4], float
     }
 }
 
-// One item by the workgroup: RT row tiles a wavefront.
-template <int RT>
-__device__ __forceinline__ void run_item(const DecodeLaunch &a, const DecodeItem &it, float (*sO)[16][kORow], float (*sM)[16], float (*sL)[16], uint32_t (*sPart)[16]) {
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-    const int m = lane & 15, g = lane >> 4;
-    const int Hkv = a.pool.num_kv_heads, G = a.num_q_heads / Hkv, rows = it.n_req * G;
-    // wavefronts: groups of RT row tiles x shares of the steps
-    const int n_rg = RT == 1 || rows <= 32 ? 1 : rows <= 64 ? 2 : 4, n_ts = kWaves / n_rg;
-    const int row0 = wave % n_rg * (16 * RT), ts = wave / n_rg;
-    const float c = fmaxf(fabsf(a.scale) * kLog2e, 1e-30f);  // (scores times 0: a weight of 1 each, and -inf stays)
-
-    const int n_blk = (it.n_tokens + kStep - 1) / kStep, last_page = (it.n_tokens - 1) >> 4;
-    const uint8_t *kc = static_cast<const uint8_t *>(a.pool.k_pages) + (m & 3) * 64 + g * 16, *vc = static_cast<const uint8_t *>(a.pool.v_pages) + m * 16;
-    const uint8_t *ks = reinterpret_cast<const uint8_t *>(a.pool.k_scale) + g * 16 + 4 * (m & 3), *vs = reinterpret_cast<const uint8_t *>(a.pool.v_scale) + (m >> 2) * 16;
-    auto load_ids = [&](int (&id)[4], int b) {  // wavefront-uniform: scalar loads; clamped, so always in bounds
+// A wavefront's lane, item and pool: where its operands lie.
+struct Reader {
+    const DecodeLaunch &a;
+    const DecodeItem &it;
+    const uint8_t *k, *v, *k_scale, *v_scale;  // with the lane's offsets inside a block
+    int lane, m, g, last_page;
+    __device__ __forceinline__ Reader(const DecodeLaunch &a, const DecodeItem &it) : a(a), it(it) {
+        lane = (int)threadIdx.x & 63;
+        m = lane & 15;
+        g = lane >> 4;
+        last_page = (it.n_tokens - 1) >> 4;
+        k = static_cast<const uint8_t *>(a.pool.k_pages) + (m & 3) * 64 + g * 16;
+        v = static_cast<const uint8_t *>(a.pool.v_pages) + m * 16;
+        k_scale = reinterpret_cast<const uint8_t *>(a.pool.k_scale) + g * 16 + 4 * (m & 3);
+        v_scale = reinterpret_cast<const uint8_t *>(a.pool.v_scale) + (m >> 2) * 16;
+    }
+    // page ids of a step, wavefront-uniform (scalar loads); clamped, so always in bounds
+    __device__ __forceinline__ void ids(int (&id)[4], int b) const {
 #pragma unroll
         for (int i = 0; i < 4; ++i) id[i] = a.pages[it.page_off + min(4 * b + i, last_page)];
-    };
-    auto issue_k = [&](Operands &x, const int (&id)[4]) {
-        const size_t blk = (size_t)pick4(id, m >> 2) * Hkv + it.kv_head;
-        const uint8_t *p = kc + blk * four::kCodeBytes;
-        x.k_scale = *reinterpret_cast<const uint32_t *>(ks + blk * four::kScaleBytes);
+    }
+    __device__ __forceinline__ size_t block(const int (&id)[4], int sel) const { return (size_t)pick4(id, sel) * a.pool.num_kv_heads + it.kv_head; }
+    __device__ __forceinline__ void keys(Operands &x, const int (&id)[4]) const {
+        const size_t blk = block(id, m >> 2);
+        x.k_scale = *reinterpret_cast<const uint32_t *>(k_scale + blk * four::kScaleBytes);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x.k[j] = ld16(p + 256 * j);
-    };
-    auto issue_v = [&](Operands &x, const int (&id)[4]) {
-        const size_t blk = (size_t)pick4(id, g) * Hkv + it.kv_head;
-        const uint8_t *p = vc + blk * four::kCodeBytes;
-        x.v_scale = ld16(vs + blk * four::kScaleBytes);
+        for (int j = 0; j < 4; ++j) x.k[j] = ld16(k + blk * four::kCodeBytes + 256 * j);
+    }
+    __device__ __forceinline__ void values(Operands &x, const int (&id)[4]) const {
+        const size_t blk = block(id, g);
+        x.v_scale = ld16(v_scale + blk * four::kScaleBytes);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x.v[j] = ld16(p + 256 * j);
-    };
+        for (int j = 0; j < 4; ++j) x.v[j] = ld16(v + blk * four::kCodeBytes + 256 * j);
+    }
+};
 
-    RowTile tile[RT];
-    auto load_rows = [&]() {
-        u32x4 w[RT][4];
+template <int RT>
+__device__ __forceinline__ void load_rows(const Reader &rd, int row0, RowTile (&tile)[RT]) {
+    const DecodeLaunch &a = rd.a;
+    const DecodeItem &it = rd.it;
+    const int G = a.num_q_heads / a.pool.num_kv_heads, rows = it.n_req * G;
+    u32x4 w[RT][4];
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            const int row = row0 + 16 * r + m, rowc = min(row, rows - 1);
-            const int req = a.node_req_idx[it.req_off + rowc / G], head = it.kv_head * G + rowc % G;
-            const int q_row = a.q_rows ? a.q_rows[req] : req;
-            const char *qp = static_cast<const char *>(a.q) + ((size_t)q_row * a.num_q_heads + head) * (kHeadDim * 2) + 32 * g;
-            w[r][0] = ld16(qp);
-            w[r][1] = ld16(qp + 16);
-            w[r][2] = ld16(qp + 128);
-            w[r][3] = ld16(qp + 144);
-            tile[r].part = (uint32_t)((req * a.num_q_heads + head) * a.max_parts + it.part_slot);
-            tile[r].lim = it.n_tokens;
-            tile[r].vis = 0;
-            if (a.row_leaf && a.row_leaf[req] == it.node) {
-                tile[r].lim = a.row_limit[req] - it.tok_begin;
-                tile[r].vis = a.row_mask[req];
-            }
+    for (int r = 0; r < RT; ++r) {
+        const int row = min(row0 + 16 * r + rd.m, rows - 1);
+        const int req = a.node_req_idx[it.req_off + row / G], head = it.kv_head * G + row % G;
+        const int q_row = a.q_rows ? a.q_rows[req] : req;
+        const char *qp = static_cast<const char *>(a.q) + ((size_t)q_row * a.num_q_heads + head) * (kHeadDim * 2) + 32 * rd.g;
+        w[r][0] = ld16(qp);
+        w[r][1] = ld16(qp + 16);
+        w[r][2] = ld16(qp + 128);
+        w[r][3] = ld16(qp + 144);
+        tile[r].part = (uint32_t)((req * a.num_q_heads + head) * a.max_parts + it.part_slot);
+        tile[r].lim = it.n_tokens;
+        tile[r].vis = 0;
+        if (a.row_leaf && a.row_leaf[req] == it.node) {
+            tile[r].lim = a.row_limit[req] - it.tok_begin;
+            tile[r].vis = a.row_mask[req];
         }
+    }
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            split_row(tile[r], w[r], a.scale < 0.f ? -1.f : 1.f);
+    for (int r = 0; r < RT; ++r) {
+        split_row(tile[r], w[r], a.scale < 0.f ? -1.f : 1.f);
 #pragma unroll
-            for (int dt = 0; dt < 8; ++dt) tile[r].o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-            tile[r].m = -INFINITY;
-            tile[r].l = 0.f;
-        }
-    };
+        for (int dt = 0; dt < 8; ++dt) tile[r].o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        tile[r].m = -INFINITY;
+        tile[r].l = 0.f;
+    }
+}
 
-    // The first product, softmax and second product of a step; `between` comes where K's registers are free.
-    auto step = [&](Operands &x, int b, auto between) {
-        const int tok0 = b * kStep + 16 * g;  // of this lane's 16 tokens the first
-        f32x4 acc[RT][4];
+// S^T of a step.
+template <int RT>
+__device__ __forceinline__ void scores(const Operands &x, const RowTile (&tile)[RT], f32x4 (&acc)[RT][4]) {
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const RowTile &t = tile[r];
+#pragma unroll
+        for (int t4 = 0; t4 < 4; ++t4) acc[r][t4] = f32x4{0.f, 0.f, 0.f, 0.f};
+        acc[r][0] = mfma_four<0>(x.k[0], t.hi, acc[r][0], x.k_scale, t.q_scale);
+        acc[r][1] = mfma_four<1>(x.k[1], t.hi, acc[r][1], x.k_scale, t.q_scale);
+        acc[r][2] = mfma_four<2>(x.k[2], t.hi, acc[r][2], x.k_scale, t.q_scale);
+        acc[r][3] = mfma_four<3>(x.k[3], t.hi, acc[r][3], x.k_scale, t.q_scale);
+        acc[r][0] = mfma_four<0>(x.k[0], t.lo, acc[r][0], x.k_scale, t.q_scale);
+        acc[r][1] = mfma_four<1>(x.k[1], t.lo, acc[r][1], x.k_scale, t.q_scale);
+        acc[r][2] = mfma_four<2>(x.k[2], t.lo, acc[r][2], x.k_scale, t.q_scale);
+        acc[r][3] = mfma_four<3>(x.k[3], t.lo, acc[r][3], x.k_scale, t.q_scale);
+    }
+}
+
+// Probabilities of a step whose scores are acc; tok0: of the lane's 16 tokens the first.  A row's reference stays until a score exceeds it by more
+// than 2^kSlack in weight: with a maximum that follows every step some row of 32 moves nearly always, 66 instructions of a step's 450.
+constexpr float kSlack = 8.f;
+template <int RT>
+__device__ __forceinline__ void weights(RowTile (&tile)[RT], const f32x4 (&acc)[RT][4], int tok0, float c, u32x4 (&pw)[RT][2]) {
+    float s[RT][16];
+    int most = -INT_MAX;  // tokens of the step behind what a row sees at once
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        most = max(most, tok0 - tile[r].lim);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) s[r][j] = acc[r][j & 3][j >> 2];
+    }
+    if (__builtin_amdgcn_ballot_w64(most > -16)) {  // some row does not see the whole step, the item's last one among them
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            const RowTile &t = tile[r];
+            const unsigned long long vis = tile[r].vis;
+            const int d0 = tok0 - tile[r].lim;
+            const uint32_t seen = d0 < 0 ? (d0 <= -16 ? 0xFFFFu : (1u << -d0) - 1u | (uint32_t)vis << -d0) : d0 < 64 ? (uint32_t)(vis >> d0) : 0u;
 #pragma unroll
-            for (int t4 = 0; t4 < 4; ++t4) acc[r][t4] = f32x4{0.f, 0.f, 0.f, 0.f};
-            acc[r][0] = mfma_four<0>(x.k[0], t.hi, acc[r][0], x.k_scale, t.q_scale);
-            acc[r][1] = mfma_four<1>(x.k[1], t.hi, acc[r][1], x.k_scale, t.q_scale);
-            acc[r][2] = mfma_four<2>(x.k[2], t.hi, acc[r][2], x.k_scale, t.q_scale);
-            acc[r][3] = mfma_four<3>(x.k[3], t.hi, acc[r][3], x.k_scale, t.q_scale);
-            acc[r][0] = mfma_four<0>(x.k[0], t.lo, acc[r][0], x.k_scale, t.q_scale);
-            acc[r][1] = mfma_four<1>(x.k[1], t.lo, acc[r][1], x.k_scale, t.q_scale);
-            acc[r][2] = mfma_four<2>(x.k[2], t.lo, acc[r][2], x.k_scale, t.q_scale);
-            acc[r][3] = mfma_four<3>(x.k[3], t.lo, acc[r][3], x.k_scale, t.q_scale);
+            for (int j = 0; j < 16; ++j) s[r][j] = (seen >> j & 1u) ? s[r][j] : -INFINITY;
         }
-        between();
-        u32x4 pw[RT][2];
+    }
+    float top[RT];
+    bool beyond = false;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        top[r] = s[r][0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j) top[r] = fmaxf(top[r], s[r][j]);
+        beyond = beyond || (top[r] - tile[r].m) * c > kSlack;  // (-inf - -inf: no)
+    }
+    if (__builtin_amdgcn_ballot_w64(beyond)) {
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             RowTile &t = tile[r];
-            float s[16];
-#pragma unroll
-            for (int j = 0; j < 16; ++j) s[j] = acc[r][j & 3][j >> 2];
-            const int d0 = tok0 - t.lim;
-            if (__builtin_amdgcn_ballot_w64(d0 > -16)) {  // some row does not see the whole step, the item's last one among them
-                const uint32_t seen = d0 < 0 ? (d0 <= -16 ? 0xFFFFu : (1u << -d0) - 1u | (uint32_t)t.vis << -d0) : d0 < 64 ? (uint32_t)(t.vis >> d0) : 0u;
-#pragma unroll
-                for (int j = 0; j < 16; ++j) s[j] = (seen >> j & 1u) ? s[j] : -INFINITY;
-            }
-            float mx = s[0];
-#pragma unroll
-            for (int j = 1; j < 16; ++j) mx = fmaxf(mx, s[j]);
-            const float m_new = fmaxf(t.m, rows_max(mx));
-            const float mc = m_new == -INFINITY ? 0.f : m_new * c;  // (a row that has seen nothing: no inf - inf)
-            const float alpha = fast_exp2(__builtin_fmaf(t.m, c, -mc));
-            float sum = 0.f;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) {
-                s[j] = fast_exp2(__builtin_fmaf(s[j], c, -mc));
-                sum += s[j];
-            }
-            t.l = t.l * alpha + sum;
+            const float m_new = fmaxf(t.m, rows_max(top[r]));
+            const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((t.m - m_new) * c);
             t.m = m_new;
-            if (__builtin_amdgcn_ballot_w64(alpha != 1.0f)) {
+            t.l *= alpha;
 #pragma unroll
-                for (int dt = 0; dt < 8; ++dt) t.o[dt] *= alpha;
+            for (int dt = 0; dt < 8; ++dt) t.o[dt] *= alpha;
+        }
+    }
+    // probabilities are rounded to bf16, half a step of 2^-8 each, as over the other pools
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        const float mc = tile[r].m == -INFINITY ? 0.f : tile[r].m * c;  // (a row that has seen nothing: no inf - inf)
+        float sum = 0.f;
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            s[r][j] = fast_exp2(__builtin_fmaf(s[r][j], c, -mc));
+            sum += s[r][j];
+        }
+        tile[r].l += sum;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) pw[r][j >> 2][j & 3] = pack_bf16(s[r][2 * j], s[r][2 * j + 1]);
+    }
+}
+
+// Two dims (8 m + 2 B, + 1) of tokens 0 .. 3 from their words and scales: lo, hi [tokens 0 1 | 2 3].
+template <int B>
+__device__ __forceinline__ void widen_pairs(const uint32_t (&w)[4], const float (&sc)[4], u32x2 &lo, u32x2 &hi) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+        const uint32_t v0 = four::widen2<B>(w[2 * j], sc[2 * j]), v1 = four::widen2<B>(w[2 * j + 1], sc[2 * j + 1]);
+        lo[j] = __builtin_amdgcn_perm(v1, v0, 0x05040100u);
+        hi[j] = __builtin_amdgcn_perm(v1, v0, 0x07060302u);
+    }
+}
+
+// Slots of four tokens from first_bad (of them) on may hold anything: no codes, a scale of 1.
+__device__ __forceinline__ void clear_from(u32x4 &w, uint32_t &scale, int first_bad) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (j >= first_bad) {
+            w[j] = 0u;
+            scale = (scale & ~(0xFFu << (8 * j))) | (127u << (8 * j));
+        }
+}
+
+// O^T += V^T P^T of a step, V from the lane's own registers.
+template <int RT>
+__device__ __forceinline__ void add_values(RowTile (&tile)[RT], const Operands &x, const u32x4 (&pw)[RT][2]) {
+#pragma unroll
+    for (int half = 0; half < 2; ++half) {  // eight tokens of every block
+        float sc[2][4];
+        uint32_t w[2][4];
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                sc[q][j] = four::scale_of(x.v_scale[2 * half + q], j);
+                w[q][j] = x.v[2 * half + q][j];
             }
-            // probabilities are rounded to bf16, half a step of 2^-8 each, as over the other pools
+        auto dims = [&](auto byte) {
+            constexpr int B = decltype(byte)::value;
+            u32x2 lo[2], hi[2];
+            widen_pairs<B>(w[0], sc[0], lo[0], hi[0]);
+            widen_pairs<B>(w[1], sc[1], lo[1], hi[1]);
+            const bf16x8 va = as_bf16x8(u32x4{lo[0][0], lo[0][1], lo[1][0], lo[1][1]}), vb = as_bf16x8(u32x4{hi[0][0], hi[0][1], hi[1][0], hi[1][1]});
 #pragma unroll
-            for (int j = 0; j < 8; ++j) pw[r][j >> 2][j & 3] = pack_bf16(s[2 * j], s[2 * j + 1]);
+            for (int r = 0; r < RT; ++r) {
+                tile[r].o[2 * B] = mfma16(va, as_bf16x8(pw[r][half]), tile[r].o[2 * B]);
+                tile[r].o[2 * B + 1] = mfma16(vb, as_bf16x8(pw[r][half]), tile[r].o[2 * B + 1]);
+            }
+        };
+        dims(std::integral_constant<int, 0>{});
+        dims(std::integral_constant<int, 1>{});
+        dims(std::integral_constant<int, 2>{});
+        dims(std::integral_constant<int, 3>{});
+    }
+}
+
+// Rows whose tokens a wavefront has seen all go out from its registers, 32 dims a lane.
+template <int RT>
+__device__ __forceinline__ void write_rows(const Reader &rd, int row0, float c, RowTile (&tile)[RT]) {
+    const int rows = rd.it.n_req * (rd.a.num_q_heads / rd.a.pool.num_kv_heads);
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        RowTile &t = tile[r];
+        const float l_row = rows_sum(t.l), inv = l_row > 0.f ? 1.0f / l_row : 0.f;
+        float top = 0.f;
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) {
+            t.o[dt] *= inv;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) top = fmaxf(top, fabsf(t.o[dt][i]));
         }
-        if ((b + 1) * kStep > it.n_tokens) {  // slots behind the end may hold anything
-            const int first_bad = it.n_tokens - tok0;
+        top = rows_max(top);
+        float up, down;
+        part_factors(top, up, down);
+        if (row0 + 16 * r + rd.m >= rows) continue;
+        uint16_t *out = rd.a.o_parts + (size_t)t.part * kHeadDim + 32 * rd.g;
 #pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (j >= first_bad) {
-                    x.v[j >> 2][j & 3] = 0u;
-                    x.v_scale[j >> 2] = (x.v_scale[j >> 2] & ~(0xFFu << (8 * (j & 3)))) | (127u << (8 * (j & 3)));
-                }
+        for (int i = 0; i < 4; ++i) {
+            u32x4 w;
+#pragma unroll
+            for (int q = 0; q < 4; ++q) w[q] = pack_f16(t.o[2 * q][i] * up, t.o[2 * q + 1][i] * up);
+            *reinterpret_cast<u32x4 *>(out + 8 * i) = w;
         }
-#pragma unroll
-        for (int half = 0; half < 2; ++half) {  // eight tokens of every block
-            float sc[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) sc[j] = four::scale_of(x.v_scale[2 * half + (j >> 2)], j & 3);
-            auto dims = [&](auto byte) {  // dims 8 m + 2 B, + 1
-                constexpr int B = decltype(byte)::value;
-                u32x4 lo, hi;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t v0 = four::widen2<B>(x.v[2 * half + (j >> 1)][2 * (j & 1)], sc[2 * j]);
-                    const uint32_t v1 = four::widen2<B>(x.v[2 * half + (j >> 1)][2 * (j & 1) + 1], sc[2 * j + 1]);
-                    lo[j] = __builtin_amdgcn_perm(v1, v0, 0x05040100u);
-                    hi[j] = __builtin_amdgcn_perm(v1, v0, 0x07060302u);
-                }
-#pragma unroll
-                for (int r = 0; r < RT; ++r) {
-                    tile[r].o[2 * B] = mfma16(as_bf16x8(lo), as_bf16x8(pw[r][half]), tile[r].o[2 * B]);
-                    tile[r].o[2 * B + 1] = mfma16(as_bf16x8(hi), as_bf16x8(pw[r][half]), tile[r].o[2 * B + 1]);
-                }
-            };
-            dims(std::integral_constant<int, 0>{});
-            dims(std::integral_constant<int, 1>{});
-            dims(std::integral_constant<int, 2>{});
-            dims(std::integral_constant<int, 3>{});
+        if (rd.g == 0) {
+            rd.a.down_parts[t.part] = down;
+            rd.a.lse_parts[t.part] = partial_lse(l_row == l_row ? t.m * c : INFINITY, l_row);
         }
+    }
+}
+
+__device__ __forceinline__ float exponent_factor(float scale) { return fmaxf(fabsf(scale) * kLog2e, 1e-30f); }  // (scores times 0: a weight of 1 each, and -inf stays)
+
+// What a wavefront does with a share of an item's steps, ts, ts + n_ts, ..: the operands of one step travel while another is computed, page ids a step
+// further ahead (behind the last step once more, clamped to its last page: a condition would keep two sets of registers apart).
+template <int RT>
+__device__ __forceinline__ void stream(const Reader &rd, int row0, int ts, int n_ts, float c, RowTile (&tile)[RT]) {
+    const int n_blk = (rd.it.n_tokens + kStep - 1) / kStep;
+    int id[4], b = ts;
+    rd.ids(id, b);
+    Operands x;
+    rd.keys(x, id);
+    rd.values(x, id);
+    rd.ids(id, b + n_ts);
+    load_rows(rd, row0, tile);
+    auto second_half = [&](Operands &v, const u32x4 (&pw)[RT][2]) {
+        if ((b + 1) * kStep > rd.it.n_tokens) {
+            const int first_bad = rd.it.n_tokens - (b * kStep + 16 * rd.g);
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                uint32_t sc = v.v_scale[q];
+                clear_from(v.v[q], sc, first_bad - 4 * q);
+                v.v_scale[q] = sc;
+            }
+        }
+        add_values(tile, v, pw);
     };
-
-    const bool active = row0 < rows && ts < n_blk;
-    if (active) {
-        int id[4];
-        int b = ts;
-        load_ids(id, b);
-        Operands x;
-        issue_k(x, id);
-        issue_v(x, id);
-        load_ids(id, b + n_ts);
-        load_rows();
-        if constexpr (RT == 1) {  // the operands of one step travel while another is computed, page ids a step further ahead
-            Operands y;
-            auto ahead = [&](Operands &next) {
-                issue_k(next, id);
-                issue_v(next, id);
-                load_ids(id, b + 2 * n_ts);
-                __builtin_amdgcn_sched_barrier(0);
-            };
-            for (;;) {
-                if (b + n_ts < n_blk) ahead(y);
-                step(x, b, [] {});
-                if ((b += n_ts) >= n_blk) break;
-                if (b + n_ts < n_blk) ahead(x);
-                step(y, b, [] {});
-                if ((b += n_ts) >= n_blk) break;
-            }
-        } else {  // two tiles fill the registers: K of the next step is requested behind the first product, V behind the second
-            for (; b < n_blk; b += n_ts) {
-                const bool more = b + n_ts < n_blk;
-                step(x, b, [&] {
-                    __builtin_amdgcn_sched_barrier(0);
-                    if (more) issue_k(x, id);
-                    __builtin_amdgcn_sched_barrier(0);
-                });
-                __builtin_amdgcn_sched_barrier(0);
-                if (more) issue_v(x, id);
-                load_ids(id, b + 2 * n_ts);
-                __builtin_amdgcn_sched_barrier(0);
-            }
+    f32x4 acc[RT][4];
+    u32x4 pw[RT][2];
+    if constexpr (RT == 1) {
+        Operands y;
+        auto step = [&](Operands &now, Operands &next) {
+            rd.keys(next, id);
+            rd.values(next, id);
+            rd.ids(id, b + 2 * n_ts);
+            __builtin_amdgcn_sched_barrier(0);
+            scores(now, tile, acc);
+            weights(tile, acc, b * kStep + 16 * rd.g, c, pw);
+            second_half(now, pw);
+            return (b += n_ts) < n_blk;
+        };
+        while (step(x, y) && step(y, x)) {
+        }
+    } else {  // two tiles fill the registers: K of the next step is requested behind the first product, V behind the second
+        for (; b < n_blk; b += n_ts) {
+            scores(x, tile, acc);
+            __builtin_amdgcn_sched_barrier(0);
+            rd.keys(x, id);
+            __builtin_amdgcn_sched_barrier(0);
+            weights(tile, acc, b * kStep + 16 * rd.g, c, pw);
+            second_half(x, pw);
+            __builtin_amdgcn_sched_barrier(0);
+            rd.values(x, id);
+            rd.ids(id, b + 2 * n_ts);
+            __builtin_amdgcn_sched_barrier(0);
         }
     }
+}
 
-    if (n_ts == 1) {  // a wavefront has seen all tokens of its rows: they go out from its registers, 32 dims a lane
-        if (!active) return;
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            RowTile &t = tile[r];
-            const float l_row = rows_sum(t.l), inv = l_row > 0.f ? 1.0f / l_row : 0.f;
-            float top = 0.f;
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt) {
-                t.o[dt] *= inv;
-#pragma unroll
-                for (int i = 0; i < 4; ++i) top = fmaxf(top, fabsf(t.o[dt][i]));
-            }
-            top = rows_max(top);
-            float up, down;
-            part_factors(top, up, down);
-            if (row0 + 16 * r + m >= rows) continue;
-            uint16_t *out = a.o_parts + (size_t)t.part * kHeadDim + 32 * g;
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                u32x4 w;
-#pragma unroll
-                for (int q = 0; q < 4; ++q) w[q] = pack_f16(t.o[2 * q][i] * up, t.o[2 * q + 1][i] * up);
-                *reinterpret_cast<u32x4 *>(out + 8 * i) = w;
-            }
-            if (g == 0) {
-                a.down_parts[t.part] = down;
-                a.lse_parts[t.part] = partial_lse(l_row == l_row ? t.m * c : INFINITY, l_row);
-            }
-        }
-        return;
-    }
-    // The shares of a row tile's tokens are brought together in LDS, a tile of every wavefront at a time; then thread (row = tid / 16, tid % 16)
-    // has eight dims of a row, whose 16 threads are a row of lanes.
-    const int col = lane & 15, out_row = (int)threadIdx.x >> 4;
+// LDS of a workgroup: partial results of wavefronts that share a row tile's tokens, or two steps' V in bf16 as the second product's operands.
+struct Shares {
+    float o[kWaves][16][kORow], m[kWaves][16], l[kWaves][16];
+    uint32_t part[kWaves][16];
+};
+struct Widened {
+    u32x4 v[2][2][8][64];  // [step % 2][half][dt][lane]
+};
+union Lds {
+    Shares s;
+    Widened w;
+};
+
+// Items of up to 16 RT rows: the four wavefronts share the tokens, and bring their results together in LDS, a row tile at a time; then thread
+// (row = tid / 16, tid % 16) has eight dims of a row, whose 16 threads are a row of lanes.
+template <int RT>
+__device__ __forceinline__ void run_shared_tokens(const DecodeLaunch &a, const DecodeItem &it, Shares &s) {
+    const Reader rd(a, it);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), rows = it.n_req * (a.num_q_heads / a.pool.num_kv_heads);
+    const float c = exponent_factor(a.scale);
+    const bool active = wave * kStep < it.n_tokens;
+    RowTile tile[RT];
+    if (active) stream(rd, 0, wave, kWaves, c, tile);
+    const int col = rd.lane & 15, out_row = (int)threadIdx.x >> 4;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         if (r > 0) __syncthreads();
@@ -332,70 +420,161 @@ __device__ __forceinline__ void run_item(const DecodeLaunch &a, const DecodeItem
             for (int i = 0; i < 4; ++i)
 #pragma unroll
                 for (int q = 0; q < 2; ++q)
-                    *reinterpret_cast<f32x4 *>(&sO[wave][m][32 * g + 8 * i + 4 * q]) = f32x4{t.o[4 * q][i], t.o[4 * q + 1][i], t.o[4 * q + 2][i], t.o[4 * q + 3][i]};
-            if (g == 0) {
-                sM[wave][m] = l_row == l_row ? t.m : INFINITY;  // (a NaN or +inf among the scores: the row's sum is no number below)
-                sL[wave][m] = l_row;
-                if (ts == 0) sPart[wave][m] = t.part;
+                    *reinterpret_cast<f32x4 *>(&s.o[wave][rd.m][32 * rd.g + 8 * i + 4 * q]) = f32x4{t.o[4 * q][i], t.o[4 * q + 1][i], t.o[4 * q + 2][i], t.o[4 * q + 3][i]};
+            if (rd.g == 0) {
+                s.m[wave][rd.m] = l_row == l_row ? t.m : INFINITY;  // (a NaN or +inf among the scores: the row's sum is no number below)
+                s.l[wave][rd.m] = l_row;
+                if (wave == 0) s.part[0][rd.m] = t.part;
             }
-        } else if (g == 0) {
-            sM[wave][m] = -INFINITY;
+        } else if (rd.g == 0) {
+            s.m[wave][rd.m] = -INFINITY;
         }
         __syncthreads();
-        for (int rg = 0; rg < n_rg; ++rg) {
-            const int row = rg * (16 * RT) + 16 * r + out_row;
-            if (rg * (16 * RT) + 16 * r >= rows) break;  // (the same for all threads)
-            float M = -INFINITY, L = 0.f;
-            for (int w = rg; w < kWaves; w += n_rg) M = fmaxf(M, sM[w][out_row]);
-            f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
-            for (int w = rg; w < kWaves; w += n_rg) {
-                const float mw = sM[w][out_row];
-                if (mw == -INFINITY) continue;  // that wavefront's tokens were all invisible to the row
-                const float wgt = fast_exp2((mw - M) * c);
-                L += sL[w][out_row] * wgt;
-                x += *reinterpret_cast<const f32x4 *>(&sO[w][out_row][8 * col]) * wgt;
-                y += *reinterpret_cast<const f32x4 *>(&sO[w][out_row][8 * col + 4]) * wgt;
-            }
-            const float inv = L > 0.f ? 1.0f / L : 0.f;
-            x *= inv;
-            y *= inv;
-            float top = 0.f;
+        if (16 * r >= rows) break;  // (the same for all threads)
+        float M = -INFINITY, L = 0.f;
 #pragma unroll
-            for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(x[j]), fabsf(y[j])));
-            top = fmaxf(top, dpp<kQuadXor1>(top));
-            top = fmaxf(top, dpp<kQuadXor2>(top));
-            top = fmaxf(top, dpp<kRor4>(top));
-            top = fmaxf(top, dpp<kRor8>(top));
-            float up, down;
-            part_factors(top, up, down);
-            if (row >= rows) continue;
-            const size_t part = sPart[rg][out_row];
-            *reinterpret_cast<u32x4 *>(a.o_parts + part * kHeadDim + 8 * col) =
-                u32x4{pack_f16(x[0] * up, x[1] * up), pack_f16(x[2] * up, x[3] * up), pack_f16(y[0] * up, y[1] * up), pack_f16(y[2] * up, y[3] * up)};
-            if (col == 0) {
-                a.down_parts[part] = down;
-                a.lse_parts[part] = partial_lse(M * c, L);
-            }
+        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s.m[w][out_row]);
+        f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
+#pragma unroll
+        for (int w = 0; w < kWaves; ++w) {
+            const float mw = s.m[w][out_row];
+            if (mw == -INFINITY) continue;  // that wavefront's tokens were all invisible to the row
+            const float wgt = fast_exp2((mw - M) * c);
+            L += s.l[w][out_row] * wgt;
+            x += *reinterpret_cast<const f32x4 *>(&s.o[w][out_row][8 * col]) * wgt;
+            y += *reinterpret_cast<const f32x4 *>(&s.o[w][out_row][8 * col + 4]) * wgt;
+        }
+        const float inv = L > 0.f ? 1.0f / L : 0.f;
+        x *= inv;
+        y *= inv;
+        float top = 0.f;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(x[j]), fabsf(y[j])));
+        top = fmaxf(top, dpp<kQuadXor1>(top));
+        top = fmaxf(top, dpp<kQuadXor2>(top));
+        top = fmaxf(top, dpp<kRor4>(top));
+        top = fmaxf(top, dpp<kRor8>(top));
+        float up, down;
+        part_factors(top, up, down);
+        if (16 * r + out_row >= rows) continue;
+        const size_t part = s.part[0][out_row];
+        *reinterpret_cast<u32x4 *>(a.o_parts + part * kHeadDim + 8 * col) =
+            u32x4{pack_f16(x[0] * up, x[1] * up), pack_f16(x[2] * up, x[3] * up), pack_f16(y[0] * up, y[1] * up), pack_f16(y[2] * up, y[3] * up)};
+        if (col == 0) {
+            a.down_parts[part] = down;
+            a.lse_parts[part] = partial_lse(M * c, L);
         }
     }
 }
 
+// Items of more rows: RT row tiles a wavefront, which sees all tokens, and V is widened once for all four: wavefront w takes tokens 4 w .. 4 w + 3 of every
+// block of the next step, 40 vector instructions instead of 152, and writes them where the second product's operands are read, 16 bytes a lane.  One
+// barrier a step: it waits for LDS, not for what is on its way from memory.
+template <int RT>
+__device__ __forceinline__ void run_shared_values(const DecodeLaunch &a, const DecodeItem &it, Widened &lds) {
+    const Reader rd(a, it);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), rows = it.n_req * (a.num_q_heads / a.pool.num_kv_heads);
+    const int row0 = wave * (16 * RT), n_blk = (it.n_tokens + kStep - 1) / kStep;
+    const float c = exponent_factor(a.scale);
+    const bool active = row0 < rows;
+    const int half = wave >> 1;
+    u32x4 v;
+    uint32_t v_scale;
+    auto load_v = [&](const int (&id)[4]) {
+        const size_t blk = rd.block(id, rd.g);
+        v_scale = *reinterpret_cast<const uint32_t *>(rd.v_scale + blk * four::kScaleBytes + 4 * wave);
+        v = ld16(rd.v + blk * four::kCodeBytes + 256 * wave);
+    };
+    auto widen = [&](int b) {  // v of step b
+        if ((b + 1) * kStep > it.n_tokens) clear_from(v, v_scale, it.n_tokens - (b * kStep + 16 * rd.g + 4 * wave));
+        const uint32_t w[4] = {v[0], v[1], v[2], v[3]};
+        const float sc[4] = {four::scale_of(v_scale, 0), four::scale_of(v_scale, 1), four::scale_of(v_scale, 2), four::scale_of(v_scale, 3)};
+        char *to = reinterpret_cast<char *>(&lds.v[b & 1][half][0][rd.lane]) + 8 * (wave & 1);
+        auto dims = [&](auto byte) {
+            constexpr int B = decltype(byte)::value;
+            u32x2 lo, hi;
+            widen_pairs<B>(w, sc, lo, hi);
+            *reinterpret_cast<u32x2 *>(to + (2 * B) * 1024) = lo;
+            *reinterpret_cast<u32x2 *>(to + (2 * B + 1) * 1024) = hi;
+        };
+        dims(std::integral_constant<int, 0>{});
+        dims(std::integral_constant<int, 1>{});
+        dims(std::integral_constant<int, 2>{});
+        dims(std::integral_constant<int, 3>{});
+    };
+    auto barrier = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    int id[4];
+    rd.ids(id, 0);
+    load_v(id);
+    Operands x;
+    rd.keys(x, id);
+    rd.ids(id, 1);
+    RowTile tile[RT];
+    load_rows(rd, row0, tile);
+    widen(0);
+    load_v(id);
+    barrier();
+    f32x4 acc[RT][4];
+    u32x4 pw[RT][2];
+    for (int b = 0; b < n_blk; ++b) {
+        if (active) {
+            scores(x, tile, acc);
+            __builtin_amdgcn_sched_barrier(0);
+            rd.keys(x, id);
+            __builtin_amdgcn_sched_barrier(0);
+            weights(tile, acc, b * kStep + 16 * rd.g, c, pw);
+        }
+        rd.ids(id, b + 2);
+        widen(b + 1);  // (behind the last step: of no use, and of no harm)
+        load_v(id);
+        if (active) {
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf)
+#pragma unroll
+                for (int dt = 0; dt < 8; ++dt) {
+                    const bf16x8 va = as_bf16x8(lds.v[b & 1][hf][dt][rd.lane]);
+#pragma unroll
+                    for (int r = 0; r < RT; ++r) tile[r].o[dt] = mfma16(va, as_bf16x8(pw[r][hf]), tile[r].o[dt]);
+                }
+        }
+        barrier();
+    }
+    if (active) write_rows(rd, row0, c, tile);
+}
+
+// Items [0, n_single) get a workgroup each, the items behind them (at most 16 rows) one for four, a wavefront each (no LDS, no barrier).  The two
+// kinds of workgroups are spread evenly over the grid: those of many rows are bound by their instructions, the others by memory.
 __global__ __launch_bounds__(kWaves * 64, 2) void four_decode_kernel(DecodeLaunch a) {
-    __shared__ float sO[kWaves][16][kORow];
-    __shared__ float sM[kWaves][16], sL[kWaves][16];
-    __shared__ uint32_t sPart[kWaves][16];
-    const DecodeItem it = a.items[blockIdx.x];
-    if (it.n_req * (a.num_q_heads / a.pool.num_kv_heads) <= 16)
-        run_item<1>(a, it, sO, sM, sL, sPart);
+    __shared__ Lds lds;
+    const int G = a.num_q_heads / a.pool.num_kv_heads, i = (int)blockIdx.x, single = (int)((uint64_t)i * a.n_single / gridDim.x);
+    if ((int)(((uint64_t)i + 1) * a.n_single / gridDim.x) == single) {
+        const int at = a.n_single + kWaves * (i - single) + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        if (at >= a.n_items) return;
+        const DecodeItem it = a.items[at];
+        const Reader rd(a, it);
+        const float c = exponent_factor(a.scale);
+        RowTile tile[1];
+        stream(rd, 0, 0, 1, c, tile);
+        write_rows(rd, 0, c, tile);
+        return;
+    }
+    const DecodeItem it = a.items[single];
+    const int rows = it.n_req * G;
+    if (rows <= 16)
+        run_shared_tokens<1>(a, it, lds.s);
+    else if (rows <= 32)
+        run_shared_tokens<2>(a, it, lds.s);
+    else if (rows <= 64)
+        run_shared_values<1>(a, it, lds.w);
     else
-        run_item<2>(a, it, sO, sM, sL, sPart);
+        run_shared_values<2>(a, it, lds.w);
 }
 
 }  // namespace
 
 hipError_t launch_four_decode(const DecodeLaunch &a, hipStream_t s, hipEvent_t ev_begin, hipEvent_t ev_end) {
     if (a.n_items <= 0) return hipSuccess;
-    hipExtLaunchKernelGGL(four_decode_kernel, dim3(a.n_items), dim3(kWaves * 64), 0, s, ev_begin, ev_end, 0, a);
+    hipExtLaunchKernelGGL(four_decode_kernel, dim3(a.n_single + (a.n_items - a.n_single + kWaves - 1) / kWaves), dim3(kWaves * 64), 0, s, ev_begin, ev_end, 0, a);
     return hipGetLastError();
 }
 

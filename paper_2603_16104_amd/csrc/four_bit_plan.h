@@ -39,10 +39,29 @@ static void plan_four_bit(hkv_decode_plan &pl, int n_cu) {
                                       (int64_t)nt * std::max(16, (nr * G + 15) / 16 * 16)});
             }
     }
-    std::stable_sort(protos.begin(), protos.end(), [](const Proto &a, const Proto &b) { return a.cost > b.cost; });  // heavy ones first
+    // Heavy items first.  Many items of few rows: a wavefront each instead of a workgroup each.
+    int64_t few = 0;
+    for (const Proto &x : protos) few += x.it.n_req * G <= 16;
+    const bool pack = pl.opt.pack == 3 || (pl.opt.pack != 1 && few > 8 * n_cu);
+    auto packed = [&](const Proto &x) { return pack && x.it.n_req * G <= 16; };
+    std::stable_sort(protos.begin(), protos.end(), [&](const Proto &a, const Proto &b) { return packed(a) != packed(b) ? packed(b) : a.cost > b.cost; });
+    if (pl.opt.interleave >= 0) {  // items of many and of few rows with a workgroup each, side by side
+        std::vector<Proto> many, others, rest;
+        for (const Proto &x : protos) (packed(x) ? rest : x.it.n_req * G > 16 ? many : others).push_back(x);
+        protos.clear();
+        for (size_t a = 0, b = 0; a < many.size() || b < others.size();)
+            if (b >= others.size() || (a < many.size() && (a + 1) * others.size() <= (b + 1) * many.size()))
+                protos.push_back(many[a++]);
+            else
+                protos.push_back(others[b++]);
+        protos.insert(protos.end(), rest.begin(), rest.end());
+    }
     pl.items.clear();
-    for (const Proto &p : protos) pl.items.push_back(p.it);
-    pl.n_single = (int32_t)pl.items.size();
+    pl.n_single = 0;
+    for (const Proto &x : protos) {
+        pl.items.push_back(x.it);
+        pl.n_single += !packed(x);
+    }
     pl.concurrent = false;
     pl.part_count.assign(pl.n_req, 0);
     pl.max_parts = 1;
