@@ -95,6 +95,7 @@ static hipError_t setup_device(DeviceSetup &st) {
     for (const void *fn : fused)
         if (hipError_t e = hipFuncSetAttribute(fn, hipFuncAttributeMaxDynamicSharedMemorySize, kFusedLds); e != hipSuccess)
             return e;
+    if (hipError_t e = prepare_four_decode(); e != hipSuccess) return e;
     return hipGetSymbolAddress(&st.static_ws, HIP_SYMBOL(scratch));
 }
 

@@ -180,19 +180,12 @@ __device__ __forceinline__ void scores(const Operands &x, const RowTile (&tile)[
     }
 }
 
-// Probabilities of a step whose scores are acc; tok0: of the lane's 16 tokens the first.  A row's reference stays until a score exceeds it by more
-// than 2^kSlack in weight: with a maximum that follows every step some row of 32 moves nearly always, 66 instructions of a step's 450.
-constexpr float kSlack = 8.f;
+// Scores of tokens that a row does not see are -inf; tok0: of the lane's 16 tokens the first, score j of a row is acc[j % 4][j / 4].
 template <int RT>
-__device__ __forceinline__ void weights(RowTile (&tile)[RT], const f32x4 (&acc)[RT][4], int tok0, float c, u32x4 (&pw)[RT][2]) {
-    float s[RT][16];
+__device__ __forceinline__ void hide(const RowTile (&tile)[RT], f32x4 (&acc)[RT][4], int tok0) {
     int most = -INT_MAX;  // tokens of the step behind what a row sees at once
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        most = max(most, tok0 - tile[r].lim);
-#pragma unroll
-        for (int j = 0; j < 16; ++j) s[r][j] = acc[r][j & 3][j >> 2];
-    }
+    for (int r = 0; r < RT; ++r) most = max(most, tok0 - tile[r].lim);
     if (__builtin_amdgcn_ballot_w64(most > -16)) {  // some row does not see the whole step, the item's last one among them
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
@@ -200,18 +193,28 @@ __device__ __forceinline__ void weights(RowTile (&tile)[RT], const f32x4 (&acc)[
             const int d0 = tok0 - tile[r].lim;
             const uint32_t seen = d0 < 0 ? (d0 <= -16 ? 0xFFFFu : (1u << -d0) - 1u | (uint32_t)vis << -d0) : d0 < 64 ? (uint32_t)(vis >> d0) : 0u;
 #pragma unroll
-            for (int j = 0; j < 16; ++j) s[r][j] = (seen >> j & 1u) ? s[r][j] : -INFINITY;
+            for (int j = 0; j < 16; ++j) acc[r][j & 3][j >> 2] = (seen >> j & 1u) ? acc[r][j & 3][j >> 2] : -INFINITY;
         }
     }
-    float top[RT];
-    bool beyond = false;
+}
+// The largest of the lane's scores of each row.
+template <int RT>
+__device__ __forceinline__ void tops(const f32x4 (&acc)[RT][4], float (&top)[RT]) {
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        top[r] = s[r][0];
+        top[r] = acc[r][0][0];
 #pragma unroll
-        for (int j = 1; j < 16; ++j) top[r] = fmaxf(top[r], s[r][j]);
-        beyond = beyond || (top[r] - tile[r].m) * c > kSlack;  // (-inf - -inf: no)
+        for (int j = 1; j < 16; ++j) top[r] = fmaxf(top[r], acc[r][j & 3][j >> 2]);
     }
+}
+// A row's reference stays until a score exceeds it by more than 2^kSlack in weight: with a maximum that follows every step some row of 32 moves nearly
+// always, 66 instructions of a step's 450.
+constexpr float kSlack = 8.f;
+template <int RT>
+__device__ __forceinline__ void follow(RowTile (&tile)[RT], const float (&top)[RT], float c) {
+    bool beyond = false;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) beyond = beyond || (top[r] - tile[r].m) * c > kSlack;  // (-inf - -inf: no)
     if (__builtin_amdgcn_ballot_w64(beyond)) {
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
@@ -224,20 +227,31 @@ __device__ __forceinline__ void weights(RowTile (&tile)[RT], const f32x4 (&acc)[
             for (int dt = 0; dt < 8; ++dt) t.o[dt] *= alpha;
         }
     }
-    // probabilities are rounded to bf16, half a step of 2^-8 each, as over the other pools
+}
+// Probabilities, rounded to bf16, half a step of 2^-8 each, as over the other pools.
+template <int RT>
+__device__ __forceinline__ void weigh(RowTile (&tile)[RT], const f32x4 (&acc)[RT][4], float c, u32x4 (&pw)[RT][2]) {
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const float mc = tile[r].m == -INFINITY ? 0.f : tile[r].m * c;  // (a row that has seen nothing: no inf - inf)
-        float sum = 0.f;
+        float sum = 0.f, p[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
-            s[r][j] = fast_exp2(__builtin_fmaf(s[r][j], c, -mc));
-            sum += s[r][j];
+            p[j] = fast_exp2(__builtin_fmaf(acc[r][j & 3][j >> 2], c, -mc));
+            sum += p[j];
         }
         tile[r].l += sum;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) pw[r][j >> 2][j & 3] = pack_bf16(s[r][2 * j], s[r][2 * j + 1]);
+        for (int j = 0; j < 8; ++j) pw[r][j >> 2][j & 3] = pack_bf16(p[2 * j], p[2 * j + 1]);
     }
+}
+template <int RT>
+__device__ __forceinline__ void weights(RowTile (&tile)[RT], f32x4 (&acc)[RT][4], int tok0, float c, u32x4 (&pw)[RT][2]) {
+    float top[RT];
+    hide(tile, acc, tok0);
+    tops(acc, top);
+    follow(tile, top, c);
+    weigh(tile, acc, c, pw);
 }
 
 // Two dims (8 m + 2 B, + 1) of tokens 0 .. 3 from their words and scales: lo, hi [tokens 0 1 | 2 3].
@@ -330,8 +344,8 @@ __device__ __forceinline__ void write_rows(const Reader &rd, int row0, float c, 
 
 __device__ __forceinline__ float exponent_factor(float scale) { return fmaxf(fabsf(scale) * kLog2e, 1e-30f); }  // (scores times 0: a weight of 1 each, and -inf stays)
 
-// What a wavefront does with a share of an item's steps, ts, ts + n_ts, ..: the operands of one step travel while another is computed, page ids a step
-// further ahead (behind the last step once more, clamped to its last page: a condition would keep two sets of registers apart).
+// What a wavefront does with a share of an item's steps, ts, ts + n_ts, ..: the operands of two steps travel while another is computed, page ids a step
+// further ahead (behind the last steps once more, clamped to its last page: a condition would keep two sets of registers apart).
 template <int RT>
 __device__ __forceinline__ void stream(const Reader &rd, int row0, int ts, int n_ts, float c, RowTile (&tile)[RT]) {
     const int n_blk = (rd.it.n_tokens + kStep - 1) / kStep;
@@ -357,18 +371,21 @@ __device__ __forceinline__ void stream(const Reader &rd, int row0, int ts, int n
     f32x4 acc[RT][4];
     u32x4 pw[RT][2];
     if constexpr (RT == 1) {
-        Operands y;
-        auto step = [&](Operands &now, Operands &next) {
-            rd.keys(next, id);
-            rd.values(next, id);
-            rd.ids(id, b + 2 * n_ts);
+        Operands y, z;
+        rd.keys(y, id);
+        rd.values(y, id);
+        rd.ids(id, b + 2 * n_ts);
+        auto step = [&](Operands &now, Operands &after_next) {
+            rd.keys(after_next, id);
+            rd.values(after_next, id);
+            rd.ids(id, b + 3 * n_ts);
             __builtin_amdgcn_sched_barrier(0);
             scores(now, tile, acc);
             weights(tile, acc, b * kStep + 16 * rd.g, c, pw);
             second_half(now, pw);
             return (b += n_ts) < n_blk;
         };
-        while (step(x, y) && step(y, x)) {
+        while (step(x, z) && step(y, x) && step(z, y)) {
         }
     } else {  // two tiles fill the registers: K of the next step is requested behind the first product, V behind the second
         for (; b < n_blk; b += n_ts) {
@@ -391,7 +408,13 @@ struct Shares {
     float o[kWaves][16][kORow], m[kWaves][16], l[kWaves][16];
     uint32_t part[kWaves][16];
 };
+constexpr int kRing = 4;
+struct Stage {  // a step's codes and scales as the lanes take them
+    u32x4 k[4][64], v[4][64];
+    uint32_t k_scale[64], v_scale[4][64];
+};
 struct Widened {
+    Stage ring[kRing];
     u32x4 v[2][2][8][64];  // [step % 2][half][dt][lane]
 };
 union Lds {
@@ -467,9 +490,13 @@ __device__ __forceinline__ void run_shared_tokens(const DecodeLaunch &a, const D
     }
 }
 
-// Items of more rows: RT row tiles a wavefront, which sees all tokens, and V is widened once for all four: wavefront w takes tokens 4 w .. 4 w + 3 of every
-// block of the next step, 40 vector instructions instead of 152, and writes them where the second product's operands are read, 16 bytes a lane.  One
-// barrier a step: it waits for LDS, not for what is on its way from memory.
+// Items of more rows: RT row tiles a wavefront, which sees all tokens.  Codes and scales come through a ring in LDS, a quarter of a step by each
+// wavefront, three steps ahead: a workgroup's two steps in flight at most would be 4.4 MB on the chip, 2 TB/s.  V is widened once for all four:
+// wavefront w takes tokens 4 w .. 4 w + 3 of every block of the next step, 40 vector instructions instead of 152, and writes them where the
+// second product's operands are read, 16 bytes a lane.  One barrier a step: it waits for LDS, not for what is on its way from memory.
+__device__ __forceinline__ void load_to_lds4(const void *gptr, uint32_t lds_base) {
+    asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(gptr), "s"(lds_base) : "memory");
+}
 template <int RT>
 __device__ __forceinline__ void run_shared_values(const DecodeLaunch &a, const DecodeItem &it, Widened &lds) {
     const Reader rd(a, it);
@@ -478,74 +505,166 @@ __device__ __forceinline__ void run_shared_values(const DecodeLaunch &a, const D
     const float c = exponent_factor(a.scale);
     const bool active = row0 < rows;
     const int half = wave >> 1;
+    constexpr int kLoads = 4;  // of a wavefront and step
+    auto issue = [&](const int (&id)[4], int b) {
+        const size_t kblk = rd.block(id, rd.m >> 2), vblk = rd.block(id, rd.g);
+        const uint32_t to = lds_address(&lds.ring[b % kRing]);
+        load_to_lds16(rd.k + kblk * four::kCodeBytes + 256 * wave, to + (uint32_t)offsetof(Stage, k) + 1024 * wave);
+        load_to_lds16(rd.v + vblk * four::kCodeBytes + 256 * wave, to + (uint32_t)offsetof(Stage, v) + 1024 * wave);
+        load_to_lds4(rd.k_scale + kblk * four::kScaleBytes, to + (uint32_t)offsetof(Stage, k_scale));  // (the same by all four: as many loads for each)
+        load_to_lds4(rd.v_scale + vblk * four::kScaleBytes + 4 * wave, to + (uint32_t)offsetof(Stage, v_scale) + 256 * wave);
+    };
     u32x4 v;
     uint32_t v_scale;
-    auto load_v = [&](const int (&id)[4]) {
-        const size_t blk = rd.block(id, rd.g);
-        v_scale = *reinterpret_cast<const uint32_t *>(rd.v_scale + blk * four::kScaleBytes + 4 * wave);
-        v = ld16(rd.v + blk * four::kCodeBytes + 256 * wave);
-    };
-    auto widen = [&](int b) {  // v of step b
+    auto take = [&](int b) {  // this wavefront's share of step b
+        const Stage &st = lds.ring[b % kRing];
+        v = st.v[wave][rd.lane];
+        v_scale = st.v_scale[wave][rd.lane];
         if ((b + 1) * kStep > it.n_tokens) clear_from(v, v_scale, it.n_tokens - (b * kStep + 16 * rd.g + 4 * wave));
+    };
+    auto widen_dims = [&](auto byte, int b) {  // dims 8 m + 2 B, + 1 of it
+        constexpr int B = decltype(byte)::value;
         const uint32_t w[4] = {v[0], v[1], v[2], v[3]};
         const float sc[4] = {four::scale_of(v_scale, 0), four::scale_of(v_scale, 1), four::scale_of(v_scale, 2), four::scale_of(v_scale, 3)};
         char *to = reinterpret_cast<char *>(&lds.v[b & 1][half][0][rd.lane]) + 8 * (wave & 1);
-        auto dims = [&](auto byte) {
-            constexpr int B = decltype(byte)::value;
-            u32x2 lo, hi;
-            widen_pairs<B>(w, sc, lo, hi);
-            *reinterpret_cast<u32x2 *>(to + (2 * B) * 1024) = lo;
-            *reinterpret_cast<u32x2 *>(to + (2 * B + 1) * 1024) = hi;
-        };
-        dims(std::integral_constant<int, 0>{});
-        dims(std::integral_constant<int, 1>{});
-        dims(std::integral_constant<int, 2>{});
-        dims(std::integral_constant<int, 3>{});
+        u32x2 lo, hi;
+        widen_pairs<B>(w, sc, lo, hi);
+        *reinterpret_cast<u32x2 *>(to + (2 * B) * 1024) = lo;
+        *reinterpret_cast<u32x2 *>(to + (2 * B + 1) * 1024) = hi;
+    };
+    auto widen = [&](int b) {
+        widen_dims(std::integral_constant<int, 0>{}, b);
+        widen_dims(std::integral_constant<int, 1>{}, b);
+        widen_dims(std::integral_constant<int, 2>{}, b);
+        widen_dims(std::integral_constant<int, 3>{}, b);
     };
     auto barrier = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
+    auto landed = [] { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads * (kRing - 2)) : "memory"); };  // all but the last kRing - 2 steps requested
     int id[4];
-    rd.ids(id, 0);
-    load_v(id);
-    Operands x;
-    rd.keys(x, id);
-    rd.ids(id, 1);
+#pragma unroll
+    for (int b = 0; b < kRing; ++b) {
+        rd.ids(id, b);
+        issue(id, b);
+    }
+    rd.ids(id, kRing);
     RowTile tile[RT];
     load_rows(rd, row0, tile);
+    landed();
+    take(0);
     widen(0);
-    load_v(id);
     barrier();
-    f32x4 acc[RT][4];
-    u32x4 pw[RT][2];
-    for (int b = 0; b < n_blk; ++b) {
-        if (active) {
-            scores(x, tile, acc);
-            __builtin_amdgcn_sched_barrier(0);
-            rd.keys(x, id);
-            __builtin_amdgcn_sched_barrier(0);
-            weights(tile, acc, b * kStep + 16 * rd.g, c, pw);
-        }
-        rd.ids(id, b + 2);
-        widen(b + 1);  // (behind the last step: of no use, and of no harm)
-        load_v(id);
-        if (active) {
-#pragma unroll
-            for (int hf = 0; hf < 2; ++hf)
-#pragma unroll
-                for (int dt = 0; dt < 8; ++dt) {
-                    const bf16x8 va = as_bf16x8(lds.v[b & 1][hf][dt][rd.lane]);
-#pragma unroll
-                    for (int r = 0; r < RT; ++r) tile[r].o[dt] = mfma16(va, as_bf16x8(pw[r][hf]), tile[r].o[dt]);
-                }
-        }
+    if (!active) {
         barrier();
+        for (int b = 0; b < n_blk; ++b) {
+            issue(id, b + kRing);
+            rd.ids(id, b + kRing + 1);
+            take(b + 1);
+            widen(b + 1);
+            landed();
+            barrier();
+        }
+        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        return;
     }
-    if (active) write_rows(rd, row0, c, tile);
+    // Matrix instructions and those of the softmax do not overlap between wavefronts of a SIMD by themselves (the sum of both was the kernel's time), so
+    // each wavefront mixes its own: the first product of step b + 1 and the second of step b with the exponentials of step b and V's widening.
+    auto first_product = [&](f32x4 (&acc)[RT][4], int b) {
+        const Stage &st = lds.ring[b % kRing];
+        Operands x;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x.k[j] = st.k[j][rd.lane];
+        x.k_scale = st.k_scale[rd.lane];
+        scores(x, tile, acc);
+    };
+    f32x4 acc0[RT][4], acc1[RT][4];
+    u32x4 pw[RT][2];
+    float top[RT];
+    first_product(acc0, 0);
+    hide(tile, acc0, 16 * rd.g);
+    tops(acc0, top);
+    follow(tile, top, c);
+    barrier();  // all are done with K of step 0
+    auto step = [&](f32x4 (&now)[RT][4], f32x4 (&next)[RT][4], int b) {
+        issue(id, b + kRing);  // where step b was: its keys and values left in step b - 1
+        rd.ids(id, b + kRing + 1);
+        take(b + 1);  // (behind the last step: of no use, and of no harm)
+        // every chunk up to a sched_barrier: matrix instructions (32 cycles each of the first product, 16 of the second) and about as many cycles of others
+        const Stage &st = lds.ring[(b + 1) % kRing];
+        u32x4 k[4], va[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k[j] = st.k[j][rd.lane];
+        const uint32_t k_scale = st.k_scale[rd.lane];
+        float mc[RT], sum[RT];
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            mc[r] = tile[r].m == -INFINITY ? 0.f : tile[r].m * c;
+            sum[r] = 0.f;
+#pragma unroll
+            for (int t4 = 0; t4 < 4; ++t4) next[r][t4] = f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        auto weigh_pair = [&](int i) {  // probabilities of two neighbouring tokens of a row, those of the second product's first half first
+            const int hf = i / (4 * RT), r = i / 4 % RT, j = 8 * hf + 2 * (i % 4);
+            const float p0 = fast_exp2(__builtin_fmaf(now[r][j & 3][j >> 2], c, -mc[r])), p1 = fast_exp2(__builtin_fmaf(now[r][(j + 1) & 3][(j + 1) >> 2], c, -mc[r]));
+            sum[r] += p0 + p1;
+            pw[r][hf][i % 4] = pack_bf16(p0, p1);
+        };
+        constexpr int kFirst = 5 * RT;  // pairs beside the first product
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 8 * RT; ++i) {
+            const int lo = i / (4 * RT), r = i / 4 % RT, t4 = i % 4;
+            const i32x8 q = lo ? tile[r].lo : tile[r].hi;
+            f32x4 &to = next[r][t4];
+            to = t4 == 0 ? mfma_four<0>(k[0], q, to, k_scale, tile[r].q_scale) : t4 == 1 ? mfma_four<1>(k[1], q, to, k_scale, tile[r].q_scale)
+               : t4 == 2 ? mfma_four<2>(k[2], q, to, k_scale, tile[r].q_scale) : mfma_four<3>(k[3], q, to, k_scale, tile[r].q_scale);
+#pragma unroll
+            for (int p = kFirst * i / (8 * RT); p < kFirst * (i + 1) / (8 * RT); ++p) weigh_pair(p);
+            if (i >= 8 * RT - 4) va[i - (8 * RT - 4)] = lds.v[b & 1][0][i - (8 * RT - 4)][rd.lane];
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const int hf = i >> 3, dt = i & 7;
+            const bf16x8 v8 = as_bf16x8(va[i & 3]);
+#pragma unroll
+            for (int r = 0; r < RT; ++r) tile[r].o[dt] = mfma16(v8, as_bf16x8(pw[r][hf]), tile[r].o[dt]);
+            if (i + 4 < 16) va[i & 3] = lds.v[b & 1][(i + 4) >> 3][(i + 4) & 7][rd.lane];
+            if (i < 8) {
+                constexpr int kRest = 8 * RT - kFirst;
+#pragma unroll
+                for (int p = kFirst + kRest * i / 8; p < kFirst + kRest * (i + 1) / 8; ++p) weigh_pair(p);
+            } else if (i % 2 == 0) {
+                i == 8 ? widen_dims(std::integral_constant<int, 0>{}, b + 1) : i == 10 ? widen_dims(std::integral_constant<int, 1>{}, b + 1)
+                : i == 12 ? widen_dims(std::integral_constant<int, 2>{}, b + 1) : widen_dims(std::integral_constant<int, 3>{}, b + 1);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            asm volatile("" : "+v"(sum[r]));
+            tile[r].l += sum[r];
+        }
+        landed();  // the share of step b + 2; of all wavefronts behind the barrier
+        barrier();
+        hide(tile, next, (b + 1) * kStep + 16 * rd.g);
+        tops(next, top);
+        follow(tile, top, c);
+    };
+    for (int b = 0;;) {
+        step(acc0, acc1, b);
+        if (++b >= n_blk) break;
+        step(acc1, acc0, b);
+        if (++b >= n_blk) break;
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may land in LDS that is another workgroup's by then
+    write_rows(rd, row0, c, tile);
 }
 
 // Items [0, n_single) get a workgroup each, the items behind them (at most 16 rows) one for four, a wavefront each (no LDS, no barrier).  The two
 // kinds of workgroups are spread evenly over the grid: those of many rows are bound by their instructions, the others by memory.
 __global__ __launch_bounds__(kWaves * 64, 2) void four_decode_kernel(DecodeLaunch a) {
-    __shared__ Lds lds;
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    Lds &lds = *reinterpret_cast<Lds *>(smem);
     const int G = a.num_q_heads / a.pool.num_kv_heads, i = (int)blockIdx.x, single = (int)((uint64_t)i * a.n_single / gridDim.x);
     if ((int)(((uint64_t)i + 1) * a.n_single / gridDim.x) == single) {
         const int at = a.n_single + kWaves * (i - single) + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -572,9 +691,15 @@ __global__ __launch_bounds__(kWaves * 64, 2) void four_decode_kernel(DecodeLaunc
 
 }  // namespace
 
+hipError_t prepare_four_decode() {
+    return hipFuncSetAttribute(reinterpret_cast<const void *>(four_decode_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(Lds));
+}
+
 hipError_t launch_four_decode(const DecodeLaunch &a, hipStream_t s, hipEvent_t ev_begin, hipEvent_t ev_end) {
     if (a.n_items <= 0) return hipSuccess;
-    hipExtLaunchKernelGGL(four_decode_kernel, dim3(a.n_single + (a.n_items - a.n_single + kWaves - 1) / kWaves), dim3(kWaves * 64), 0, s, ev_begin, ev_end, 0, a);
+    if (hipError_t e = prepare_decode_device(nullptr); e != hipSuccess) return e;
+    const dim3 grid(a.n_single + (a.n_items - a.n_single + kWaves - 1) / kWaves);
+    hipExtLaunchKernelGGL(four_decode_kernel, grid, dim3(kWaves * 64), (unsigned)sizeof(Lds), s, ev_begin, ev_end, 0, a);
     return hipGetLastError();
 }
 
