@@ -117,13 +117,13 @@ struct Reader {
         const size_t blk = block(id, m >> 2);
         x.k_scale = *reinterpret_cast<const uint32_t *>(k_scale + blk * four::kScaleBytes);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x.k[j] = ld16(k + blk * four::kCodeBytes + 256 * j);
+        for (int j = 0; j < 4; ++j) x.k[j] = ld16_stream(k + blk * four::kCodeBytes + 256 * j);
     }
     __device__ __forceinline__ void values(Operands &x, const int (&id)[4]) const {
         const size_t blk = block(id, g);
         x.v_scale = ld16(v_scale + blk * four::kScaleBytes);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) x.v[j] = ld16(v + blk * four::kCodeBytes + 256 * j);
+        for (int j = 0; j < 4; ++j) x.v[j] = ld16_stream(v + blk * four::kCodeBytes + 256 * j);
     }
 };
 
@@ -660,14 +660,20 @@ __device__ __forceinline__ void run_shared_values(const DecodeLaunch &a, const D
     write_rows(rd, row0, c, tile);
 }
 
-// Items [0, n_single) get a workgroup each, the items behind them (at most 16 rows) one for four, a wavefront each (no LDS, no barrier).  The two
-// kinds of workgroups are spread evenly over the grid: those of many rows are bound by their instructions, the others by memory.
+// Items [0, n_single) get a workgroup each, the items behind them (at most 16 rows) one for four, a wavefront each (no LDS, no barrier).  Those of
+// many rows are bound by their instructions, the others by memory, so a compute unit should hold one of either kind.  Workgroups go to the XCDs
+// in turn, and on each of them to its 32 compute units in turn, two a unit: of every 64 sets of eight workgroups (one for each XCD) the items' share
+// comes first, then the wavefronts' items.
+constexpr int kXcds = 8, kPeriod = 64;
 __global__ __launch_bounds__(kWaves * 64, 2) void four_decode_kernel(DecodeLaunch a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     Lds &lds = *reinterpret_cast<Lds *>(smem);
-    const int G = a.num_q_heads / a.pool.num_kv_heads, i = (int)blockIdx.x, single = (int)((uint64_t)i * a.n_single / gridDim.x);
-    if ((int)(((uint64_t)i + 1) * a.n_single / gridDim.x) == single) {
-        const int at = a.n_single + kWaves * (i - single) + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int G = a.num_q_heads / a.pool.num_kv_heads;
+    const uint32_t set = blockIdx.x / kXcds, sets = gridDim.x / kXcds, single_sets = (uint32_t)(a.n_single + kXcds - 1) / kXcds;
+    const uint32_t first = set / kPeriod * kPeriod, end = min(first + kPeriod, sets);
+    const uint32_t before = (uint32_t)((uint64_t)first * single_sets / sets), upto = (uint32_t)((uint64_t)end * single_sets / sets);  // sets of the first kind
+    if (set - first >= upto - before) {
+        const int at = a.n_single + kWaves * (int)(kXcds * (set - upto) + blockIdx.x % kXcds) + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
         if (at >= a.n_items) return;
         const DecodeItem it = a.items[at];
         const Reader rd(a, it);
@@ -677,7 +683,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void four_decode_kernel(DecodeLaunc
         write_rows(rd, 0, c, tile);
         return;
     }
-    const DecodeItem it = a.items[single];
+    const int at = (int)(kXcds * (before + set - first) + blockIdx.x % kXcds);
+    if (at >= a.n_single) return;
+    const DecodeItem it = a.items[at];
     const int rows = it.n_req * G;
     if (rows <= 16)
         run_shared_tokens<1>(a, it, lds.s);
@@ -698,7 +706,8 @@ hipError_t prepare_four_decode() {
 hipError_t launch_four_decode(const DecodeLaunch &a, hipStream_t s, hipEvent_t ev_begin, hipEvent_t ev_end) {
     if (a.n_items <= 0) return hipSuccess;
     if (hipError_t e = prepare_decode_device(nullptr); e != hipSuccess) return e;
-    const dim3 grid(a.n_single + (a.n_items - a.n_single + kWaves - 1) / kWaves);
+    const int packs = (a.n_items - a.n_single + kWaves - 1) / kWaves;
+    const dim3 grid(kXcds * ((a.n_single + kXcds - 1) / kXcds + (packs + kXcds - 1) / kXcds));
     hipExtLaunchKernelGGL(four_decode_kernel, grid, dim3(kWaves * 64), (unsigned)sizeof(Lds), s, ev_begin, ev_end, 0, a);
     return hipGetLastError();
 }

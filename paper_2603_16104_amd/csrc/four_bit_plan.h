@@ -45,15 +45,19 @@ static void plan_four_bit(hkv_decode_plan &pl, int n_cu) {
     const bool pack = pl.opt.pack == 3 || (pl.opt.pack != 1 && few > 8 * n_cu);
     auto packed = [&](const Proto &x) { return pack && x.it.n_req * G <= 16; };
     std::stable_sort(protos.begin(), protos.end(), [&](const Proto &a, const Proto &b) { return packed(a) != packed(b) ? packed(b) : a.cost > b.cost; });
-    if (pl.opt.interleave >= 0) {  // items of many and of few rows with a workgroup each, side by side
+    if (pl.opt.interleave >= 0) {  // items of many and of few rows with a workgroup each, side by side in whole sets of KV heads, which stay on their XCDs
         std::vector<Proto> many, others, rest;
         for (const Proto &x : protos) (packed(x) ? rest : x.it.n_req * G > 16 ? many : others).push_back(x);
         protos.clear();
-        for (size_t a = 0, b = 0; a < many.size() || b < others.size();)
-            if (b >= others.size() || (a < many.size() && (a + 1) * others.size() <= (b + 1) * many.size()))
-                protos.push_back(many[a++]);
-            else
-                protos.push_back(others[b++]);
+        const size_t set = (8 + Hkv - 1) / Hkv * Hkv;
+        for (size_t a = 0, b = 0; a < many.size() || b < others.size();) {
+            const bool first = b >= others.size() || (a < many.size() && (a + set) * others.size() <= (b + set) * many.size());
+            for (size_t i = 0; i < set; ++i)
+                if (first && a < many.size())
+                    protos.push_back(many[a++]);
+                else if (!first && b < others.size())
+                    protos.push_back(others[b++]);
+        }
         protos.insert(protos.end(), rest.begin(), rest.end());
     }
     pl.items.clear();
