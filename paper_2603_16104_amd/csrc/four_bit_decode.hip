@@ -54,9 +54,8 @@ struct RowTile {
     uint32_t q_scale;
     f32x4 o[8];         // o[dt][i]: dim 32 g + 8 i + dt
     float m, l;         // reference (raw scores), this lane's share of the row sum
-    uint32_t part;      // the partial that the row writes
-    int lim;            // tokens of the item that the row may see, and of those behind them, the visible ones
-    unsigned long long vis;
+    int req;            // the plan's row of it
+    int lim;            // tokens of the item that the row may see (and of those behind them the ones in row_mask)
 };
 
 // Four values, |x| <= 448, as e4m3 (to nearest).
@@ -127,32 +126,43 @@ struct Reader {
     }
 };
 
+// The partial that a row of the item writes.
+__device__ __forceinline__ size_t part_of(const DecodeLaunch &a, const DecodeItem &it, int req, int row) {
+    const int G = a.num_q_heads / a.pool.num_kv_heads;
+    return (size_t)((req * a.num_q_heads + it.kv_head * G + row % G) * a.max_parts + it.part_slot);
+}
+
+// The rows' place in the plan, asked for in front of everything else: the queries' loads wait for it.
 template <int RT>
-__device__ __forceinline__ void load_rows(const Reader &rd, int row0, RowTile (&tile)[RT]) {
+__device__ __forceinline__ void find_rows(const Reader &rd, int row0, RowTile (&tile)[RT]) {
+    const int G = rd.a.num_q_heads / rd.a.pool.num_kv_heads, rows = rd.it.n_req * G;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) tile[r].req = rd.a.node_req_idx[rd.it.req_off + min(row0 + 16 * r + rd.m, rows - 1) / G];
+}
+// The queries, 16 bytes of dims 16 g, 16 g + 8, 64 + 16 g, 64 + 16 g + 8 a lane.
+template <int RT>
+__device__ __forceinline__ void load_rows(const Reader &rd, int row0, RowTile (&tile)[RT], u32x4 (&w)[RT][4]) {
     const DecodeLaunch &a = rd.a;
     const DecodeItem &it = rd.it;
     const int G = a.num_q_heads / a.pool.num_kv_heads, rows = it.n_req * G;
-    u32x4 w[RT][4];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
-        const int row = min(row0 + 16 * r + rd.m, rows - 1);
-        const int req = a.node_req_idx[it.req_off + row / G], head = it.kv_head * G + row % G;
+        const int head = it.kv_head * G + min(row0 + 16 * r + rd.m, rows - 1) % G, req = tile[r].req;
         const int q_row = a.q_rows ? a.q_rows[req] : req;
         const char *qp = static_cast<const char *>(a.q) + ((size_t)q_row * a.num_q_heads + head) * (kHeadDim * 2) + 32 * rd.g;
         w[r][0] = ld16(qp);
         w[r][1] = ld16(qp + 16);
         w[r][2] = ld16(qp + 128);
         w[r][3] = ld16(qp + 144);
-        tile[r].part = (uint32_t)((req * a.num_q_heads + head) * a.max_parts + it.part_slot);
-        tile[r].lim = it.n_tokens;
-        tile[r].vis = 0;
-        if (a.row_leaf && a.row_leaf[req] == it.node) {
-            tile[r].lim = a.row_limit[req] - it.tok_begin;
-            tile[r].vis = a.row_mask[req];
-        }
     }
+}
+template <int RT>
+__device__ __forceinline__ void begin_rows(const Reader &rd, RowTile (&tile)[RT], const u32x4 (&w)[RT][4]) {
+    const DecodeLaunch &a = rd.a;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
+        const int req = tile[r].req;
+        tile[r].lim = a.row_leaf && a.row_leaf[req] == rd.it.node ? a.row_limit[req] - rd.it.tok_begin : rd.it.n_tokens;
         split_row(tile[r], w[r], a.scale < 0.f ? -1.f : 1.f);
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) tile[r].o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -182,14 +192,15 @@ __device__ __forceinline__ void scores(const Operands &x, const RowTile (&tile)[
 
 // Scores of tokens that a row does not see are -inf; tok0: of the lane's 16 tokens the first, score j of a row is acc[j % 4][j / 4].
 template <int RT>
-__device__ __forceinline__ void hide(const RowTile (&tile)[RT], f32x4 (&acc)[RT][4], int tok0) {
+__device__ __forceinline__ void hide(const Reader &rd, const RowTile (&tile)[RT], f32x4 (&acc)[RT][4], int tok0) {
     int most = -INT_MAX;  // tokens of the step behind what a row sees at once
 #pragma unroll
     for (int r = 0; r < RT; ++r) most = max(most, tok0 - tile[r].lim);
     if (__builtin_amdgcn_ballot_w64(most > -16)) {  // some row does not see the whole step, the item's last one among them
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
-            const unsigned long long vis = tile[r].vis;
+            const bool last = rd.a.row_leaf && rd.a.row_leaf[tile[r].req] == rd.it.node;  // (looked up here: this is the exception)
+            const unsigned long long vis = last ? rd.a.row_mask[tile[r].req] : 0ull;
             const int d0 = tok0 - tile[r].lim;
             const uint32_t seen = d0 < 0 ? (d0 <= -16 ? 0xFFFFu : (1u << -d0) - 1u | (uint32_t)vis << -d0) : d0 < 64 ? (uint32_t)(vis >> d0) : 0u;
 #pragma unroll
@@ -246,9 +257,9 @@ __device__ __forceinline__ void weigh(RowTile (&tile)[RT], const f32x4 (&acc)[RT
     }
 }
 template <int RT>
-__device__ __forceinline__ void weights(RowTile (&tile)[RT], f32x4 (&acc)[RT][4], int tok0, float c, u32x4 (&pw)[RT][2]) {
+__device__ __forceinline__ void weights(const Reader &rd, RowTile (&tile)[RT], f32x4 (&acc)[RT][4], int tok0, float c, u32x4 (&pw)[RT][2]) {
     float top[RT];
-    hide(tile, acc, tok0);
+    hide(rd, tile, acc, tok0);
     tops(acc, top);
     follow(tile, top, c);
     weigh(tile, acc, c, pw);
@@ -327,7 +338,8 @@ __device__ __forceinline__ void write_rows(const Reader &rd, int row0, float c, 
         float up, down;
         part_factors(top, up, down);
         if (row0 + 16 * r + rd.m >= rows) continue;
-        uint16_t *out = rd.a.o_parts + (size_t)t.part * kHeadDim + 32 * rd.g;
+        const size_t part = part_of(rd.a, rd.it, t.req, row0 + 16 * r + rd.m);
+        uint16_t *out = rd.a.o_parts + part * kHeadDim + 32 * rd.g;
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             u32x4 w;
@@ -336,8 +348,8 @@ __device__ __forceinline__ void write_rows(const Reader &rd, int row0, float c, 
             *reinterpret_cast<u32x4 *>(out + 8 * i) = w;
         }
         if (rd.g == 0) {
-            rd.a.down_parts[t.part] = down;
-            rd.a.lse_parts[t.part] = partial_lse(l_row == l_row ? t.m * c : INFINITY, l_row);
+            rd.a.down_parts[part] = down;
+            rd.a.lse_parts[part] = partial_lse(l_row == l_row ? t.m * c : INFINITY, l_row);
         }
     }
 }
@@ -350,12 +362,16 @@ template <int RT>
 __device__ __forceinline__ void stream(const Reader &rd, int row0, int ts, int n_ts, float c, RowTile (&tile)[RT]) {
     const int n_blk = (rd.it.n_tokens + kStep - 1) / kStep;
     int id[4], b = ts;
+    find_rows(rd, row0, tile);
     rd.ids(id, b);
     Operands x;
+    u32x4 w[RT][4];
     rd.keys(x, id);
+    __builtin_amdgcn_sched_barrier(0);
+    load_rows(rd, row0, tile, w);
+    __builtin_amdgcn_sched_barrier(0);
     rd.values(x, id);
     rd.ids(id, b + n_ts);
-    load_rows(rd, row0, tile);
     auto second_half = [&](Operands &v, const u32x4 (&pw)[RT][2]) {
         if ((b + 1) * kStep > rd.it.n_tokens) {
             const int first_bad = rd.it.n_tokens - (b * kStep + 16 * rd.g);
@@ -375,25 +391,28 @@ __device__ __forceinline__ void stream(const Reader &rd, int row0, int ts, int n
         rd.keys(y, id);
         rd.values(y, id);
         rd.ids(id, b + 2 * n_ts);
+        __builtin_amdgcn_sched_barrier(0);
+        begin_rows(rd, tile, w);
         auto step = [&](Operands &now, Operands &after_next) {
             rd.keys(after_next, id);
             rd.values(after_next, id);
             rd.ids(id, b + 3 * n_ts);
             __builtin_amdgcn_sched_barrier(0);
             scores(now, tile, acc);
-            weights(tile, acc, b * kStep + 16 * rd.g, c, pw);
+            weights(rd, tile, acc, b * kStep + 16 * rd.g, c, pw);
             second_half(now, pw);
             return (b += n_ts) < n_blk;
         };
         while (step(x, z) && step(y, x) && step(z, y)) {
         }
     } else {  // two tiles fill the registers: K of the next step is requested behind the first product, V behind the second
+        begin_rows(rd, tile, w);
         for (; b < n_blk; b += n_ts) {
             scores(x, tile, acc);
             __builtin_amdgcn_sched_barrier(0);
             rd.keys(x, id);
             __builtin_amdgcn_sched_barrier(0);
-            weights(tile, acc, b * kStep + 16 * rd.g, c, pw);
+            weights(rd, tile, acc, b * kStep + 16 * rd.g, c, pw);
             second_half(x, pw);
             __builtin_amdgcn_sched_barrier(0);
             rd.values(x, id);
@@ -406,7 +425,7 @@ __device__ __forceinline__ void stream(const Reader &rd, int row0, int ts, int n
 // LDS of a workgroup: partial results of wavefronts that share a row tile's tokens, or two steps' V in bf16 as the second product's operands.
 struct Shares {
     float o[kWaves][16][kORow], m[kWaves][16], l[kWaves][16];
-    uint32_t part[kWaves][16];
+    int req[16];
 };
 constexpr int kRing = 4;
 struct Stage {  // a step's codes and scales as the lanes take them
@@ -447,7 +466,7 @@ __device__ __forceinline__ void run_shared_tokens(const DecodeLaunch &a, const D
             if (rd.g == 0) {
                 s.m[wave][rd.m] = l_row == l_row ? t.m : INFINITY;  // (a NaN or +inf among the scores: the row's sum is no number below)
                 s.l[wave][rd.m] = l_row;
-                if (wave == 0) s.part[0][rd.m] = t.part;
+                if (wave == 0) s.req[rd.m] = t.req;
             }
         } else if (rd.g == 0) {
             s.m[wave][rd.m] = -INFINITY;
@@ -480,7 +499,7 @@ __device__ __forceinline__ void run_shared_tokens(const DecodeLaunch &a, const D
         float up, down;
         part_factors(top, up, down);
         if (16 * r + out_row >= rows) continue;
-        const size_t part = s.part[0][out_row];
+        const size_t part = part_of(a, it, s.req[out_row], 16 * r + out_row);
         *reinterpret_cast<u32x4 *>(a.o_parts + part * kHeadDim + 8 * col) =
             u32x4{pack_f16(x[0] * up, x[1] * up), pack_f16(x[2] * up, x[3] * up), pack_f16(y[0] * up, y[1] * up), pack_f16(y[2] * up, y[3] * up)};
         if (col == 0) {
@@ -516,11 +535,18 @@ __device__ __forceinline__ void run_shared_values(const DecodeLaunch &a, const D
     };
     u32x4 v;
     uint32_t v_scale;
-    auto take = [&](int b) {  // this wavefront's share of step b
-        const Stage &st = lds.ring[b % kRing];
-        v = st.v[wave][rd.lane];
-        v_scale = st.v_scale[wave][rd.lane];
-        if ((b + 1) * kStep > it.n_tokens) clear_from(v, v_scale, it.n_tokens - (b * kStep + 16 * rd.g + 4 * wave));
+    auto clean = [&](int b) {  // slots behind the item's end, in this wavefront's share of step b
+        if ((b + 1) * kStep <= it.n_tokens) return;
+        Stage &st = lds.ring[b % kRing];
+        u32x4 w = st.v[wave][rd.lane];
+        uint32_t sc = st.v_scale[wave][rd.lane];
+        clear_from(w, sc, it.n_tokens - (b * kStep + 16 * rd.g + 4 * wave));
+        st.v[wave][rd.lane] = w;
+        st.v_scale[wave][rd.lane] = sc;
+    };
+    auto take = [&](int b) {
+        v = lds.ring[b % kRing].v[wave][rd.lane];
+        v_scale = lds.ring[b % kRing].v_scale[wave][rd.lane];
     };
     auto widen_dims = [&](auto byte, int b) {  // dims 8 m + 2 B, + 1 of it
         constexpr int B = decltype(byte)::value;
@@ -541,15 +567,22 @@ __device__ __forceinline__ void run_shared_values(const DecodeLaunch &a, const D
     auto barrier = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
     auto landed = [] { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads * (kRing - 2)) : "memory"); };  // all but the last kRing - 2 steps requested
     int id[4];
+    RowTile tile[RT];
+    u32x4 w[RT][4];
+    find_rows(rd, row0, tile);
+    rd.ids(id, 0);
+    issue(id, 0);
+    load_rows(rd, row0, tile, w);
+    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int b = 0; b < kRing; ++b) {
+    for (int b = 1; b < kRing; ++b) {
         rd.ids(id, b);
         issue(id, b);
     }
     rd.ids(id, kRing);
-    RowTile tile[RT];
-    load_rows(rd, row0, tile);
+    begin_rows(rd, tile, w);
     landed();
+    clean(0);
     take(0);
     widen(0);
     barrier();
@@ -558,6 +591,7 @@ __device__ __forceinline__ void run_shared_values(const DecodeLaunch &a, const D
         for (int b = 0; b < n_blk; ++b) {
             issue(id, b + kRing);
             rd.ids(id, b + kRing + 1);
+            clean(b + 1);
             take(b + 1);
             widen(b + 1);
             landed();
@@ -580,20 +614,21 @@ __device__ __forceinline__ void run_shared_values(const DecodeLaunch &a, const D
     u32x4 pw[RT][2];
     float top[RT];
     first_product(acc0, 0);
-    hide(tile, acc0, 16 * rd.g);
+    hide(rd, tile, acc0, 16 * rd.g);
     tops(acc0, top);
     follow(tile, top, c);
     barrier();  // all are done with K of step 0
     auto step = [&](f32x4 (&now)[RT][4], f32x4 (&next)[RT][4], int b) {
-        issue(id, b + kRing);  // where step b was: its keys and values left in step b - 1
-        rd.ids(id, b + kRing + 1);
-        take(b + 1);  // (behind the last step: of no use, and of no harm)
-        // every chunk up to a sched_barrier: matrix instructions (32 cycles each of the first product, 16 of the second) and about as many cycles of others
         const Stage &st = lds.ring[(b + 1) % kRing];
         u32x4 k[4], va[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) k[j] = st.k[j][rd.lane];
         const uint32_t k_scale = st.k_scale[rd.lane];
+        __builtin_amdgcn_sched_barrier(0);
+        issue(id, b + kRing);  // where step b was: its keys and values left in step b - 1
+        rd.ids(id, b + kRing + 1);
+        clean(b + 1);  // (behind the last step: of no use, and of no harm)
+        // every chunk up to a sched_barrier: matrix instructions (32 cycles each of the first product, 16 of the second) and about as many cycles of others
         float mc[RT], sum[RT];
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
@@ -628,6 +663,7 @@ __device__ __forceinline__ void run_shared_values(const DecodeLaunch &a, const D
             const bf16x8 v8 = as_bf16x8(va[i & 3]);
 #pragma unroll
             for (int r = 0; r < RT; ++r) tile[r].o[dt] = mfma16(v8, as_bf16x8(pw[r][hf]), tile[r].o[dt]);
+            if (i == 2) take(b + 1);
             if (i + 4 < 16) va[i & 3] = lds.v[b & 1][(i + 4) >> 3][(i + 4) & 7][rd.lane];
             if (i < 8) {
                 constexpr int kRest = 8 * RT - kFirst;
@@ -644,11 +680,11 @@ __device__ __forceinline__ void run_shared_values(const DecodeLaunch &a, const D
             asm volatile("" : "+v"(sum[r]));
             tile[r].l += sum[r];
         }
-        landed();  // the share of step b + 2; of all wavefronts behind the barrier
-        barrier();
-        hide(tile, next, (b + 1) * kStep + 16 * rd.g);
+        hide(rd, tile, next, (b + 1) * kStep + 16 * rd.g);
         tops(next, top);
         follow(tile, top, c);
+        landed();  // the share of step b + 2; of all wavefronts behind the barrier
+        barrier();
     };
     for (int b = 0;;) {
         step(acc0, acc1, b);

@@ -26,7 +26,7 @@ static void plan_four_bit(hkv_decode_plan &pl, int n_cu) {
         if (nd.parent >= 0) slot_base[v] = slot_base[nd.parent] + node_chunks[nd.parent];
         const int R = requests(v);
         if (nd.n_tokens == 0 || R == 0) continue;
-        const int asked = R * G > 16 ? pl.opt.shared_chunk : pl.opt.leaf_chunk;
+        const int asked = R * G > 16 ? (pl.opt.tile_chunk ? pl.opt.tile_chunk : pl.opt.shared_chunk) : pl.opt.leaf_chunk;
         const int most = asked ? asked : chunk, cuts = (nd.n_tokens + most - 1) / most;
         const int per_chunk = std::min(nd.n_pages, ((nd.n_pages + cuts - 1) / cuts + 3) / 4 * 4);  // whole steps of four blocks
         node_chunks[v] = (nd.n_pages + per_chunk - 1) / per_chunk;
