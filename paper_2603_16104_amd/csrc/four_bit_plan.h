@@ -5,16 +5,122 @@
 
 #include "hkv_objects.h"
 
+namespace four_plan {
+
+// Kinds of items by query rows (up to 16, 32, 64, 128 with a workgroup each; up to 16 with a wavefront each), microseconds: what an item costs beside its
+// steps of 64 tokens, a step on a full chip (two workgroups a compute unit) and on an empty one.
+struct Kind {
+    double fixed, full, alone;
+};
+constexpr Kind kKinds[5] = {{3.8, 0.50, 0.20}, {5.7, 0.65, 0.31}, {4.6, 0.95, 0.82}, {6.5, 1.40, 1.10}, {3.7, 1.90, 0.81}};
+constexpr int kRowCaps[4] = {16, 32, 64, 128};
+constexpr int kChunks[7] = {64, 128, 256, 512, 1024, 2048, 4096};
+
+struct Load {  // items of one kind
+    int64_t items = 0, steps = 0;
+    int32_t longest = 0;
+    void add(int64_t n, int32_t tokens, int64_t all_tokens) {
+        items += n;
+        steps += all_tokens;
+        longest = std::max(longest, (tokens + 63) / 64);
+    }
+};
+
+// A step's length: the items' costs over the chip's slots and part of the longest one, that one alone, or the bytes; then the merge's partials.
+// 3983 timings of 150 random plans of 8 to 340 us, cut in 28 ways each: 7 % rms; the way that the estimate prefers takes 1.03 of the best one's
+// time in the mean, 1.09 for one plan in ten, 1.24 at most.
+inline double estimate_us(const Load (&load)[5], double bytes, double partials, int n_cu) {
+    double busy = 0, longest = 0;
+    for (int k = 0; k < 5; ++k) {
+        if (load[k].items == 0) continue;
+        busy += (load[k].items * kKinds[k].fixed + load[k].steps * kKinds[k].full) * (k == 4 ? 0.25 : 1.0);
+        longest = std::max(longest, kKinds[k].fixed + load[k].longest * kKinds[k].alone);
+    }
+    busy /= 2 * n_cu;
+    return 4.2 + std::max({busy + 0.59 * longest, longest, bytes / 6.9e6}) + partials * 528 / 3.9e6;
+}
+
+struct Cut {
+    int max_rows, shared_chunk, leaf_chunk;
+    bool pack;
+};
+struct Pieces {
+    int count, blocks;  // chunks of a node, blocks of one (whole steps of four, the last one shorter)
+};
+inline Pieces pieces_of(int blocks, int chunk) {
+    const int most = std::max(1, chunk / HKV_PAGE_SIZE), cuts = (blocks + most - 1) / most;
+    const int each = std::min(blocks, ((blocks + cuts - 1) / cuts + 3) / 4 * 4);
+    return {(blocks + each - 1) / each, each};
+}
+
+// The cut of the shortest estimated step among those whose partials fit the static workspace, or among all.  What the caller sets stays.
+inline Cut choose(const hkv_decode_plan &pl, int n_cu) {
+    const int G = pl.group, Hkv = pl.pool->d.num_kv_heads, n_nodes = (int)pl.nodes.size();
+    Load few[7], shared[4][7][5];
+    std::vector<int32_t> few_parts(n_nodes), shared_parts(n_nodes);
+    int32_t most_few[7] = {}, most_shared[7] = {};  // chunks on the longest path
+    double bytes = 0;
+    for (int i = 0; i < 7; ++i)
+        for (int v = 0; v < n_nodes; ++v) {
+            const hkv_node &nd = pl.nodes[v];
+            const int R = pl.node_req_indptr[v + 1] - pl.node_req_indptr[v];
+            few_parts[v] = nd.parent >= 0 ? few_parts[nd.parent] : 0;
+            shared_parts[v] = nd.parent >= 0 ? shared_parts[nd.parent] : 0;
+            if (R == 0 || nd.n_tokens == 0) continue;
+            if (i == 0) bytes += 136.0 * Hkv * nd.n_tokens;
+            const bool is_few = R * G <= 16;
+            const int set = is_few ? pl.opt.leaf_chunk : pl.opt.shared_chunk;
+            const Pieces p = pieces_of(nd.n_pages, set ? set : kChunks[i]);
+            const int tokens = std::min(nd.n_tokens, p.blocks * HKV_PAGE_SIZE);
+            const int64_t steps = (int64_t)(nd.n_pages + 3) / 4 * Hkv;
+            (is_few ? few_parts : shared_parts)[v] += p.count;
+            most_few[i] = std::max(most_few[i], few_parts[v]);
+            most_shared[i] = std::max(most_shared[i], shared_parts[v]);
+            if (is_few) {
+                few[i].add((int64_t)p.count * Hkv, tokens, steps);
+                continue;
+            }
+            for (int c = 0; c < 4; ++c) {
+                const int max_req = std::max(1, (pl.opt.max_rows ? pl.opt.max_rows : kRowCaps[c]) / G), groups = (R + max_req - 1) / max_req;
+                const int rows = (R + groups - 1) / groups * G;
+                shared[c][i][rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : 3].add((int64_t)p.count * groups * Hkv, tokens, steps * groups);
+            }
+        }
+    Cut best{128, 2048, 4096, false};
+    double least = 1e300;
+    bool best_fits = false;
+    for (int c = 0; c < 4; ++c)
+        for (int s = 0; s < 7; ++s)
+            for (int f = 0; f < 7; ++f)
+                for (const bool pack : {false, true}) {
+                    if (pl.opt.pack == 1 ? pack : pl.opt.pack == 3 ? !pack : false) continue;
+                    Load load[5];
+                    for (int k = 0; k < 4; ++k) load[k] = shared[c][s][k];
+                    load[0].items += few[f].items;
+                    load[0].steps += few[f].steps;
+                    load[0].longest = std::max(load[0].longest, few[f].longest);
+                    if (pack) std::swap(load[0], load[4]);
+                    const double partials = (double)pl.n_req * pl.num_q_heads * (most_few[f] + most_shared[s]);
+                    const bool fits = partials * 264 + 768 <= (double)kStaticWorkspaceBytes;
+                    const double us = estimate_us(load, bytes, partials, n_cu);
+                    if (fits == best_fits ? us >= least : !fits) continue;
+                    least = us;
+                    best_fits = fits;
+                    best = Cut{pl.opt.max_rows ? pl.opt.max_rows : kRowCaps[c], kChunks[s], kChunks[f], pack};
+                }
+    if (pl.opt.shared_chunk) best.shared_chunk = pl.opt.shared_chunk;
+    if (pl.opt.leaf_chunk) best.leaf_chunk = pl.opt.leaf_chunk;
+    return best;
+}
+
+}  // namespace four_plan
+
 // A node with T tokens that R requests pass through becomes items of up to max_rows query rows and a chunk of whole blocks each, every one of which leaves
 // a partial per row; the chunks of a node take the same places in the partial lists of all requests below it (as in the other pools' plans).
 static void plan_four_bit(hkv_decode_plan &pl, int n_cu) {
     const int G = pl.group, Hkv = pl.pool->d.num_kv_heads, n_nodes = (int)pl.nodes.size();
-    const int max_rows = pl.opt.max_rows ? pl.opt.max_rows : 128, max_req = std::max(1, max_rows / G);
-    auto requests = [&](int v) { return pl.node_req_indptr[v + 1] - pl.node_req_indptr[v]; };
-    int64_t work = 0;  // blocks times row groups and heads
-    for (int v = 0; v < n_nodes; ++v)
-        if (requests(v) > 0) work += (int64_t)pl.nodes[v].n_pages * Hkv * ((requests(v) + max_req - 1) / max_req);
-    const int chunk = (int)std::min<int64_t>(1 << 26, std::max<int64_t>(256, work * HKV_PAGE_SIZE / (4 * n_cu) / 64 * 64));
+    const four_plan::Cut cut = four_plan::choose(pl, n_cu);
+    const int max_req = std::max(1, cut.max_rows / G);
     struct Proto {
         DecodeItem it;
         int64_t cost;
@@ -24,26 +130,21 @@ static void plan_four_bit(hkv_decode_plan &pl, int n_cu) {
     for (int v = 0; v < n_nodes; ++v) {
         const hkv_node &nd = pl.nodes[v];
         if (nd.parent >= 0) slot_base[v] = slot_base[nd.parent] + node_chunks[nd.parent];
-        const int R = requests(v);
+        const int R = pl.node_req_indptr[v + 1] - pl.node_req_indptr[v];
         if (nd.n_tokens == 0 || R == 0) continue;
-        const int asked = R * G > 16 ? (pl.opt.tile_chunk ? pl.opt.tile_chunk : pl.opt.shared_chunk) : pl.opt.leaf_chunk;
-        const int most = asked ? asked : chunk, cuts = (nd.n_tokens + most - 1) / most;
-        const int per_chunk = std::min(nd.n_pages, ((nd.n_pages + cuts - 1) / cuts + 3) / 4 * 4);  // whole steps of four blocks
-        node_chunks[v] = (nd.n_pages + per_chunk - 1) / per_chunk;
+        const four_plan::Pieces p = four_plan::pieces_of(nd.n_pages, R * G > 16 ? cut.shared_chunk : cut.leaf_chunk);
+        node_chunks[v] = p.count;
         const int groups = (R + max_req - 1) / max_req, per_group = (R + groups - 1) / groups;
         for (int r0 = 0; r0 < R; r0 += per_group)
-            for (int pg = 0, ci = 0; pg < nd.n_pages; pg += per_chunk, ++ci) {
-                const int nr = std::min(per_group, R - r0), nt = std::min(per_chunk * HKV_PAGE_SIZE, nd.n_tokens - pg * HKV_PAGE_SIZE);
+            for (int pg = 0, ci = 0; pg < nd.n_pages; pg += p.blocks, ++ci) {
+                const int nr = std::min(per_group, R - r0), nt = std::min(p.blocks * HKV_PAGE_SIZE, nd.n_tokens - pg * HKV_PAGE_SIZE);
                 for (int h = 0; h < Hkv; ++h)
                     protos.push_back({DecodeItem{nd.page_begin + pg, nt, h, pl.node_req_indptr[v] + r0, nr, slot_base[v] + ci, pg * HKV_PAGE_SIZE, v},
                                       (int64_t)nt * std::max(16, (nr * G + 15) / 16 * 16)});
             }
     }
-    // Heavy items first.  Many items of few rows: a wavefront each instead of a workgroup each.
-    int64_t few = 0;
-    for (const Proto &x : protos) few += x.it.n_req * G <= 16;
-    const bool pack = pl.opt.pack == 3 || (pl.opt.pack != 1 && few > 8 * n_cu);
-    auto packed = [&](const Proto &x) { return pack && x.it.n_req * G <= 16; };
+    // Heavy items first, those with a wavefront each behind the others.
+    auto packed = [&](const Proto &x) { return cut.pack && x.it.n_req * G <= 16; };
     std::stable_sort(protos.begin(), protos.end(), [&](const Proto &a, const Proto &b) { return packed(a) != packed(b) ? packed(b) : a.cost > b.cost; });
     if (pl.opt.interleave >= 0) {  // items of many and of few rows with a workgroup each, side by side in whole sets of KV heads, which stay on their XCDs
         std::vector<Proto> many, others, rest;
