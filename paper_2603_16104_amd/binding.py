@@ -216,11 +216,14 @@ def kv_pool_fork(pool, pages, n_tokens, parent, release: bool = False, stream=No
     """pages: the sequences' page lists, one after the other; returns those of the forks, fork j of sequence parent[j]."""
     pages, n_tokens, parent = _host_i32(pages), _host_i32(n_tokens), _host_i32(parent)
     page = kv_pool_page_size(pool)
-    count = -(-n_tokens.astype(np.int64) // page)
-    if (n_tokens >= 0).all() and len(pages) != count.sum():
+    count = (n_tokens + (page - 1)) // page
+    if len(pages) != count.sum():
         raise HkvError(EINVAL, f"kv_pool_fork: {count.sum()} page ids needed, {len(pages)} given")
-    known = len(parent) > 0 and len(n_tokens) > 0 and 0 <= parent.min() and parent.max() < len(n_tokens)
-    out = np.empty(int(count[parent].sum()) if known else 0, dtype=np.int32)
+    try:
+        room = int(count[parent].sum())
+    except IndexError:  # (refused by the call)
+        room = 0
+    out = np.empty(room, dtype=np.int32)
     _run(lib().kv_pool_fork, pool, len(n_tokens), _host_addr(pages), _host_addr(n_tokens), len(parent), _host_addr(parent), int(release),
          _host_addr(out), _stream_addr(stream))
     return out

@@ -6,6 +6,7 @@
 #include <climits>
 #include <cstring>
 #include <exception>
+#include <numeric>
 
 namespace {
 
@@ -198,6 +199,7 @@ extern "C" int32_t kv_pool_compact(hkv_pool *pool, int32_t *new_ids, void *strea
     const int32_t live = n - (int32_t)pool->free_list.size();
     std::vector<int32_t> map(n);
     std::vector<PagePair> moves;
+    moves.reserve(live);
     int32_t gap = 0;
     for (int32_t id = 0; id < n; ++id) {
         map[id] = pool->refcnt[id] > 0 ? id : -1;
@@ -206,8 +208,8 @@ extern "C" int32_t kv_pool_compact(hkv_pool *pool, int32_t *new_ids, void *strea
         map[id] = gap;
         moves.push_back({id, gap++, pool->d.page_size});
     }
-    std::deque<int32_t> free_list;
-    for (int32_t id = live; id < n; ++id) free_list.push_back(id);
+    std::deque<int32_t> free_list(n - live);
+    std::iota(free_list.begin(), free_list.end(), live);
     for (const hkv_pool::Follower &f : pool->followers) f.prepare(f.object, map.data());
     if (int rc = queue_copies(pool, pool, moves, s)) return rc;
     for (const PagePair &m : moves) {
