@@ -1314,7 +1314,8 @@ static int upload_decode_plan(hkv_decode_plan &pl) {
     size_t off_qrows = align_up(off_tiles + sizeof(DecodeItem) * pl.tile_items.size(), 256);
     size_t off_paths = align_up(off_qrows + sizeof(int32_t) * pl.q_rows.size(), 256);
     size_t off_store = align_up(off_paths + sizeof(int32_t) * pl.paths.size(), 256);
-    size_t total = align_up(off_store + sizeof(StoreRequest) * pl.store.size(), 256) + 256;
+    size_t off_order = align_up(off_store + sizeof(StoreRequest) * pl.store.size(), 256);
+    size_t total = align_up(off_order + sizeof(int32_t) * pl.order.size(), 256) + 256;
     HKV_HIP(hipMalloc(&pl.dev, total));
     char *base = static_cast<char *>(pl.dev);
     pl.d_items = reinterpret_cast<DecodeItem *>(base + off_items);
@@ -1324,6 +1325,7 @@ static int upload_decode_plan(hkv_decode_plan &pl) {
     pl.d_tile_items = reinterpret_cast<DecodeItem *>(base + off_tiles);
     pl.d_paths = reinterpret_cast<int32_t *>(base + off_paths);
     pl.d_store = reinterpret_cast<StoreRequest *>(base + off_store);
+    pl.d_order = pl.order.empty() ? nullptr : reinterpret_cast<int32_t *>(base + off_order);
     pl.d_q_rows = pl.q_rows.empty() ? nullptr : reinterpret_cast<int32_t *>(base + off_qrows);
     // one host image, one copy
     std::vector<char> image(total, 0);
@@ -1338,6 +1340,7 @@ static int upload_decode_plan(hkv_decode_plan &pl) {
     put(off_qrows, pl.q_rows.data(), sizeof(int32_t) * pl.q_rows.size());
     put(off_paths, pl.paths.data(), sizeof(int32_t) * pl.paths.size());
     put(off_store, pl.store.data(), sizeof(StoreRequest) * pl.store.size());
+    put(off_order, pl.order.data(), sizeof(int32_t) * pl.order.size());
     HKV_HIP(hipMemcpy(pl.dev, image.data(), total, hipMemcpyHostToDevice));
     if (pl.reserve_tokens > 0 && pl.n_req <= kMaxInlineAppend && !pl.grow_items.empty() && !pl.opt.large_batch_updates) {
         HKV_HIP(hipMalloc((void **)&pl.d_grow_items, sizeof(int32_t) * pl.grow_items.size()));
@@ -1937,7 +1940,7 @@ static int run_decode_plan(hkv_decode_plan *plan, const void *q, float scale, vo
     const DecodeLaunch a{view_of(plan->pool), q, plan->d_items, plan->d_pages, plan->d_node_req_idx, o_parts, lse_parts,
                          down_parts, (int32_t)plan->items.size(), plan->num_q_heads, plan->max_parts, scale,
                          plan->d_row_leaf, plan->d_row_limit, plan->d_row_mask, plan->n_single, plan->n_stages,
-                         plan->fp8_matrix ? 1 : 0, plan->d_q_rows, plan->has_shared ? 1 : 0, plan->restart_tokens};
+                         plan->fp8_matrix ? 1 : 0, plan->d_q_rows, plan->has_shared ? 1 : 0, plan->restart_tokens, plan->d_order};
     if (plan->path_waves) {
         DecodePathLaunch p{};
         static_cast<DecodeLaunch &>(p) = a;

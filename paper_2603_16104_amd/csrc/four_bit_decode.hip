@@ -696,20 +696,18 @@ __device__ __forceinline__ void run_shared_values(const DecodeLaunch &a, const D
     write_rows(rd, row0, c, tile);
 }
 
-// Items [0, n_single) get a workgroup each, the items behind them (at most 16 rows) one for four, a wavefront each (no LDS, no barrier).  Those of
-// many rows are bound by their instructions, the others by memory, so a compute unit should hold one of either kind.  Workgroups go to the XCDs
-// in turn, and on each of them to its 32 compute units in turn, two a unit: of every 64 sets of eight workgroups (one for each XCD) the items' share
-// comes first, then the wavefronts' items.
-constexpr int kXcds = 8, kPeriod = 64;
+// Items [0, n_single) get a workgroup each, the items behind them (at most 16 rows) one for four, a wavefront each (no LDS, no barrier), in the plan's order
+// of sets of eight workgroups, one for each XCD.  Those of many rows are bound by their instructions, the others by memory, so a compute unit should hold one
+// of either kind, to the end.
+constexpr int kXcds = 8;
 __global__ __launch_bounds__(kWaves * 64, 2) void four_decode_kernel(DecodeLaunch a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     Lds &lds = *reinterpret_cast<Lds *>(smem);
     const int G = a.num_q_heads / a.pool.num_kv_heads;
-    const uint32_t set = blockIdx.x / kXcds, sets = gridDim.x / kXcds, single_sets = (uint32_t)(a.n_single + kXcds - 1) / kXcds;
-    const uint32_t first = set / kPeriod * kPeriod, end = min(first + kPeriod, sets);
-    const uint32_t before = (uint32_t)((uint64_t)first * single_sets / sets), upto = (uint32_t)((uint64_t)end * single_sets / sets);  // sets of the first kind
-    if (set - first >= upto - before) {
-        const int at = a.n_single + kWaves * (int)(kXcds * (set - upto) + blockIdx.x % kXcds) + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int set = blockIdx.x / kXcds, single_sets = (a.n_single + kXcds - 1) / kXcds;
+    const int place = a.order ? a.order[set] : set < single_sets ? set : ~(set - single_sets);
+    if (place < 0) {
+        const int at = a.n_single + kWaves * (kXcds * ~place + (int)(blockIdx.x % kXcds)) + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
         if (at >= a.n_items) return;
         const DecodeItem it = a.items[at];
         const Reader rd(a, it);
@@ -719,7 +717,7 @@ __global__ __launch_bounds__(kWaves * 64, 2) void four_decode_kernel(DecodeLaunc
         write_rows(rd, 0, c, tile);
         return;
     }
-    const int at = (int)(kXcds * (before + set - first) + blockIdx.x % kXcds);
+    const int at = kXcds * place + (int)(blockIdx.x % kXcds);
     if (at >= a.n_single) return;
     const DecodeItem it = a.items[at];
     const int rows = it.n_req * G;

@@ -2,6 +2,10 @@
 #pragma once
 
 #include <algorithm>
+#include <array>
+#include <functional>
+#include <queue>
+#include <utility>
 
 #include "hkv_objects.h"
 
@@ -14,6 +18,7 @@ struct Kind {
 };
 constexpr Kind kKinds[5] = {{3.8, 0.50, 0.20}, {5.7, 0.65, 0.31}, {4.6, 0.95, 0.82}, {6.5, 1.40, 1.10}, {3.7, 1.90, 0.81}};
 constexpr int kRowCaps[4] = {16, 32, 64, 128};
+constexpr int kXcds = 8;  // (workgroups go to them in turn)
 constexpr int kChunks[7] = {64, 128, 256, 512, 1024, 2048, 4096};
 
 struct Load {  // items of one kind
@@ -113,6 +118,46 @@ inline Cut choose(const hkv_decode_plan &pl, int n_cu) {
     return best;
 }
 
+// Estimated microseconds of items in sets (of `set` items, the first ones of the longest), a wavefront or a workgroup each.
+template <class Proto>
+std::vector<double> lengths(const std::vector<Proto> &items, size_t set, int group, bool packed) {
+    std::vector<double> us;
+    for (size_t i = 0; i < items.size(); i += set) {
+        const int rows = items[i].it.n_req * group;
+        const Kind &k = kKinds[packed ? 4 : rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : 3];
+        us.push_back(k.fixed + (items[i].it.n_tokens + 63) / 64 * k.full);
+    }
+    return us;
+}
+
+// The order in which sets of two kinds go out to `slots` places: set i of the first kind as i, of the second as ~i.  Whenever a place is free, the kind
+// goes on whose remaining time over the places it would have, plus one set's time, is longer: both share the chip all the while (one is bound by
+// its instructions, the other by memory), and neither is left alone with long sets at the end.  Of those that start at once the first kind's come
+// first: workgroups go to an XCD's compute units in turn, so each gets one of them before any gets two.
+inline std::vector<int32_t> dispatch_order(const std::array<std::vector<double>, 2> &us, int slots) {
+    std::vector<int32_t> order;
+    std::priority_queue<std::pair<double, int>, std::vector<std::pair<double, int>>, std::greater<>> running;  // (end, kind)
+    double left[2] = {}, now = 0;
+    for (int k = 0; k < 2; ++k)
+        for (const double x : us[k]) left[k] += x;
+    size_t next[2] = {}, count[2] = {};
+    auto urgency = [&](int k) { return next[k] < us[k].size() ? left[k] / (double)(count[k] + 1) + us[k][next[k]] : -1.0; };
+    while (next[0] < us[0].size() || next[1] < us[1].size()) {
+        if ((int)running.size() >= slots) {
+            now = running.top().first;
+            --count[running.top().second];
+            running.pop();
+        }
+        const int k = urgency(0) >= urgency(1) ? 0 : 1;
+        order.push_back(k ? ~(int32_t)next[1] : (int32_t)next[0]);
+        running.push({now + us[k][next[k]], k});
+        left[k] -= us[k][next[k]++];
+        ++count[k];
+    }
+    std::stable_partition(order.begin(), order.begin() + std::min<size_t>(order.size(), (size_t)std::max(slots, 0)), [](int32_t i) { return i >= 0; });
+    return order;
+}
+
 }  // namespace four_plan
 
 // A node with T tokens that R requests pass through becomes items of up to max_rows query rows and a chunk of whole blocks each, every one of which leaves
@@ -146,20 +191,22 @@ static void plan_four_bit(hkv_decode_plan &pl, int n_cu) {
     // Heavy items first, those with a wavefront each behind the others.
     auto packed = [&](const Proto &x) { return cut.pack && x.it.n_req * G <= 16; };
     std::stable_sort(protos.begin(), protos.end(), [&](const Proto &a, const Proto &b) { return packed(a) != packed(b) ? packed(b) : a.cost > b.cost; });
-    if (pl.opt.interleave >= 0) {  // items of many and of few rows with a workgroup each, side by side in whole sets of KV heads, which stay on their XCDs
-        std::vector<Proto> many, others, rest;
-        for (const Proto &x : protos) (packed(x) ? rest : x.it.n_req * G > 16 ? many : others).push_back(x);
-        protos.clear();
-        const size_t set = (8 + Hkv - 1) / Hkv * Hkv;
-        for (size_t a = 0, b = 0; a < many.size() || b < others.size();) {
-            const bool first = b >= others.size() || (a < many.size() && (a + set) * others.size() <= (b + set) * many.size());
-            for (size_t i = 0; i < set; ++i)
-                if (first && a < many.size())
-                    protos.push_back(many[a++]);
-                else if (!first && b < others.size())
-                    protos.push_back(others[b++]);
+    pl.order.clear();
+    if (pl.opt.interleave >= 0) {  // items of many and of few rows side by side, in whole sets of KV heads, which stay on their XCDs
+        std::vector<Proto> many, few;
+        for (const Proto &x : protos) (x.it.n_req * G > 16 ? many : few).push_back(x);
+        const int set = cut.pack ? four_plan::kXcds : (four_plan::kXcds + Hkv - 1) / Hkv * Hkv;
+        const auto order = four_plan::dispatch_order({four_plan::lengths(many, set, G, false), four_plan::lengths(few, cut.pack ? 4 * set : set, G, cut.pack)}, 2 * n_cu / set);
+        if (cut.pack) {
+            if (!many.empty() && (int)order.size() > 2 * n_cu / set) pl.order = order;  // (what starts all at once is in order)
+        } else {
+            protos.clear();
+            for (const int32_t i : order) {
+                const std::vector<Proto> &from = i < 0 ? few : many;
+                const size_t first = (size_t)(i < 0 ? ~i : i) * set;
+                protos.insert(protos.end(), from.begin() + first, from.begin() + std::min(first + set, from.size()));
+            }
         }
-        protos.insert(protos.end(), rest.begin(), rest.end());
     }
     pl.items.clear();
     pl.n_single = 0;

@@ -99,6 +99,9 @@ struct DecodeLaunch {
     const int32_t *q_rows;
     int32_t has_shared;          // items shared by more than 16 query rows are run by shared::body
     int32_t restart_tokens;      // bf16 pools: after so many tokens such an item takes its rows' references anew (a multiple of 64)
+    // fp4 pools: the order in which sets of eight workgroups go out, the i-th of items with a workgroup each as i, the i-th of those with a
+    // wavefront each as ~i (device; null: as the items are).
+    const int32_t *order;
 };
 // Whole paths instead of items (of the base, what describes items is not read): a record of path_stride ints per leaf and up
 // to 16 / G of its rows, run by a workgroup per KV head, which writes out / lse_out (may be null) itself.

@@ -39,6 +39,8 @@ struct hkv_decode_plan {
     void *dev = nullptr;
     DecodeItem *d_items = nullptr, *d_tile_items = nullptr;
     int32_t n_single = 0;  // items [0, n_single) run one per workgroup, the rest four per workgroup
+    std::vector<int32_t> order;  // fp4 pools: DecodeLaunch::order
+    int32_t *d_order = nullptr;
     int32_t n_stages = 3;  // LDS stages of 16 KiB per workgroup of the per-node kernel
     bool has_shared = false;  // items of `items` shared by more than 16 query rows are run by shared::body
     int tile_form = 0;  // bf16 pools: -1 never, 1 always shared::body, 2 with tall tiles (HKV_PLAN_NARROW_TILES, _WIDE_TILES, _TALL_TILES)
