@@ -26,6 +26,7 @@ constexpr int kWaves = 4, kStep = 64;  // wavefronts; tokens of a step
 constexpr int kORow = kHeadDim + 4;    // padded LDS row
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(16))) float f32x16;
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
 // 16 tokens (e2m1, scale byte T of k_scale) x 128 dims by 128 dims x 16 rows (e4m3, scale byte 0 of q_scale).  Lane (m, g): of the tokens dims 32 g .. + 31, of
@@ -65,28 +66,30 @@ __device__ __forceinline__ int e4m3x4(float a, float b, float c, float d) {
 
 // A row as two e4m3 terms: its largest magnitude is brought into [128, 256) by a power of two, the first term holds four significant bits, the second
 // what is left: exact for a bf16 value down to 2^-9 of the row's largest, from there on to 2^-17 of it.  sign: -1 for a negative softmax scale.
+__device__ __forceinline__ float row_factor(float top, float sign, uint32_t &q_scale) {
+    const int ex = min(max((int)(__float_as_uint(top) >> 23), 8), 254);  // where both powers are normal numbers
+    q_scale = (uint32_t)(ex - 7);
+    return __uint_as_float((uint32_t)(261 - ex) << 23) * (sign < 0.f ? -1.f : 1.f);
+}
+__device__ __forceinline__ void split_four(uint32_t w0, uint32_t w1, float up, int &hi, int &lo) {
+    const float a = __uint_as_float(w0 << 16) * up, b = __uint_as_float(w0 & 0xFFFF0000u) * up, c = __uint_as_float(w1 << 16) * up, d = __uint_as_float(w1 & 0xFFFF0000u) * up;
+    hi = e4m3x4(a, b, c, d);
+    const auto h0 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), h1 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
+    lo = e4m3x4(a - h0[0], b - h0[1], c - h1[0], d - h1[1]);
+}
 __device__ __forceinline__ void split_row(RowTile &x, const u32x4 (&w)[4], float sign) {
-    float q[32], top = 0.f;
+    float top = 0.f;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            q[8 * i + 2 * j] = __uint_as_float(w[i][j] << 16);
-            q[8 * i + 2 * j + 1] = __uint_as_float(w[i][j] & 0xFFFF0000u);
-        }
-#pragma unroll
-    for (int j = 0; j < 32; ++j) top = fmaxf(top, fabsf(q[j]));
-    top = rows_max(top);
-    const int ex = min(max((int)(__float_as_uint(top) >> 23), 8), 254);  // where both powers are normal numbers
-    const float up = __uint_as_float((uint32_t)(261 - ex) << 23) * sign;
-    x.q_scale = (uint32_t)(ex - 7);
+        for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i][j] << 16)), fabsf(__uint_as_float(w[i][j] & 0xFFFF0000u))));
+    const float up = row_factor(rows_max(top), sign, x.q_scale);
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-        const float a = q[4 * j] * up, b = q[4 * j + 1] * up, c = q[4 * j + 2] * up, d = q[4 * j + 3] * up;
-        const int h = e4m3x4(a, b, c, d);
-        const auto h0 = __builtin_amdgcn_cvt_pk_f32_fp8(h, false), h1 = __builtin_amdgcn_cvt_pk_f32_fp8(h, true);
+        int h, l;
+        split_four(w[j >> 1][2 * (j & 1)], w[j >> 1][2 * (j & 1) + 1], up, h, l);
         x.hi[j] = h;
-        x.lo[j] = e4m3x4(a - h0[0], b - h0[1], c - h1[0], d - h1[1]);
+        x.lo[j] = l;
     }
 }
 
@@ -163,7 +166,7 @@ __device__ __forceinline__ void begin_rows(const Reader &rd, RowTile (&tile)[RT]
     for (int r = 0; r < RT; ++r) {
         const int req = tile[r].req;
         tile[r].lim = a.row_leaf && a.row_leaf[req] == rd.it.node ? a.row_limit[req] - rd.it.tok_begin : rd.it.n_tokens;
-        split_row(tile[r], w[r], a.scale < 0.f ? -1.f : 1.f);
+        split_row(tile[r], w[r], a.scale);
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) tile[r].o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         tile[r].m = -INFINITY;
@@ -422,19 +425,20 @@ __device__ __forceinline__ void stream(const Reader &rd, int row0, int ts, int n
     }
 }
 
-// LDS of a workgroup: partial results of wavefronts that share a row tile's tokens, or two steps' V in bf16 as the second product's operands.
+// LDS of a workgroup: partial results of wavefronts that share a row tile's tokens, or a ring of steps and two steps' V in bf16 as the second
+// product's operands.
 struct Shares {
     float o[kWaves][16][kORow], m[kWaves][16], l[kWaves][16];
     int req[16];
 };
 constexpr int kRing = 4;
-struct Stage {  // a step's codes and scales as the lanes take them
+struct Stage {  // four blocks as they lie in the pool, 16 bytes in the order of the lanes that brought them
     u32x4 k[4][64], v[4][64];
-    uint32_t k_scale[64], v_scale[4][64];
+    uint32_t scale[4][64];  // K's 16 words, V's 16, and both again
 };
 struct Widened {
     Stage ring[kRing];
-    u32x4 v[2][2][8][64];  // [step % 2][half][dt][lane]
+    u32x4 v[2][16][64];  // [step % 2], a matrix instruction's operand each
 };
 union Lds {
     Shares s;
@@ -509,54 +513,98 @@ __device__ __forceinline__ void run_shared_tokens(const DecodeLaunch &a, const D
     }
 }
 
-// Items of more rows: RT row tiles a wavefront, which sees all tokens.  Codes and scales come through a ring in LDS, a quarter of a step by each
-// wavefront, three steps ahead: a workgroup's two steps in flight at most would be 4.4 MB on the chip, 2 TB/s.  V is widened once for all four:
-// wavefront w takes tokens 4 w .. 4 w + 3 of every block of the next step, 40 vector instructions instead of 152, and writes them where the
-// second product's operands are read, 16 bytes a lane.  One barrier a step: it waits for LDS, not for what is on its way from memory.
+// Items of more rows: a wavefront has rows of its own and sees all tokens.  Codes and scales come through a ring in LDS, a block of a step by each
+// wavefront, three steps ahead: a workgroup's two steps in flight at most would be 4.4 MB on the chip, 2 TB/s.  V is widened once for all four, by
+// wavefront w that of block w of the next step, 40 vector instructions instead of 152, and written where the second product's operands are read, 16 bytes a
+// lane.  One barrier a step: it waits for LDS, not for what is on its way from memory.
 __device__ __forceinline__ void load_to_lds4(const void *gptr, uint32_t lds_base) {
     asm volatile("s_mov_b32 m0, %1\n\ts_nop 0\n\tglobal_load_lds_dword %0, off" ::"v"(gptr), "s"(lds_base) : "memory");
 }
-template <int RT>
-__device__ __forceinline__ void run_shared_values(const DecodeLaunch &a, const DecodeItem &it, Widened &lds) {
-    const Reader rd(a, it);
-    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), rows = it.n_req * (a.num_q_heads / a.pool.num_kv_heads);
-    const int row0 = wave * (16 * RT), n_blk = (it.n_tokens + kStep - 1) / kStep;
-    const float c = exponent_factor(a.scale);
-    const bool active = row0 < rows;
-    const int half = wave >> 1;
-    constexpr int kLoads = 4;  // of a wavefront and step
-    auto issue = [&](const int (&id)[4], int b) {
-        const size_t kblk = rd.block(id, rd.m >> 2), vblk = rd.block(id, rd.g);
+struct RingReader {
+    const DecodeItem &it;
+    Widened &lds;
+    const uint8_t *k, *v, *scale;  // the pool's; of a lane's words of scales
+    const __attribute__((address_space(4))) int32_t *pages;  // (read by the scalar unit: a vector load would wait for the ring's loads in front of it)
+    uint32_t k_at, v_at, v_word;  // a lane's bytes of a block, its word of V's scales
+    int lane, wave, heads, last_page, t4;  // t4: of V it has tokens 4 t4 .. + 3, dims 8 (lane % 16) .. + 7
+    int id;  // the page of the block that comes next
+    u32x4 x;
+    uint32_t x_scale;
+    static constexpr int kLoads = 3;  // of a wavefront and step
+    __device__ __forceinline__ RingReader(const DecodeLaunch &a, const DecodeItem &it, Widened &lds, uint32_t k_at, int t4) : it(it), lds(lds), k_at(k_at), t4(t4) {
+        lane = (int)threadIdx.x & 63;
+        wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+        heads = a.pool.num_kv_heads;
+        last_page = (it.n_tokens - 1) >> 4;
+        k = static_cast<const uint8_t *>(a.pool.k_pages);
+        v = static_cast<const uint8_t *>(a.pool.v_pages);
+        scale = reinterpret_cast<const uint8_t *>(lane & 16 ? a.pool.v_scale : a.pool.k_scale) + 4 * (lane & 15);
+        pages = (const __attribute__((address_space(4))) int32_t *)(a.pages + it.page_off);
+        v_at = t4 * 256 + (lane & 15) * 16;
+        v_word = 16 + (lane >> 2 & 3) * 4 + t4;
+    }
+    __device__ __forceinline__ void page_of(int b) { id = pages[min(4 * b + wave, last_page)]; }  // clamped, so always in bounds
+    __device__ __forceinline__ void issue(int b) {
+        const size_t block = (size_t)id * heads + it.kv_head;
         const uint32_t to = lds_address(&lds.ring[b % kRing]);
-        load_to_lds16(rd.k + kblk * four::kCodeBytes + 256 * wave, to + (uint32_t)offsetof(Stage, k) + 1024 * wave);
-        load_to_lds16(rd.v + vblk * four::kCodeBytes + 256 * wave, to + (uint32_t)offsetof(Stage, v) + 1024 * wave);
-        load_to_lds4(rd.k_scale + kblk * four::kScaleBytes, to + (uint32_t)offsetof(Stage, k_scale));  // (the same by all four: as many loads for each)
-        load_to_lds4(rd.v_scale + vblk * four::kScaleBytes + 4 * wave, to + (uint32_t)offsetof(Stage, v_scale) + 256 * wave);
-    };
-    u32x4 v;
-    uint32_t v_scale;
-    auto clean = [&](int b) {  // slots behind the item's end, in this wavefront's share of step b
+        load_to_lds16(k + block * four::kCodeBytes, k_at, to + (uint32_t)offsetof(Stage, k) + 1024 * wave);
+        load_to_lds16(v + block * four::kCodeBytes, v_at, to + (uint32_t)offsetof(Stage, v) + 1024 * wave);
+        load_to_lds4(scale + block * four::kScaleBytes, to + (uint32_t)offsetof(Stage, scale) + 256 * wave);
+        page_of(b + 1);
+    }
+    __device__ __forceinline__ void clean(int b) {  // V's slots behind the item's end, in this wavefront's block of step b
         if ((b + 1) * kStep <= it.n_tokens) return;
         Stage &st = lds.ring[b % kRing];
-        u32x4 w = st.v[wave][rd.lane];
-        uint32_t sc = st.v_scale[wave][rd.lane];
-        clear_from(w, sc, it.n_tokens - (b * kStep + 16 * rd.g + 4 * wave));
-        st.v[wave][rd.lane] = w;
-        st.v_scale[wave][rd.lane] = sc;
-    };
-    auto take = [&](int b) {
-        v = lds.ring[b % kRing].v[wave][rd.lane];
-        v_scale = lds.ring[b % kRing].v_scale[wave][rd.lane];
-    };
-    auto widen_dims = [&](auto byte, int b) {  // dims 8 m + 2 B, + 1 of it
-        constexpr int B = decltype(byte)::value;
-        const uint32_t w[4] = {v[0], v[1], v[2], v[3]};
-        const float sc[4] = {four::scale_of(v_scale, 0), four::scale_of(v_scale, 1), four::scale_of(v_scale, 2), four::scale_of(v_scale, 3)};
-        char *to = reinterpret_cast<char *>(&lds.v[b & 1][half][0][rd.lane]) + 8 * (wave & 1);
+        u32x4 w = st.v[wave][lane];
+        uint32_t sc = st.scale[wave][v_word];
+        clear_from(w, sc, it.n_tokens - (b * kStep + 16 * wave + 4 * t4));
+        st.v[wave][lane] = w;
+        st.scale[wave][v_word] = sc;  // (four lanes the same)
+    }
+    __device__ __forceinline__ void take(int b) {
+        x = lds.ring[b % kRing].v[wave][lane];
+        x_scale = lds.ring[b % kRing].scale[wave][v_word];
+    }
+    template <int B>
+    __device__ __forceinline__ void widen(char *lo_to, char *hi_to) {  // dims 2 B, 2 B + 1 of the lane's eight
+        const uint32_t w[4] = {x[0], x[1], x[2], x[3]};
+        const float sc[4] = {four::scale_of(x_scale, 0), four::scale_of(x_scale, 1), four::scale_of(x_scale, 2), four::scale_of(x_scale, 3)};
         u32x2 lo, hi;
         widen_pairs<B>(w, sc, lo, hi);
-        *reinterpret_cast<u32x2 *>(to + (2 * B) * 1024) = lo;
-        *reinterpret_cast<u32x2 *>(to + (2 * B + 1) * 1024) = hi;
+        *reinterpret_cast<u32x2 *>(lo_to) = lo;
+        *reinterpret_cast<u32x2 *>(hi_to) = hi;
+    }
+    static __device__ __forceinline__ void barrier() { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); }
+    static __device__ __forceinline__ void landed() { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads * (kRing - 2)) : "memory"); }  // all but the last kRing - 2 steps requested
+    static __device__ __forceinline__ void all_landed() { asm volatile("s_waitcnt vmcnt(0)" ::: "memory"); }  // nothing may land in LDS that is another workgroup's by then
+    // What a wavefront without rows does, from the first step's V on.
+    template <class Widen>
+    __device__ __forceinline__ void serve(int n_blk, Widen &&widen_all) {
+        barrier();
+        for (int b = 0; b < n_blk; ++b) {
+            issue(b + kRing);
+            clean(b + 1);
+            take(b + 1);
+            widen_all(b + 1);
+            landed();
+            barrier();
+        }
+        all_landed();
+    }
+};
+
+// 33 to 64 rows, 16 a wavefront.
+__device__ __forceinline__ void run_rows(const DecodeLaunch &a, const DecodeItem &it, Widened &lds) {
+    const Reader rd(a, it);
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), rows = it.n_req * (a.num_q_heads / a.pool.num_kv_heads);
+    const int row0 = 16 * wave, n_blk = (it.n_tokens + kStep - 1) / kStep;
+    const float c = exponent_factor(a.scale);
+    // K's 16 bytes of token 4 tq + j and dims 32 dg lie at place 16 j + 4 ((block + dg) % 4) + tq, so that 16 lanes that differ in block and tq read 256 bytes of LDS
+    RingReader ring(a, it, lds, (rd.lane >> 4) * 256 + (rd.lane & 3) * 64 + ((rd.lane >> 2) - wave & 3) * 16, rd.lane >> 4);
+    auto widen_dims = [&](auto byte, int b) {
+        constexpr int B = decltype(byte)::value;
+        char *to = reinterpret_cast<char *>(&lds.v[b & 1][8 * (rd.lane >> 5) + 2 * B][16 * wave + (rd.lane & 15)]) + 8 * (rd.lane >> 4 & 1);
+        ring.widen<B>(to, to + 1024);
     };
     auto widen = [&](int b) {
         widen_dims(std::integral_constant<int, 0>{}, b);
@@ -564,127 +612,94 @@ __device__ __forceinline__ void run_shared_values(const DecodeLaunch &a, const D
         widen_dims(std::integral_constant<int, 2>{}, b);
         widen_dims(std::integral_constant<int, 3>{}, b);
     };
-    auto barrier = [] { asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory"); };
-    auto landed = [] { asm volatile("s_waitcnt vmcnt(%0)" ::"n"(kLoads * (kRing - 2)) : "memory"); };  // all but the last kRing - 2 steps requested
-    int id[4];
-    RowTile tile[RT];
-    u32x4 w[RT][4];
+    RowTile tile[1];
+    u32x4 w[1][4];
     find_rows(rd, row0, tile);
-    rd.ids(id, 0);
-    issue(id, 0);
+    ring.page_of(0);
+    ring.issue(0);
     load_rows(rd, row0, tile, w);
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-    for (int b = 1; b < kRing; ++b) {
-        rd.ids(id, b);
-        issue(id, b);
-    }
-    rd.ids(id, kRing);
+    for (int b = 1; b < kRing; ++b) ring.issue(b);
     begin_rows(rd, tile, w);
-    landed();
-    clean(0);
-    take(0);
+    ring.landed();
+    ring.clean(0);
+    ring.take(0);
     widen(0);
-    barrier();
-    if (!active) {
-        barrier();
-        for (int b = 0; b < n_blk; ++b) {
-            issue(id, b + kRing);
-            rd.ids(id, b + kRing + 1);
-            clean(b + 1);
-            take(b + 1);
-            widen(b + 1);
-            landed();
-            barrier();
-        }
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        return;
-    }
+    ring.barrier();
+    if (row0 >= rows) return ring.serve(n_blk, widen);
+    RowTile &t = tile[0];
+    auto keys = [&](int b, u32x4 (&k)[4]) {
+        const Stage &st = lds.ring[b % kRing];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) k[j] = st.k[rd.m >> 2][16 * j + 4 * ((rd.m >> 2) + rd.g & 3) + (rd.m & 3)];
+        return st.scale[rd.m >> 2][4 * rd.g + (rd.m & 3)];
+    };
     // Matrix instructions and those of the softmax do not overlap between wavefronts of a SIMD by themselves (the sum of both was the kernel's time), so
     // each wavefront mixes its own: the first product of step b + 1 and the second of step b with the exponentials of step b and V's widening.
-    auto first_product = [&](f32x4 (&acc)[RT][4], int b) {
-        const Stage &st = lds.ring[b % kRing];
+    f32x4 acc0[1][4], acc1[1][4];
+    u32x4 pw[2];
+    float top[1];
+    {
         Operands x;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) x.k[j] = st.k[j][rd.lane];
-        x.k_scale = st.k_scale[rd.lane];
-        scores(x, tile, acc);
-    };
-    f32x4 acc0[RT][4], acc1[RT][4];
-    u32x4 pw[RT][2];
-    float top[RT];
-    first_product(acc0, 0);
+        x.k_scale = keys(0, x.k);
+        scores(x, tile, acc0);
+    }
     hide(rd, tile, acc0, 16 * rd.g);
     tops(acc0, top);
     follow(tile, top, c);
-    barrier();  // all are done with K of step 0
-    auto step = [&](f32x4 (&now)[RT][4], f32x4 (&next)[RT][4], int b) {
-        const Stage &st = lds.ring[(b + 1) % kRing];
+    ring.barrier();  // all are done with K of step 0
+    auto step = [&](f32x4 (&now)[1][4], f32x4 (&next)[1][4], int b) {
         u32x4 k[4], va[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) k[j] = st.k[j][rd.lane];
-        const uint32_t k_scale = st.k_scale[rd.lane];
+        const uint32_t k_scale = keys(b + 1, k);
         __builtin_amdgcn_sched_barrier(0);
-        issue(id, b + kRing);  // where step b was: its keys and values left in step b - 1
-        rd.ids(id, b + kRing + 1);
-        clean(b + 1);  // (behind the last step: of no use, and of no harm)
-        // every chunk up to a sched_barrier: matrix instructions (32 cycles each of the first product, 16 of the second) and about as many cycles of others
-        float mc[RT], sum[RT];
+        ring.issue(b + kRing);  // where step b was: its keys and values left in step b - 1
+        ring.clean(b + 1);      // (behind the last step: of no use, and of no harm)
+        // every chunk up to a sched_barrier: a matrix instruction (32 cycles of the first product, 16 of the second) and about as many cycles of others
+        const float mc = t.m == -INFINITY ? 0.f : t.m * c;
+        float sum = 0.f;
 #pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            mc[r] = tile[r].m == -INFINITY ? 0.f : tile[r].m * c;
-            sum[r] = 0.f;
-#pragma unroll
-            for (int t4 = 0; t4 < 4; ++t4) next[r][t4] = f32x4{0.f, 0.f, 0.f, 0.f};
-        }
-        auto weigh_pair = [&](int i) {  // probabilities of two neighbouring tokens of a row, those of the second product's first half first
-            const int hf = i / (4 * RT), r = i / 4 % RT, j = 8 * hf + 2 * (i % 4);
-            const float p0 = fast_exp2(__builtin_fmaf(now[r][j & 3][j >> 2], c, -mc[r])), p1 = fast_exp2(__builtin_fmaf(now[r][(j + 1) & 3][(j + 1) >> 2], c, -mc[r]));
-            sum[r] += p0 + p1;
-            pw[r][hf][i % 4] = pack_bf16(p0, p1);
+        for (int t4 = 0; t4 < 4; ++t4) next[0][t4] = f32x4{0.f, 0.f, 0.f, 0.f};
+        auto weigh_pair = [&](int i) {  // probabilities of two neighbouring tokens, those of the second product's first half first
+            const int j = 2 * i;
+            const float p0 = fast_exp2(__builtin_fmaf(now[0][j & 3][j >> 2], c, -mc)), p1 = fast_exp2(__builtin_fmaf(now[0][(j + 1) & 3][(j + 1) >> 2], c, -mc));
+            sum += p0 + p1;
+            pw[i >> 2][i & 3] = pack_bf16(p0, p1);
         };
-        constexpr int kFirst = 5 * RT;  // pairs beside the first product
+        constexpr int kFirst = 5;  // pairs beside the first product
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < 8 * RT; ++i) {
-            const int lo = i / (4 * RT), r = i / 4 % RT, t4 = i % 4;
-            const i32x8 q = lo ? tile[r].lo : tile[r].hi;
-            f32x4 &to = next[r][t4];
-            to = t4 == 0 ? mfma_four<0>(k[0], q, to, k_scale, tile[r].q_scale) : t4 == 1 ? mfma_four<1>(k[1], q, to, k_scale, tile[r].q_scale)
-               : t4 == 2 ? mfma_four<2>(k[2], q, to, k_scale, tile[r].q_scale) : mfma_four<3>(k[3], q, to, k_scale, tile[r].q_scale);
+        for (int i = 0; i < 8; ++i) {
+            const i32x8 q = i >= 4 ? t.lo : t.hi;
+            f32x4 &to = next[0][i & 3];
+            to = (i & 3) == 0 ? mfma_four<0>(k[0], q, to, k_scale, t.q_scale) : (i & 3) == 1 ? mfma_four<1>(k[1], q, to, k_scale, t.q_scale)
+               : (i & 3) == 2 ? mfma_four<2>(k[2], q, to, k_scale, t.q_scale) : mfma_four<3>(k[3], q, to, k_scale, t.q_scale);
 #pragma unroll
-            for (int p = kFirst * i / (8 * RT); p < kFirst * (i + 1) / (8 * RT); ++p) weigh_pair(p);
-            if (i >= 8 * RT - 4) va[i - (8 * RT - 4)] = lds.v[b & 1][0][i - (8 * RT - 4)][rd.lane];
+            for (int p = kFirst * i / 8; p < kFirst * (i + 1) / 8; ++p) weigh_pair(p);
+            if (i >= 4) va[i - 4] = lds.v[b & 1][i - 4][rd.lane];
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
-            const int hf = i >> 3, dt = i & 7;
-            const bf16x8 v8 = as_bf16x8(va[i & 3]);
-#pragma unroll
-            for (int r = 0; r < RT; ++r) tile[r].o[dt] = mfma16(v8, as_bf16x8(pw[r][hf]), tile[r].o[dt]);
-            if (i == 2) take(b + 1);
-            if (i + 4 < 16) va[i & 3] = lds.v[b & 1][(i + 4) >> 3][(i + 4) & 7][rd.lane];
+            t.o[i & 7] = mfma16(as_bf16x8(va[i & 3]), as_bf16x8(pw[i >> 3]), t.o[i & 7]);
+            if (i == 2) ring.take(b + 1);
+            if (i + 4 < 16) va[i & 3] = lds.v[b & 1][i + 4][rd.lane];
             if (i < 8) {
-                constexpr int kRest = 8 * RT - kFirst;
 #pragma unroll
-                for (int p = kFirst + kRest * i / 8; p < kFirst + kRest * (i + 1) / 8; ++p) weigh_pair(p);
+                for (int p = kFirst + (8 - kFirst) * i / 8; p < kFirst + (8 - kFirst) * (i + 1) / 8; ++p) weigh_pair(p);
             } else if (i % 2 == 0) {
                 i == 8 ? widen_dims(std::integral_constant<int, 0>{}, b + 1) : i == 10 ? widen_dims(std::integral_constant<int, 1>{}, b + 1)
                 : i == 12 ? widen_dims(std::integral_constant<int, 2>{}, b + 1) : widen_dims(std::integral_constant<int, 3>{}, b + 1);
             }
             __builtin_amdgcn_sched_barrier(0);
         }
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            asm volatile("" : "+v"(sum[r]));
-            tile[r].l += sum[r];
-        }
+        asm volatile("" : "+v"(sum));
+        t.l += sum;
         hide(rd, tile, next, (b + 1) * kStep + 16 * rd.g);
         tops(next, top);
         follow(tile, top, c);
-        landed();  // the share of step b + 2; of all wavefronts behind the barrier
-        barrier();
+        ring.landed();  // the share of step b + 2; of all wavefronts behind the barrier
+        ring.barrier();
     };
     for (int b = 0;;) {
         step(acc0, acc1, b);
@@ -692,8 +707,225 @@ __device__ __forceinline__ void run_shared_values(const DecodeLaunch &a, const D
         step(acc1, acc0, b);
         if (++b >= n_blk) break;
     }
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");  // nothing may land in LDS that is another workgroup's by then
+    ring.all_landed();
     write_rows(rd, row0, c, tile);
+}
+
+// Items of more than 64 rows: 32 a wavefront, which sees all tokens, by the 32x32 forms of both instructions.  Beside one of those another wavefront issues
+// more vector instructions than beside two of the 16x16 forms (measured: three quarters of the time beside the first product's, against a half).
+//   S^T  v_mfma_scale_f32_32x32x64_f8f6f4: row r of tile T is token 32 T + r of the step; lane (r, h) brings dims 64 kk + 32 h .. + 31 of it, and of query
+//        row r dims 64 kk + 16 h .. + 15 and 64 kk + 32 + 16 h .. + 15.  It ends up with tokens 32 T + 8 (i / 4) + 4 h + i % 4 of its row.
+//   O^T  v_mfma_f32_32x32x16_bf16: the tokens of block B that a lane has are 4 h .. + 3 and 8 + 4 h .. + 3, so those are what it brings of V for
+//        dims 8 (m % 16) + 2 dt + m / 16 of tile dt.
+// V is widened by wavefront w for block w, 4 tokens and 8 dims a lane.
+struct TallRows {
+    i32x8 q[2][2];  // [kk][term]
+    uint32_t q_scale;
+    f32x16 o[4];
+    float m, l;
+    int req, lim;
+};
+__device__ __forceinline__ float half_max(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+__device__ __forceinline__ float half_sum(float x) {
+    const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+    return __uint_as_float(r[0]) + __uint_as_float(r[1]);
+}
+__device__ __forceinline__ f32x16 mfma_four_tall(u32x4 k, i32x8 q, f32x16 c, uint32_t k_scale, uint32_t q_scale) {
+    const i32x8 a = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, q, c, 4, 0, 0, k_scale, 0, q_scale);
+}
+__device__ __forceinline__ void run_tall(const DecodeLaunch &a, const DecodeItem &it, Widened &lds) {
+    const int lane = (int)threadIdx.x & 63, r = lane & 31, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int G = a.num_q_heads / a.pool.num_kv_heads, rows = it.n_req * G, row0 = 32 * wave, row = min(row0 + r, rows - 1), n_blk = (it.n_tokens + kStep - 1) / kStep;
+    const float c = exponent_factor(a.scale);
+    // K's 16 bytes of token t and dims 32 dg lie at place 16 dg + t
+    RingReader ring(a, it, lds, (lane & 3) * 256 + (lane >> 2 & 3) * 64 + (lane >> 4) * 16, (lane >> 4 & 1) * 2 + h);
+    auto widen_dims = [&](auto byte, int b) {
+        constexpr int B = decltype(byte)::value;
+        char *to = reinterpret_cast<char *>(&lds.v[b & 1][4 * wave + B][32 * h + (lane & 15)]) + 8 * (lane >> 4 & 1);
+        ring.widen<B>(to, to + 256);
+    };
+    auto widen = [&](int b) {
+        widen_dims(std::integral_constant<int, 0>{}, b);
+        widen_dims(std::integral_constant<int, 1>{}, b);
+        widen_dims(std::integral_constant<int, 2>{}, b);
+        widen_dims(std::integral_constant<int, 3>{}, b);
+    };
+    TallRows x;
+    x.req = a.node_req_idx[it.req_off + row / G];
+    ring.page_of(0);
+    ring.issue(0);
+    u32x4 w[8];  // dims 64 kk + 32 p + 16 h + 8 e, [4 kk + 2 p + e]
+    {
+        const int q_row = a.q_rows ? a.q_rows[x.req] : x.req;
+        const char *qp = static_cast<const char *>(a.q) + ((size_t)q_row * a.num_q_heads + it.kv_head * G + row % G) * (kHeadDim * 2) + 32 * h;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) w[i] = ld16(qp + 64 * (i >> 1) + 16 * (i & 1));
+    }
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int b = 1; b < kRing; ++b) ring.issue(b);
+    {  // the row as two e4m3 terms, as in split_row
+        float top = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i][j] << 16)), fabsf(__uint_as_float(w[i][j] & 0xFFFF0000u))));
+        const float up = row_factor(half_max(top), a.scale, x.q_scale);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {  // four dims each
+            const uint32_t w0 = w[i >> 1][2 * (i & 1)], w1 = w[i >> 1][2 * (i & 1) + 1];
+            int hi, lo;
+            split_four(w0, w1, up, hi, lo);
+            x.q[i >> 3][0][i & 7] = hi;
+            x.q[i >> 3][1][i & 7] = lo;
+        }
+    }
+    x.lim = a.row_leaf && a.row_leaf[x.req] == it.node ? a.row_limit[x.req] - it.tok_begin : it.n_tokens;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) x.o[dt][i] = 0.f;
+    x.m = -INFINITY;
+    x.l = 0.f;
+    ring.landed();
+    ring.clean(0);
+    ring.take(0);
+    widen(0);
+    ring.barrier();
+    if (row0 >= rows) return ring.serve(n_blk, widen);
+    auto hide_tall = [&](f32x16 (&acc)[2], int tok0) {
+        if (__builtin_amdgcn_ballot_w64(tok0 + kStep > x.lim)) {  // some row does not see the whole step, the item's last one among them
+            const bool last = a.row_leaf && a.row_leaf[x.req] == it.node;
+            const unsigned long long vis = last ? a.row_mask[x.req] : 0ull;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int d0 = tok0 + 8 * j + 4 * h - x.lim;
+                const uint32_t seen = d0 < 0 ? (d0 <= -4 ? 0xFu : (1u << -d0) - 1u | (uint32_t)vis << -d0) : d0 < 64 ? (uint32_t)(vis >> d0) : 0u;
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[j >> 2][4 * (j & 3) + i] = (seen >> i & 1u) ? acc[j >> 2][4 * (j & 3) + i] : -INFINITY;
+            }
+        }
+    };
+    auto follow_tall = [&](const f32x16 (&acc)[2]) {
+        float top = acc[0][0];
+#pragma unroll
+        for (int i = 1; i < 32; ++i) top = fmaxf(top, acc[i >> 4][i & 15]);
+        if (__builtin_amdgcn_ballot_w64((top - x.m) * c > kSlack)) {
+            const float m_new = fmaxf(x.m, half_max(top));
+            const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((x.m - m_new) * c);
+            x.m = m_new;
+            x.l *= alpha;
+#pragma unroll
+            for (int dt = 0; dt < 4; ++dt) x.o[dt] *= alpha;
+        }
+    };
+    const uint8_t *scale_at = reinterpret_cast<const uint8_t *>(&lds.ring[0].scale[0][0]) + (r >> 4) * 256 + 16 * h + (r & 15);
+    auto keys = [&](int b, u32x4 (&k)[4], uint32_t (&ks)[4]) {  // [2 kk + T]
+        const Stage &st = lds.ring[b % kRing];
+        const uint8_t *sp = scale_at + (b % kRing) * sizeof(Stage);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            k[i] = st.k[2 * (i & 1) + (r >> 4)][16 * (2 * (i >> 1) + h) + (r & 15)];
+            ks[i] = sp[512 * (i & 1) + 32 * (i >> 1)];
+        }
+    };
+    f32x16 acc0[2], acc1[2];
+    u32x4 pw[4];
+    {
+        u32x4 k[4];
+        uint32_t ks[4];
+        keys(0, k, ks);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc0[0][i] = acc0[1][i] = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) acc0[i & 1] = mfma_four_tall(k[i & 3], x.q[i >> 1 & 1][i >> 2], acc0[i & 1], ks[i & 3], x.q_scale);
+    }
+    hide_tall(acc0, 0);
+    follow_tall(acc0);
+    ring.barrier();  // all are done with K of step 0
+    auto step = [&](f32x16 (&now)[2], f32x16 (&next)[2], int b) {
+        u32x4 k[4], va[4];
+        uint32_t ks[4];
+        keys(b + 1, k, ks);
+        __builtin_amdgcn_sched_barrier(0);
+        ring.issue(b + kRing);  // where step b was: its keys and values left in step b - 1
+        ring.clean(b + 1);      // (behind the last step: of no use, and of no harm)
+        const float mc = x.m == -INFINITY ? 0.f : x.m * c;
+        float sum = 0.f;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) next[0][i] = next[1][i] = 0.f;
+        auto weigh_pair = [&](int p) {  // probabilities of two neighbouring tokens, in the order in which the second product takes them
+            const int at = 8 * (p >> 2 & 1) + 2 * (p & 3);
+            const float p0 = fast_exp2(__builtin_fmaf(now[p >> 3][at], c, -mc)), p1 = fast_exp2(__builtin_fmaf(now[p >> 3][at + 1], c, -mc));
+            sum += p0 + p1;
+            pw[p >> 2][p & 3] = pack_bf16(p0, p1);
+        };
+        // every chunk up to a sched_barrier: a matrix instruction (64 cycles of the first product, 32 of the second) and what fits beside it
+        constexpr int kFirst = 11;  // pairs beside the first product
+        __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            next[i & 1] = mfma_four_tall(k[i & 3], x.q[i >> 1 & 1][i >> 2], next[i & 1], ks[i & 3], x.q_scale);
+#pragma unroll
+            for (int p = kFirst * i / 8; p < kFirst * (i + 1) / 8; ++p) weigh_pair(p);
+            if (i >= 4) va[i - 4] = lds.v[b & 1][i - 4][lane];
+            __builtin_amdgcn_sched_barrier(0);
+        }
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            x.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(va[i & 3]), as_bf16x8(pw[i >> 2]), x.o[i & 3], 0, 0, 0);
+            if (i == 2) ring.take(b + 1);
+            if (i + 4 < 16) va[i & 3] = lds.v[b & 1][i + 4][lane];
+            if (i < 5) {
+                if (kFirst + i < 16) weigh_pair(kFirst + i);
+            } else if (i % 2 == 0 && i >= 8) {
+                i == 8 ? widen_dims(std::integral_constant<int, 0>{}, b + 1) : i == 10 ? widen_dims(std::integral_constant<int, 1>{}, b + 1)
+                : i == 12 ? widen_dims(std::integral_constant<int, 2>{}, b + 1) : widen_dims(std::integral_constant<int, 3>{}, b + 1);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
+        asm volatile("" : "+v"(sum));
+        x.l += sum;
+        hide_tall(next, (b + 1) * kStep);
+        follow_tall(next);
+        ring.landed();  // the share of step b + 2; of all wavefronts behind the barrier
+        ring.barrier();
+    };
+    for (int b = 0;;) {
+        step(acc0, acc1, b);
+        if (++b >= n_blk) break;
+        step(acc1, acc0, b);
+        if (++b >= n_blk) break;
+    }
+    ring.all_landed();
+    const float l_row = half_sum(x.l), inv = l_row > 0.f ? 1.0f / l_row : 0.f;
+    float top = 0.f;
+#pragma unroll
+    for (int dt = 0; dt < 4; ++dt) {
+        x.o[dt] *= inv;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top = fmaxf(top, fabsf(x.o[dt][i]));
+    }
+    float up, down;
+    part_factors(half_max(top), up, down);
+    if (row0 + r >= rows) return;
+    const size_t part = part_of(a, it, x.req, row);
+    uint16_t *out = a.o_parts + part * kHeadDim + 32 * h;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        u32x4 word;
+#pragma unroll
+        for (int dt = 0; dt < 4; ++dt) word[dt] = pack_f16(x.o[dt][i] * up, x.o[dt][i + 8] * up);
+        *reinterpret_cast<u32x4 *>(out + 64 * (i >> 2) + 8 * (i & 3)) = word;
+    }
+    if (h == 0) {
+        a.down_parts[part] = down;
+        a.lse_parts[part] = partial_lse(l_row == l_row ? x.m * c : INFINITY, l_row);
+    }
 }
 
 // Items [0, n_single) get a workgroup each, the items behind them (at most 16 rows) one for four, a wavefront each (no LDS, no barrier), in the plan's order
@@ -726,9 +958,9 @@ __global__ __launch_bounds__(kWaves * 64, 2) void four_decode_kernel(DecodeLaunc
     else if (rows <= 32)
         run_shared_tokens<2>(a, it, lds.s);
     else if (rows <= 64)
-        run_shared_values<1>(a, it, lds.w);
+        run_rows(a, it, lds.w);
     else
-        run_shared_values<2>(a, it, lds.w);
+        run_tall(a, it, lds.w);
 }
 
 }  // namespace
