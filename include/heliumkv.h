@@ -90,10 +90,12 @@ enum {
  * of fp32 inputs is 1e-4).
  * fp32 block format: K in 64-byte chunks of 16 floats ((d/16)*256 + slot*16 + d%16), V
  * dimension-major (d*16 + slot).
- * fp4 pools hold a token in 136 bytes per KV head (bf16 512, fp8 256): bf16 sources, q and out, as bf16 pools; attention over
- * one equals attention over a bf16 pool that holds the same values (code * scale is a bf16 number) up to the order of sums.  Their decode plans
- * know the settings leaf_chunk, shared_chunk and max_rows of the planner's, and run all nodes as items of up to 64 query
- * rows (no tiles, no whole paths); prefill widens the batch's pages into workspace first, as over fp8 pools. */
+ * fp4 pools hold a token in 136 bytes per KV head (bf16 512, fp8 256): bf16 sources, q and out, as bf16 pools.  Attention over one
+ * equals attention over a bf16 pool that holds the same values (code * scale is a bf16 number) up to the order of sums; in decode, elements of
+ * q below 2^-9 of their row's largest count to 2^-17 of that, and a score's products below about 2^-16 of its largest are cut off.
+ * Decode plans over fp4 pools run all nodes as items of up to 128 query rows (no tiles, no whole paths); of the planner's settings they know
+ * leaf_chunk, shared_chunk, max_rows, pack (1 and 3) and interleave (-1).  Prefill widens the batch's pages into workspace first, as over fp8
+ * pools. */
 enum { HKV_BF16 = 0, HKV_FP8_E4M3 = 1, HKV_FP32 = 2, HKV_FP4_E2M1 = 3 };
 
 typedef struct hkv_pool hkv_pool;
@@ -405,7 +407,7 @@ typedef struct {
     int32_t leaf_chunk;       /* tokens per item of nodes read by at most 16 query rows; multiple of 16 */
     int32_t shared_chunk;     /* tokens per item of nodes shared by more rows; multiple of 16, at most 2048 (default: by
                                  the estimated step, 128 to 2048) */
-    int32_t max_rows;         /* query rows per item of such nodes: 16..64 */
+    int32_t max_rows;         /* query rows per item of such nodes: 16..64 (fp4 pools: 16..128) */
     int32_t pack;             /* four short items per workgroup, one per wavefront: 1 never, 2 when the forest has
                                  more items than the chip holds at once (the default), 3 always */
     int32_t pack_tokens;      /* longest item of that mode, tokens */

@@ -1408,12 +1408,12 @@ static int build_fp32_rows(hkv_decode_plan &pl, bool upload) {
 constexpr uint32_t kPlanRowVisibility = 0x40000000u;
 
 // the planner's settings, each 0 (the library's choice) or inside its documented range
-static int check_plan_settings(const hkv_decode_plan_params *o) {
+static int check_plan_settings(const hkv_decode_plan_params *o, const hkv_pool *pool) {
     if (!o) return HKV_OK;
     auto bad = [](const char *name, int32_t v) { return fail(HKV_EINVAL, "hkv_decode_plan_create_ex: %s = %d is out of range", name, v); };
     if (o->leaf_chunk < 0 || o->leaf_chunk % 16) return bad("leaf_chunk", o->leaf_chunk);
     if (o->shared_chunk < 0 || o->shared_chunk % 16 || o->shared_chunk > kMaxSharedItemTokens) return bad("shared_chunk", o->shared_chunk);
-    if (o->max_rows != 0 && (o->max_rows < 16 || o->max_rows > 64)) return bad("max_rows", o->max_rows);
+    if (o->max_rows != 0 && (o->max_rows < 16 || o->max_rows > (pool && pool->d.dtype == HKV_FP4_E2M1 ? 128 : 64))) return bad("max_rows", o->max_rows);
     if (o->pack < 0 || o->pack > 3) return bad("pack", o->pack);
     if (o->pack_tokens < 0) return bad("pack_tokens", o->pack_tokens);
     if (o->stages != 0 && (o->stages < 3 || o->stages > 5)) return bad("stages", o->stages);
@@ -1433,7 +1433,7 @@ static int create_decode_plan(hkv_pool *pool, const hkv_node *nodes, int32_t n_n
                               hkv_decode_plan **out, int32_t tokens_per_req = 1) {
     if (!pool || !out) return fail(HKV_EINVAL, "hkv_decode_plan_create: null argument");
     *out = nullptr;
-    if (int rc = check_plan_settings(opt)) return rc;
+    if (int rc = check_plan_settings(opt, pool)) return rc;
     const int Hkv = pool->d.num_kv_heads;
     if (num_q_heads <= 0 || num_q_heads % Hkv || num_q_heads / Hkv > 16)
         return fail(HKV_ESHAPE, "hkv_decode_plan_create: %d query heads over %d KV heads", num_q_heads, Hkv);

@@ -195,11 +195,12 @@ __device__ __forceinline__ void scores(const Operands &x, const RowTile (&tile)[
 
 // Scores of tokens that a row does not see are -inf; tok0: of the lane's 16 tokens the first, score j of a row is acc[j % 4][j / 4].
 template <int RT>
-__device__ __forceinline__ void hide(const Reader &rd, const RowTile (&tile)[RT], f32x4 (&acc)[RT][4], int tok0) {
+__device__ __forceinline__ bool hide(const Reader &rd, const RowTile (&tile)[RT], f32x4 (&acc)[RT][4], int tok0) {
     int most = -INT_MAX;  // tokens of the step behind what a row sees at once
 #pragma unroll
     for (int r = 0; r < RT; ++r) most = max(most, tok0 - tile[r].lim);
-    if (__builtin_amdgcn_ballot_w64(most > -16)) {  // some row does not see the whole step, the item's last one among them
+    const bool some = __builtin_amdgcn_ballot_w64(most > -16);  // some row does not see the whole step, the item's last one among them
+    if (some) {
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             const bool last = rd.a.row_leaf && rd.a.row_leaf[tile[r].req] == rd.it.node;  // (looked up here: this is the exception)
@@ -210,62 +211,58 @@ __device__ __forceinline__ void hide(const Reader &rd, const RowTile (&tile)[RT]
             for (int j = 0; j < 16; ++j) acc[r][j & 3][j >> 2] = (seen >> j & 1u) ? acc[r][j & 3][j >> 2] : -INFINITY;
         }
     }
+    return some;
 }
-// The largest of the lane's scores of each row.
-template <int RT>
-__device__ __forceinline__ void tops(const f32x4 (&acc)[RT][4], float (&top)[RT]) {
+// A row's reference, of which its weights are powers: it stays until they would be large.  One that is the largest score of every step so far moves for some
+// row of 32 nearly always, 66 instructions of a step's 450.
+__device__ __forceinline__ void follow(RowTile &t, float top, float c) {
+    const float m_new = fmaxf(t.m, rows_max(top));
+    const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((t.m - m_new) * c);
+    t.m = m_new;
+    t.l *= alpha;
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        top[r] = acc[r][0][0];
-#pragma unroll
-        for (int j = 1; j < 16; ++j) top[r] = fmaxf(top[r], acc[r][j & 3][j >> 2]);
-    }
+    for (int dt = 0; dt < 8; ++dt) t.o[dt] *= alpha;
 }
-// A row's reference stays until a score exceeds it by more than 2^kSlack in weight: with a maximum that follows every step some row of 32 moves nearly
-// always, 66 instructions of a step's 450.
-constexpr float kSlack = 8.f;
-template <int RT>
-__device__ __forceinline__ void follow(RowTile (&tile)[RT], const float (&top)[RT], float c) {
-    bool beyond = false;
-#pragma unroll
-    for (int r = 0; r < RT; ++r) beyond = beyond || (top[r] - tile[r].m) * c > kSlack;  // (-inf - -inf: no)
-    if (__builtin_amdgcn_ballot_w64(beyond)) {
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            RowTile &t = tile[r];
-            const float m_new = fmaxf(t.m, rows_max(top[r]));
-            const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((t.m - m_new) * c);
-            t.m = m_new;
-            t.l *= alpha;
-#pragma unroll
-            for (int dt = 0; dt < 8; ++dt) t.o[dt] *= alpha;
-        }
-    }
-}
+// Where the scores are at hand until all weights are made, those tell: a lane's of a step sum up to more than kMostWeight (8 instructions a row tile fewer than
+// the largest score).  Elsewhere a score beyond the reference by a weight of 2^kSlack does.
+constexpr float kMostWeight = 16384.f, kSlack = 8.f;
 // Probabilities, rounded to bf16, half a step of 2^-8 each, as over the other pools.
 template <int RT>
-__device__ __forceinline__ void weigh(RowTile (&tile)[RT], const f32x4 (&acc)[RT][4], float c, u32x4 (&pw)[RT][2]) {
+__device__ __forceinline__ void weigh(const RowTile (&tile)[RT], const f32x4 (&acc)[RT][4], float c, u32x4 (&pw)[RT][2], float (&sum)[RT]) {
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const float mc = tile[r].m == -INFINITY ? 0.f : tile[r].m * c;  // (a row that has seen nothing: no inf - inf)
-        float sum = 0.f, p[16];
+        float p[16];
+        sum[r] = 0.f;
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
             p[j] = fast_exp2(__builtin_fmaf(acc[r][j & 3][j >> 2], c, -mc));
-            sum += p[j];
+            sum[r] += p[j];
         }
-        tile[r].l += sum;
 #pragma unroll
         for (int j = 0; j < 8; ++j) pw[r][j >> 2][j & 3] = pack_bf16(p[2 * j], p[2 * j + 1]);
     }
 }
 template <int RT>
 __device__ __forceinline__ void weights(const Reader &rd, RowTile (&tile)[RT], f32x4 (&acc)[RT][4], int tok0, float c, u32x4 (&pw)[RT][2]) {
-    float top[RT];
+    float sum[RT];
     hide(rd, tile, acc, tok0);
-    tops(acc, top);
-    follow(tile, top, c);
-    weigh(tile, acc, c, pw);
+    weigh(tile, acc, c, pw, sum);
+    bool any = false;
+#pragma unroll
+    for (int r = 0; r < RT; ++r) any = any || !(sum[r] <= kMostWeight) || tile[r].m == -INFINITY;  // (a NaN, too)
+    if (__builtin_amdgcn_ballot_w64(any)) {
+#pragma unroll
+        for (int r = 0; r < RT; ++r) {
+            float top = acc[r][0][0];
+#pragma unroll
+            for (int j = 1; j < 16; ++j) top = fmaxf(top, acc[r][j & 3][j >> 2]);
+            follow(tile[r], top, c);
+        }
+        weigh(tile, acc, c, pw, sum);
+    }
+#pragma unroll
+    for (int r = 0; r < RT; ++r) tile[r].l += sum[r];
 }
 
 // Two dims (8 m + 2 B, + 1) of tokens 0 .. 3 from their words and scales: lo, hi [tokens 0 1 | 2 3].
@@ -601,16 +598,16 @@ __device__ __forceinline__ void run_rows(const DecodeLaunch &a, const DecodeItem
     const float c = exponent_factor(a.scale);
     // K's 16 bytes of token 4 tq + j and dims 32 dg lie at place 16 j + 4 ((block + dg) % 4) + tq, so that 16 lanes that differ in block and tq read 256 bytes of LDS
     RingReader ring(a, it, lds, (rd.lane >> 4) * 256 + (rd.lane & 3) * 64 + ((rd.lane >> 2) - wave & 3) * 16, rd.lane >> 4);
-    auto widen_dims = [&](auto byte, int b) {
+    auto widen_dims = [&](auto byte, int parity) {
         constexpr int B = decltype(byte)::value;
-        char *to = reinterpret_cast<char *>(&lds.v[b & 1][8 * (rd.lane >> 5) + 2 * B][16 * wave + (rd.lane & 15)]) + 8 * (rd.lane >> 4 & 1);
+        char *to = reinterpret_cast<char *>(&lds.v[parity][8 * (rd.lane >> 5) + 2 * B][16 * wave + (rd.lane & 15)]) + 8 * (rd.lane >> 4 & 1);
         ring.widen<B>(to, to + 1024);
     };
     auto widen = [&](int b) {
-        widen_dims(std::integral_constant<int, 0>{}, b);
-        widen_dims(std::integral_constant<int, 1>{}, b);
-        widen_dims(std::integral_constant<int, 2>{}, b);
-        widen_dims(std::integral_constant<int, 3>{}, b);
+        widen_dims(std::integral_constant<int, 0>{}, b & 1);
+        widen_dims(std::integral_constant<int, 1>{}, b & 1);
+        widen_dims(std::integral_constant<int, 2>{}, b & 1);
+        widen_dims(std::integral_constant<int, 3>{}, b & 1);
     };
     RowTile tile[1];
     u32x4 w[1][4];
@@ -639,25 +636,34 @@ __device__ __forceinline__ void run_rows(const DecodeLaunch &a, const DecodeItem
     // each wavefront mixes its own: the first product of step b + 1 and the second of step b with the exponentials of step b and V's widening.
     f32x4 acc0[1][4], acc1[1][4];
     u32x4 pw[2];
-    float top[1];
+    auto most = [](const f32x4 (&acc)[1][4], int j, float top) { return fmaxf(fmaxf(top, acc[0][j & 3][j >> 2]), acc[0][(j + 1) & 3][(j + 1) >> 2]); };
+    auto settle = [&](f32x4 (&acc)[1][4], int b, float top) {  // scores of step b are what weights can be made of
+        if (hide(rd, tile, acc, b * kStep + 16 * rd.g)) {
+            top = -INFINITY;
+#pragma unroll
+            for (int j = 0; j < 16; j += 2) top = most(acc, j, top);
+        }
+        if (__builtin_amdgcn_ballot_w64((top - t.m) * c > kSlack)) follow(t, top, c);  // (-inf - -inf: no)
+    };
     {
         Operands x;
         x.k_scale = keys(0, x.k);
         scores(x, tile, acc0);
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 16; j += 2) top = most(acc0, j, top);
+        settle(acc0, 0, top);
     }
-    hide(rd, tile, acc0, 16 * rd.g);
-    tops(acc0, top);
-    follow(tile, top, c);
     ring.barrier();  // all are done with K of step 0
-    auto step = [&](f32x4 (&now)[1][4], f32x4 (&next)[1][4], int b) {
+    auto step = [&](f32x4 (&now)[1][4], f32x4 (&next)[1][4], int b, auto parity) {
+        constexpr int P = decltype(parity)::value;
         u32x4 k[4], va[4];
+        ring.clean(b + 1);  // (behind the last step: of no use, and of no harm)
         const uint32_t k_scale = keys(b + 1, k);
         __builtin_amdgcn_sched_barrier(0);
-        ring.issue(b + kRing);  // where step b was: its keys and values left in step b - 1
-        ring.clean(b + 1);      // (behind the last step: of no use, and of no harm)
         // every chunk up to a sched_barrier: a matrix instruction (32 cycles of the first product, 16 of the second) and about as many cycles of others
         const float mc = t.m == -INFINITY ? 0.f : t.m * c;
-        float sum = 0.f;
+        float sum = 0.f, top = -INFINITY;
 #pragma unroll
         for (int t4 = 0; t4 < 4; ++t4) next[0][t4] = f32x4{0.f, 0.f, 0.f, 0.f};
         auto weigh_pair = [&](int i) {  // probabilities of two neighbouring tokens, those of the second product's first half first
@@ -666,8 +672,9 @@ __device__ __forceinline__ void run_rows(const DecodeLaunch &a, const DecodeItem
             sum += p0 + p1;
             pw[i >> 2][i & 3] = pack_bf16(p0, p1);
         };
-        constexpr int kFirst = 5;  // pairs beside the first product
+        weigh_pair(0);  // while K comes from LDS
         __builtin_amdgcn_sched_barrier(0);
+        constexpr int kFirst = 6;  // pairs up to the end of the first product
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const i32x8 q = i >= 4 ? t.lo : t.hi;
@@ -675,36 +682,34 @@ __device__ __forceinline__ void run_rows(const DecodeLaunch &a, const DecodeItem
             to = (i & 3) == 0 ? mfma_four<0>(k[0], q, to, k_scale, t.q_scale) : (i & 3) == 1 ? mfma_four<1>(k[1], q, to, k_scale, t.q_scale)
                : (i & 3) == 2 ? mfma_four<2>(k[2], q, to, k_scale, t.q_scale) : mfma_four<3>(k[3], q, to, k_scale, t.q_scale);
 #pragma unroll
-            for (int p = kFirst * i / 8; p < kFirst * (i + 1) / 8; ++p) weigh_pair(p);
-            if (i >= 4) va[i - 4] = lds.v[b & 1][i - 4][rd.lane];
+            for (int p = 1 + (kFirst - 1) * i / 8; p < 1 + (kFirst - 1) * (i + 1) / 8; ++p) weigh_pair(p);
+            if (i >= 4) va[i - 4] = lds.v[P][i - 4][rd.lane];
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             t.o[i & 7] = mfma16(as_bf16x8(va[i & 3]), as_bf16x8(pw[i >> 3]), t.o[i & 7]);
             if (i == 2) ring.take(b + 1);
-            if (i + 4 < 16) va[i & 3] = lds.v[b & 1][i + 4][rd.lane];
-            if (i < 8) {
-#pragma unroll
-                for (int p = kFirst + (8 - kFirst) * i / 8; p < kFirst + (8 - kFirst) * (i + 1) / 8; ++p) weigh_pair(p);
-            } else if (i % 2 == 0) {
-                i == 8 ? widen_dims(std::integral_constant<int, 0>{}, b + 1) : i == 10 ? widen_dims(std::integral_constant<int, 1>{}, b + 1)
-                : i == 12 ? widen_dims(std::integral_constant<int, 2>{}, b + 1) : widen_dims(std::integral_constant<int, 3>{}, b + 1);
-            }
+            if (i + 4 < 16) va[i & 3] = lds.v[P][i + 4][rd.lane];
+            if (i < 8 - kFirst) weigh_pair(kFirst + i);
+            if (i == 4) ring.issue(b + kRing);  // where step b was: its keys and values left in step b - 1
+            if (i >= 8) top = most(next, 2 * (i - 8), top);
+            if (i == 6) widen_dims(std::integral_constant<int, 0>{}, std::integral_constant<int, 1 - P>{});
+            if (i == 9) widen_dims(std::integral_constant<int, 1>{}, std::integral_constant<int, 1 - P>{});
+            if (i == 11) widen_dims(std::integral_constant<int, 2>{}, std::integral_constant<int, 1 - P>{});
+            if (i == 13) widen_dims(std::integral_constant<int, 3>{}, std::integral_constant<int, 1 - P>{});
             __builtin_amdgcn_sched_barrier(0);
         }
         asm volatile("" : "+v"(sum));
         t.l += sum;
-        hide(rd, tile, next, (b + 1) * kStep + 16 * rd.g);
-        tops(next, top);
-        follow(tile, top, c);
+        settle(next, b + 1, top);
         ring.landed();  // the share of step b + 2; of all wavefronts behind the barrier
         ring.barrier();
     };
     for (int b = 0;;) {
-        step(acc0, acc1, b);
+        step(acc0, acc1, b, std::integral_constant<int, 0>{});
         if (++b >= n_blk) break;
-        step(acc1, acc0, b);
+        step(acc1, acc0, b, std::integral_constant<int, 1>{});
         if (++b >= n_blk) break;
     }
     ring.all_landed();
@@ -743,16 +748,16 @@ __device__ __forceinline__ void run_tall(const DecodeLaunch &a, const DecodeItem
     const float c = exponent_factor(a.scale);
     // K's 16 bytes of token t and dims 32 dg lie at place 16 dg + t
     RingReader ring(a, it, lds, (lane & 3) * 256 + (lane >> 2 & 3) * 64 + (lane >> 4) * 16, (lane >> 4 & 1) * 2 + h);
-    auto widen_dims = [&](auto byte, int b) {
+    auto widen_dims = [&](auto byte, int parity) {
         constexpr int B = decltype(byte)::value;
-        char *to = reinterpret_cast<char *>(&lds.v[b & 1][4 * wave + B][32 * h + (lane & 15)]) + 8 * (lane >> 4 & 1);
+        char *to = reinterpret_cast<char *>(&lds.v[parity][4 * wave + B][32 * h + (lane & 15)]) + 8 * (lane >> 4 & 1);
         ring.widen<B>(to, to + 256);
     };
     auto widen = [&](int b) {
-        widen_dims(std::integral_constant<int, 0>{}, b);
-        widen_dims(std::integral_constant<int, 1>{}, b);
-        widen_dims(std::integral_constant<int, 2>{}, b);
-        widen_dims(std::integral_constant<int, 3>{}, b);
+        widen_dims(std::integral_constant<int, 0>{}, b & 1);
+        widen_dims(std::integral_constant<int, 1>{}, b & 1);
+        widen_dims(std::integral_constant<int, 2>{}, b & 1);
+        widen_dims(std::integral_constant<int, 3>{}, b & 1);
     };
     TallRows x;
     x.req = a.node_req_idx[it.req_off + row / G];
@@ -797,24 +802,22 @@ __device__ __forceinline__ void run_tall(const DecodeLaunch &a, const DecodeItem
     widen(0);
     ring.barrier();
     if (row0 >= rows) return ring.serve(n_blk, widen);
-    auto hide_tall = [&](f32x16 (&acc)[2], int tok0) {
-        if (__builtin_amdgcn_ballot_w64(tok0 + kStep > x.lim)) {  // some row does not see the whole step, the item's last one among them
+    auto most = [](const f32x16 (&acc)[2], int j, float top) { return fmaxf(fmaxf(top, acc[j >> 4][j & 15]), acc[j >> 4][(j & 15) + 1]); };
+    auto settle = [&](f32x16 (&acc)[2], int b, float top) {  // scores of step b are what weights can be made of
+        if (__builtin_amdgcn_ballot_w64((b + 1) * kStep > x.lim)) {  // some row does not see the whole step, the item's last one among them
             const bool last = a.row_leaf && a.row_leaf[x.req] == it.node;
             const unsigned long long vis = last ? a.row_mask[x.req] : 0ull;
+            top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
-                const int d0 = tok0 + 8 * j + 4 * h - x.lim;
+                const int d0 = b * kStep + 8 * j + 4 * h - x.lim;
                 const uint32_t seen = d0 < 0 ? (d0 <= -4 ? 0xFu : (1u << -d0) - 1u | (uint32_t)vis << -d0) : d0 < 64 ? (uint32_t)(vis >> d0) : 0u;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[j >> 2][4 * (j & 3) + i] = (seen >> i & 1u) ? acc[j >> 2][4 * (j & 3) + i] : -INFINITY;
+                top = most(acc, 4 * j, most(acc, 4 * j + 2, top));
             }
         }
-    };
-    auto follow_tall = [&](const f32x16 (&acc)[2]) {
-        float top = acc[0][0];
-#pragma unroll
-        for (int i = 1; i < 32; ++i) top = fmaxf(top, acc[i >> 4][i & 15]);
-        if (__builtin_amdgcn_ballot_w64((top - x.m) * c > kSlack)) {
+        if (__builtin_amdgcn_ballot_w64((top - x.m) * c > kSlack)) {  // (-inf - -inf: no)
             const float m_new = fmaxf(x.m, half_max(top));
             const float alpha = m_new == -INFINITY ? 1.f : fast_exp2((x.m - m_new) * c);
             x.m = m_new;
@@ -843,19 +846,21 @@ __device__ __forceinline__ void run_tall(const DecodeLaunch &a, const DecodeItem
         for (int i = 0; i < 16; ++i) acc0[0][i] = acc0[1][i] = 0.f;
 #pragma unroll
         for (int i = 0; i < 8; ++i) acc0[i & 1] = mfma_four_tall(k[i & 3], x.q[i >> 1 & 1][i >> 2], acc0[i & 1], ks[i & 3], x.q_scale);
+        float top = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 32; j += 2) top = most(acc0, j, top);
+        settle(acc0, 0, top);
     }
-    hide_tall(acc0, 0);
-    follow_tall(acc0);
     ring.barrier();  // all are done with K of step 0
-    auto step = [&](f32x16 (&now)[2], f32x16 (&next)[2], int b) {
+    auto step = [&](f32x16 (&now)[2], f32x16 (&next)[2], int b, auto parity) {
+        constexpr int P = decltype(parity)::value;
         u32x4 k[4], va[4];
         uint32_t ks[4];
+        ring.clean(b + 1);  // (behind the last step: of no use, and of no harm)
         keys(b + 1, k, ks);
         __builtin_amdgcn_sched_barrier(0);
-        ring.issue(b + kRing);  // where step b was: its keys and values left in step b - 1
-        ring.clean(b + 1);      // (behind the last step: of no use, and of no harm)
         const float mc = x.m == -INFINITY ? 0.f : x.m * c;
-        float sum = 0.f;
+        float sum = 0.f, top = -INFINITY;
 #pragma unroll
         for (int i = 0; i < 16; ++i) next[0][i] = next[1][i] = 0.f;
         auto weigh_pair = [&](int p) {  // probabilities of two neighbouring tokens, in the order in which the second product takes them
@@ -865,40 +870,42 @@ __device__ __forceinline__ void run_tall(const DecodeLaunch &a, const DecodeItem
             pw[p >> 2][p & 3] = pack_bf16(p0, p1);
         };
         // every chunk up to a sched_barrier: a matrix instruction (64 cycles of the first product, 32 of the second) and what fits beside it
-        constexpr int kFirst = 11;  // pairs beside the first product
+        constexpr int kBefore = 2, kFirst = 12, kIssue = 5;  // pairs while K comes from LDS, and up to the end of the first product; where the ring's loads go out
+#pragma unroll
+        for (int p = 0; p < kBefore; ++p) weigh_pair(p);
         __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             next[i & 1] = mfma_four_tall(k[i & 3], x.q[i >> 1 & 1][i >> 2], next[i & 1], ks[i & 3], x.q_scale);
 #pragma unroll
-            for (int p = kFirst * i / 8; p < kFirst * (i + 1) / 8; ++p) weigh_pair(p);
-            if (i >= 4) va[i - 4] = lds.v[b & 1][i - 4][lane];
+            for (int p = kBefore + (kFirst - kBefore) * i / 8; p < kBefore + (kFirst - kBefore) * (i + 1) / 8; ++p) weigh_pair(p);
+            if (i >= 4) va[i - 4] = lds.v[P][i - 4][lane];
             __builtin_amdgcn_sched_barrier(0);
         }
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             x.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(va[i & 3]), as_bf16x8(pw[i >> 2]), x.o[i & 3], 0, 0, 0);
             if (i == 2) ring.take(b + 1);
-            if (i + 4 < 16) va[i & 3] = lds.v[b & 1][i + 4][lane];
-            if (i < 5) {
-                if (kFirst + i < 16) weigh_pair(kFirst + i);
-            } else if (i % 2 == 0 && i >= 8) {
-                i == 8 ? widen_dims(std::integral_constant<int, 0>{}, b + 1) : i == 10 ? widen_dims(std::integral_constant<int, 1>{}, b + 1)
-                : i == 12 ? widen_dims(std::integral_constant<int, 2>{}, b + 1) : widen_dims(std::integral_constant<int, 3>{}, b + 1);
-            }
+            if (i + 4 < 16) va[i & 3] = lds.v[P][i + 4][lane];
+            if (i < 16 - kFirst) weigh_pair(kFirst + i);
+            if (i == kIssue) ring.issue(b + kRing);  // where step b was: its keys and values left in step b - 1
+            if (i >= 6 && i < 14) top = most(next, 4 * (i - 6), most(next, 4 * (i - 6) + 2, top));
+            if (i == 8) widen_dims(std::integral_constant<int, 0>{}, std::integral_constant<int, 1 - P>{});
+            if (i == 10) widen_dims(std::integral_constant<int, 1>{}, std::integral_constant<int, 1 - P>{});
+            if (i == 12) widen_dims(std::integral_constant<int, 2>{}, std::integral_constant<int, 1 - P>{});
+            if (i == 14) widen_dims(std::integral_constant<int, 3>{}, std::integral_constant<int, 1 - P>{});
             __builtin_amdgcn_sched_barrier(0);
         }
         asm volatile("" : "+v"(sum));
         x.l += sum;
-        hide_tall(next, (b + 1) * kStep);
-        follow_tall(next);
+        settle(next, b + 1, top);
         ring.landed();  // the share of step b + 2; of all wavefronts behind the barrier
         ring.barrier();
     };
     for (int b = 0;;) {
-        step(acc0, acc1, b);
+        step(acc0, acc1, b, std::integral_constant<int, 0>{});
         if (++b >= n_blk) break;
-        step(acc1, acc0, b);
+        step(acc1, acc0, b, std::integral_constant<int, 1>{});
         if (++b >= n_blk) break;
     }
     ring.all_landed();

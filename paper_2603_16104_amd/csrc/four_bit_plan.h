@@ -16,7 +16,7 @@ namespace four_plan {
 struct Kind {
     double fixed, full, alone;
 };
-constexpr Kind kKinds[5] = {{3.8, 0.50, 0.20}, {5.7, 0.65, 0.31}, {4.6, 0.95, 0.82}, {6.5, 1.40, 1.10}, {3.7, 1.90, 0.81}};
+constexpr Kind kKinds[5] = {{3.1, 0.47, 0.21}, {5.2, 0.61, 0.34}, {3.3, 0.85, 0.79}, {4.3, 1.04, 1.31}, {3.1, 1.78, 0.76}};
 constexpr int kRowCaps[4] = {16, 32, 64, 128};
 constexpr int kXcds = 8;  // (workgroups go to them in turn)
 constexpr int kChunks[7] = {64, 128, 256, 512, 1024, 2048, 4096};
@@ -31,10 +31,10 @@ struct Load {  // items of one kind
     }
 };
 
-// A step's length: the items' costs over the chip's slots and part of the longest one, that one alone, or the bytes; then the merge's partials.
-// 3983 timings of 150 random plans of 8 to 340 us, cut in 28 ways each: 7 % rms; the way that the estimate prefers takes 1.03 of the best one's
-// time in the mean, 1.09 for one plan in ten, 1.24 at most.
-inline double estimate_us(const Load (&load)[5], double bytes, double partials, int n_cu) {
+// A step's length: the items' costs over the chip's slots and part of the longest one, that one alone, or the bytes; then the merge of the partials, of
+// which a row has `parts`.  6648 timings of 360 random plans of 8 to 340 us, cut in about 18 ways each: 7 % rms; the way that the estimate prefers takes
+// 1.02 of the best one's time in the mean, 1.07 for one plan in ten, 1.33 at most.
+inline double estimate_us(const Load (&load)[5], double bytes, int32_t parts, double partials, int n_cu) {
     double busy = 0, longest = 0;
     for (int k = 0; k < 5; ++k) {
         if (load[k].items == 0) continue;
@@ -42,7 +42,7 @@ inline double estimate_us(const Load (&load)[5], double bytes, double partials, 
         longest = std::max(longest, kKinds[k].fixed + load[k].longest * kKinds[k].alone);
     }
     busy /= 2 * n_cu;
-    return 4.2 + std::max({busy + 0.59 * longest, longest, bytes / 6.9e6}) + partials * 528 / 3.9e6;
+    return 4.7 + std::max({busy + 0.52 * longest, longest, bytes / 5.2e6}) + 0.028 * parts + partials * 528 / 3.2e6;
 }
 
 struct Cut {
@@ -105,9 +105,10 @@ inline Cut choose(const hkv_decode_plan &pl, int n_cu) {
                     load[0].steps += few[f].steps;
                     load[0].longest = std::max(load[0].longest, few[f].longest);
                     if (pack) std::swap(load[0], load[4]);
-                    const double partials = (double)pl.n_req * pl.num_q_heads * (most_few[f] + most_shared[s]);
+                    const int32_t parts = most_few[f] + most_shared[s];
+                    const double partials = (double)pl.n_req * pl.num_q_heads * parts;
                     const bool fits = partials * 264 + 768 <= (double)kStaticWorkspaceBytes;
-                    const double us = estimate_us(load, bytes, partials, n_cu);
+                    const double us = estimate_us(load, bytes, parts, partials, n_cu);
                     if (fits == best_fits ? us >= least : !fits) continue;
                     least = us;
                     best_fits = fits;
@@ -131,8 +132,9 @@ std::vector<double> lengths(const std::vector<Proto> &items, size_t set, int gro
 }
 
 // The order in which sets of two kinds go out to `slots` places: set i of the first kind as i, of the second as ~i.  Whenever a place is free, the kind
-// goes on whose remaining time over the places it would have, plus one set's time, is longer: both share the chip all the while (one is bound by
-// its instructions, the other by memory), and neither is left alone with long sets at the end.  Of those that start at once the first kind's come
+// goes on whose remaining time over the places it would have, plus five times a set's, is longer: both share the chip all the while (one is bound by
+// its instructions, the other by memory), and neither is left alone with long sets at the end (512 requests over
+// 16 prompts of 8192 tokens: 239 us; with one set's time 254, with twenty 246, both kinds in even shares 284).  Of those that start at once the first kind's come
 // first: workgroups go to an XCD's compute units in turn, so each gets one of them before any gets two.
 inline std::vector<int32_t> dispatch_order(const std::array<std::vector<double>, 2> &us, int slots) {
     std::vector<int32_t> order;
@@ -141,7 +143,7 @@ inline std::vector<int32_t> dispatch_order(const std::array<std::vector<double>,
     for (int k = 0; k < 2; ++k)
         for (const double x : us[k]) left[k] += x;
     size_t next[2] = {}, count[2] = {};
-    auto urgency = [&](int k) { return next[k] < us[k].size() ? left[k] / (double)(count[k] + 1) + us[k][next[k]] : -1.0; };
+    auto urgency = [&](int k) { return next[k] < us[k].size() ? left[k] / (double)(count[k] + 1) + 5 * us[k][next[k]] : -1.0; };
     while (next[0] < us[0].size() || next[1] < us[1].size()) {
         if ((int)running.size() >= slots) {
             now = running.top().first;

@@ -235,6 +235,78 @@ def test_decode_rows_of_q():
     pool.close()
 
 
+ITEM_ROWS = [(32, 17), (32, 32), (64, 33), (64, 56), (64, 64), (128, 65), (128, 96), (128, 100), (128, 128)]
+
+
+@pytest.mark.parametrize("max_rows,rows", ITEM_ROWS)
+@pytest.mark.parametrize("tokens", [1, 16, 63, 64, 65, 200, 256, 500])
+def test_items_of_many_rows(max_rows, rows, tokens):
+    """A node of so many tokens under items of each kind; requests of one token of their own, some of none."""
+    group = next(g for g in (16, 8, 5, 4, 3, 1) if rows % g == 0)
+    n = rows // group
+    f = Forest([(-1, tokens)] + [(0, 1 if i % 3 else 0) for i in range(n)], list(range(1, n + 1)), 16, seed=tokens)
+    pool = Pool(f.n_pages, 2, seed=rows)
+    poison_unused_slots(pool, f)
+    q = queries(n, 2 * group)
+    q[0] *= 4  # (scores that leave the first step's reference)
+    plan = hkv.hkv_decode_plan_create_ex(pool.handle, f.nodes, f.node_pages, f.leaves, 2 * group, max_rows=max_rows, shared_chunk=2048)
+    items = hkv.hkv_decode_plan_items(plan)
+    assert group * items[items[:, 7] == 0][0, 4] == rows and items[items[:, 7] == 0][0, 1] == tokens
+    out, lse = decode(plan, q)
+    pool.k_scale[pool.k_scale == 255] = 127
+    pool.v_scale[pool.v_scale == 255] = 127
+    check_decode(f, pool, q, out, lse)
+    hkv.hkv_decode_plan_destroy(plan)
+    pool.close()
+
+
+@pytest.mark.parametrize("max_rows", [16, 32, 64, 128])
+@pytest.mark.parametrize("hq,hk,T,tree", [(16, 1, 8, True), (32, 2, 5, False), (8, 1, 16, False)])
+def test_masks_in_items_of_many_rows(max_rows, hq, hk, T, tree):
+    """Drafted tokens in the only node: its items have all of a request's rows, some of which see nothing of an item."""
+    f = Forest([(-1, T + 60), (-1, 130), (-1, T)], [0, 1, 2], 16, seed=2)
+    pool = Pool(f.n_pages, hk, seed=4)
+    poison_unused_slots(pool, f)
+    q = queries(3 * T, hq)
+    visible = None
+    if tree:
+        rng = np.random.default_rng(0)
+        parent = [-1] + [int(rng.integers(0, j)) for j in range(1, T)]
+        one = []
+        for j in range(T):
+            m, u = 0, j
+            while u >= 0:
+                m, u = m | 1 << u, parent[u]
+            one.append(m)
+        visible = np.array(one * 3, dtype=np.uint64)
+    plan = hkv.hkv_decode_plan_create_ex(pool.handle, f.nodes, f.node_pages, f.leaves, hq, tokens_per_req=T, visible=visible, max_rows=max_rows, shared_chunk=64)
+    out, lse = decode(plan, q)
+    pool.k_scale[pool.k_scale == 255] = 127
+    pool.v_scale[pool.v_scale == 255] = 127
+    check_decode(f, pool, q, out, lse, T, visible)
+    hkv.hkv_decode_plan_destroy(plan)
+    pool.close()
+
+
+@pytest.mark.parametrize("max_rows,rows", [(16, 16), (32, 32), (64, 64), (128, 128)])
+def test_references_that_move(max_rows, rows):
+    """Scores that grow from step to step by more than a reference's slack, and a first step of the lowest: weights of the last one count alone."""
+    f = Forest([(-1, 512)], [0] * (rows // 16), 16)
+    pool = Pool(f.n_pages, 1, seed=6)
+    b = f.pages[0]
+    step = np.repeat(np.arange(8), 4)  # K's values grow by 4 a step
+    for i, page in enumerate(b):
+        pool.k_scale.view(pool.blocks, 1, 64)[int(page)] = int(121 + step[i])
+    pool.k.fill_(0x22)  # ones
+    q = torch.ones(rows // 16, 16, 128, dtype=torch.bfloat16, device="cuda")
+    q[:, 1::2] = -1
+    plan = hkv.hkv_decode_plan_create_ex(pool.handle, f.nodes, f.node_pages, f.leaves, 16, max_rows=max_rows, shared_chunk=512)
+    out, lse = decode(plan, q, scale=4.0)
+    check_decode(f, pool, q, out, lse, scale=4.0)
+    hkv.hkv_decode_plan_destroy(plan)
+    pool.close()
+
+
 @pytest.mark.parametrize("scale", [0.0, -0.05, 3.0])
 def test_decode_scales(scale):
     f = Forest([(-1, 200), (0, 40), (0, 90)], [1, 2], 16)

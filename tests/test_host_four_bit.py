@@ -49,6 +49,8 @@ def test_plans():
     nodes, pages = [(-1, 0, 2, 32), (0, 2, 1, 9), (0, 3, 1, 16)], [0, 1, 2, 3]
     assert code(hkv.hkv_decode_plan_create, pool, nodes, pages, [1, 2], 8, hkv.PLAN_HOST_ONLY | hkv.PLAN_FP8_MATRIX) == hkv.ESHAPE
     assert code(hkv.hkv_decode_plan_create, pool, nodes, pages, [1, 2], 34, hkv.PLAN_HOST_ONLY) == hkv.ESHAPE
+    for bad in (15, 129):
+        assert code(hkv.hkv_decode_plan_create_ex, pool, nodes, pages, [1, 2], 8, hkv.PLAN_HOST_ONLY, max_rows=bad) == hkv.EINVAL
     assert code(hkv.hkv_decode_plan_create, pool, nodes, pages, [1, 2], 3, hkv.PLAN_HOST_ONLY) == hkv.ESHAPE
     assert code(hkv.hkv_decode_plan_create, pool, nodes, [0, 1, 2, 64], [1, 2], 8, hkv.PLAN_HOST_ONLY) == hkv.ERANGE
     plan = hkv.hkv_decode_plan_create(pool, nodes, pages, [1, 2], 8, hkv.PLAN_HOST_ONLY)
@@ -87,7 +89,7 @@ def random_forest(rng, page):
 
 
 SETTINGS = [{}, dict(max_rows=16), dict(max_rows=64, leaf_chunk=64), dict(shared_chunk=128), dict(pack=1), dict(pack=3), dict(leaf_chunk=16, shared_chunk=2048, pack=3),
-            dict(max_rows=32, shared_chunk=1024)]
+            dict(max_rows=32, shared_chunk=1024), dict(max_rows=128)]
 
 
 @pytest.mark.parametrize("hq,hk,T", [(8, 2, 1), (32, 8, 1), (16, 1, 1), (5, 1, 1), (40, 8, 8), (4, 4, 16)])
