@@ -31,9 +31,10 @@ struct Load {  // items of one kind
     }
 };
 
-// A step's length: the items' costs over the chip's slots and part of the longest one, that one alone, or the bytes; then the merge of the partials, of
+// A step's length: the items' costs over the chip's slots and part of the longest one, that one alone, or the bytes (512 sequences of 1024 to 2048 tokens:
+// 142 us with a wavefront each, 160 with a workgroup each); then the merge of the partials, of
 // which a row has `parts`.  6648 timings of 360 random plans of 8 to 340 us, cut in about 18 ways each: 7 % rms; the way that the estimate prefers takes
-// 1.02 of the best one's time in the mean over 300 others, 1.07 for one plan in ten, 1.19 at most.
+// 1.02 of the best one's time in the mean over 300 others, 1.07 for one plan in ten, 1.21 at most.
 inline double estimate_us(const Load (&load)[5], double bytes, int32_t parts, double partials, int n_cu) {
     double busy = 0, longest = 0;
     for (int k = 0; k < 5; ++k) {
@@ -42,7 +43,7 @@ inline double estimate_us(const Load (&load)[5], double bytes, int32_t parts, do
         longest = std::max(longest, kKinds[k].fixed + load[k].longest * kKinds[k].alone);
     }
     busy /= 2 * n_cu;
-    return 4.7 + std::max({busy + 0.52 * longest, longest, bytes / 6.2e6}) + 0.028 * parts + partials * 528 / 3.2e6;
+    return 4.7 + std::max({busy + 0.52 * longest, longest, bytes / (load[0].items ? 5.3e6 : 6.2e6)}) + 0.028 * parts + partials * 528 / 3.2e6;
 }
 
 struct Cut {
