@@ -1,4 +1,7 @@
 """Calls that move pages: copies between pools of every pair of types, forks, compaction, against plain forms on the host."""
+import os
+import textwrap
+
 import numpy as np
 import pytest
 import torch
@@ -273,3 +276,26 @@ def test_beams_in_use():
     hkv.kv_pool_release(pool.handle, np.concatenate([prompt, *pages]))
     assert hkv.kv_pool_num_free(pool.handle) == 80
     pool.close()
+
+
+def test_the_readmes_lines():
+    """What README.md has a program do with pages, run as it is written there."""
+    with open(os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "README.md")) as f:
+        text = f.read()
+    lines = textwrap.dedent(text[text.index("    # a prompt that no call waits for"): text.index("    hkv.kv_cache_release(cache, pages)")])
+    warm, cold = make(40, 2, hkv.BF16, 16, 1), make(20, 2, hkv.FP4_E2M1, 16, 2)
+    ids = hkv.kv_pool_alloc(warm.handle, 30)
+    hkv.kv_pool_release(warm.handle, ids[3:9])
+    pages, prompt, back, n = ids[20:25], ids[10:14], ids[14:18], 70
+    at = lambda x: torch.from_numpy(np.asarray(x, dtype=np.int64)).cuda()
+    content = warm.k.view(40, -1)[at(pages)].clone()
+    names = dict(hkv=hkv, pool=warm.handle, four_bit_pool=cold.handle, cold_pages=np.arange(5, 9, dtype=np.int32), prompt_pages=prompt, warm_pages=back, pages=pages, n=n)
+    exec(lines, names)
+    new, branches = names["new_ids"], names["branches"]
+    assert list(names["pages"]) == list(new[pages]) and branches.shape == (4, 5)
+    for b in branches:  # four full pages of their own sequence's, and a copy of the fifth
+        assert list(b[:4]) == list(pages[:4]) and torch.equal(warm.k.view(40, -1)[at(new[b])], content)
+    assert len({int(b[4]) for b in branches} | {int(pages[4])}) == 5
+    assert torch.equal(warm.k.view(40, -1)[at(names["pages"])], content)
+    warm.close()
+    cold.close()
