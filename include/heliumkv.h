@@ -172,7 +172,7 @@ int kv_pool_copy_pages(hkv_pool *dst, const int32_t *dst_ids, hkv_pool *src, con
 
 /* Forks sequences: fork j begins as sequence parent[j] (host, n_out entries, in any order, a sequence any number of times) and goes on by itself.  It shares
  * every full page of its sequence (one reference more) and gets a page of its own for a last page that is not full: the next free one
- * (in the order of the forks), to which the 16-token blocks in use are copied on `stream`, all in one launch.
+ * (in the order of the forks), to which the 16-token blocks in use are copied on `stream`, one launch per 21845 blocks.
  *   pages: host, ceil(n_tokens[i] / page size) ids of each sequence, one sequence after the other.  out_pages: host, the same of each fork.
  * release != 0: the sequences end here, and their references (one per listing) are dropped, as a step of a beam search replaces its beams
  * by others: a sequence that no fork continues is gone (its pages return to the free list, in the order listed), and one that owns its last page

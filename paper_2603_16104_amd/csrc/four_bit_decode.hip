@@ -1,16 +1,19 @@
 // Decode attention over 4-bit pools: one workgroup per item (a chunk of a prefix-tree node, one KV head, up to 128 query rows), partial results to
 // the log-sum-exp merge.  (Section 5, "Proactive Cache Management": a node's pages are read once for all requests below it.)
 //
-// A wavefront takes 64 tokens (four blocks) a step, for one or two tiles of 16 query rows:
+// A wavefront takes 64 tokens (four blocks) a step, for one or two tiles of 16 query rows, or for 32 rows (run_tall has its layout):
 //   S^T = K Q^T   v_mfma_scale_f32_16x16x128_f8f6f4: K's codes and scales as they lie in the pool, lane (m, g) dims 32 g .. + 31 of token 4 m + t4 in
 //                 tile t4 (its four scales are one word); a query row as two e4m3 terms, x * 2^e = hi + lo, whose 2^-e is the other scale.  Against bf16
 //                 operands widened from the codes that is the same matrix time and 68 fewer vector instructions a step.
 //   O^T = V^T P^T v_mfma_f32_16x16x32_bf16: lane (m, g) brings dim 8 m + dt of eight tokens of block g.  A scale stands for one token and 32 dims, the
 //                 instruction's for 32 tokens of a dim, so V is widened: two codes (neighbouring dims of a token) an instruction, then one more to
-//                 bring two tokens of a dim together.  Two tiles share that: 160 of the 690 vector instructions (in quarters of 16
-//                 lanes) of a step of two.
+//                 bring two tokens of a dim together, 152 of a step's some 260 vector instructions; rows of more than one tile share that.
 // A lane of a score tile t4 holds tokens 16 g + 4 i + t4 of its query row m: over the four tiles all 16 tokens of block g, which is what its
 // share of P^T is made of, so probabilities stay where they are.  Widened values are exact (two significant bits, a power of two).
+//
+// What bounds it: items of few rows memory (512 sequences of 1024 to 2048 tokens, 8 KV heads: 142 us, 6.0 TB/s), items of many rows their
+// instructions (16 x 8192 tokens under 256 rows of 8 KV heads: 141 us; matrix cores 49 % busy, vector units 53 %); both together, 512 requests on a
+// 70B-shaped layer, 250 us at the 1.9 GHz that the card keeps under them.  Small steps wait for their loads: item, page ids and rows, queries, codes.
 #include <hip/hip_ext.h>
 
 #include <climits>

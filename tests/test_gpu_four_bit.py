@@ -336,6 +336,26 @@ def test_decode_row_with_nan():
     pool.close()
 
 
+@pytest.mark.parametrize("max_rows", [16, 32, 64, 128])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf")])
+def test_rows_that_are_not_finite(value, max_rows):
+    """That row and head alone have no result, in items of every kind; an infinity times a key of both signs is no number either."""
+    n = max_rows // 4
+    f = Forest([(-1, 200)] + [(0, 5)] * n, list(range(1, n + 1)), 16)
+    pool = Pool(f.n_pages, 2)
+    q = queries(n, 8)
+    plan = hkv.hkv_decode_plan_create_ex(pool.handle, f.nodes, f.node_pages, f.leaves, 8, max_rows=max_rows, shared_chunk=256)
+    clean = decode(plan, q)
+    q[1, 3, 77] = value
+    out, lse = decode(plan, q)
+    assert np.isnan(out[1, 3]).all() and np.isnan(lse[1, 3])
+    out[1, 3], lse[1, 3] = clean[0][1, 3], clean[1][1, 3]
+    np.testing.assert_array_equal(out, clean[0])
+    np.testing.assert_array_equal(lse, clean[1])
+    hkv.hkv_decode_plan_destroy(plan)
+    pool.close()
+
+
 @pytest.mark.parametrize("n_req,page,large", [(3, 16, 0), (3, 32, 1), (260, 16, 0)])
 def test_growing_plan(n_req, page, large):
     """Tokens are stored and decoded step by step, over the border of pages."""
