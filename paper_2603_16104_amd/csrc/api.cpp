@@ -1261,12 +1261,13 @@ static void estimate_paths(hkv_decode_plan &pl, RowsByLeaf &by) {
     const bool fp8 = pl.pool->d.dtype == HKV_FP8_E4M3;
     int xcds = 8;  // a KV head's workgroups lie Hkv apart
     for (int h = Hkv; h % 2 == 0 && xcds > 1; h /= 2) xcds /= 2;
-    unique *= 2.0 * HKV_HEAD_DIM * Hkv * (fp8 ? 1 : 2) * xcds;
+    const bool fp4 = pl.pool->d.dtype == HKV_FP4_E2M1;  // (11387 timings: 8 % rms; against items by both estimates 1.002 of the better one's time, items always 1.24)
+    unique *= 2.0 * HKV_HEAD_DIM * Hkv * (fp4 ? 0.53125 : fp8 ? 1 : 2) * xcds;
     const int waves = units <= n_cu ? 8 : 4;
     // in 1000 tokens: the longest path, and what a compute unit takes in beyond it (between the mean and that of whole workgroups)
     const double per_cu = (double)units / n_cu, most = longest * 16e-3, mean = block_sum / paths * 16e-3;
     const double beside = 0.5 * std::max(0.0, per_cu * mean - most) + 0.5 * std::max(0.0, std::ceil(per_cu) * mean - most);
-    const double us = fp8 ? 6.0 + 5.2 * most + 8.0 * beside + 0.23 * per_cu + 0.017e-6 * unique : 5.2 + 6.5 * most + 10.9 * beside + 0.046e-6 * unique;
+    const double us = fp4 ? 4.9 + 3.4 * most + 4.0 * beside + 0.83 * per_cu + 0.014e-6 * unique : fp8 ? 6.0 + 5.2 * most + 8.0 * beside + 0.23 * per_cu + 0.017e-6 * unique : 5.2 + 6.5 * most + 10.9 * beside + 0.046e-6 * unique;
     if (us > 25) return;  // (hardly timed beyond; 40 leaves of 963 to 1926 tokens below 4 x 493, estimated at 45 us, took 55, as items 46)
     pl.paths_us = us;
     pl.n_paths = (int32_t)paths;
@@ -1522,14 +1523,13 @@ static int create_decode_plan(hkv_pool *pool, const hkv_node *nodes, int32_t n_n
         *out = pl;
         return HKV_OK;
     }
-    if (pool->d.dtype == HKV_FP4_E2M1) {
+    RowsByLeaf by_leaf;
+    estimate_paths(*pl, by_leaf);
+    if (pool->d.dtype == HKV_FP4_E2M1)
         plan_four_bit(*pl, chip_shape().n_cu);
-    } else {
-        RowsByLeaf by_leaf;
-        estimate_paths(*pl, by_leaf);
+    else
         plan_items(*pl);
-        plan_paths(*pl, by_leaf);
-    }
+    plan_paths(*pl, by_leaf);
     if (reserve_tokens > 0) {  // the items that grow with each request: the leaf's last chunk, one per KV head
         pl->grow_items.assign((size_t)n_req * Hkv, -1);
         for (int r = 0; r < n_req; ++r) {

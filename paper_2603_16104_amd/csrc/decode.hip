@@ -132,6 +132,7 @@ hipError_t launch_decode(const DecodeLaunch &a, hipStream_t s, hipEvent_t ev_beg
 
 hipError_t launch_decode_paths(const DecodePathLaunch &a, int waves, hipStream_t s, hipEvent_t ev_begin, hipEvent_t ev_end) {
     if (a.n_paths <= 0) return hipSuccess;
+    if (a.pool.dtype == kDtypeFp4) return launch_four_paths(a, waves, s, ev_begin, ev_end);
     if ((waves != 4 && waves != 8) || (a.pool.dtype != 0 && a.pool.dtype != 1) || a.fp8_matrix) return hipErrorInvalidValue;
     if (hipError_t e = prepare_decode_device(nullptr); e != hipSuccess) return e;
     const dim3 grid((unsigned)a.n_paths * (unsigned)a.pool.num_kv_heads), block(64 * waves);

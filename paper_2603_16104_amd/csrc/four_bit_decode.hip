@@ -196,6 +196,10 @@ __device__ __forceinline__ void scores(const Operands &x, const RowTile (&tile)[
     }
 }
 
+// Of 16 tokens those that a row sees: all in front of its limit (the first one is d0 behind that), and behind it the ones in vis.
+__device__ __forceinline__ uint32_t seen_bits(int d0, unsigned long long vis) {
+    return d0 < 0 ? (d0 <= -16 ? 0xFFFFu : (1u << -d0) - 1u | (uint32_t)vis << -d0) : d0 < 64 ? (uint32_t)(vis >> d0) : 0u;
+}
 // Scores of tokens that a row does not see are -inf; tok0: of the lane's 16 tokens the first, score j of a row is acc[j % 4][j / 4].
 template <int RT>
 __device__ __forceinline__ bool hide(const Reader &rd, const RowTile (&tile)[RT], f32x4 (&acc)[RT][4], int tok0) {
@@ -209,7 +213,7 @@ __device__ __forceinline__ bool hide(const Reader &rd, const RowTile (&tile)[RT]
             const bool last = rd.a.row_leaf && rd.a.row_leaf[tile[r].req] == rd.it.node;  // (looked up here: this is the exception)
             const unsigned long long vis = last ? rd.a.row_mask[tile[r].req] : 0ull;
             const int d0 = tok0 - tile[r].lim;
-            const uint32_t seen = d0 < 0 ? (d0 <= -16 ? 0xFFFFu : (1u << -d0) - 1u | (uint32_t)vis << -d0) : d0 < 64 ? (uint32_t)(vis >> d0) : 0u;
+            const uint32_t seen = seen_bits(d0, vis);
 #pragma unroll
             for (int j = 0; j < 16; ++j) acc[r][j & 3][j >> 2] = (seen >> j & 1u) ? acc[r][j & 3][j >> 2] : -INFINITY;
         }
@@ -247,9 +251,8 @@ __device__ __forceinline__ void weigh(const RowTile (&tile)[RT], const f32x4 (&a
     }
 }
 template <int RT>
-__device__ __forceinline__ void weights(const Reader &rd, RowTile (&tile)[RT], f32x4 (&acc)[RT][4], int tok0, float c, u32x4 (&pw)[RT][2]) {
+__device__ __forceinline__ void weights(RowTile (&tile)[RT], const f32x4 (&acc)[RT][4], float c, u32x4 (&pw)[RT][2]) {
     float sum[RT];
-    hide(rd, tile, acc, tok0);
     weigh(tile, acc, c, pw, sum);
     bool any = false;
 #pragma unroll
@@ -402,7 +405,8 @@ __device__ __forceinline__ void stream(const Reader &rd, int row0, int ts, int n
             rd.ids(id, b + 3 * n_ts);
             __builtin_amdgcn_sched_barrier(0);
             scores(now, tile, acc);
-            weights(rd, tile, acc, b * kStep + 16 * rd.g, c, pw);
+            hide(rd, tile, acc, b * kStep + 16 * rd.g);
+            weights(tile, acc, c, pw);
             second_half(now, pw);
             return (b += n_ts) < n_blk;
         };
@@ -415,7 +419,8 @@ __device__ __forceinline__ void stream(const Reader &rd, int row0, int ts, int n
             __builtin_amdgcn_sched_barrier(0);
             rd.keys(x, id);
             __builtin_amdgcn_sched_barrier(0);
-            weights(rd, tile, acc, b * kStep + 16 * rd.g, c, pw);
+            hide(rd, tile, acc, b * kStep + 16 * rd.g);
+            weights(tile, acc, c, pw);
             second_half(x, pw);
             __builtin_amdgcn_sched_barrier(0);
             rd.values(x, id);
@@ -427,9 +432,10 @@ __device__ __forceinline__ void stream(const Reader &rd, int row0, int ts, int n
 
 // LDS of a workgroup: partial results of wavefronts that share a row tile's tokens, or a ring of steps and two steps' V in bf16 as the second
 // product's operands.
+template <int W>
 struct Shares {
-    float o[kWaves][16][kORow], m[kWaves][16], l[kWaves][16];
-    int req[16];
+    float o[W][16][kORow], m[W][16], l[W][16];
+    int row[16];
 };
 constexpr int kRing = 4;
 struct Stage {  // four blocks as they lie in the pool, 16 bytes in the order of the lanes that brought them
@@ -441,14 +447,54 @@ struct Widened {
     u32x4 v[2][16][64];  // [step % 2], a matrix instruction's operand each
 };
 union Lds {
-    Shares s;
+    Shares<kWaves> s;
     Widened w;
 };
+
+// A wavefront's share of a row tile into LDS (active: it has seen tokens).
+template <int W>
+__device__ __forceinline__ void leave_share(Shares<W> &s, const RowTile &t, int wave, int m, int g, bool active) {
+    if (!active) {
+        if (g == 0) s.m[wave][m] = -INFINITY;
+        return;
+    }
+    const float l_row = rows_sum(t.l);
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int q = 0; q < 2; ++q)
+            *reinterpret_cast<f32x4 *>(&s.o[wave][m][32 * g + 8 * i + 4 * q]) = f32x4{t.o[4 * q][i], t.o[4 * q + 1][i], t.o[4 * q + 2][i], t.o[4 * q + 3][i]};
+    if (g == 0) {
+        s.m[wave][m] = l_row == l_row ? t.m : INFINITY;  // (a NaN or +inf among the scores: the row's sum is no number below)
+        s.l[wave][m] = l_row;
+    }
+}
+// The shares of a row brought together: eight dims, the reference and the sum.
+template <int W>
+__device__ __forceinline__ void join_shares(const Shares<W> &s, int row, int col, float c, f32x4 &x, f32x4 &y, float &M, float &L) {
+    M = -INFINITY;
+    L = 0.f;
+#pragma unroll
+    for (int w = 0; w < W; ++w) M = fmaxf(M, s.m[w][row]);
+    x = y = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < W; ++w) {
+        const float mw = s.m[w][row];
+        if (mw == -INFINITY) continue;  // that wavefront's tokens were all invisible to the row
+        const float wgt = fast_exp2((mw - M) * c);
+        L += s.l[w][row] * wgt;
+        x += *reinterpret_cast<const f32x4 *>(&s.o[w][row][8 * col]) * wgt;
+        y += *reinterpret_cast<const f32x4 *>(&s.o[w][row][8 * col + 4]) * wgt;
+    }
+    const float inv = L > 0.f ? 1.0f / L : 0.f;
+    x *= inv;
+    y *= inv;
+}
 
 // Items of up to 16 RT rows: the four wavefronts share the tokens, and bring their results together in LDS, a row tile at a time; then thread
 // (row = tid / 16, tid % 16) has eight dims of a row, whose 16 threads are a row of lanes.
 template <int RT>
-__device__ __forceinline__ void run_shared_tokens(const DecodeLaunch &a, const DecodeItem &it, Shares &s) {
+__device__ __forceinline__ void run_shared_tokens(const DecodeLaunch &a, const DecodeItem &it, Shares<kWaves> &s) {
     const Reader rd(a, it);
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), rows = it.n_req * (a.num_q_heads / a.pool.num_kv_heads);
     const float c = exponent_factor(a.scale);
@@ -459,40 +505,13 @@ __device__ __forceinline__ void run_shared_tokens(const DecodeLaunch &a, const D
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         if (r > 0) __syncthreads();
-        if (active) {
-            const RowTile &t = tile[r];
-            const float l_row = rows_sum(t.l);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-#pragma unroll
-                for (int q = 0; q < 2; ++q)
-                    *reinterpret_cast<f32x4 *>(&s.o[wave][rd.m][32 * rd.g + 8 * i + 4 * q]) = f32x4{t.o[4 * q][i], t.o[4 * q + 1][i], t.o[4 * q + 2][i], t.o[4 * q + 3][i]};
-            if (rd.g == 0) {
-                s.m[wave][rd.m] = l_row == l_row ? t.m : INFINITY;  // (a NaN or +inf among the scores: the row's sum is no number below)
-                s.l[wave][rd.m] = l_row;
-                if (wave == 0) s.req[rd.m] = t.req;
-            }
-        } else if (rd.g == 0) {
-            s.m[wave][rd.m] = -INFINITY;
-        }
+        leave_share(s, tile[r], wave, rd.m, rd.g, active);
+        if (wave == 0 && rd.g == 0) s.row[rd.m] = tile[r].req;  // (an item has tokens: wavefront 0 is active)
         __syncthreads();
         if (16 * r >= rows) break;  // (the same for all threads)
-        float M = -INFINITY, L = 0.f;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) M = fmaxf(M, s.m[w][out_row]);
-        f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
-#pragma unroll
-        for (int w = 0; w < kWaves; ++w) {
-            const float mw = s.m[w][out_row];
-            if (mw == -INFINITY) continue;  // that wavefront's tokens were all invisible to the row
-            const float wgt = fast_exp2((mw - M) * c);
-            L += s.l[w][out_row] * wgt;
-            x += *reinterpret_cast<const f32x4 *>(&s.o[w][out_row][8 * col]) * wgt;
-            y += *reinterpret_cast<const f32x4 *>(&s.o[w][out_row][8 * col + 4]) * wgt;
-        }
-        const float inv = L > 0.f ? 1.0f / L : 0.f;
-        x *= inv;
-        y *= inv;
+        f32x4 x, y;
+        float M, L;
+        join_shares(s, out_row, col, c, x, y, M, L);
         float top = 0.f;
 #pragma unroll
         for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(x[j]), fabsf(y[j])));
@@ -503,7 +522,7 @@ __device__ __forceinline__ void run_shared_tokens(const DecodeLaunch &a, const D
         float up, down;
         part_factors(top, up, down);
         if (16 * r + out_row >= rows) continue;
-        const size_t part = part_of(a, it, s.req[out_row], 16 * r + out_row);
+        const size_t part = part_of(a, it, s.row[out_row], 16 * r + out_row);
         *reinterpret_cast<u32x4 *>(a.o_parts + part * kHeadDim + 8 * col) =
             u32x4{pack_f16(x[0] * up, x[1] * up), pack_f16(x[2] * up, x[3] * up), pack_f16(y[0] * up, y[1] * up), pack_f16(y[2] * up, y[3] * up)};
         if (col == 0) {
@@ -511,6 +530,103 @@ __device__ __forceinline__ void run_shared_tokens(const DecodeLaunch &a, const D
             a.lse_parts[part] = partial_lse(M * c, L);
         }
     }
+}
+
+// Small steps: a workgroup of W wavefronts per KV head and leaf (and up to 16 of its rows) walks the whole path and writes the result itself: no items' partials
+// and no second launch (4 requests over 256 + 49 tokens 6.7 us, as items and merge 7.7; what bounds it is the chain of record, queries and codes).  Blocks that are not full may lie anywhere on it, at the end of every node; `gap` is how many of a block's last slots are nobody's.
+struct PathStep : Operands {
+    int gap;  // of the lane's block of V, which is that of its scores too
+};
+template <int W>
+__global__ __launch_bounds__(64 * W, 2) void four_path_kernel(DecodePathLaunch a) {
+    extern __shared__ __attribute__((aligned(16))) char smem[];
+    Shares<W> &s = *reinterpret_cast<Shares<W> *>(smem);
+    const int lane = (int)threadIdx.x & 63, m = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int Hkv = a.pool.num_kv_heads, G = a.num_q_heads / Hkv, head = (int)blockIdx.x % Hkv;
+    const int32_t *path = a.paths + (size_t)(blockIdx.x / Hkv) * a.path_stride;
+    const int n_blocks = path[0], rows = path[1] * G, n_steps = (n_blocks + 3) / 4, row = min(m, rows - 1);
+    const float c = exponent_factor(a.scale);
+    const uint8_t *k = static_cast<const uint8_t *>(a.pool.k_pages) + (m & 3) * 64 + g * 16, *v = static_cast<const uint8_t *>(a.pool.v_pages) + m * 16;
+    const uint8_t *k_scale = reinterpret_cast<const uint8_t *>(a.pool.k_scale) + g * 16 + 4 * (m & 3), *v_scale = reinterpret_cast<const uint8_t *>(a.pool.v_scale) + (m >> 2) * 16;
+    auto ids = [&](int (&id)[4], int b) {  // clamped, so always in bounds; a block behind the path's last is all gap
+#pragma unroll
+        for (int i = 0; i < 4; ++i) id[i] = path[kPathBlocks + min(4 * b + i, n_blocks - 1)] | (4 * b + i < n_blocks ? 0 : 16 << kPathIdBits);
+    };
+    auto block = [&](int id) { return (size_t)(id & kPathIdMask) * Hkv + head; };
+    auto fetch = [&](PathStep &x, const int (&id)[4]) {
+        const int mine = pick4(id, g);
+        const size_t kb = block(pick4(id, m >> 2)), vb = block(mine);
+        x.gap = (int)((uint32_t)mine >> kPathIdBits);
+        x.k_scale = *reinterpret_cast<const uint32_t *>(k_scale + kb * four::kScaleBytes);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x.k[j] = ld16(k + kb * four::kCodeBytes + 256 * j);
+        x.v_scale = ld16(v_scale + vb * four::kScaleBytes);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x.v[j] = ld16(v + vb * four::kCodeBytes + 256 * j);
+    };
+    const bool active = wave < n_steps;
+    RowTile tile[1];
+    RowTile &t = tile[0];
+    const int q_at = path[kPathQRows + row / G] * a.num_q_heads + head * G + row % G;
+    if (active) {
+        PathStep now, next;
+        int id[4], b = wave;
+        t.req = path[kPathRows + row / G];
+        ids(id, b);
+        fetch(now, id);
+        u32x4 w[4];
+        const char *qp = static_cast<const char *>(a.q) + (size_t)q_at * (kHeadDim * 2) + 32 * g;
+        w[0] = ld16(qp);
+        w[1] = ld16(qp + 16);
+        w[2] = ld16(qp + 128);
+        w[3] = ld16(qp + 144);
+        ids(id, b + W);
+        t.lim = a.row_leaf ? path[2] + a.row_limit[t.req] : INT_MAX;  // (positions count whole blocks: the leaf begins at one)
+        split_row(t, w, a.scale);
+#pragma unroll
+        for (int dt = 0; dt < 8; ++dt) t.o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+        t.m = -INFINITY;
+        t.l = 0.f;
+        f32x4 acc[1][4];
+        u32x4 pw[1][2];
+        auto step = [&](PathStep &x, PathStep &after) {
+            fetch(after, id);
+            ids(id, b + 2 * W);
+            __builtin_amdgcn_sched_barrier(0);
+            scores(x, tile, acc);
+            const int d0 = 16 * (4 * b + g) - t.lim;
+            if (__builtin_amdgcn_ballot_w64(x.gap > 0 || d0 > -16)) {
+                const uint32_t seen = seen_bits(d0, a.row_leaf ? a.row_mask[t.req] : 0ull) & 0xFFFFu >> x.gap;
+#pragma unroll
+                for (int j = 0; j < 16; ++j) acc[0][j & 3][j >> 2] = (seen >> j & 1u) ? acc[0][j & 3][j >> 2] : -INFINITY;
+#pragma unroll
+                for (int q = 0; q < 4; ++q) {
+                    uint32_t sc = x.v_scale[q];
+                    clear_from(x.v[q], sc, 16 - x.gap - 4 * q);
+                    x.v_scale[q] = sc;
+                }
+            }
+            weights(tile, acc, c, pw);
+            add_values(tile, x, pw);
+            return (b += W) < n_steps;
+        };
+        while (step(now, next) && step(next, now)) {
+        }
+    }
+    leave_share(s, t, wave, m, g, active);
+    if (wave == 0 && g == 0) s.row[m] = q_at;
+    __syncthreads();
+    const int out_row = (int)threadIdx.x >> 4, col = lane & 15;
+    if (out_row >= rows) return;
+    f32x4 x, y;
+    float M, L;
+    join_shares(s, out_row, col, c, x, y, M, L);
+    const float bad = L >= 0.f ? 0.f : __builtin_nanf("");  // a row whose scores hold a NaN or +inf
+    x += bad;
+    y += bad;
+    const size_t to = (size_t)s.row[out_row];
+    *reinterpret_cast<u32x4 *>(static_cast<uint16_t *>(a.out) + to * kHeadDim + 8 * col) = u32x4{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3]), pack_bf16(y[0], y[1]), pack_bf16(y[2], y[3])};
+    if (a.lse_out && col == 0) a.lse_out[to] = L != 0.f ? (M * c + fast_log2(L)) * kLn2 : -INFINITY;
 }
 
 // Items of more rows: a wavefront has rows of its own and sees all tokens.  Codes and scales come through a ring in LDS, a block of a step by each
@@ -976,7 +1092,20 @@ __global__ __launch_bounds__(kWaves * 64, 2) void four_decode_kernel(DecodeLaunc
 }  // namespace
 
 hipError_t prepare_four_decode() {
+    if (hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void *>(four_path_kernel<8>), hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(Shares<8>)); e != hipSuccess) return e;
     return hipFuncSetAttribute(reinterpret_cast<const void *>(four_decode_kernel), hipFuncAttributeMaxDynamicSharedMemorySize, sizeof(Lds));
+}
+
+hipError_t launch_four_paths(const DecodePathLaunch &a, int waves, hipStream_t s, hipEvent_t ev_begin, hipEvent_t ev_end) {
+    if (a.n_paths <= 0) return hipSuccess;
+    if (waves != 4 && waves != 8) return hipErrorInvalidValue;
+    if (hipError_t e = prepare_decode_device(nullptr); e != hipSuccess) return e;
+    const dim3 grid((unsigned)a.n_paths * (unsigned)a.pool.num_kv_heads), block(64 * waves);
+    if (waves == 4)
+        hipExtLaunchKernelGGL(four_path_kernel<4>, grid, block, (unsigned)sizeof(Shares<4>), s, ev_begin, ev_end, 0, a);
+    else
+        hipExtLaunchKernelGGL(four_path_kernel<8>, grid, block, (unsigned)sizeof(Shares<8>), s, ev_begin, ev_end, 0, a);
+    return hipGetLastError();
 }
 
 hipError_t launch_four_decode(const DecodeLaunch &a, hipStream_t s, hipEvent_t ev_begin, hipEvent_t ev_end) {

@@ -49,6 +49,7 @@ inline double estimate_us(const Load (&load)[5], double bytes, int32_t parts, do
 struct Cut {
     int max_rows, shared_chunk, leaf_chunk;
     bool pack;
+    double us;
 };
 struct Pieces {
     int count, blocks;  // chunks of a node, blocks of one (whole steps of four, the last one shorter)
@@ -92,7 +93,7 @@ inline Cut choose(const hkv_decode_plan &pl, int n_cu) {
                 shared[c][i][rows <= 16 ? 0 : rows <= 32 ? 1 : rows <= 64 ? 2 : 3].add((int64_t)p.count * groups * Hkv, tokens, steps * groups);
             }
         }
-    Cut best{128, 2048, 4096, false};
+    Cut best{128, 2048, 4096, false, 0};
     double least = 1e300;
     bool best_fits = false;
     for (int c = 0; c < 4; ++c)
@@ -113,7 +114,7 @@ inline Cut choose(const hkv_decode_plan &pl, int n_cu) {
                     if (fits == best_fits ? us >= least : !fits) continue;
                     least = us;
                     best_fits = fits;
-                    best = Cut{pl.opt.max_rows ? pl.opt.max_rows : kRowCaps[c], kChunks[s], kChunks[f], pack};
+                    best = Cut{pl.opt.max_rows ? pl.opt.max_rows : kRowCaps[c], kChunks[s], kChunks[f], pack, us};
                 }
     if (pl.opt.shared_chunk) best.shared_chunk = pl.opt.shared_chunk;
     if (pl.opt.leaf_chunk) best.leaf_chunk = pl.opt.leaf_chunk;
@@ -168,6 +169,8 @@ inline std::vector<int32_t> dispatch_order(const std::array<std::vector<double>,
 static void plan_four_bit(hkv_decode_plan &pl, int n_cu) {
     const int G = pl.group, Hkv = pl.pool->d.num_kv_heads, n_nodes = (int)pl.nodes.size();
     const four_plan::Cut cut = four_plan::choose(pl, n_cu);
+    pl.items_us = cut.us;
+    if (pl.paths_us == 0 || pl.paths_us > 0.93 * pl.items_us) pl.n_paths = pl.path_waves = 0;  // else paths instead (estimate_paths); the items are described as ever
     const int max_req = std::max(1, cut.max_rows / G);
     struct Proto {
         DecodeItem it;

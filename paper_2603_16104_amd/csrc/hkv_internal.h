@@ -448,6 +448,7 @@ hipError_t launch_four_step_append(const PoolAppendInline &w, const PlanGrowInli
 hipError_t launch_four_widen(const PoolDequantLaunch &a, hipStream_t s);
 hipError_t prepare_four_decode();  // (part of prepare_decode_device)
 hipError_t launch_four_decode(const DecodeLaunch &a, hipStream_t s, hipEvent_t ev_begin = nullptr, hipEvent_t ev_end = nullptr);
+hipError_t launch_four_paths(const DecodePathLaunch &a, int waves, hipStream_t s, hipEvent_t ev_begin = nullptr, hipEvent_t ev_end = nullptr);
 // Once per device (later calls only read the result), with that device current and outside graph capture:
 // allows the decode kernels their LDS and looks up the device's static workspace (kStaticWorkspaceBytes
 // bytes, 256-byte aligned), returned through static_ws unless that is null.  Safe from several threads.

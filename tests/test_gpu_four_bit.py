@@ -235,6 +235,25 @@ def test_decode_rows_of_q():
     pool.close()
 
 
+@pytest.mark.parametrize("hq,hk,page,prefix,own,n_req,T", [(8, 2, 16, 256, 49, 4, 1), (1, 1, 16, 0, 1, 1, 1), (32, 8, 32, 33, 20, 40, 1), (8, 2, 16, 736, 30, 2, 1), (64, 8, 16, 1200, 30, 16, 1), (40, 8, 64, 65, 100, 3, 2), (4, 2, 16, 129, 16, 5, 16), (16, 1, 128, 200, 3, 2, 3)])
+def test_whole_paths(hq, hk, page, prefix, own, n_req, T):
+    """Small steps: a workgroup a leaf and KV head, with 8 wavefronts or (many leaves) 4; nodes that end anywhere, a leaf of two requests, one above others."""
+    f = Forest([(-1, prefix), (0, 7)] + [(i % 2, own + i) for i in range(n_req)], list(range(2, 2 + n_req)) + ([2, 1] if T == 1 else []), page, seed=3)
+    pool = Pool(f.n_pages, hk, page, seed=5)
+    poison_unused_slots(pool, f)
+    q = queries(len(f.leaves) * T, hq)
+    plan = hkv.hkv_decode_plan_create_ex(pool.handle, f.nodes, f.node_pages, f.leaves, hq, tokens_per_req=T)
+    assert hkv.hkv_decode_plan_num_paths(plan) > 0
+    results = [decode(plan, q, static) for static in (False, True)]
+    pool.k_scale[pool.k_scale == 255] = 127
+    pool.v_scale[pool.v_scale == 255] = 127
+    check_decode(f, pool, q, *results[0], T)
+    for a, b in zip(*results):
+        np.testing.assert_array_equal(a, b)
+    hkv.hkv_decode_plan_destroy(plan)
+    pool.close()
+
+
 ITEM_ROWS = [(32, 17), (32, 32), (64, 33), (64, 56), (64, 64), (128, 65), (128, 96), (128, 100), (128, 128)]
 
 

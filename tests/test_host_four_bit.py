@@ -54,7 +54,11 @@ def test_plans():
     assert code(hkv.hkv_decode_plan_create, pool, nodes, pages, [1, 2], 3, hkv.PLAN_HOST_ONLY) == hkv.ESHAPE
     assert code(hkv.hkv_decode_plan_create, pool, nodes, [0, 1, 2, 64], [1, 2], 8, hkv.PLAN_HOST_ONLY) == hkv.ERANGE
     plan = hkv.hkv_decode_plan_create(pool, nodes, pages, [1, 2], 8, hkv.PLAN_HOST_ONLY)
-    assert hkv.hkv_decode_plan_num_paths(plan) == 0 and hkv.hkv_decode_plan_num_tile_items(plan) == 0 and not hkv.hkv_decode_plan_is_fused(plan)
+    assert hkv.hkv_decode_plan_num_paths(plan) == 2 and hkv.hkv_decode_plan_num_tile_items(plan) == 0 and not hkv.hkv_decode_plan_is_fused(plan)
+    for other in (hkv.hkv_decode_plan_create_ex(pool, nodes, pages, [1, 2], 8, hkv.PLAN_HOST_ONLY, pack=1),        # a setting of the items, a plan that grows
+                  hkv.hkv_decode_plan_create_growing(pool, nodes, pages, [1, 2], 8, 5, hkv.PLAN_HOST_ONLY)):
+        assert hkv.hkv_decode_plan_num_paths(other) == 0
+        hkv.hkv_decode_plan_destroy(other)
     assert code(hkv.hkv_decode_plan_track_weights, plan) == hkv.ESHAPE
     assert code(hkv.hkv_decode_plan_store, plan, hkv.qkv_rows(q=A, k=A, v=A, q_out=2 * A, rotary_dim=128, inv_freq=A), 0) == hkv.ESHAPE
     assert code(hkv.attn_decode_plan_run, plan, A, 0.1, A, A, A, 1 << 20, 0) == hkv.EINVAL  # a host-only plan
