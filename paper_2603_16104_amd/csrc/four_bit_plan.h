@@ -158,7 +158,7 @@ inline std::vector<int32_t> dispatch_order(const std::array<std::vector<double>,
         left[k] -= us[k][next[k]++];
         ++count[k];
     }
-    std::stable_partition(order.begin(), order.begin() + std::min<size_t>(order.size(), (size_t)std::max(slots, 0)), [](int32_t i) { return i >= 0; });
+    std::stable_partition(order.begin(), order.begin() + std::min<size_t>(order.size(), (size_t)slots), [](int32_t i) { return i >= 0; });
     return order;
 }
 
@@ -201,10 +201,10 @@ static void plan_four_bit(hkv_decode_plan &pl, int n_cu) {
     if (pl.opt.interleave >= 0) {  // items of many and of few rows side by side, in whole sets of KV heads, which stay on their XCDs
         std::vector<Proto> many, few;
         for (const Proto &x : protos) (x.it.n_req * G > 16 ? many : few).push_back(x);
-        const int set = cut.pack ? four_plan::kXcds : (four_plan::kXcds + Hkv - 1) / Hkv * Hkv;
-        const auto order = four_plan::dispatch_order({four_plan::lengths(many, set, G, false), four_plan::lengths(few, cut.pack ? 4 * set : set, G, cut.pack)}, 2 * n_cu / set);
+        const int set = cut.pack ? four_plan::kXcds : (four_plan::kXcds + Hkv - 1) / Hkv * Hkv, slots = std::max(1, 2 * n_cu / set);
+        const auto order = four_plan::dispatch_order({four_plan::lengths(many, set, G, false), four_plan::lengths(few, cut.pack ? 4 * set : set, G, cut.pack)}, slots);
         if (cut.pack) {
-            if (!many.empty() && (int)order.size() > 2 * n_cu / set) pl.order = order;  // (what starts all at once is in order)
+            if (!many.empty() && (int)order.size() > slots) pl.order = order;  // (what starts all at once is in order)
         } else {
             protos.clear();
             for (const int32_t i : order) {

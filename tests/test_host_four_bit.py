@@ -166,3 +166,17 @@ def test_the_same_forest_is_cut_the_same_way():
     for p in plans:
         hkv.hkv_decode_plan_destroy(p)
     hkv.kv_pool_destroy(pool)
+
+
+@pytest.mark.parametrize("heads", [3, 11, 513, 700])
+@pytest.mark.parametrize("setting", [dict(pack=1), dict(pack=3), dict(interleave=-1, pack=1)])
+def test_any_number_of_heads(heads, setting):
+    """Sets of items are whole sets of KV heads, however many those are; every item is listed once."""
+    nodes = [(-1, 0, 4, 64)] + [(0, 4 + i, 1, 9) for i in range(20)]
+    pool = pool_of(24, heads)
+    plan = hkv.hkv_decode_plan_create_ex(pool, nodes, np.arange(24), list(range(1, 21)), heads, hkv.PLAN_HOST_ONLY, **setting)
+    items = hkv.hkv_decode_plan_items(plan)
+    key = items[:, [7, 6, 2, 3]]
+    assert len(np.unique(key, axis=0)) == len(items) and (np.bincount(items[:, 2], minlength=heads) == len(items) // heads).all()
+    hkv.hkv_decode_plan_destroy(plan)
+    hkv.kv_pool_destroy(pool)
