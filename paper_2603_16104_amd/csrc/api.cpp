@@ -161,14 +161,19 @@ extern "C" int kv_pool_retain(hkv_pool *pool, int32_t n, const int32_t *ids) {
 }
 
 extern "C" int kv_pool_release(hkv_pool *pool, int32_t n, const int32_t *ids) {
-    if (int rc = check_held(pool, n, ids, "kv_pool_release")) return rc;
-    int held = 0;  // a page may occur several times: every listing is counted, then the counts are as they were again
-    while (held < n && pool->refcnt[ids[held]] > 0) --pool->refcnt[ids[held++]];
-    for (int i = 0; i < held; ++i) ++pool->refcnt[ids[i]];
-    if (held < n) return fail(HKV_EINVAL, "kv_pool_release: page %d released more often than it is held", ids[held]);
-    for (int i = 0; i < n; ++i)
+    if (!pool || n <= 0 || !ids) return check_held(pool, n, ids, "kv_pool_release");
+    const int32_t pages = pool->d.num_pages;
+    int i = 0;  // every listing gives a reference back (a page may occur several times) ...
+    for (; i < n; ++i) {
+        if (ids[i] < 0 || ids[i] >= pages || pool->refcnt[ids[i]] <= 0) break;
         if (--pool->refcnt[ids[i]] == 0) pool->free_list.push_back(ids[i]);
-    return HKV_OK;
+    }
+    if (i == n) return HKV_OK;
+    const int32_t bad = ids[i];  // ... or none
+    while (i-- > 0)
+        if (pool->refcnt[ids[i]]++ == 0) pool->free_list.pop_back();
+    if (int rc = check_held(pool, n, ids, "kv_pool_release")) return rc;
+    return fail(HKV_EINVAL, "kv_pool_release: page %d released more often than it is held", bad);
 }
 
 extern "C" int32_t kv_pool_num_free(const hkv_pool *pool) {

@@ -136,11 +136,12 @@ extern "C" int kv_pool_fork(hkv_pool *pool, int32_t n_seq, const int32_t *pages,
         for (int64_t i = 0; i < total; ++i)
             if (--held[pages[i]] < 0) return fail(HKV_EINVAL, "%s: page %d listed more often than it is held", who, pages[i]);
     }
-    std::vector<int32_t> first_fork(n_seq, -1);
+    std::vector<int32_t> first_fork(n_seq, -1), forks(n_seq, 0);
     int64_t out_total = 0;
     for (int j = 0; j < n_out; ++j) {
         if (parent[j] < 0 || parent[j] >= n_seq) return fail(HKV_ERANGE, "%s: fork %d of sequence %d of %d", who, j, parent[j], n_seq);
         if (first_fork[parent[j]] < 0) first_fork[parent[j]] = j;
+        ++forks[parent[j]];
         out_total += begin[parent[j] + 1] - begin[parent[j]];
     }
     if (out_total > INT_MAX) return fail(HKV_EINVAL, "%s: too many pages", who);
@@ -172,14 +173,10 @@ extern "C" int kv_pool_fork(hkv_pool *pool, int32_t n_seq, const int32_t *pages,
         pool->free_list.pop_front();
         pool->refcnt[c.dst] = 1;
     }
-    int64_t at = 0;
-    for (int j = 0; j < n_out; ++j) {
-        const int i = parent[j];
-        const int64_t n = begin[i + 1] - begin[i], whole = n_tokens[i] / P;
-        for (int64_t p = 0; p < whole; ++p) ++pool->refcnt[out[at + p]];
-        if (n > whole && out[at + whole] == pages[begin[i + 1] - 1]) ++pool->refcnt[out[at + whole]];  // (taken over: given back below)
-        at += n;
-    }
+    for (int j = 0; release && j < n_out; ++j)  // a last page that is taken over (given back by its sequence below)
+        if (n_tokens[parent[j]] % P != 0 && takes_over(j)) ++pool->refcnt[pages[begin[parent[j] + 1] - 1]];
+    for (int i = 0; i < n_seq; ++i)
+        for (int64_t p = begin[i]; p < begin[i] + n_tokens[i] / P; ++p) pool->refcnt[pages[p]] += forks[i];
     if (release)
         for (int64_t i = 0; i < total; ++i)
             if (--pool->refcnt[pages[i]] == 0) pool->free_list.push_back(pages[i]);
