@@ -819,7 +819,7 @@ __device__ __forceinline__ void run_rows(const DecodeLaunch &a, const DecodeItem
             if (i == 13) widen_dims(std::integral_constant<int, 3>{}, std::integral_constant<int, 1 - P>{});
             __builtin_amdgcn_sched_barrier(0);
         }
-        asm volatile("" : "+v"(sum));
+        asm volatile("" : "+v"(sum), "+v"(top));  // (found beside the product, not behind the branch that may find it anew)
         t.l += sum;
         settle(next, b + 1, top);
         ring.landed();  // the share of step b + 2; of all wavefronts behind the barrier
@@ -1015,7 +1015,7 @@ __device__ __forceinline__ void run_tall(const DecodeLaunch &a, const DecodeItem
             if (i == 14) widen_dims(std::integral_constant<int, 3>{}, std::integral_constant<int, 1 - P>{});
             __builtin_amdgcn_sched_barrier(0);
         }
-        asm volatile("" : "+v"(sum));
+        asm volatile("" : "+v"(sum), "+v"(top));  // (found beside the product, not behind the branch that may find it anew)
         x.l += sum;
         settle(next, b + 1, top);
         ring.landed();  // the share of step b + 2; of all wavefronts behind the barrier
