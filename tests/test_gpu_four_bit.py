@@ -221,12 +221,13 @@ def test_decode_drafts(hq, hk, T, prefix, own, tree):
     pool.close()
 
 
-def test_decode_rows_of_q():
+@pytest.mark.parametrize("setting", [{}, dict(max_rows=16), dict(max_rows=128, pack=3)])
+def test_decode_rows_of_q(setting):
     """q_rows: the plan's rows lie among others."""
     f = Forest([(-1, 90), (0, 40), (0, 17)], [1, 2], 16)
     pool = Pool(f.n_pages, 2)
     q = queries(7, 8)
-    plan = hkv.hkv_decode_plan_create_ex(pool.handle, f.nodes, f.node_pages, f.leaves, 8, q_rows=np.asarray([5, 2], dtype=np.int32))
+    plan = hkv.hkv_decode_plan_create_ex(pool.handle, f.nodes, f.node_pages, f.leaves, 8, q_rows=np.asarray([5, 2], dtype=np.int32), **setting)
     out, lse = decode(plan, q)
     others = [0, 1, 3, 4, 6]
     assert np.isnan(out[others]).all() and np.isnan(lse[others]).all()
@@ -445,6 +446,28 @@ def test_prefill(hq, hk, page, lens):
             refs.append(attention(f64(q)[cu[i] + j], kk, vv, SCALE, np.arange(total[i]) <= prefix + j))
     check_rows(*results[0], tuple(np.stack([x[i] for x in refs]) for i in range(4)))
     hkv.hkv_prefill_plan_destroy(plan)
+    pool.close()
+
+
+def test_prefill_rows_anywhere():
+    """The new tokens' rows lie where the caller says; rows between them stay as they are."""
+    pool = Pool(30, 2, seed=7)
+    order = np.random.default_rng(1).permutation(30).astype(np.int32)
+    table = np.full((2, 19), -1, dtype=np.int32)
+    table[0, :6], table[1] = order[:6], order[6:25]
+    q = queries(100, 8)
+    results = []
+    for plan, rows in ((hkv.hkv_prefill_plan_create(pool.handle, [0, 40, 60], table, [90, 300], 8), torch.cat([q[5:45], q[70:90]])),
+                       (hkv.hkv_prefill_plan_create_rows(pool.handle, [5, 70], [40, 20], table, [90, 300], 8), q)):
+        out, lse = torch.full_like(rows, float("nan")), torch.full((len(rows), 8), float("nan"), device="cuda")
+        need = hkv.hkv_prefill_plan_workspace_bytes(plan)
+        hkv.attn_prefill_plan_run(plan, rows, SCALE, out, lse, None, torch.empty(need, dtype=torch.uint8, device="cuda"), need)
+        results.append((f64(out), lse.double().cpu().numpy()))
+        hkv.hkv_prefill_plan_destroy(plan)
+    mine = np.r_[5:45, 70:90]
+    for a, b in zip(*results):
+        np.testing.assert_array_equal(a, b[mine])
+        assert np.isnan(np.delete(b, mine, axis=0)).all()
     pool.close()
 
 
