@@ -82,7 +82,7 @@ enum {
     HKV_EHIP = -6    /* a HIP runtime call failed (message holds the HIP error string) */
 };
 
-/* Pool element types.  bf16 and fp8 pools are the throughput paths (matrix cores, bf16 q and out).
+/* Pool element types.  bf16, fp8 and fp4 pools are the throughput paths (matrix cores, bf16 q and out).
  * An fp32 pool selects the full-precision path: k_src / v_src of kv_pool_write, q, and out of the
  * attention calls are then fp32 as well, all arithmetic is fp32 on the vector ALUs, one workgroup
  * per (query token, up to four query heads) without sharing between requests, no workspace is needed (a decode plan of few rows
@@ -151,7 +151,7 @@ int kv_pool_release(hkv_pool *pool, int32_t n, const int32_t *ids /* host */);
  * from another continues inside the last, partially filled page; sharing itself stays whole
  * pages, Section 6).  For each listed page: with a single reference it stays as it is; otherwise
  * the next free page is taken (reference count 1), the whole page (K and V blocks of every head
- * and, for fp8 pools, its scales) is copied to it on `stream`, one reference of the old page is
+ * and, for fp8 and fp4 pools, its scales) is copied to it on `stream`, one reference of the old page is
  * dropped and ids[i] is replaced by the new id.  Work queued earlier on `stream` that writes the
  * old page is seen by the copy; the old page must not be written on other streams meanwhile.
  *   ids: host, n entries, in/out, no page twice.
@@ -246,7 +246,7 @@ typedef struct {
     int32_t n_pages;    /* == ceil(n_tokens / 16) */
     int32_t n_tokens;   /* omega(v) >= 0.  prefix_tree_flatten, prefill and fp32 pools need a multiple
                            of 16 in every node that has children (positions along a path must map
-                           to pages without gaps); the bf16 / fp8 decode plans do not */
+                           to pages without gaps); the bf16 / fp8 / fp4 decode plans do not */
 } hkv_node;
 
 /* Host-only, integer-only.  Expands the forest into what the kernels index with:
@@ -340,7 +340,7 @@ enum {
 /* nodes, node_pages, req_leaf: host.  Validates the forest (ETREE/ERANGE, page ids against the
  * pool), builds the work list and uploads it (blocking).  ESHAPE unless num_q_heads is a
  * multiple of the pool's num_kv_heads with a ratio of at most 16.
- * With bf16 and fp8 pools every node is read through its own page list, so any node may end inside
+ * With bf16, fp8 and fp4 pools every node is read through its own page list, so any node may end inside
  * a page (its last page is then partly used and its children start on pages of their own).  That
  * makes the forest itself the attention mask of a tree of drafted tokens: one node per drafted
  * token (or run of tokens) under the request's context, one "request" per node to be verified,
@@ -373,7 +373,7 @@ int hkv_decode_plan_create_tree(hkv_pool *pool, const hkv_node *nodes, int32_t n
  * up to reserve_tokens tokens, so that generating a token does not cost a new plan (a tree walk, a
  * device allocation and a blocking upload) but one call of hkv_decode_plan_append.  Every request
  * needs a leaf of its own for that: a node without children, named by no other request, holding at
- * least one token (ETREE otherwise).  bf16 and fp8 pools (ESHAPE for fp32 pools).
+ * least one token (ETREE otherwise).  bf16, fp8 and fp4 pools (ESHAPE for fp32 pools).
  *
  * hkv_decode_plan_append: every request's leaf has grown by one token, whose K/V the caller stores
  * (kv_pool_append) before the next run.  new_page_ids: host, [n_req]; entry r is read only if the
@@ -401,7 +401,7 @@ typedef struct {
     const int32_t *q_rows;    /* host [n_req * tokens_per_req] or NULL: row i of the plan (request i / T, token i % T)
                                  reads row q_rows[i] of q and writes row q_rows[i] of out and lse_out, so that a
                                  step's decode rows may lie anywhere among the rows of other work (a mixed
-                                 step).  Entries >= 0 and all different (EINVAL); bf16 and fp8 pools (ESHAPE
+                                 step).  Entries >= 0 and all different (EINVAL); bf16, fp8 and fp4 pools (ESHAPE
                                  for fp32 pools).  NULL: row i */
     /* ---- planner settings */
     int32_t leaf_chunk;       /* tokens per item of nodes read by at most 16 query rows; multiple of 16 */
@@ -551,7 +551,7 @@ int hkv_prefill_plan_create(hkv_pool *pool, const int32_t *cu_q, const int32_t *
 /* The same for a step that mixes prefill with other work in one q / out / lse (Section 6, engine integration:
  * chunks of prompts run next to decode steps): request r's q_len[r] new tokens are rows q_row_begin[r] ..
  * q_row_begin[r] + q_len[r] - 1 of q, out and lse_out; rows no request names are neither read nor written.
- * q_row_begin, q_len: host [n_req], >= 0; EINVAL if two requests share a row.  bf16 and fp8 pools
+ * q_row_begin, q_len: host [n_req], >= 0; EINVAL if two requests share a row.  bf16, fp8 and fp4 pools
  * (ESHAPE for fp32 pools).  Everything else as hkv_prefill_plan_create. */
 int hkv_prefill_plan_create_rows(hkv_pool *pool, const int32_t *q_row_begin, const int32_t *q_len,
                                  const int32_t *block_table, int32_t max_pages, const int32_t *kv_len, int32_t n_req,
@@ -567,7 +567,7 @@ int32_t hkv_prefill_plan_num_segments(const hkv_prefill_plan *plan);
 /* The prefill kernel keeps one softmax reference per row (the maximum of its first 32 scores); a tile in which a
  * later score exceeds it by more than the exponent range allows repeats with a running maximum, at about
  * twice the cost.  count (host): how many tiles (pieces, where there are some) did so over all runs of this
- * plan so far (the call waits for the device).  bf16 and fp8 pools; always 0 for fp32 pools. */
+ * plan so far (the call waits for the device).  bf16, fp8 and fp4 pools; always 0 for fp32 pools. */
 int hkv_prefill_plan_fallback_tiles(hkv_prefill_plan *plan, int64_t *count);
 /* Tile layout for tests, 8 int32 each: (req, q_begin, n_q, kv_head, q_row0, prefix_len, kv_len, bt_off). */
 int hkv_prefill_plan_tiles(const hkv_prefill_plan *plan, int32_t *tiles_out);

@@ -311,7 +311,7 @@ extern "C" int kv_pool_append(hkv_pool *pool, const int32_t *page_ids, const int
     if (n < 0) return fail(HKV_EINVAL, "kv_pool_append: n %d", n);
     if (n == 0) return HKV_OK;
     if (!page_ids || !slots || !k_src || !v_src) return fail(HKV_EINVAL, "kv_pool_append: null argument");
-    if (pool->d.dtype == HKV_FP32) return fail(HKV_ESHAPE, "kv_pool_append: bf16 and fp8 pools only");
+    if (pool->d.dtype == HKV_FP32) return fail(HKV_ESHAPE, "kv_pool_append: bf16, fp8 and fp4 pools only");
     if ((reinterpret_cast<uintptr_t>(k_src) | reinterpret_cast<uintptr_t>(v_src)) & 15)
         return fail(HKV_EINVAL, "kv_pool_append: k_src and v_src must be 16-byte aligned");
     if (n > hkv_pool::kMaxWritePages / 2) return fail(HKV_EINVAL, "kv_pool_append: %d tokens in one call (limit %d)", n, hkv_pool::kMaxWritePages / 2);
@@ -1584,7 +1584,7 @@ static int create_growing_plan(hkv_pool *pool, const hkv_node *nodes, int32_t n_
                                hkv_decode_plan **out) {
     if (!pool || !out) return fail(HKV_EINVAL, "hkv_decode_plan_create_growing: null argument");
     *out = nullptr;
-    if (pool->d.dtype == HKV_FP32) return fail(HKV_ESHAPE, "hkv_decode_plan_create_growing: bf16 and fp8 pools only");
+    if (pool->d.dtype == HKV_FP32) return fail(HKV_ESHAPE, "hkv_decode_plan_create_growing: bf16, fp8 and fp4 pools only");
     if (reserve_tokens < 1 || reserve_tokens > (1 << 20))
         return fail(HKV_EINVAL, "hkv_decode_plan_create_growing: reserve_tokens %d", reserve_tokens);
     if (n_nodes < 0 || n_req < 0 || (n_nodes > 0 && !nodes) || (n_req > 0 && !req_leaf))
@@ -2528,7 +2528,7 @@ extern "C" int hkv_prefill_plan_create_rows(hkv_pool *pool, const int32_t *q_row
                                             int32_t n_req, int32_t num_q_heads, uint32_t flags, hkv_prefill_plan **out) {
     if (!pool || !out) return fail(HKV_EINVAL, "hkv_prefill_plan_create_rows: null argument");
     *out = nullptr;
-    if (pool->d.dtype == HKV_FP32) return fail(HKV_ESHAPE, "hkv_prefill_plan_create_rows: bf16 and fp8 pools only");
+    if (pool->d.dtype == HKV_FP32) return fail(HKV_ESHAPE, "hkv_prefill_plan_create_rows: bf16, fp8 and fp4 pools only");
     if (n_req < 0 || (n_req > 0 && (!q_row_begin || !q_len))) return fail(HKV_EINVAL, "hkv_prefill_plan_create_rows: bad argument");
     std::vector<int32_t> cu((size_t)n_req + 1, 0);
     std::vector<std::pair<int64_t, int64_t>> spans;
