@@ -1079,6 +1079,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void four_decode_kernel(DecodeLaunc
     if (at >= a.n_single) return;
     const DecodeItem it = a.items[at];
     const int rows = it.n_req * G;
+    // Measured on both sides (16 prompts of 2048 tokens, 8 KV heads): 32 rows with tokens shared 24.6 us, with 16 rows a wavefront 27.2; 48 rows
+    // with 16 a wavefront 29.8, with 32 a wavefront, two of them idle beside it, 37.  More than 64 rows only the last form takes.
     if (rows <= 16)
         run_shared_tokens<1>(a, it, lds.s);
     else if (rows <= 32)
