@@ -251,6 +251,16 @@ __device__ __forceinline__ void weigh(const RowTile (&tile)[RT], const f32x4 (&a
     }
 }
 template <int RT>
+__device__ __forceinline__ void follow_all(RowTile (&tile)[RT], const f32x4 (&acc)[RT][4], float c) {
+#pragma unroll
+    for (int r = 0; r < RT; ++r) {
+        float top = acc[r][0][0];
+#pragma unroll
+        for (int j = 1; j < 16; ++j) top = fmaxf(top, acc[r][j & 3][j >> 2]);
+        follow(tile[r], top, c);
+    }
+}
+template <int RT>
 __device__ __forceinline__ void weights(RowTile (&tile)[RT], const f32x4 (&acc)[RT][4], float c, u32x4 (&pw)[RT][2]) {
     float sum[RT];
     weigh(tile, acc, c, pw, sum);
@@ -258,13 +268,7 @@ __device__ __forceinline__ void weights(RowTile (&tile)[RT], const f32x4 (&acc)[
 #pragma unroll
     for (int r = 0; r < RT; ++r) any = any || !(sum[r] <= kMostWeight) || tile[r].m == -INFINITY;  // (a NaN, too)
     if (__builtin_amdgcn_ballot_w64(any)) {
-#pragma unroll
-        for (int r = 0; r < RT; ++r) {
-            float top = acc[r][0][0];
-#pragma unroll
-            for (int j = 1; j < 16; ++j) top = fmaxf(top, acc[r][j & 3][j >> 2]);
-            follow(tile[r], top, c);
-        }
+        follow_all(tile, acc, c);
         weigh(tile, acc, c, pw, sum);
     }
 #pragma unroll
@@ -533,7 +537,8 @@ __device__ __forceinline__ void run_shared_tokens(const DecodeLaunch &a, const D
 }
 
 // Small steps: a workgroup of W wavefronts per KV head and leaf (and up to 16 of its rows) walks the whole path and writes the result itself: no items' partials
-// and no second launch (4 requests over 256 + 49 tokens 6.7 us, as items and merge 7.7; what bounds it is the chain of record, queries and codes).  Blocks that are not full may lie anywhere on it, at the end of every node; `gap` is how many of a block's last slots are nobody's.
+// and no second launch (4 requests over 256 + 49 tokens 6.6 us, as items and merge 7.7).  What bounds it is the chain of record, codes and queries, and a
+// step's own length.  Blocks that are not full may lie anywhere on the path, at the end of every node; `gap` is how many of a block's last slots are nobody's.
 struct PathStep : Operands {
     int gap;  // of the lane's block of V, which is that of its scores too
 };
@@ -544,17 +549,18 @@ __global__ __launch_bounds__(64 * W, 2) void four_path_kernel(DecodePathLaunch a
     const int lane = (int)threadIdx.x & 63, m = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int Hkv = a.pool.num_kv_heads, G = a.num_q_heads / Hkv, head = (int)blockIdx.x % Hkv;
     const int32_t *path = a.paths + (size_t)(blockIdx.x / Hkv) * a.path_stride;
-    const int n_blocks = path[0], rows = path[1] * G, n_steps = (n_blocks + 3) / 4, row = min(m, rows - 1);
+    const int n_blocks = path[0], rows = path[1] * G, n_steps = (n_blocks + 3) / 4;
     const float c = exponent_factor(a.scale);
     const uint8_t *k = static_cast<const uint8_t *>(a.pool.k_pages) + (m & 3) * 64 + g * 16, *v = static_cast<const uint8_t *>(a.pool.v_pages) + m * 16;
     const uint8_t *k_scale = reinterpret_cast<const uint8_t *>(a.pool.k_scale) + g * 16 + 4 * (m & 3), *v_scale = reinterpret_cast<const uint8_t *>(a.pool.v_scale) + (m >> 2) * 16;
-    auto ids = [&](int (&id)[4], int b) {  // clamped, so always in bounds; a block behind the path's last is all gap
+    // Clamped to the record, whose end is zeros, so always in bounds and asked for before the path's length is known; a block behind the path's last is all gap.
+    auto ids = [&](int (&id)[4], int b) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i) id[i] = path[kPathBlocks + min(4 * b + i, n_blocks - 1)] | (4 * b + i < n_blocks ? 0 : 16 << kPathIdBits);
+        for (int i = 0; i < 4; ++i) id[i] = path[kPathBlocks + min(4 * b + i, a.path_stride - kPathBlocks - 1)];
     };
     auto block = [&](int id) { return (size_t)(id & kPathIdMask) * Hkv + head; };
-    auto fetch = [&](PathStep &x, const int (&id)[4]) {
-        const int mine = pick4(id, g);
+    auto fetch = [&](PathStep &x, const int (&id)[4], int b) {
+        const int mine = pick4(id, g) | (4 * b + g < n_blocks ? 0 : 16 << kPathIdBits);
         const size_t kb = block(pick4(id, m >> 2)), vb = block(mine);
         x.gap = (int)((uint32_t)mine >> kPathIdBits);
         x.k_scale = *reinterpret_cast<const uint32_t *>(k_scale + kb * four::kScaleBytes);
@@ -564,56 +570,61 @@ __global__ __launch_bounds__(64 * W, 2) void four_path_kernel(DecodePathLaunch a
 #pragma unroll
         for (int j = 0; j < 4; ++j) x.v[j] = ld16(v + vb * four::kCodeBytes + 256 * j);
     };
-    const bool active = wave < n_steps;
     RowTile tile[1];
     RowTile &t = tile[0];
-    const int q_at = path[kPathQRows + row / G] * a.num_q_heads + head * G + row % G;
-    if (active) {
-        PathStep now, next;
-        int id[4], b = wave;
-        t.req = path[kPathRows + row / G];
-        ids(id, b);
-        fetch(now, id);
-        u32x4 w[4];
-        const char *qp = static_cast<const char *>(a.q) + (size_t)q_at * (kHeadDim * 2) + 32 * g;
-        w[0] = ld16(qp);
-        w[1] = ld16(qp + 16);
-        w[2] = ld16(qp + 128);
-        w[3] = ld16(qp + 144);
-        ids(id, b + W);
-        t.lim = a.row_leaf ? path[2] + a.row_limit[t.req] : INT_MAX;  // (positions count whole blocks: the leaf begins at one)
-        split_row(t, w, a.scale);
+    PathStep now, next;
+    int id[4], b = wave;
+    ids(id, b);
+    const int q_at = path[kPathQRows + m / G] * a.num_q_heads + head * G + m % G;  // (the record has 16 requests, the last one again and again)
+    t.req = path[kPathRows + m / G];
+    fetch(now, id, b);
+    u32x4 w[4];
+    const char *qp = static_cast<const char *>(a.q) + (size_t)q_at * (kHeadDim * 2) + 32 * g;
+    w[0] = ld16(qp);
+    w[1] = ld16(qp + 16);
+    w[2] = ld16(qp + 128);
+    w[3] = ld16(qp + 144);
+    ids(id, b + W);
+    t.lim = a.row_leaf ? path[2] + a.row_limit[t.req] : INT_MAX;  // (positions count whole blocks: the leaf begins at one)
+    split_row(t, w, a.scale);
 #pragma unroll
-        for (int dt = 0; dt < 8; ++dt) t.o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
-        t.m = -INFINITY;
-        t.l = 0.f;
+    for (int dt = 0; dt < 8; ++dt) t.o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    t.m = -INFINITY;
+    t.l = 0.f;
+    auto step = [&](PathStep &x, PathStep &after, auto first) {
         f32x4 acc[1][4];
         u32x4 pw[1][2];
-        auto step = [&](PathStep &x, PathStep &after) {
-            fetch(after, id);
-            ids(id, b + 2 * W);
-            __builtin_amdgcn_sched_barrier(0);
-            scores(x, tile, acc);
-            const int d0 = 16 * (4 * b + g) - t.lim;
-            if (__builtin_amdgcn_ballot_w64(x.gap > 0 || d0 > -16)) {
-                const uint32_t seen = seen_bits(d0, a.row_leaf ? a.row_mask[t.req] : 0ull) & 0xFFFFu >> x.gap;
+        fetch(after, id, b + W);
+        ids(id, b + 2 * W);
+        __builtin_amdgcn_sched_barrier(0);
+        scores(x, tile, acc);
+        const int d0 = 16 * (4 * b + g) - t.lim;
+        if (__builtin_amdgcn_ballot_w64(x.gap > 0 || d0 > -16)) {
+            const uint32_t seen = seen_bits(d0, a.row_leaf ? a.row_mask[t.req] : 0ull) & 0xFFFFu >> x.gap;
 #pragma unroll
-                for (int j = 0; j < 16; ++j) acc[0][j & 3][j >> 2] = (seen >> j & 1u) ? acc[0][j & 3][j >> 2] : -INFINITY;
+            for (int j = 0; j < 16; ++j) acc[0][j & 3][j >> 2] = (seen >> j & 1u) ? acc[0][j & 3][j >> 2] : -INFINITY;
 #pragma unroll
-                for (int q = 0; q < 4; ++q) {
-                    uint32_t sc = x.v_scale[q];
-                    clear_from(x.v[q], sc, 16 - x.gap - 4 * q);
-                    x.v_scale[q] = sc;
-                }
+            for (int q = 0; q < 4; ++q) {
+                uint32_t sc = x.v_scale[q];
+                clear_from(x.v[q], sc, 16 - x.gap - 4 * q);
+                x.v_scale[q] = sc;
             }
-            weights(tile, acc, c, pw);
-            add_values(tile, x, pw);
-            return (b += W) < n_steps;
-        };
-        while (step(now, next) && step(next, now)) {
         }
-    }
-    leave_share(s, t, wave, m, g, active);
+        if constexpr (decltype(first)::value) {
+            float sum[1];
+            follow_all(tile, acc, c);
+            weigh(tile, acc, c, pw, sum);
+            t.l = sum[0];
+        } else {
+            weights(tile, acc, c, pw);
+        }
+        add_values(tile, x, pw);
+        return (b += W) < n_steps;
+    };
+    if (step(now, next, std::true_type{}))  // (a wavefront without steps takes one of gaps: nothing waits for the path's length)
+        while (step(next, now, std::false_type{}) && step(now, next, std::false_type{})) {
+        }
+    leave_share(s, t, wave, m, g, true);
     if (wave == 0 && g == 0) s.row[m] = q_at;
     __syncthreads();
     const int out_row = (int)threadIdx.x >> 4, col = lane & 15;
