@@ -3,7 +3,7 @@
 //
 // A wavefront takes 64 tokens (four blocks) a step, for one or two tiles of 16 query rows, or for 32 rows (run_tall has its layout):
 //   S^T = K Q^T   v_mfma_scale_f32_16x16x128_f8f6f4: K's codes and scales as they lie in the pool, lane (m, g) dims 32 g .. + 31 of token 4 m + t4 in
-//                 tile t4 (its four scales are one word); a query row as two e4m3 terms, x * 2^e = hi + lo, whose 2^-e is the other scale.  Against bf16
+//                 tile t4 (its four scales are one word); a query row as four e2m3 terms (split_row), whose powers of two are the other scale.  Against bf16
 //                 operands widened from the codes that is the same matrix time and 68 fewer vector instructions a step.
 //   O^T = V^T P^T v_mfma_f32_16x16x32_bf16: lane (m, g) brings dim 8 m + dt of eight tokens of block g.  A scale stands for one token and 32 dims, the
 //                 instruction's for 32 tokens of a dim, so V is widened: two codes (neighbouring dims of a token) an instruction, then one more to
@@ -18,6 +18,7 @@
 
 #include <climits>
 #include <type_traits>
+#include <utility>
 
 #include "four_bit.h"
 
@@ -29,15 +30,28 @@ constexpr int kWaves = 4, kStep = 64;  // wavefronts; tokens of a step
 constexpr int kORow = kHeadDim + 4;    // padded LDS row
 
 typedef __attribute__((ext_vector_type(8))) int i32x8;
+typedef __attribute__((ext_vector_type(6))) uint32_t u32x6;  // 32 e2m3 codes
 typedef __attribute__((ext_vector_type(16))) float f32x16;
+typedef __attribute__((ext_vector_type(32))) float f32x32;
 
 __device__ __forceinline__ f32x4 mfma16(bf16x8 a, bf16x8 b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
-// 16 tokens (e2m1, scale byte T of k_scale) x 128 dims by 128 dims x 16 rows (e4m3, scale byte 0 of q_scale).  Lane (m, g): of the tokens dims 32 g .. + 31, of
-// the rows dims 16 g .. + 15 and 64 + 16 g .. + 15.
-template <int T>
-__device__ __forceinline__ f32x4 mfma_four(u32x4 k, i32x8 q, f32x4 c, uint32_t k_scale, uint32_t q_scale) {
-    const i32x8 a = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, q, c, 4, 0, T, k_scale, 0, q_scale);
+constexpr int kTerms = 4;  // of a query row
+// The instruction's operands for its 6-bit and 4-bit types: the six and four registers in front count.
+__device__ __forceinline__ i32x8 as_six(u32x6 q) { return i32x8{(int)q[0], (int)q[1], (int)q[2], (int)q[3], (int)q[4], (int)q[5], 0, 0}; }
+__device__ __forceinline__ i32x8 as_four(u32x4 k) { return i32x8{(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0}; }
+// 16 tokens (e2m1, scale byte T of k_scale) x 128 dims by 128 dims x 16 rows (e2m3, scale byte Term of q_scale).  Lane (m, g): dims 32 g .. + 31 of either.
+template <int T, int Term>
+__device__ __forceinline__ f32x4 mfma_four(u32x4 k, const u32x6 (&q)[kTerms], f32x4 c, uint32_t k_scale, uint32_t q_scale) {
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(as_four(k), as_six(q[Term]), c, 4, 2, T, k_scale, Term, q_scale);
+}
+// f(0), f(1), .. f(N - 1), each with its number as a constant.
+template <class F, int... I>
+__device__ __forceinline__ void in_turn(F &&f, std::integer_sequence<int, I...>) {
+    (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void in_turn(F &&f) {
+    in_turn(f, std::make_integer_sequence<int, N>{});
 }
 
 __device__ __forceinline__ int pick4(const int (&v)[4], int sel) {
@@ -54,46 +68,48 @@ struct Operands {
 
 // What a tile of 16 query rows has: lane (m, g) row m.
 struct RowTile {
-    i32x8 hi, lo;       // the query row
-    uint32_t q_scale;
+    u32x6 q[kTerms];    // dims 32 g .. + 31 of the query row
+    uint32_t q_scale;   // the terms' scale bytes
     f32x4 o[8];         // o[dt][i]: dim 32 g + 8 i + dt
     float m, l;         // reference (raw scores), this lane's share of the row sum
     int req;            // the plan's row of it
     int lim;            // tokens of the item that the row may see (and of those behind them the ones in row_mask)
 };
 
-// Four values, |x| <= 448, as e4m3 (to nearest).
-__device__ __forceinline__ int e4m3x4(float a, float b, float c, float d) {
-    return __builtin_amdgcn_cvt_pk_fp8_f32(c, d, __builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false), true);
-}
-
-// A row as two e4m3 terms: its largest magnitude is brought into [128, 256) by a power of two, the first term holds four significant bits, the second
-// what is left: exact for a bf16 value down to 2^-9 of the row's largest, from there on to 2^-17 of it.  sign: -1 for a negative softmax scale.
-__device__ __forceinline__ float row_factor(float top, float sign, uint32_t &q_scale) {
-    const int ex = min(max((int)(__float_as_uint(top) >> 23), 8), 254);  // where both powers are normal numbers
-    q_scale = (uint32_t)(ex - 7);
-    return __uint_as_float((uint32_t)(261 - ex) << 23) * (sign < 0.f ? -1.f : 1.f);
-}
-__device__ __forceinline__ void split_four(uint32_t w0, uint32_t w1, float up, int &hi, int &lo) {
-    const float a = __uint_as_float(w0 << 16) * up, b = __uint_as_float(w0 & 0xFFFF0000u) * up, c = __uint_as_float(w1 << 16) * up, d = __uint_as_float(w1 & 0xFFFF0000u) * up;
-    hi = e4m3x4(a, b, c, d);
-    const auto h0 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, false), h1 = __builtin_amdgcn_cvt_pk_f32_fp8(hi, true);
-    lo = e4m3x4(a - h0[0], b - h0[1], c - h1[0], d - h1[1]);
-}
-__device__ __forceinline__ void split_row(RowTile &x, const u32x4 (&w)[4], float sign) {
-    float top = 0.f;
+// 32 dims of a query row as four e2m3 terms (three bits behind the point, at most 7.5, multiples of 1/8): the largest magnitude is brought into [4, 8) by a power of two, and
+// each term is what those in front leave, under scales 2^4, 2^10 and 2^15 below the first one's.  bf16 values down to 2^-12 of the largest of the 32 are exact, of smaller ones
+// 2^-20 of that is lost.  Products of e2m1 and e2m3 are added without loss inside the matrix instruction, and its sums are those of fp32; of products with e4m3 or e5m2 (two terms
+// in the same matrix time) it cuts off what lies below 2^-13 of the largest among eight neighbouring dims: lse off by 1e-3 for rows with an outlier.
+// A row that holds a NaN or an infinity gets a scale that is no number.  sign: -1 for a negative softmax scale.
+__device__ __forceinline__ void split_row(u32x4 (&w)[4], float sign, u32x6 (&q)[kTerms], uint32_t &q_scale) {
+    typedef __attribute__((ext_vector_type(2))) uint16_t u16x2;
+    const uint32_t flip = sign < 0.f ? 0x80008000u : 0u;
+    u16x2 tops = {0, 0};
+    f32x16 even, odd;  // (the conversion takes the dims in this order)
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i][j] << 16)), fabsf(__uint_as_float(w[i][j] & 0xFFFF0000u))));
-    const float up = row_factor(rows_max(top), sign, x.q_scale);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) {
-        int h, l;
-        split_four(w[j >> 1][2 * (j & 1)], w[j >> 1][2 * (j & 1) + 1], up, h, l);
-        x.hi[j] = h;
-        x.lo[j] = l;
+    for (int i = 0; i < 16; ++i) {
+        const uint32_t word = w[i >> 2][i & 3] ^ flip;
+        tops = __builtin_elementwise_max(tops, __builtin_bit_cast(u16x2, word & 0x7FFF7FFFu));
+        even[i] = __uint_as_float(word << 16);
+        odd[i] = __uint_as_float(word & 0xFFFF0000u);
     }
+    const int ex = max(tops[0], tops[1]) >> 7, first = min(max(ex - 2, 16), 252);  // (the last term's scale is a normal number, too)
+    constexpr int kBelow[kTerms] = {0, 4, 10, 15};
+    q_scale = 0;
+#pragma unroll
+    for (int t = 0; t < kTerms; ++t) {
+        const float scale = __uint_as_float((uint32_t)(first - kBelow[t]) << 23);
+        q_scale |= (uint32_t)(first - kBelow[t]) << (8 * t);
+        q[t] = __builtin_amdgcn_cvt_scalef32_2xpk16_fp6_f32(even, odd, scale);
+        if (t + 1 == kTerms) break;
+        const f32x32 term = __builtin_amdgcn_cvt_scalef32_pk32_f32_fp6(q[t], scale);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            even[i] -= term[2 * i];
+            odd[i] -= term[2 * i + 1];
+        }
+    }
+    if (ex == 255) q_scale = 0xFFFFFFFFu;
 }
 
 // A wavefront's lane, item and pool: where its operands lie.
@@ -145,7 +161,7 @@ __device__ __forceinline__ void find_rows(const Reader &rd, int row0, RowTile (&
 #pragma unroll
     for (int r = 0; r < RT; ++r) tile[r].req = rd.a.node_req_idx[rd.it.req_off + min(row0 + 16 * r + rd.m, rows - 1) / G];
 }
-// The queries, 16 bytes of dims 16 g, 16 g + 8, 64 + 16 g, 64 + 16 g + 8 a lane.
+// The queries, dims 32 g .. + 31 a lane.
 template <int RT>
 __device__ __forceinline__ void load_rows(const Reader &rd, int row0, RowTile (&tile)[RT], u32x4 (&w)[RT][4]) {
     const DecodeLaunch &a = rd.a;
@@ -155,21 +171,19 @@ __device__ __forceinline__ void load_rows(const Reader &rd, int row0, RowTile (&
     for (int r = 0; r < RT; ++r) {
         const int head = it.kv_head * G + min(row0 + 16 * r + rd.m, rows - 1) % G, req = tile[r].req;
         const int q_row = a.q_rows ? a.q_rows[req] : req;
-        const char *qp = static_cast<const char *>(a.q) + ((size_t)q_row * a.num_q_heads + head) * (kHeadDim * 2) + 32 * rd.g;
-        w[r][0] = ld16(qp);
-        w[r][1] = ld16(qp + 16);
-        w[r][2] = ld16(qp + 128);
-        w[r][3] = ld16(qp + 144);
+        const char *qp = static_cast<const char *>(a.q) + ((size_t)q_row * a.num_q_heads + head) * (kHeadDim * 2) + 64 * rd.g;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[r][i] = ld16(qp + 16 * i);
     }
 }
 template <int RT>
-__device__ __forceinline__ void begin_rows(const Reader &rd, RowTile (&tile)[RT], const u32x4 (&w)[RT][4]) {
+__device__ __forceinline__ void begin_rows(const Reader &rd, RowTile (&tile)[RT], u32x4 (&w)[RT][4]) {
     const DecodeLaunch &a = rd.a;
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         const int req = tile[r].req;
         tile[r].lim = a.row_leaf && a.row_leaf[req] == rd.it.node ? a.row_limit[req] - rd.it.tok_begin : rd.it.n_tokens;
-        split_row(tile[r], w[r], a.scale);
+        split_row(w[r], a.scale, tile[r].q, tile[r].q_scale);
 #pragma unroll
         for (int dt = 0; dt < 8; ++dt) tile[r].o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
         tile[r].m = -INFINITY;
@@ -185,14 +199,10 @@ __device__ __forceinline__ void scores(const Operands &x, const RowTile (&tile)[
         const RowTile &t = tile[r];
 #pragma unroll
         for (int t4 = 0; t4 < 4; ++t4) acc[r][t4] = f32x4{0.f, 0.f, 0.f, 0.f};
-        acc[r][0] = mfma_four<0>(x.k[0], t.hi, acc[r][0], x.k_scale, t.q_scale);
-        acc[r][1] = mfma_four<1>(x.k[1], t.hi, acc[r][1], x.k_scale, t.q_scale);
-        acc[r][2] = mfma_four<2>(x.k[2], t.hi, acc[r][2], x.k_scale, t.q_scale);
-        acc[r][3] = mfma_four<3>(x.k[3], t.hi, acc[r][3], x.k_scale, t.q_scale);
-        acc[r][0] = mfma_four<0>(x.k[0], t.lo, acc[r][0], x.k_scale, t.q_scale);
-        acc[r][1] = mfma_four<1>(x.k[1], t.lo, acc[r][1], x.k_scale, t.q_scale);
-        acc[r][2] = mfma_four<2>(x.k[2], t.lo, acc[r][2], x.k_scale, t.q_scale);
-        acc[r][3] = mfma_four<3>(x.k[3], t.lo, acc[r][3], x.k_scale, t.q_scale);
+        in_turn<4 * kTerms>([&](auto n) {
+            constexpr int T = decltype(n)::value & 3, Term = decltype(n)::value >> 2;
+            acc[r][T] = mfma_four<T, Term>(x.k[T], t.q, acc[r][T], x.k_scale, t.q_scale);
+        });
     }
 }
 
@@ -441,6 +451,7 @@ struct Shares {
     float o[W][16][kORow], m[W][16], l[W][16];
     int row[16];
 };
+static_assert(sizeof(Shares<4>) >= 3 * 64 * 4 * sizeof(u32x4), "two terms of the rows, in whole paths");
 constexpr int kRing = 4;
 struct Stage {  // four blocks as they lie in the pool, 16 bytes in the order of the lanes that brought them
     u32x4 k[4][64], v[4][64];
@@ -543,7 +554,7 @@ struct PathStep : Operands {
     int gap;  // of the lane's block of V, which is that of its scores too
 };
 template <int W>
-__global__ __launch_bounds__(64 * W, 2) void four_path_kernel(DecodePathLaunch a) {
+__global__ __launch_bounds__(64 * W, W == 4 ? 3 : 2) void four_path_kernel(DecodePathLaunch a) {
     extern __shared__ __attribute__((aligned(16))) char smem[];
     Shares<W> &s = *reinterpret_cast<Shares<W> *>(smem);
     const int lane = (int)threadIdx.x & 63, m = lane & 15, g = lane >> 4, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -559,13 +570,16 @@ __global__ __launch_bounds__(64 * W, 2) void four_path_kernel(DecodePathLaunch a
         for (int i = 0; i < 4; ++i) id[i] = path[kPathBlocks + min(4 * b + i, a.path_stride - kPathBlocks - 1)];
     };
     auto block = [&](int id) { return (size_t)(id & kPathIdMask) * Hkv + head; };
-    auto fetch = [&](PathStep &x, const int (&id)[4], int b) {
-        const int mine = pick4(id, g) | (4 * b + g < n_blocks ? 0 : 16 << kPathIdBits);
-        const size_t kb = block(pick4(id, m >> 2)), vb = block(mine);
-        x.gap = (int)((uint32_t)mine >> kPathIdBits);
+    auto fetch_keys = [&](PathStep &x, const int (&id)[4]) {
+        const size_t kb = block(pick4(id, m >> 2));
         x.k_scale = *reinterpret_cast<const uint32_t *>(k_scale + kb * four::kScaleBytes);
 #pragma unroll
         for (int j = 0; j < 4; ++j) x.k[j] = ld16(k + kb * four::kCodeBytes + 256 * j);
+    };
+    auto fetch_values = [&](PathStep &x, const int (&id)[4], int b) {
+        const int mine = pick4(id, g) | (4 * b + g < n_blocks ? 0 : 16 << kPathIdBits);
+        const size_t vb = block(mine);
+        x.gap = (int)((uint32_t)mine >> kPathIdBits);
         x.v_scale = ld16(v_scale + vb * four::kScaleBytes);
 #pragma unroll
         for (int j = 0; j < 4; ++j) x.v[j] = ld16(v + vb * four::kCodeBytes + 256 * j);
@@ -577,27 +591,49 @@ __global__ __launch_bounds__(64 * W, 2) void four_path_kernel(DecodePathLaunch a
     ids(id, b);
     const int q_at = path[kPathQRows + m / G] * a.num_q_heads + head * G + m % G;  // (the record has 16 requests, the last one again and again)
     t.req = path[kPathRows + m / G];
-    fetch(now, id, b);
+    fetch_keys(now, id);
+    fetch_values(now, id, b);
     u32x4 w[4];
-    const char *qp = static_cast<const char *>(a.q) + (size_t)q_at * (kHeadDim * 2) + 32 * g;
-    w[0] = ld16(qp);
-    w[1] = ld16(qp + 16);
-    w[2] = ld16(qp + 128);
-    w[3] = ld16(qp + 144);
+    const char *qp = static_cast<const char *>(a.q) + (size_t)q_at * (kHeadDim * 2) + 64 * g;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = ld16(qp + 16 * i);
     ids(id, b + W);
     t.lim = a.row_leaf ? path[2] + a.row_limit[t.req] : INT_MAX;  // (positions count whole blocks: the leaf begins at one)
-    split_row(t, w, a.scale);
+    split_row(w, a.scale, t.q, t.q_scale);
 #pragma unroll
     for (int dt = 0; dt < 8; ++dt) t.o[dt] = f32x4{0.f, 0.f, 0.f, 0.f};
     t.m = -INFINITY;
     t.l = 0.f;
+    // With four wavefronts a workgroup (more workgroups than compute units) the third and fourth term come from LDS in every step, and V of the next step is asked for
+    // behind the scores: three wavefronts a SIMD instead of two (96 requests over 200 + 60 tokens, 32 + 8 heads, 9.2 us; with all in registers 11.0). Of eight there is
+    // one workgroup a compute unit, and waiting for LDS costs (4 requests over 256 + 49 tokens 6.6 us, like that 6.9).
+    constexpr bool kSpare = W == 4;
+    u32x4 *terms = reinterpret_cast<u32x4 *>(smem) + threadIdx.x;
+    if constexpr (kSpare) {
+        terms[0] = u32x4{t.q[2][0], t.q[2][1], t.q[2][2], t.q[2][3]};
+        terms[64 * W] = u32x4{t.q[2][4], t.q[2][5], t.q[3][0], t.q[3][1]};
+        terms[128 * W] = u32x4{t.q[3][2], t.q[3][3], t.q[3][4], t.q[3][5]};
+    }
     auto step = [&](PathStep &x, PathStep &after, auto first) {
         f32x4 acc[1][4];
         u32x4 pw[1][2];
-        fetch(after, id, b + W);
-        ids(id, b + 2 * W);
+        if constexpr (kSpare) {
+            asm volatile("" ::: "memory");  // (or they would stay in registers)
+            const u32x4 t0 = terms[0], t1 = terms[64 * W], t2 = terms[128 * W];
+            t.q[2] = u32x6{t0[0], t0[1], t0[2], t0[3], t1[0], t1[1]};
+            t.q[3] = u32x6{t1[2], t1[3], t2[0], t2[1], t2[2], t2[3]};
+        }
+        auto fetch_rest = [&] {
+            fetch_values(after, id, b + W);
+            ids(id, b + 2 * W);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        fetch_keys(after, id);
+        if constexpr (!kSpare) fetch_rest();
         __builtin_amdgcn_sched_barrier(0);
         scores(x, tile, acc);
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (kSpare) fetch_rest();
         const int d0 = 16 * (4 * b + g) - t.lim;
         if (__builtin_amdgcn_ballot_w64(x.gap > 0 || d0 > -16)) {
             const uint32_t seen = seen_bits(d0, a.row_leaf ? a.row_mask[t.req] : 0ull) & 0xFFFFu >> x.gap;
@@ -624,6 +660,7 @@ __global__ __launch_bounds__(64 * W, 2) void four_path_kernel(DecodePathLaunch a
     if (step(now, next, std::true_type{}))  // (a wavefront without steps takes one of gaps: nothing waits for the path's length)
         while (step(next, now, std::false_type{}) && step(now, next, std::false_type{})) {
         }
+    if constexpr (kSpare) __syncthreads();  // (the terms have been read)
     leave_share(s, t, wave, m, g, true);
     if (wave == 0 && g == 0) s.row[m] = q_at;
     __syncthreads();
@@ -791,7 +828,7 @@ __device__ __forceinline__ void run_rows(const DecodeLaunch &a, const DecodeItem
         ring.clean(b + 1);  // (behind the last step: of no use, and of no harm)
         const uint32_t k_scale = keys(b + 1, k);
         __builtin_amdgcn_sched_barrier(0);
-        // every chunk up to a sched_barrier: a matrix instruction (32 cycles of the first product, 16 of the second) and about as many cycles of others
+        // every chunk up to a sched_barrier: two matrix instructions of the first product or one of the second, and about as many cycles of others
         const float mc = t.m == -INFINITY ? 0.f : t.m * c;
         float sum = 0.f, top = -INFINITY;
 #pragma unroll
@@ -805,17 +842,14 @@ __device__ __forceinline__ void run_rows(const DecodeLaunch &a, const DecodeItem
         weigh_pair(0);  // while K comes from LDS
         __builtin_amdgcn_sched_barrier(0);
         constexpr int kFirst = 6;  // pairs up to the end of the first product
+        in_turn<4 * kTerms>([&](auto n) {
+            constexpr int i = decltype(n)::value;
+            next[0][i & 3] = mfma_four<(i & 3), (i >> 2)>(k[i & 3], t.q, next[0][i & 3], k_scale, t.q_scale);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const i32x8 q = i >= 4 ? t.lo : t.hi;
-            f32x4 &to = next[0][i & 3];
-            to = (i & 3) == 0 ? mfma_four<0>(k[0], q, to, k_scale, t.q_scale) : (i & 3) == 1 ? mfma_four<1>(k[1], q, to, k_scale, t.q_scale)
-               : (i & 3) == 2 ? mfma_four<2>(k[2], q, to, k_scale, t.q_scale) : mfma_four<3>(k[3], q, to, k_scale, t.q_scale);
-#pragma unroll
-            for (int p = 1 + (kFirst - 1) * i / 8; p < 1 + (kFirst - 1) * (i + 1) / 8; ++p) weigh_pair(p);
-            if (i >= 4) va[i - 4] = lds.v[P][i - 4][rd.lane];
-            __builtin_amdgcn_sched_barrier(0);
-        }
+            for (int p = 1 + (kFirst - 1) * i / 16; p < 1 + (kFirst - 1) * (i + 1) / 16; ++p) weigh_pair(p);
+            if constexpr (i >= 12) va[i - 12] = lds.v[P][i - 12][rd.lane];
+            if constexpr (i & 1) __builtin_amdgcn_sched_barrier(0);
+        });
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             t.o[i & 7] = mfma16(as_bf16x8(va[i & 3]), as_bf16x8(pw[i >> 3]), t.o[i & 7]);
@@ -849,13 +883,13 @@ __device__ __forceinline__ void run_rows(const DecodeLaunch &a, const DecodeItem
 // Items of more than 64 rows: 32 a wavefront, which sees all tokens, by the 32x32 forms of both instructions.  Beside one of those another wavefront issues
 // more vector instructions than beside two of the 16x16 forms (measured: three quarters of the time beside the first product's, against a half).
 //   S^T  v_mfma_scale_f32_32x32x64_f8f6f4: row r of tile T is token 32 T + r of the step; lane (r, h) brings dims 64 kk + 32 h .. + 31 of it, and of query
-//        row r dims 64 kk + 16 h .. + 15 and 64 kk + 32 + 16 h .. + 15.  It ends up with tokens 32 T + 8 (i / 4) + 4 h + i % 4 of its row.
+//        row r the same.  It ends up with tokens 32 T + 8 (i / 4) + 4 h + i % 4 of its row.
 //   O^T  v_mfma_f32_32x32x16_bf16: the tokens of block B that a lane has are 4 h .. + 3 and 8 + 4 h .. + 3, so those are what it brings of V for
 //        dims 8 (m % 16) + 2 dt + m / 16 of tile dt.
 // V is widened by wavefront w for block w, 4 tokens and 8 dims a lane.
 struct TallRows {
-    i32x8 q[2][2];  // [kk][term]
-    uint32_t q_scale;
+    u32x6 q[2][kTerms];  // [kk]
+    uint32_t q_scale[2];
     f32x16 o[4];
     float m, l;
     int req, lim;
@@ -868,9 +902,9 @@ __device__ __forceinline__ float half_sum(float x) {
     const auto r = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
     return __uint_as_float(r[0]) + __uint_as_float(r[1]);
 }
-__device__ __forceinline__ f32x16 mfma_four_tall(u32x4 k, i32x8 q, f32x16 c, uint32_t k_scale, uint32_t q_scale) {
-    const i32x8 a = {(int)k[0], (int)k[1], (int)k[2], (int)k[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(a, q, c, 4, 0, 0, k_scale, 0, q_scale);
+template <int Term>
+__device__ __forceinline__ f32x16 mfma_four_tall(u32x4 k, const u32x6 (&q)[kTerms], f32x16 c, uint32_t k_scale, uint32_t q_scale) {
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(as_four(k), as_six(q[Term]), c, 4, 2, 0, k_scale, Term, q_scale);
 }
 __device__ __forceinline__ void run_tall(const DecodeLaunch &a, const DecodeItem &it, Widened &lds) {
     const int lane = (int)threadIdx.x & 63, r = lane & 31, h = lane >> 5, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
@@ -893,32 +927,18 @@ __device__ __forceinline__ void run_tall(const DecodeLaunch &a, const DecodeItem
     x.req = a.node_req_idx[it.req_off + row / G];
     ring.page_of(0);
     ring.issue(0);
-    u32x4 w[8];  // dims 64 kk + 32 p + 16 h + 8 e, [4 kk + 2 p + e]
+    u32x4 w[2][4];  // dims 64 kk + 32 h .. + 31
     {
         const int q_row = a.q_rows ? a.q_rows[x.req] : x.req;
-        const char *qp = static_cast<const char *>(a.q) + ((size_t)q_row * a.num_q_heads + it.kv_head * G + row % G) * (kHeadDim * 2) + 32 * h;
+        const char *qp = static_cast<const char *>(a.q) + ((size_t)q_row * a.num_q_heads + it.kv_head * G + row % G) * (kHeadDim * 2) + 64 * h;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) w[i] = ld16(qp + 64 * (i >> 1) + 16 * (i & 1));
+        for (int i = 0; i < 8; ++i) w[i >> 2][i & 3] = ld16(qp + 128 * (i >> 2) + 16 * (i & 3));
     }
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int b = 1; b < kRing; ++b) ring.issue(b);
-    {  // the row as two e4m3 terms, as in split_row
-        float top = 0.f;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) top = fmaxf(top, fmaxf(fabsf(__uint_as_float(w[i][j] << 16)), fabsf(__uint_as_float(w[i][j] & 0xFFFF0000u))));
-        const float up = row_factor(half_max(top), a.scale, x.q_scale);
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {  // four dims each
-            const uint32_t w0 = w[i >> 1][2 * (i & 1)], w1 = w[i >> 1][2 * (i & 1) + 1];
-            int hi, lo;
-            split_four(w0, w1, up, hi, lo);
-            x.q[i >> 3][0][i & 7] = hi;
-            x.q[i >> 3][1][i & 7] = lo;
-        }
-    }
+    for (int kk = 0; kk < 2; ++kk) split_row(w[kk], a.scale, x.q[kk], x.q_scale[kk]);
     x.lim = a.row_leaf && a.row_leaf[x.req] == it.node ? a.row_limit[x.req] - it.tok_begin : it.n_tokens;
 #pragma unroll
     for (int dt = 0; dt < 4; ++dt)
@@ -974,8 +994,10 @@ __device__ __forceinline__ void run_tall(const DecodeLaunch &a, const DecodeItem
         keys(0, k, ks);
 #pragma unroll
         for (int i = 0; i < 16; ++i) acc0[0][i] = acc0[1][i] = 0.f;
-#pragma unroll
-        for (int i = 0; i < 8; ++i) acc0[i & 1] = mfma_four_tall(k[i & 3], x.q[i >> 1 & 1][i >> 2], acc0[i & 1], ks[i & 3], x.q_scale);
+        in_turn<4 * kTerms>([&](auto n) {
+            constexpr int i = decltype(n)::value;
+            acc0[i & 1] = mfma_four_tall<(i >> 2)>(k[i & 3], x.q[i >> 1 & 1], acc0[i & 1], ks[i & 3], x.q_scale[i >> 1 & 1]);
+        });
         float top = -INFINITY;
 #pragma unroll
         for (int j = 0; j < 32; j += 2) top = most(acc0, j, top);
@@ -999,19 +1021,19 @@ __device__ __forceinline__ void run_tall(const DecodeLaunch &a, const DecodeItem
             sum += p0 + p1;
             pw[p >> 2][p & 3] = pack_bf16(p0, p1);
         };
-        // every chunk up to a sched_barrier: a matrix instruction (64 cycles of the first product, 32 of the second) and what fits beside it
+        // every chunk up to a sched_barrier: a matrix instruction (32 cycles) and what fits beside it
         constexpr int kBefore = 2, kFirst = 12, kIssue = 5;  // pairs while K comes from LDS, and up to the end of the first product; where the ring's loads go out
 #pragma unroll
         for (int p = 0; p < kBefore; ++p) weigh_pair(p);
         __builtin_amdgcn_sched_barrier(0);
+        in_turn<4 * kTerms>([&](auto n) {
+            constexpr int i = decltype(n)::value;
+            next[i & 1] = mfma_four_tall<(i >> 2)>(k[i & 3], x.q[i >> 1 & 1], next[i & 1], ks[i & 3], x.q_scale[i >> 1 & 1]);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            next[i & 1] = mfma_four_tall(k[i & 3], x.q[i >> 1 & 1][i >> 2], next[i & 1], ks[i & 3], x.q_scale);
-#pragma unroll
-            for (int p = kBefore + (kFirst - kBefore) * i / 8; p < kBefore + (kFirst - kBefore) * (i + 1) / 8; ++p) weigh_pair(p);
-            if (i >= 4) va[i - 4] = lds.v[P][i - 4][lane];
+            for (int p = kBefore + (kFirst - kBefore) * i / 16; p < kBefore + (kFirst - kBefore) * (i + 1) / 16; ++p) weigh_pair(p);
+            if constexpr (i >= 12) va[i - 12] = lds.v[P][i - 12][lane];
             __builtin_amdgcn_sched_barrier(0);
-        }
+        });
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             x.o[i & 3] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(as_bf16x8(va[i & 3]), as_bf16x8(pw[i >> 2]), x.o[i & 3], 0, 0, 0);
