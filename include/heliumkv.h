@@ -701,7 +701,9 @@ int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_pages, const
  * oldest last use goes first, ties by lower page id; the clock ticks once per acquire / release. */
 typedef struct hkv_cache hkv_cache;
 int kv_cache_create(hkv_pool *pool, hkv_cache **out);
-int kv_cache_destroy(hkv_cache *cache); /* returns every page it holds to the pool */
+/* Returns every page the cache holds to the pool, unless that is destroyed: a cache may go before or after its pool (in between, kv_cache_acquire is
+ * EINVAL). */
+int kv_cache_destroy(hkv_cache *cache);
 /* Looks up the longest cached prefix of tokens (host, n_tokens ids) in whole blocks, takes a
  * reference on each hit, and gives every remaining block a page (free list first, then by
  * eviction); new full blocks enter the cache at once, so the caller must fill them (kv_pool_write

@@ -115,6 +115,7 @@ extern "C" int kv_pool_create(const hkv_pool_desc *desc, hkv_pool **out) {
 
 extern "C" int kv_pool_destroy(hkv_pool *pool) {
     if (!pool) return HKV_OK;
+    for (const hkv_pool::Follower &f : pool->followers) f.pool_goes(f.object);
     if (pool->cached_decode) hkv_decode_plan_destroy(pool->cached_decode);
     if (pool->cached_prefill) hkv_prefill_plan_destroy(pool->cached_prefill);
     for (hipEvent_t e : pool->slot_free)

@@ -35,7 +35,7 @@ struct Block {
 }  // namespace
 
 struct hkv_cache {
-    hkv_pool *pool = nullptr;
+    hkv_pool *pool = nullptr;  // null once it is destroyed
     int32_t block = HKV_PAGE_SIZE;  // tokens per cached block = the pool's page size
     Block root;
     std::unordered_map<int32_t, Block *> by_page;      // cached full blocks
@@ -79,7 +79,7 @@ struct hkv_cache {
             auto pv = private_pages.find(pages[i]);
             if (pv != private_pages.end()) {
                 private_pages.erase(pv);
-                (void)kv_pool_release(pool, 1, &pages[i]);
+                if (pool) (void)kv_pool_release(pool, 1, &pages[i]);
                 continue;
             }
             auto it = by_page.find(pages[i]);
@@ -125,7 +125,8 @@ extern "C" int kv_cache_create(hkv_pool *pool, hkv_cache **out) {
     c->pool = pool;
     c->block = kv_pool_page_size(pool);
     try {
-        pool->followers.push_back({c, [](void *p, const int32_t *ids) { static_cast<hkv_cache *>(p)->prepare(ids); }, [](void *p) { static_cast<hkv_cache *>(p)->commit(); }});
+        pool->followers.push_back({c, [](void *p, const int32_t *ids) { static_cast<hkv_cache *>(p)->prepare(ids); }, [](void *p) { static_cast<hkv_cache *>(p)->commit(); },
+                                   [](void *p) { static_cast<hkv_cache *>(p)->pool = nullptr; }});
     } catch (const std::exception &) {
         delete c;
         return fail(HKV_ENOMEM, "kv_cache_create: out of host memory");
@@ -136,10 +137,12 @@ extern "C" int kv_cache_create(hkv_pool *pool, hkv_cache **out) {
 
 extern "C" int kv_cache_destroy(hkv_cache *c) {
     if (!c) return HKV_OK;
-    auto &followers = c->pool->followers;
-    followers.erase(std::remove_if(followers.begin(), followers.end(), [c](const hkv_pool::Follower &f) { return f.object == c; }), followers.end());
-    for (auto &kv : c->by_page) (void)kv_pool_release(c->pool, 1, &kv.first);
-    for (auto &kv : c->private_pages) (void)kv_pool_release(c->pool, 1, &kv.first);
+    if (c->pool) {
+        auto &followers = c->pool->followers;
+        followers.erase(std::remove_if(followers.begin(), followers.end(), [c](const hkv_pool::Follower &f) { return f.object == c; }), followers.end());
+        for (auto &kv : c->by_page) (void)kv_pool_release(c->pool, 1, &kv.first);
+        for (auto &kv : c->private_pages) (void)kv_pool_release(c->pool, 1, &kv.first);
+    }
     c->free_tree(&c->root);
     delete c;
     return HKV_OK;
@@ -149,6 +152,7 @@ extern "C" int kv_cache_acquire(hkv_cache *c, const int32_t *tokens, int32_t n_t
                                 int32_t *n_cached_tokens) {
     if (!c || n_tokens < 0 || (n_tokens > 0 && (!tokens || !page_ids)) || !n_cached_tokens)
         return fail(HKV_EINVAL, "kv_cache_acquire: bad argument");
+    if (!c->pool) return fail(HKV_EINVAL, "kv_cache_acquire: the cache's pool is destroyed");
     ++c->clock;
     const int P = c->block;
     const int n_full = n_tokens / P;

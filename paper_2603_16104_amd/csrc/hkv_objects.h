@@ -130,11 +130,12 @@ struct hkv_pool {
     hipEvent_t slot_free[kWriteSlots] = {};
     bool slot_in_flight[kWriteSlots] = {};
     int next_slot = 0;
-    // What else holds page ids of the pool and follows kv_pool_compact (prefix caches): prepare may throw, commit does not.
+    // What else holds page ids of the pool (prefix caches).  It follows kv_pool_compact: prepare may throw, commit does not; and is told when the pool goes.
     struct Follower {
         void *object;
         void (*prepare)(void *object, const int32_t *new_ids);
         void (*commit)(void *object);
+        void (*pool_goes)(void *object);
     };
     std::vector<Follower> followers;
     std::vector<uint32_t> mark;  // kv_pool_evict, kv_pool_copy_pages: pages marked in the present call (mark[id] == mark_now)

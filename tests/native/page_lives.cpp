@@ -1,0 +1,137 @@
+// Lives of pools, caches, pages and lists that end in an unusual order, for a build with AddressSanitizer and UndefinedBehaviorSanitizer: the host
+// files as they are, no GPU and no HIP library (launches do nothing unless a program says otherwise).  Argument: the program.  Exit status 0 = clean.
+#include <algorithm>
+#include <cstdio>
+#include <cstdlib>
+#include <cstring>
+#include <map>
+#include <numeric>
+#include <vector>
+
+#include "../../paper_2603_16104_amd/csrc/hkv_objects.h"
+
+static int failures = 0;
+#define CHECK(cond)                                                        \
+    do {                                                                   \
+        if (!(cond)) {                                                     \
+            std::fprintf(stderr, "%s:%d: %s\n", __FILE__, __LINE__, #cond); \
+            ++failures;                                                    \
+        }                                                                  \
+    } while (0)
+
+using namespace hkv;
+
+// ---- HIP, as far as the host files call it
+static intptr_t events = 0;
+extern "C" {
+hipError_t hipMalloc(void **p, size_t n) { return (*p = std::calloc(1, n ? n : 1)) ? hipSuccess : hipErrorOutOfMemory; }
+hipError_t hipFree(void *p) { std::free(p); return hipSuccess; }
+hipError_t hipMemcpy(void *d, const void *s, size_t n, hipMemcpyKind) { if (n) std::memcpy(d, s, n); return hipSuccess; }
+hipError_t hipHostMalloc(void **p, size_t n, unsigned) { return hipMalloc(p, n); }
+hipError_t hipHostFree(void *p) { return hipFree(p); }
+hipError_t hipHostGetDevicePointer(void **d, void *p, unsigned) { *d = p; return hipSuccess; }
+hipError_t hipEventCreateWithFlags(hipEvent_t *e, unsigned) { *e = reinterpret_cast<hipEvent_t>(++events); return hipSuccess; }
+hipError_t hipEventCreate(hipEvent_t *e) { return hipEventCreateWithFlags(e, 0); }
+hipError_t hipEventDestroy(hipEvent_t) { return hipSuccess; }
+hipError_t hipEventRecord(hipEvent_t, hipStream_t);
+hipError_t hipEventSynchronize(hipEvent_t);
+hipError_t hipEventElapsedTime(float *ms, hipEvent_t, hipEvent_t) { *ms = 0; return hipSuccess; }
+hipError_t hipStreamCreateWithFlags(hipStream_t *s, unsigned) { *s = reinterpret_cast<hipStream_t>(8); return hipSuccess; }
+hipError_t hipStreamDestroy(hipStream_t) { return hipSuccess; }
+hipError_t hipStreamWaitEvent(hipStream_t, hipEvent_t, unsigned) { return hipSuccess; }
+hipError_t hipStreamIsCapturing(hipStream_t, hipStreamCaptureStatus *s) { *s = hipStreamCaptureStatusNone; return hipSuccess; }
+hipError_t hipGetDevice(int *) { return hipErrorNoDevice; }
+hipError_t hipGetDeviceProperties(hipDeviceProp_t *, int) { return hipErrorNoDevice; }
+hipError_t hipGetLastError() { return hipSuccess; }
+const char *hipGetErrorString(hipError_t) { return "?"; }
+}
+hipError_t hipEventRecord(hipEvent_t, hipStream_t) { return hipSuccess; }
+hipError_t hipEventSynchronize(hipEvent_t) { return hipSuccess; }
+
+namespace hkv {
+hipError_t launch_page_copy(const PageCopyLaunch &, hipStream_t) { return hipSuccess; }
+hipError_t launch_page_copy(const PageCopyInline &, hipStream_t) { return hipSuccess; }
+hipError_t launch_upload(const void *s, void *d, size_t n, hipStream_t) { std::memcpy(d, s, n); return hipSuccess; }
+hipError_t launch_plan_grow_inline(const PlanGrowInline &, hipStream_t) { return hipSuccess; }
+hipError_t launch_pool_write(const PoolWriteLaunch &, hipStream_t) { return hipSuccess; }
+hipError_t launch_pool_write_fp32(const PoolWriteLaunch &, hipStream_t) { return hipSuccess; }
+hipError_t launch_pool_copy(const PoolCopyLaunch &, hipStream_t) { return hipSuccess; }
+hipError_t launch_pool_append_inline(const PoolAppendInline &, hipStream_t) { return hipSuccess; }
+hipError_t launch_decode_step_append(const PoolAppendInline &, const PlanGrowInline &, hipStream_t) { return hipSuccess; }
+hipError_t launch_pool_dequant(const PoolDequantLaunch &, hipStream_t) { return hipSuccess; }
+hipError_t launch_decode(const DecodeLaunch &, hipStream_t, hipEvent_t, hipEvent_t) { return hipSuccess; }
+hipError_t launch_decode_paths(const DecodePathLaunch &, int, hipStream_t, hipEvent_t, hipEvent_t) { return hipSuccess; }
+hipError_t prepare_decode_device(void **ws) {
+    if (ws) *ws = nullptr;
+    return hipSuccess;
+}
+hipError_t launch_rows_fp32(const RowsLaunch &, hipStream_t) { return hipSuccess; }
+hipError_t launch_prefill(const PrefillLaunch &, hipStream_t) { return hipSuccess; }
+hipError_t launch_decode_tiles(const DecodeTilesLaunch &, hipStream_t, hipEvent_t, hipEvent_t) { return hipSuccess; }
+hipError_t launch_decode_fused(const DecodeLaunch &, const DecodeTilesLaunch &, hipStream_t, hipEvent_t, hipEvent_t) { return hipSuccess; }
+hipError_t launch_lse_merge(const float *, const float *, const int32_t *, const int32_t *, int32_t, void *, int32_t, float *, hipStream_t) { return hipSuccess; }
+hipError_t launch_lse_merge_dense(const void *, const float *, const int32_t *, int32_t, int32_t, int32_t, void *, int32_t, float *, hipStream_t, hipEvent_t, hipEvent_t,
+                                  const int32_t *, const float *) { return hipSuccess; }
+hipError_t run_read_probe(const void *const *, int, size_t, int, int, float *, hipStream_t) { return hipSuccess; }
+hipError_t run_mfma_probe(int, int, int, int, float *, float *, hipStream_t) { return hipSuccess; }
+int prefill_tile_tokens(int group) { return 256 / group; }
+}  // namespace hkv
+
+static hkv_pool *make_pool(int pages, int page_size = 16, int dtype = HKV_BF16, void *k = reinterpret_cast<void *>(0x100000), void *v = reinterpret_cast<void *>(0x40000000)) {
+    hkv_pool_desc d{};
+    d.num_pages = pages;
+    d.page_size = page_size;
+    d.num_kv_heads = 2;
+    d.head_dim = 128;
+    d.dtype = dtype;
+    d.k_pages = k;
+    d.v_pages = v;
+    if (dtype == HKV_FP8_E4M3 || dtype == HKV_FP4_E2M1) {
+        d.k_scale = reinterpret_cast<float *>(0x80000000);
+        d.v_scale = reinterpret_cast<float *>(0xC0000000);
+    }
+    hkv_pool *pool = nullptr;
+    CHECK(kv_pool_create(&d, &pool) == HKV_OK);
+    return pool;
+}
+static std::vector<int32_t> acquire(hkv_cache *cache, int n, int first = 0, int want = HKV_OK) {
+    std::vector<int32_t> tokens(n), ids((n + 15) / 16);
+    std::iota(tokens.begin(), tokens.end(), first);
+    int32_t cached = 0;
+    CHECK(kv_cache_acquire(cache, tokens.data(), n, 0, ids.data(), &cached) == want);
+    return ids;
+}
+
+// A cache that outlives its pool: never used, with blocks, with a sequence's pages still out; and one that does not.
+static void caches_after_their_pool() {
+    for (int used = 0; used < 3; ++used) {
+        hkv_pool *pool = make_pool(8);
+        hkv_cache *cache = nullptr, *early = nullptr;
+        CHECK(kv_cache_create(pool, &early) == HKV_OK && kv_cache_create(pool, &cache) == HKV_OK);
+        CHECK(kv_cache_destroy(early) == HKV_OK);
+        std::vector<int32_t> ids(1, 0);
+        if (used) ids = acquire(cache, 40);
+        if (used == 1) CHECK(kv_cache_release(cache, ids.data(), (int)ids.size()) == HKV_OK);
+        CHECK(kv_pool_destroy(pool) == HKV_OK);
+        if (used) {
+            acquire(cache, 10, 0, HKV_EINVAL);  // there is nothing that it could take pages from, or give them back to
+            CHECK(kv_cache_unpin(cache, ids.data(), (int)ids.size()) == HKV_OK);
+            CHECK(kv_cache_release(cache, ids.data(), (int)ids.size()) == (used == 1 ? HKV_ERANGE : HKV_OK));
+            int64_t blocks = -1;
+            CHECK(kv_cache_stats(cache, &blocks, nullptr, nullptr, nullptr) == HKV_OK && blocks == 2);
+        }
+        CHECK(kv_cache_destroy(cache) == HKV_OK);
+    }
+}
+
+int main(int argc, char **argv) {
+    const std::pair<const char *, void (*)()> programs[] = {{"caches_after_their_pool", caches_after_their_pool}};
+    int ran = 0;
+    for (const auto &p : programs)
+        if (argc < 2 || !std::strcmp(argv[1], p.first)) {
+            p.second();
+            ++ran;
+        }
+    std::printf("%d programs, %d failed checks\n", ran, failures);
+    return failures != 0;
+}
