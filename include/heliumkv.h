@@ -697,7 +697,8 @@ int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_pages, const
  * A block is 16 tokens; its identity is (preceding block, its 16 token ids).  Only full blocks are
  * shared; a sequence's partial last block is private.  The cache takes its pages from the pool
  * (kv_pool_alloc: lowest free id first) and holds one pool reference per page it owns.
- * Evictable = no live sequence uses it, not pinned, no cached block extends it; among those the
+ * Evictable = no live sequence uses it, not pinned, no cached block extends it, nobody else holds
+ * a reference of its page (kv_pool_retain, kv_pool_fork); among those the
  * oldest last use goes first, ties by lower page id; the clock ticks once per acquire / release. */
 typedef struct hkv_cache hkv_cache;
 int kv_cache_create(hkv_pool *pool, hkv_cache **out);

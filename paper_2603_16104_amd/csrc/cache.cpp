@@ -7,7 +7,7 @@
 // its token ids), so two sequences share
 // a block exactly when they agree on everything up to its end.  Only full blocks are shared; a
 // sequence's partial last block is private.  Evictable = no live user, not pinned, nothing cached
-// extends it; among those the oldest last use goes first, ties by lower page id; the clock ticks
+// extends it, no reference of its page beside the cache's; among those the oldest last use goes first, ties by lower page id; the clock ticks
 // once per acquire / release call.
 #include <cstdint>
 #include <cstring>
@@ -59,8 +59,9 @@ struct hkv_cache {
             if (kv_pool_alloc(pool, 1, &id) != HKV_OK) return -1;
             return id;
         }
-        if (evictable.empty()) return -1;
-        auto it = evictable.begin();
+        auto it = evictable.begin();  // of those whose page nobody else holds (a fork goes on using it)
+        while (it != evictable.end() && kv_pool_refcount(pool, it->second) > 1) ++it;
+        if (it == evictable.end()) return -1;
         Block *b = by_page[it->second];
         evictable.erase(it);
         Block *par = b->parent;

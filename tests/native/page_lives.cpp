@@ -124,8 +124,32 @@ static void caches_after_their_pool() {
     }
 }
 
+// Branches of a cached prompt go on when the cache no longer needs its blocks: their pages have another owner and go to nobody else.
+static void evictions_beside_forks() {
+    hkv_pool *pool = make_pool(8);
+    hkv_cache *cache = nullptr;
+    CHECK(kv_cache_create(pool, &cache) == HKV_OK);
+    const std::vector<int32_t> old = acquire(cache, 32), young = acquire(cache, 16, 1000);
+    std::vector<int32_t> fork(2);
+    const int32_t n = 32, parent = 0;
+    CHECK(kv_pool_fork(pool, 1, old.data(), &n, 1, &parent, 0, fork.data(), nullptr) == HKV_OK && fork == old);
+    CHECK(kv_cache_release(cache, old.data(), 2) == HKV_OK && kv_cache_release(cache, young.data(), 1) == HKV_OK);
+    const std::vector<int32_t> rest = acquire(cache, 80, 2000);  // the free pages
+    CHECK(kv_pool_num_free(pool) == 0);
+    const std::vector<int32_t> one = acquire(cache, 16, 3000);   // the oldest block is the fork's last page: the younger one's goes
+    CHECK(one == young);
+    acquire(cache, 16, 4000, HKV_ENOMEM);
+    CHECK(kv_pool_refcount(pool, fork[0]) == 2 && kv_pool_refcount(pool, fork[1]) == 2);
+    CHECK(acquire(cache, 32) == old && kv_cache_release(cache, old.data(), 2) == HKV_OK);  // still cached
+    CHECK(kv_pool_release(pool, 2, fork.data()) == HKV_OK);
+    const std::vector<int32_t> two = acquire(cache, 16, 4000);
+    CHECK(two[0] == old[1]);
+    CHECK(kv_cache_destroy(cache) == HKV_OK && kv_pool_num_free(pool) == 8);
+    CHECK(kv_pool_destroy(pool) == HKV_OK);
+}
+
 int main(int argc, char **argv) {
-    const std::pair<const char *, void (*)()> programs[] = {{"caches_after_their_pool", caches_after_their_pool}};
+    const std::pair<const char *, void (*)()> programs[] = {{"caches_after_their_pool", caches_after_their_pool}, {"evictions_beside_forks", evictions_beside_forks}};
     int ran = 0;
     for (const auto &p : programs)
         if (argc < 2 || !std::strcmp(argv[1], p.first)) {
