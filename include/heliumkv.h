@@ -178,7 +178,8 @@ int kv_pool_copy_pages(hkv_pool *dst, const int32_t *dst_ids, hkv_pool *src, con
  * by others: a sequence that no fork continues is gone (its pages return to the free list, in the order listed), and one that owns its last page
  * alone hands that to its first fork without a copy.  release == 0: the sequences stay as they are.
  * A copied page has no key_weights of the old one's: they are the caller's to copy.
- * ERANGE: page ids, parents.  EINVAL: pages that are not allocated, or listed more often than held (release).  ENOMEM: fewer free pages than copies.  Nothing
+ * ERANGE: page ids, parents.  EINVAL: pages that are not allocated, or listed more often than held beside prefix caches (release: the pages of
+ * kv_cache_acquire are given back by kv_cache_release, their forks by this).  ENOMEM: fewer free pages than copies.  Nothing
  * changes on error.  Not for capture into a graph where something is copied (EINVAL): a replay would take the same pages. */
 int kv_pool_fork(hkv_pool *pool, int32_t n_seq, const int32_t *pages, const int32_t *n_tokens, int32_t n_out, const int32_t *parent, int32_t release,
                  int32_t *out_pages, void *stream);

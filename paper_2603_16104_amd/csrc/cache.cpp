@@ -110,6 +110,7 @@ struct hkv_cache {
         evictable.swap(moved_evictable);
         for (auto &kv : by_page) kv.second->page = kv.first;
     }
+    int32_t holds(int32_t page) const { return (int32_t)(by_page.count(page) + private_pages.count(page)); }
     void free_tree(Block *b) {
         for (auto &kv : b->children) {
             free_tree(kv.second);
@@ -127,7 +128,8 @@ extern "C" int kv_cache_create(hkv_pool *pool, hkv_cache **out) {
     c->block = kv_pool_page_size(pool);
     try {
         pool->followers.push_back({c, [](void *p, const int32_t *ids) { static_cast<hkv_cache *>(p)->prepare(ids); }, [](void *p) { static_cast<hkv_cache *>(p)->commit(); },
-                                   [](void *p) { static_cast<hkv_cache *>(p)->pool = nullptr; }});
+                                   [](void *p) { static_cast<hkv_cache *>(p)->pool = nullptr; },
+                                   [](const void *p, int32_t page) { return static_cast<const hkv_cache *>(p)->holds(page); }});
     } catch (const std::exception &) {
         delete c;
         return fail(HKV_ENOMEM, "kv_cache_create: out of host memory");

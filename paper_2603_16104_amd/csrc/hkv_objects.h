@@ -130,12 +130,14 @@ struct hkv_pool {
     hipEvent_t slot_free[kWriteSlots] = {};
     bool slot_in_flight[kWriteSlots] = {};
     int next_slot = 0;
-    // What else holds page ids of the pool (prefix caches).  It follows kv_pool_compact: prepare may throw, commit does not; and is told when the pool goes.
+    // What else holds page ids of the pool (prefix caches).  It follows kv_pool_compact: prepare may throw, commit does not; is told when the pool goes; and says
+    // how many of a page's references are its own.
     struct Follower {
         void *object;
         void (*prepare)(void *object, const int32_t *new_ids);
         void (*commit)(void *object);
         void (*pool_goes)(void *object);
+        int32_t (*holds)(const void *object, int32_t page);
     };
     std::vector<Follower> followers;
     std::vector<uint32_t> mark;  // kv_pool_evict, kv_pool_copy_pages: pages marked in the present call (mark[id] == mark_now)

@@ -131,10 +131,15 @@ extern "C" int kv_pool_fork(hkv_pool *pool, int32_t n_seq, const int32_t *pages,
             return fail(HKV_ERANGE, "%s: page id %d (entry %lld) outside pool of %d pages", who, pages[i], (long long)i, pool->d.num_pages);
         if (pool->refcnt[pages[i]] <= 0) return fail(HKV_EINVAL, "%s: page %d is not allocated", who, pages[i]);
     }
-    if (release && total > 0) {  // every listing gives a reference back
-        std::vector<int32_t> held(pool->refcnt);
-        for (int64_t i = 0; i < total; ++i)
-            if (--held[pages[i]] < 0) return fail(HKV_EINVAL, "%s: page %d listed more often than it is held", who, pages[i]);
+    if (release) {  // every listing gives a reference back, none of them a prefix cache's (counted in place, and put back)
+        int64_t n = 0, bad = -1;
+        for (; n < total && bad < 0; ++n) {
+            int32_t cached = 0;
+            for (const hkv_pool::Follower &f : pool->followers) cached += f.holds(f.object, pages[n]);
+            if (--pool->refcnt[pages[n]] < cached) bad = n;
+        }
+        while (n-- > 0) ++pool->refcnt[pages[n]];
+        if (bad >= 0) return fail(HKV_EINVAL, "%s: page %d listed more often than it is held beside prefix caches", who, pages[bad]);
     }
     std::vector<int32_t> first_fork(n_seq, -1), forks(n_seq, 0);
     int64_t out_total = 0;

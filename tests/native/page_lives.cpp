@@ -148,8 +148,43 @@ static void evictions_beside_forks() {
     CHECK(kv_pool_destroy(pool) == HKV_OK);
 }
 
+// A fork that ends its sequences gives back what they hold, never a prefix cache's own references.
+static void forks_that_end_cached_sequences() {
+    hkv_pool *pool = make_pool(8);
+    hkv_cache *cache = nullptr, *other = nullptr;
+    CHECK(kv_cache_create(pool, &other) == HKV_OK && kv_cache_create(pool, &cache) == HKV_OK);
+    const std::vector<int32_t> ids = acquire(cache, 40);  // two cached blocks and a private one
+    const int32_t n = 40, full = 32, last = 8, parent[3] = {0, 0, 0};
+    std::vector<int32_t> out(9, -5);
+    auto counts = [&] { std::vector<int32_t> c; for (int i = 0; i < 8; ++i) c.push_back(kv_pool_refcount(pool, i)); return c; };
+    const std::vector<int32_t> before = counts();
+    for (int forks = 0; forks < 4; ++forks) {
+        CHECK(kv_pool_fork(pool, 1, ids.data(), &n, forks, parent, 1, out.data(), nullptr) == HKV_EINVAL);
+        CHECK(kv_pool_fork(pool, 1, ids.data(), &full, forks, parent, 1, out.data(), nullptr) == HKV_EINVAL);
+        CHECK(kv_pool_fork(pool, 1, &ids[2], &last, forks, parent, 1, out.data(), nullptr) == HKV_EINVAL);
+    }
+    CHECK(counts() == before && kv_pool_num_free(pool) == 5 && out[0] == -5);
+    // a sequence of its own over the same pages: forked, then ended by the next fork; the cache keeps its references
+    CHECK(kv_pool_fork(pool, 1, ids.data(), &n, 2, parent, 0, out.data(), nullptr) == HKV_OK);
+    const std::vector<int32_t> beams(out.begin(), out.begin() + 6);
+    const int32_t lengths[2] = {40, 40}, both[2] = {1, 1};
+    CHECK(kv_pool_fork(pool, 2, beams.data(), lengths, 2, both, 1, out.data(), nullptr) == HKV_OK);
+    CHECK(kv_pool_refcount(pool, ids[0]) == 3 && kv_pool_refcount(pool, ids[2]) == 1);
+    const std::vector<int32_t> now(out.begin(), out.begin() + 6);
+    CHECK(kv_pool_fork(pool, 2, now.data(), lengths, 0, both, 1, out.data(), nullptr) == HKV_OK);
+    CHECK(counts() == before && kv_pool_num_free(pool) == 5);
+    CHECK(kv_cache_release(cache, ids.data(), 3) == HKV_OK && acquire(cache, 32) == std::vector<int32_t>(ids.begin(), ids.begin() + 2));
+    CHECK(kv_cache_destroy(cache) == HKV_OK && kv_pool_num_free(pool) == 8);
+    // pages that a cache held once are like any others
+    std::vector<int32_t> mine(3);
+    CHECK(kv_pool_alloc(pool, 3, mine.data()) == HKV_OK);
+    CHECK(kv_pool_fork(pool, 1, mine.data(), &n, 1, parent, 1, out.data(), nullptr) == HKV_OK);
+    CHECK(kv_cache_destroy(other) == HKV_OK && kv_pool_destroy(pool) == HKV_OK);
+}
+
 int main(int argc, char **argv) {
-    const std::pair<const char *, void (*)()> programs[] = {{"caches_after_their_pool", caches_after_their_pool}, {"evictions_beside_forks", evictions_beside_forks}};
+    const std::pair<const char *, void (*)()> programs[] = {{"caches_after_their_pool", caches_after_their_pool}, {"evictions_beside_forks", evictions_beside_forks},
+                                                           {"forks_that_end_cached_sequences", forks_that_end_cached_sequences}};
     int ran = 0;
     for (const auto &p : programs)
         if (argc < 2 || !std::strcmp(argv[1], p.first)) {
