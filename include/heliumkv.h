@@ -165,7 +165,8 @@ int kv_pool_copy_on_write(hkv_pool *pool, int32_t n, int32_t *ids /* host, in/ou
  * Same type: whole 16-token blocks up to the last token, scales with them.  Other type: the tokens' values (code * scale) by the rules of
  * kv_pool_write, a block at a time as one written from its slot 0 (bf16: round to nearest even; fp8: one scale for the block's tokens; fp4: as
  * there; fp32: as they are), from the values in fp32, not from a bf16 rounding of them; slots behind the last token keep what they hold.
- *   src_ids, dst_ids: host, n entries.  dst_ids all different, of one owner at most, and, within one pool, none of src_ids (EINVAL).
+ *   src_ids, dst_ids: host, n entries.  dst_ids all different, of one owner at most, and no bytes of a page that is read: within one pool none of
+ *   src_ids, and pools over the same or overlapping buffers are looked at byte by byte (EINVAL).
  * References do not change, and key_weights are the caller's to copy.  ERANGE: page ids.  Nothing is queued on error.  Not for capture into a graph
  * (EINVAL): longer lists pass through the target pool's staging ring.  The pools' buffers may be on one device only, the current one. */
 int kv_pool_copy_pages(hkv_pool *dst, const int32_t *dst_ids, hkv_pool *src, const int32_t *src_ids, int32_t n, const int32_t *n_tokens, void *stream);

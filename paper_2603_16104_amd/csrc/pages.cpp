@@ -7,6 +7,7 @@
 #include <cstring>
 #include <exception>
 #include <numeric>
+#include <utility>
 
 namespace {
 
@@ -27,6 +28,47 @@ void mark_anew(hkv_pool *pool) {
 struct PagePair {
     int32_t src, dst, tokens;  // tokens: of the page
 };
+
+// A pool's buffers and what a page has of each.
+struct Buffer {
+    uintptr_t base;
+    size_t page, bytes;
+    std::pair<uintptr_t, uintptr_t> of(int32_t id) const { return {base + page * (size_t)id, base + page * (size_t)(id + 1)}; }
+};
+std::vector<Buffer> buffers_of(const hkv_pool *pool) {
+    const size_t heads = (size_t)pool->blocks_per_page * pool->d.num_kv_heads;
+    const int dtype = pool->d.dtype;
+    const size_t codes = heads * (HKV_PAGE_SIZE * HKV_HEAD_DIM / 8) * (dtype == HKV_BF16 ? 16 : dtype == HKV_FP8_E4M3 ? 8 : dtype == HKV_FP32 ? 32 : 4);
+    const size_t scales = dtype == HKV_FP8_E4M3 ? heads * sizeof(float) : dtype == HKV_FP4_E2M1 ? heads * (HKV_PAGE_SIZE * HKV_HEAD_DIM / 32) : 0;
+    std::vector<Buffer> out;
+    auto add = [&](const void *p, size_t page) { out.push_back({reinterpret_cast<uintptr_t>(p), page, page * (size_t)pool->d.num_pages}); };
+    add(pool->d.k_pages, codes);
+    add(pool->d.v_pages, codes);
+    if (scales > 0) {
+        add(pool->d.k_scale, scales);
+        add(pool->d.v_scale, scales);
+    }
+    return out;
+}
+// Of pages that go from one pool to another one whose bytes are partly the same: the first that is read where another (or it itself) is written, or -1.
+int32_t read_and_written(const hkv_pool *dst, const hkv_pool *src, const std::vector<PagePair> &pages) {
+    const std::vector<Buffer> to = buffers_of(dst), from = buffers_of(src);
+    std::vector<std::pair<uintptr_t, uintptr_t>> written;
+    for (const Buffer &w : to)
+        if (std::any_of(from.begin(), from.end(), [&](const Buffer &r) { return w.base < r.base + r.bytes && r.base < w.base + w.bytes; }))
+            for (const PagePair &p : pages) written.push_back(w.of(p.dst));
+    if (written.empty()) return -1;  // (as good as always)
+    std::sort(written.begin(), written.end());
+    std::vector<uintptr_t> ends;  // the furthest end so far (the target's own buffers may overlap, too)
+    for (const auto &w : written) ends.push_back(std::max(w.second, ends.empty() ? 0 : ends.back()));
+    for (const PagePair &p : pages)
+        for (const Buffer &r : from) {
+            const auto read = r.of(p.src);
+            const size_t before = (size_t)(std::lower_bound(written.begin(), written.end(), std::make_pair(read.second, (uintptr_t)0)) - written.begin());
+            if (before > 0 && ends[before - 1] > read.first) return p.src;
+        }
+    return -1;
+}
 
 // Queues the copies of pages (blocks behind a page's last token are left): lists that fit travel in the kernel's arguments, others through the
 // target pool's staging ring.
@@ -85,7 +127,6 @@ extern "C" int kv_pool_copy_pages(hkv_pool *dst, const int32_t *dst_ids, hkv_poo
         return fail(HKV_ESHAPE, "%s: pages of %d tokens and %d KV heads into pages of %d and %d", who, src->d.page_size, src->d.num_kv_heads, dst->d.page_size,
                     dst->d.num_kv_heads);
     if (dst->d.num_kv_heads > 65535) return fail(HKV_ESHAPE, "%s: %d KV heads (65535 at most)", who, dst->d.num_kv_heads);
-    const bool same_buffers = dst == src || dst->d.k_pages == src->d.k_pages || dst->d.v_pages == src->d.v_pages;
     mark_anew(dst);
     std::vector<PagePair> pairs;
     pairs.reserve(n);
@@ -101,9 +142,13 @@ extern "C" int kv_pool_copy_pages(hkv_pool *dst, const int32_t *dst_ids, hkv_poo
         if (tokens < 0 || tokens > dst->d.page_size) return fail(HKV_EINVAL, "%s: %d tokens (entry %d) of a page of %d", who, tokens, i, dst->d.page_size);
         pairs.push_back({src_ids[i], dst_ids[i], tokens});
     }
-    if (same_buffers)
-        for (int i = 0; i < n; ++i)
-            if (src_ids[i] < dst->d.num_pages && dst->mark[src_ids[i]] == dst->mark_now) return fail(HKV_EINVAL, "%s: page %d is read and written", who, src_ids[i]);
+    int32_t both = -1;
+    if (dst != src)
+        both = read_and_written(dst, src, pairs);
+    else
+        for (int i = 0; i < n && both < 0; ++i)
+            if (dst->mark[src_ids[i]] == dst->mark_now) both = src_ids[i];
+    if (both >= 0) return fail(HKV_EINVAL, "%s: page %d is read and written", who, both);
     if (n == 0) return HKV_OK;
     hipStream_t s = static_cast<hipStream_t>(stream);
     if (is_capturing(s)) return fail(HKV_EINVAL, "%s: not for capture into a graph", who);

@@ -182,9 +182,57 @@ static void forks_that_end_cached_sequences() {
     CHECK(kv_cache_destroy(other) == HKV_OK && kv_pool_destroy(pool) == HKV_OK);
 }
 
+// Pools that share bytes: a page that is read is not written in the same call, whatever its ids in the two pools are.
+static void copies_between_pools_that_overlap() {
+    char *const k = reinterpret_cast<char *>(0x100000), *const v = reinterpret_cast<char *>(0x40000000);
+    constexpr int kPageBytes = 2 * 2048 * 2;  // bf16, two heads
+    auto copy = [](hkv_pool *dst, std::vector<int32_t> to, hkv_pool *src, std::vector<int32_t> from) {
+        const int rc = kv_pool_copy_pages(dst, to.data(), src, from.data(), (int)to.size(), nullptr, nullptr);
+        CHECK(rc == HKV_OK || !std::strncmp(hkv_last_error(), "kv_pool_copy_pages: page", 24));
+        return rc;
+    };
+    hkv_pool *a = make_pool(8, 16, HKV_BF16, k, v);
+    {  // the same type, two pages further on; K alone, V alone
+        for (const int both : {0, 1, 2}) {
+            hkv_pool *b = make_pool(8, 16, HKV_BF16, both == 2 ? k + 0x20000000 : k + 2 * kPageBytes, both == 1 ? v + 0x20000000 : v + 2 * kPageBytes);
+            CHECK(copy(b, {3}, a, {5}) == HKV_EINVAL && copy(a, {5}, b, {3}) == HKV_EINVAL);
+            CHECK(copy(b, {3}, a, {3}) == HKV_OK && copy(a, {4}, b, {3}) == HKV_OK);
+            CHECK(copy(b, {0, 1, 2}, a, {0, 1, 4}) == HKV_EINVAL);  // written as b's page 2, read as a's page 4
+            CHECK(copy(b, {0, 1, 7}, a, {0, 1, 4}) == HKV_OK);
+            CHECK(kv_pool_destroy(b) == HKV_OK);
+        }
+    }
+    {  // K of one pool is V of the other
+        hkv_pool *b = make_pool(8, 16, HKV_BF16, v, v + 0x20000000);
+        CHECK(copy(b, {3}, a, {3}) == HKV_EINVAL && copy(b, {3}, a, {4}) == HKV_OK);
+        CHECK(kv_pool_destroy(b) == HKV_OK);
+    }
+    {  // another type over the same bytes: bf16 page 1 is fp8 pages 2 and 3, fp4 pages 4 to 7, half of fp32 page 0
+        hkv_pool *eight = make_pool(16, 16, HKV_FP8_E4M3, k, v), *four = make_pool(32, 16, HKV_FP4_E2M1, k, v), *wide = make_pool(4, 16, HKV_FP32, k, v);
+        CHECK(copy(eight, {1}, a, {1}) == HKV_OK && copy(eight, {2}, a, {1}) == HKV_EINVAL && copy(eight, {3}, a, {1}) == HKV_EINVAL && copy(eight, {4}, a, {1}) == HKV_OK);
+        CHECK(copy(four, {1}, a, {1}) == HKV_OK && copy(four, {3}, a, {1}) == HKV_OK && copy(four, {4}, a, {1}) == HKV_EINVAL && copy(four, {7}, a, {1}) == HKV_EINVAL &&
+              copy(four, {8}, a, {1}) == HKV_OK);
+        CHECK(copy(wide, {0}, a, {1}) == HKV_EINVAL && copy(wide, {1}, a, {1}) == HKV_OK && copy(wide, {1}, a, {3}) == HKV_EINVAL);
+        for (hkv_pool *p : {eight, four, wide}) CHECK(kv_pool_destroy(p) == HKV_OK);
+    }
+    {  // scales alone
+        hkv_pool *b = make_pool(16, 16, HKV_FP8_E4M3, k + 0x20000000, v + 0x20000000), *c = make_pool(16, 16, HKV_FP8_E4M3, k + 0x30000000, v + 0x30000000);
+        CHECK(copy(b, {3}, c, {3}) == HKV_EINVAL && copy(b, {3}, c, {4}) == HKV_OK);
+        CHECK(kv_pool_destroy(b) == HKV_OK && kv_pool_destroy(c) == HKV_OK);
+    }
+    {  // another handle over the same pool, and buffers that only touch
+        hkv_pool *b = make_pool(8, 16, HKV_BF16, k, v), *c = make_pool(8, 16, HKV_BF16, k + 8 * kPageBytes, v + 8 * kPageBytes);
+        CHECK(copy(a, {3}, b, {3}) == HKV_EINVAL && copy(a, {3}, b, {4}) == HKV_OK);
+        for (int i = 0; i < 8; ++i) CHECK(copy(a, {i}, c, {7 - i}) == HKV_OK && copy(c, {i}, a, {i}) == HKV_OK);
+        CHECK(kv_pool_destroy(b) == HKV_OK && kv_pool_destroy(c) == HKV_OK);
+    }
+    CHECK(kv_pool_destroy(a) == HKV_OK);
+}
+
 int main(int argc, char **argv) {
     const std::pair<const char *, void (*)()> programs[] = {{"caches_after_their_pool", caches_after_their_pool}, {"evictions_beside_forks", evictions_beside_forks},
-                                                           {"forks_that_end_cached_sequences", forks_that_end_cached_sequences}};
+                                                           {"forks_that_end_cached_sequences", forks_that_end_cached_sequences},
+                                                           {"copies_between_pools_that_overlap", copies_between_pools_that_overlap}};
     int ran = 0;
     for (const auto &p : programs)
         if (argc < 2 || !std::strcmp(argv[1], p.first)) {

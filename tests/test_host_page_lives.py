@@ -22,7 +22,7 @@ def program(tmp_path_factory):
 
 
 @pytest.mark.timeout(600)
-@pytest.mark.parametrize("name", ["caches_after_their_pool", "evictions_beside_forks", "forks_that_end_cached_sequences"])
+@pytest.mark.parametrize("name", ["caches_after_their_pool", "evictions_beside_forks", "forks_that_end_cached_sequences", "copies_between_pools_that_overlap"])
 def test_lives(program, name):
     r = subprocess.run([program, name], capture_output=True, text=True, timeout=300, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=0"))
     out = r.stdout + r.stderr
