@@ -245,21 +245,25 @@ static int ensure_write_staging(hkv_pool *pool) {
     return HKV_OK;
 }
 
-int hkv::take_staging(hkv_pool *pool, int32_t *slot, int32_t **host, int32_t **host_on_device, int32_t **device) {
-    if (int rc = ensure_write_staging(pool)) return rc;
-    *slot = pool->next_slot;
-    pool->next_slot = (*slot + 1) % hkv_pool::kWriteSlots;
-    if (pool->slot_in_flight[*slot]) HKV_HIP(hipEventSynchronize(pool->slot_free[*slot]));  // its last use is done
-    const size_t at = (size_t)*slot * hkv_pool::kMaxWritePages;
-    *host = pool->h_ids + at;
-    *host_on_device = pool->hd_ids + at;
-    *device = pool->d_ids + at;
+int hkv::Staging::take() {
+    if (int rc = ensure_write_staging(pool_)) return rc;
+    const int32_t slot = pool_->next_slot;
+    pool_->next_slot = (slot + 1) % hkv_pool::kWriteSlots;
+    if (pool_->slot_in_flight[slot]) HKV_HIP(hipEventSynchronize(pool_->slot_free[slot]));  // its last use is done
+    const size_t at = (size_t)slot * hkv_pool::kMaxWritePages;
+    host = pool_->h_ids + at;
+    host_on_device = pool_->hd_ids + at;
+    device = pool_->d_ids + at;
+    slot_ = slot;
     return HKV_OK;
 }
 
-int hkv::leave_staging(hkv_pool *pool, int32_t slot, hipStream_t s) {
-    HKV_HIP(hipEventRecord(pool->slot_free[slot], s));
-    pool->slot_in_flight[slot] = true;
+int hkv::Staging::leave() {
+    if (slot_ < 0) return HKV_OK;
+    const int32_t slot = slot_;
+    slot_ = -1;
+    HKV_HIP(hipEventRecord(pool_->slot_free[slot], stream_));
+    pool_->slot_in_flight[slot] = true;
     return HKV_OK;
 }
 
@@ -292,18 +296,19 @@ extern "C" int kv_pool_write(hkv_pool *pool, const int32_t *page_ids, int32_t fi
         HKV_HIP(launch_pool_write(a, s));
         return HKV_OK;
     }
-    int32_t slot, *h, *hd, *d;
-    if (int rc = take_staging(pool, &slot, &h, &hd, &d)) return rc;
-    for (int64_t b = b0; b <= b1; ++b) h[b - b0] = page_ids[b / S] * S + (int32_t)(b % S);
+    Staging list(pool, s);
+    if (int rc = list.take()) return rc;
+    int32_t *const d = list.device;
+    for (int64_t b = b0; b <= b1; ++b) list.host[b - b0] = page_ids[b / S] * S + (int32_t)(b % S);
     // a copy kernel on the stream reads the pinned slot (a DMA copy between kernels of one stream costs more)
-    HKV_HIP(launch_upload(hd, d, align_up(sizeof(int32_t) * (size_t)n_pg, 16), s));
+    HKV_HIP(launch_upload(list.host_on_device, d, align_up(sizeof(int32_t) * (size_t)n_pg, 16), s));
     PoolWriteLaunch a{pool->d.k_pages, pool->d.v_pages, pool->d.k_scale, pool->d.v_scale, pool->d.num_kv_heads,
                       pool->d.dtype, d, (int32_t)n_pg, first_slot % HKV_PAGE_SIZE, n_tokens, k_src, v_src, nullptr, nullptr};
     if (pool->d.dtype == HKV_FP32)
         HKV_HIP(launch_pool_write_fp32(a, s));
     else
         HKV_HIP(launch_pool_write(a, s));
-    return leave_staging(pool, slot, s);
+    return list.leave();
 }
 
 extern "C" int kv_pool_append(hkv_pool *pool, const int32_t *page_ids, const int32_t *slots, int32_t n,
@@ -345,17 +350,18 @@ extern "C" int kv_pool_append(hkv_pool *pool, const int32_t *page_ids, const int
         HKV_HIP(launch_pool_append_inline(a, s));
         return HKV_OK;
     }
-    int32_t slot, *h, *hd, *d;
-    if (int rc = take_staging(pool, &slot, &h, &hd, &d)) return rc;
+    Staging list(pool, s);
+    if (int rc = list.take()) return rc;
+    int32_t *const d = list.device;
     for (int i = 0; i < n; ++i) {  // block ids, then the slots inside them
-        h[i] = page_ids[i] * S + slots[i] / HKV_PAGE_SIZE;
-        h[n + i] = slots[i] % HKV_PAGE_SIZE;
+        list.host[i] = page_ids[i] * S + slots[i] / HKV_PAGE_SIZE;
+        list.host[n + i] = slots[i] % HKV_PAGE_SIZE;
     }
-    HKV_HIP(launch_upload(hd, d, align_up(sizeof(int32_t) * 2 * (size_t)n, 16), s));
+    HKV_HIP(launch_upload(list.host_on_device, d, align_up(sizeof(int32_t) * 2 * (size_t)n, 16), s));
     PoolWriteLaunch a{pool->d.k_pages, pool->d.v_pages, pool->d.k_scale, pool->d.v_scale, pool->d.num_kv_heads,
                       pool->d.dtype, d, n, 0, n, k_src, v_src, d + n, nullptr};
     HKV_HIP(launch_pool_write(a, s));
-    return leave_staging(pool, slot, s);
+    return list.leave();
 }
 
 // ---------------------------------------------------------------------------------------------

@@ -168,9 +168,23 @@ inline PoolView view_of(const hkv_pool *p) {
     return PoolView{p->d.k_pages, p->d.v_pages, p->d.k_scale, p->d.v_scale, p->d.num_kv_heads, p->d.dtype};
 }
 
-// Slots of the pool's staging ring (kv_pool_write): `take` waits until the next one is free, `leave` marks it as used by what is queued on s.
-int take_staging(hkv_pool *pool, int32_t *slot, int32_t **host, int32_t **host_on_device, int32_t **device);
-int leave_staging(hkv_pool *pool, int32_t slot, hipStream_t s);
+// A slot of the pool's staging ring (kv_pool_write): `take` waits until the next one is free, `leave` marks it as used by what is queued on the stream.  One that a
+// call gives up on its way is left all the same, since the upload of its list may be queued already.
+class Staging {
+   public:
+    Staging(hkv_pool *pool, hipStream_t s) : pool_(pool), stream_(s) {}
+    Staging(const Staging &) = delete;
+    Staging &operator=(const Staging &) = delete;
+    ~Staging() { (void)leave(); }
+    int take();
+    int leave();
+    int32_t *host = nullptr, *host_on_device = nullptr, *device = nullptr;
+
+   private:
+    hkv_pool *pool_;
+    hipStream_t stream_;
+    int32_t slot_ = -1;
+};
 
 // hkv_decode_plan_append with what happens to the new tokens: neither k_src nor hook: nothing; k_src / v_src: they are stored
 // as hkv_decode_plan_append_tokens says; hook: called in place of the kernel that applies the update `g`, where that travels in arguments

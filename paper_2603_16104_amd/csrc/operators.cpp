@@ -465,9 +465,10 @@ extern "C" int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_p
         while (i1 < n_seq && ints + ints_of(i1) <= hkv_pool::kMaxWritePages) ints += ints_of(i1++);
         // what the kernels index with: in their arguments where it fits (2.2 us of a call less), else through the ring
         const bool in_arguments = ints <= kMaxInlineEvict;
-        int32_t slot = 0, *hm = a.list, *hdm = nullptr, *dm = nullptr;
+        Staging list(pool, s);
         if (!in_arguments)
-            if (int rc = take_staging(pool, &slot, &hm, &hdm, &dm)) return rc;
+            if (int rc = list.take()) return rc;
+        int32_t *const hm = in_arguments ? a.list : list.host;
         int32_t at = (i1 - i0) * kRecord, unit = 0;
         for (int i = i0; i < i1; ++i) {
             const int nb = (n_tokens[i] + 15) / 16, mb = (n_keep[i] + 15) / 16;
@@ -481,16 +482,16 @@ extern "C" int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_p
             dp += (mb + S - 1) / S;
             kept_at += n_keep[i];
         }
-        a.meta = dm;
+        a.meta = list.device;
         a.n_seq = i1 - i0;
         a.n_units = unit;
         a.most_tokens = *std::max_element(n_tokens + i0, n_tokens + i1);
         if (in_arguments) {
             HKV_HIP(launch_evict(a, s));
         } else {
-            HKV_HIP(launch_upload(hdm, dm, align_up(sizeof(int32_t) * (size_t)at, 16), s));
+            HKV_HIP(launch_upload(list.host_on_device, list.device, align_up(sizeof(int32_t) * (size_t)at, 16), s));
             HKV_HIP(launch_evict(static_cast<const EvictLaunch &>(a), s));
-            if (int rc = leave_staging(pool, slot, s)) return rc;
+            if (int rc = list.leave()) return rc;
         }
         i0 = i1;
     }

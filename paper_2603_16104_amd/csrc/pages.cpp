@@ -84,9 +84,10 @@ int queue_copies(hkv_pool *dst, const hkv_pool *src, const std::vector<PagePair>
     size_t page = 0;
     int block = 0;  // of the page
     while (page < pages.size()) {
-        int32_t slot = 0, *list = a.entries, *on_device = nullptr, *device = nullptr;
+        Staging staged(dst, s);
         if (!in_arguments)
-            if (int rc = take_staging(dst, &slot, &list, &on_device, &device)) return rc;
+            if (int rc = staged.take()) return rc;
+        int32_t *const list = in_arguments ? a.entries : staged.host;
         int n = 0;
         while (page < pages.size() && n < (in_arguments ? kMaxInlineCopies : kMost)) {
             const PagePair &p = pages[page];
@@ -102,15 +103,15 @@ int queue_copies(hkv_pool *dst, const hkv_pool *src, const std::vector<PagePair>
             ++block;
         }
         a.n = n;
-        a.list = device;
+        a.list = staged.device;
         if (in_arguments) {
             HKV_HIP(launch_page_copy(a, s));
         } else {
             if (n > 0) {
-                HKV_HIP(launch_upload(on_device, device, align_up(sizeof(int32_t) * 3 * (size_t)n, 16), s));
+                HKV_HIP(launch_upload(staged.host_on_device, staged.device, align_up(sizeof(int32_t) * 3 * (size_t)n, 16), s));
                 HKV_HIP(launch_page_copy(static_cast<const PageCopyLaunch &>(a), s));
             }
-            if (int rc = leave_staging(dst, slot, s)) return rc;
+            if (int rc = staged.leave()) return rc;
         }
     }
     return HKV_OK;

@@ -45,16 +45,37 @@ hipError_t hipGetDeviceProperties(hipDeviceProp_t *, int) { return hipErrorNoDev
 hipError_t hipGetLastError() { return hipSuccess; }
 const char *hipGetErrorString(hipError_t) { return "?"; }
 }
-hipError_t hipEventRecord(hipEvent_t, hipStream_t) { return hipSuccess; }
-hipError_t hipEventSynchronize(hipEvent_t) { return hipSuccess; }
+// Uploads that read a list are on their way until an event recorded behind them has been waited for.
+static std::map<const void *, hipEvent_t> on_their_way;  // by the list's address: the event behind it (null: none yet)
+static int overtaken = 0, launches_until_failure = -1;
+hipError_t hipEventRecord(hipEvent_t e, hipStream_t) {
+    for (auto &u : on_their_way)
+        if (!u.second) u.second = e;
+    return hipSuccess;
+}
+hipError_t hipEventSynchronize(hipEvent_t e) {
+    for (auto u = on_their_way.begin(); u != on_their_way.end();) u = u->second == e ? on_their_way.erase(u) : std::next(u);
+    return hipSuccess;
+}
+static hipError_t launched() { return launches_until_failure-- == 0 ? hipErrorInvalidValue : hipSuccess; }
 
 namespace hkv {
-hipError_t launch_page_copy(const PageCopyLaunch &, hipStream_t) { return hipSuccess; }
+hipError_t launch_page_copy(const PageCopyLaunch &, hipStream_t) { return launched(); }
 hipError_t launch_page_copy(const PageCopyInline &, hipStream_t) { return hipSuccess; }
-hipError_t launch_upload(const void *s, void *d, size_t n, hipStream_t) { std::memcpy(d, s, n); return hipSuccess; }
+hipError_t launch_upload(const void *s, void *d, size_t n, hipStream_t) {
+    overtaken += !on_their_way.insert({s, nullptr}).second;  // (the list was written anew under an upload)
+    std::memcpy(d, s, n);
+    return launched();
+}
+hipError_t launch_evict(const EvictLaunch &, hipStream_t) { return launched(); }
+hipError_t launch_evict(const EvictInline &, hipStream_t) { return launched(); }
+hipError_t launch_projection_store(const ProjectionLaunch &, hipStream_t) { return hipSuccess; }
+hipError_t launch_projection_store(const ProjectionPrefill &, hipStream_t) { return hipSuccess; }
+hipError_t launch_projection_append(const ProjectionAppend &, const PlanGrowInline &, hipStream_t) { return hipSuccess; }
+hipError_t launch_key_weights(const KeyWeightsLaunch &, hipStream_t) { return hipSuccess; }
 hipError_t launch_plan_grow_inline(const PlanGrowInline &, hipStream_t) { return hipSuccess; }
-hipError_t launch_pool_write(const PoolWriteLaunch &, hipStream_t) { return hipSuccess; }
-hipError_t launch_pool_write_fp32(const PoolWriteLaunch &, hipStream_t) { return hipSuccess; }
+hipError_t launch_pool_write(const PoolWriteLaunch &, hipStream_t) { return launched(); }
+hipError_t launch_pool_write_fp32(const PoolWriteLaunch &, hipStream_t) { return launched(); }
 hipError_t launch_pool_copy(const PoolCopyLaunch &, hipStream_t) { return hipSuccess; }
 hipError_t launch_pool_append_inline(const PoolAppendInline &, hipStream_t) { return hipSuccess; }
 hipError_t launch_decode_step_append(const PoolAppendInline &, const PlanGrowInline &, hipStream_t) { return hipSuccess; }
@@ -229,10 +250,40 @@ static void copies_between_pools_that_overlap() {
     CHECK(kv_pool_destroy(a) == HKV_OK);
 }
 
+// A call whose launch fails behind its list's upload: the list's place is not written anew while the upload may still read it.
+static void lists_that_fail_on_their_way() {
+    hkv_pool *pool = make_pool(3000), *wide = make_pool(3000, 16, HKV_FP32, reinterpret_cast<void *>(0x200000000), reinterpret_cast<void *>(0x300000000));
+    std::vector<int32_t> to(1400), from(1400), slots(1400, 3), kept(1);
+    std::iota(to.begin(), to.end(), 0);
+    std::iota(from.begin(), from.end(), 1400);
+    void *const x = reinterpret_cast<void *>(0x400000000);
+    const int32_t n_tokens = 1400 * 16;
+    const auto copy = [&] { return kv_pool_copy_pages(pool, to.data(), pool, from.data(), 1400, nullptr, nullptr); };
+    const auto write = [&] { return kv_pool_write(pool, to.data(), 0, n_tokens, x, x, nullptr); };
+    const auto write_wide = [&] { return kv_pool_write(wide, to.data(), 0, 64, x, x, nullptr); };
+    const auto append = [&] { return kv_pool_append(pool, to.data(), slots.data(), 1400, x, x, nullptr); };
+    const auto evict = [&] { return kv_pool_evict(pool, 1, from.data(), &n_tokens, to.data(), &n_tokens, 4, 4, static_cast<float *>(x), static_cast<int32_t *>(x), nullptr); };
+    const auto each = [&](auto &&f) { f(copy); f(write); f(append); f(evict); f(write_wide); };
+    each([&](auto call) {
+        CHECK(call() == HKV_OK);
+        for (int fails = 0; fails < 2; ++fails) {
+            launches_until_failure = fails;
+            CHECK(call() == HKV_EHIP);
+            launches_until_failure = -1;
+            for (int i = 0; i < 2 * hkv_pool::kWriteSlots; ++i) CHECK(call() == HKV_OK);
+        }
+        CHECK(overtaken == 0);
+        overtaken = 0;
+        on_their_way.clear();
+    });
+    CHECK(kv_pool_destroy(pool) == HKV_OK && kv_pool_destroy(wide) == HKV_OK);
+}
+
 int main(int argc, char **argv) {
     const std::pair<const char *, void (*)()> programs[] = {{"caches_after_their_pool", caches_after_their_pool}, {"evictions_beside_forks", evictions_beside_forks},
                                                            {"forks_that_end_cached_sequences", forks_that_end_cached_sequences},
-                                                           {"copies_between_pools_that_overlap", copies_between_pools_that_overlap}};
+                                                           {"copies_between_pools_that_overlap", copies_between_pools_that_overlap},
+                                                           {"lists_that_fail_on_their_way", lists_that_fail_on_their_way}};
     int ran = 0;
     for (const auto &p : programs)
         if (argc < 2 || !std::strcmp(argv[1], p.first)) {

@@ -17,12 +17,13 @@ def program(tmp_path_factory):
     csrc = os.path.join(ROOT, "paper_2603_16104_amd", "csrc")
     subprocess.check_call(["g++", "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined", "-fno-sanitize-recover=undefined", "-D__HIP_PLATFORM_AMD__",
                            "-I/opt/rocm/include", os.path.join(ROOT, "tests", "native", "page_lives.cpp"),
-                           *(os.path.join(csrc, f) for f in ("api.cpp", "pages.cpp", "cache.cpp")), "-o", exe])
+                           *(os.path.join(csrc, f) for f in ("api.cpp", "operators.cpp", "pages.cpp", "cache.cpp")), "-o", exe])
     return exe
 
 
 @pytest.mark.timeout(600)
-@pytest.mark.parametrize("name", ["caches_after_their_pool", "evictions_beside_forks", "forks_that_end_cached_sequences", "copies_between_pools_that_overlap"])
+@pytest.mark.parametrize("name", ["caches_after_their_pool", "evictions_beside_forks", "forks_that_end_cached_sequences", "copies_between_pools_that_overlap",
+                                  "lists_that_fail_on_their_way"])
 def test_lives(program, name):
     r = subprocess.run([program, name], capture_output=True, text=True, timeout=300, env=dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=0"))
     out = r.stdout + r.stderr
