@@ -342,6 +342,7 @@ enum {
 /* nodes, node_pages, req_leaf: host.  Validates the forest (ETREE/ERANGE, page ids against the
  * pool), builds the work list and uploads it (blocking).  ESHAPE unless num_q_heads is a
  * multiple of the pool's num_kv_heads with a ratio of at most 16.
+ * EINVAL where n_req * num_q_heads * (items on the longest path) is more than 2^31 - 1, which short leaf_chunk on long sequences can make it.
  * With bf16, fp8 and fp4 pools every node is read through its own page list, so any node may end inside
  * a page (its last page is then partly used and its children start on pages of their own).  That
  * makes the forest itself the attention mask of a tree of drafted tokens: one node per drafted

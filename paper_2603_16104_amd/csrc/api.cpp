@@ -1212,7 +1212,6 @@ static void plan_items(hkv_decode_plan &pl) {
         pl.part_count[r] = slot_base[leaf] + node_chunks[leaf];
         pl.max_parts = std::max(pl.max_parts, pl.part_count[r]);
     }
-    pl.n_parts = pl.n_req * pl.num_q_heads * pl.max_parts;
     // One launch for both kinds of items where the kernel allows it: its workgroups of the other items run two
     // blocks side by side, which works as long as no item synchronises per step (more than 16 query rows).
     pl.fused = !pl.tile_items.empty() && !pl.items.empty() && opt.fused >= 0 && !pl.fp8_matrix;
@@ -1542,6 +1541,12 @@ static int create_decode_plan(hkv_pool *pool, const hkv_node *nodes, int32_t n_n
     else
         plan_items(*pl);
     plan_paths(*pl, by_leaf);
+    const int64_t n_parts = (int64_t)pl->n_req * pl->num_q_heads * pl->max_parts;
+    if (n_parts > INT32_MAX) {  // (the kernels number them in 32 bits)
+        delete pl;
+        return fail(HKV_EINVAL, "hkv_decode_plan_create: %lld partial results; longer chunks make fewer", (long long)n_parts);
+    }
+    pl->n_parts = (int32_t)n_parts;
     if (reserve_tokens > 0) {  // the items that grow with each request: the leaf's last chunk, one per KV head
         pl->grow_items.assign((size_t)n_req * Hkv, -1);
         for (int r = 0; r < n_req; ++r) {

@@ -228,5 +228,4 @@ static void plan_four_bit(hkv_decode_plan &pl, int n_cu) {
         pl.part_count[r] = slot_base[leaf] + node_chunks[leaf];
         pl.max_parts = std::max(pl.max_parts, pl.part_count[r]);
     }
-    pl.n_parts = pl.n_req * pl.num_q_heads * pl.max_parts;
 }
