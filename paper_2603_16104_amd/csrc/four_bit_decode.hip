@@ -210,20 +210,23 @@ __device__ __forceinline__ void scores(const Operands &x, const RowTile (&tile)[
 __device__ __forceinline__ uint32_t seen_bits(int d0, unsigned long long vis) {
     return d0 < 0 ? (d0 <= -16 ? 0xFFFFu : (1u << -d0) - 1u | (uint32_t)vis << -d0) : d0 < 64 ? (uint32_t)(vis >> d0) : 0u;
 }
-// Scores of tokens that a row does not see are -inf; tok0: of the lane's 16 tokens the first, score j of a row is acc[j % 4][j / 4].
+// Scores of tokens that a row does not see are -inf, and those of tokens behind the item's end (a chunk may end inside a step, and its rows see what follows in the
+// next one); of the lane's 16 tokens score j of a row is acc[j % 4][j / 4].
 template <int RT>
-__device__ __forceinline__ bool hide(const Reader &rd, const RowTile (&tile)[RT], f32x4 (&acc)[RT][4], int tok0) {
+__device__ __forceinline__ bool hide(const Reader &rd, const RowTile (&tile)[RT], f32x4 (&acc)[RT][4], int b) {
+    const int tok0 = b * kStep + 16 * rd.g;
     int most = -INT_MAX;  // tokens of the step behind what a row sees at once
 #pragma unroll
-    for (int r = 0; r < RT; ++r) most = max(most, tok0 - tile[r].lim);
+    for (int r = 0; r < RT; ++r) most = max(most, tok0 - min(tile[r].lim, rd.it.n_tokens));
     const bool some = __builtin_amdgcn_ballot_w64(most > -16);  // some row does not see the whole step, the item's last one among them
     if (some) {
+        const uint32_t in_item = 0xFFFFu >> min(max(tok0 + 16 - rd.it.n_tokens, 0), 16);
 #pragma unroll
         for (int r = 0; r < RT; ++r) {
             const bool last = rd.a.row_leaf && rd.a.row_leaf[tile[r].req] == rd.it.node;  // (looked up here: this is the exception)
             const unsigned long long vis = last ? rd.a.row_mask[tile[r].req] : 0ull;
             const int d0 = tok0 - tile[r].lim;
-            const uint32_t seen = seen_bits(d0, vis);
+            const uint32_t seen = seen_bits(d0, vis) & in_item;
 #pragma unroll
             for (int j = 0; j < 16; ++j) acc[r][j & 3][j >> 2] = (seen >> j & 1u) ? acc[r][j & 3][j >> 2] : -INFINITY;
         }
@@ -419,7 +422,7 @@ __device__ __forceinline__ void stream(const Reader &rd, int row0, int ts, int n
             rd.ids(id, b + 3 * n_ts);
             __builtin_amdgcn_sched_barrier(0);
             scores(now, tile, acc);
-            hide(rd, tile, acc, b * kStep + 16 * rd.g);
+            hide(rd, tile, acc, b);
             weights(tile, acc, c, pw);
             second_half(now, pw);
             return (b += n_ts) < n_blk;
@@ -433,7 +436,7 @@ __device__ __forceinline__ void stream(const Reader &rd, int row0, int ts, int n
             __builtin_amdgcn_sched_barrier(0);
             rd.keys(x, id);
             __builtin_amdgcn_sched_barrier(0);
-            hide(rd, tile, acc, b * kStep + 16 * rd.g);
+            hide(rd, tile, acc, b);
             weights(tile, acc, c, pw);
             second_half(x, pw);
             __builtin_amdgcn_sched_barrier(0);
@@ -805,7 +808,7 @@ __device__ __forceinline__ void run_rows(const DecodeLaunch &a, const DecodeItem
     u32x4 pw[2];
     auto most = [](const f32x4 (&acc)[1][4], int j, float top) { return fmaxf(fmaxf(top, acc[0][j & 3][j >> 2]), acc[0][(j + 1) & 3][(j + 1) >> 2]); };
     auto settle = [&](f32x4 (&acc)[1][4], int b, float top) {  // scores of step b are what weights can be made of
-        if (hide(rd, tile, acc, b * kStep + 16 * rd.g)) {
+        if (hide(rd, tile, acc, b)) {
             top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 16; j += 2) top = most(acc, j, top);
@@ -954,14 +957,15 @@ __device__ __forceinline__ void run_tall(const DecodeLaunch &a, const DecodeItem
     if (row0 >= rows) return ring.serve(n_blk, widen);
     auto most = [](const f32x16 (&acc)[2], int j, float top) { return fmaxf(fmaxf(top, acc[j >> 4][j & 15]), acc[j >> 4][(j & 15) + 1]); };
     auto settle = [&](f32x16 (&acc)[2], int b, float top) {  // scores of step b are what weights can be made of
-        if (__builtin_amdgcn_ballot_w64((b + 1) * kStep > x.lim)) {  // some row does not see the whole step, the item's last one among them
+        if (__builtin_amdgcn_ballot_w64((b + 1) * kStep > min(x.lim, it.n_tokens))) {  // some row does not see the whole step, the item's last one among them
             const bool last = a.row_leaf && a.row_leaf[x.req] == it.node;
             const unsigned long long vis = last ? a.row_mask[x.req] : 0ull;
             top = -INFINITY;
 #pragma unroll
             for (int j = 0; j < 8; ++j) {
                 const int d0 = b * kStep + 8 * j + 4 * h - x.lim;
-                const uint32_t seen = d0 < 0 ? (d0 <= -4 ? 0xFu : (1u << -d0) - 1u | (uint32_t)vis << -d0) : d0 < 64 ? (uint32_t)(vis >> d0) : 0u;
+                const uint32_t in_item = 0xFu >> min(max(b * kStep + 8 * j + 4 * h + 4 - it.n_tokens, 0), 4);
+                const uint32_t seen = (d0 < 0 ? (d0 <= -4 ? 0xFu : (1u << -d0) - 1u | (uint32_t)vis << -d0) : d0 < 64 ? (uint32_t)(vis >> d0) : 0u) & in_item;
 #pragma unroll
                 for (int i = 0; i < 4; ++i) acc[j >> 2][4 * (j & 3) + i] = (seen >> i & 1u) ? acc[j >> 2][4 * (j & 3) + i] : -INFINITY;
                 top = most(acc, 4 * j, most(acc, 4 * j + 2, top));

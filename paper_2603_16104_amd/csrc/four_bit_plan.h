@@ -52,11 +52,11 @@ struct Cut {
     double us;
 };
 struct Pieces {
-    int count, blocks;  // chunks of a node, blocks of one (whole steps of four, the last one shorter)
+    int count, blocks;  // chunks of a node, blocks of one (the last one shorter)
 };
-inline Pieces pieces_of(int blocks, int chunk) {
+inline Pieces pieces_of(int blocks, int chunk) {  // evenly, in whole steps of four blocks where the chunk has room for them
     const int most = std::max(1, chunk / HKV_PAGE_SIZE), cuts = (blocks + most - 1) / most;
-    const int each = std::min(blocks, ((blocks + cuts - 1) / cuts + 3) / 4 * 4);
+    const int each = std::min({blocks, most, ((blocks + cuts - 1) / cuts + 3) / 4 * 4});
     return {(blocks + each - 1) / each, each};
 }
 
