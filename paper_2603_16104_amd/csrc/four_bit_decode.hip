@@ -377,7 +377,11 @@ __device__ __forceinline__ void write_rows(const Reader &rd, int row0, float c, 
     }
 }
 
-__device__ __forceinline__ float exponent_factor(float scale) { return fmaxf(fabsf(scale) * kLog2e, 1e-30f); }  // (scores times 0: a weight of 1 each, and -inf stays)
+// Of a scale of 0 the smallest number: a weight of 1 for every score, and -inf stays.
+__device__ __forceinline__ float exponent_factor(float scale) {
+    const float c = fabsf(scale) * kLog2e;
+    return c == 0.f ? 0x1p-149f : c;
+}
 
 // What a wavefront does with a share of an item's steps, ts, ts + n_ts, ..: the operands of two steps travel while another is computed, page ids a step
 // further ahead (behind the last steps once more, clamped to its last page: a condition would keep two sets of registers apart).
