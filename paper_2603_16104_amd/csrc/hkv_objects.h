@@ -1,6 +1,7 @@
 // The library's opaque objects and what its host files share.  Not part of the C ABI.
 #pragma once
 
+#include <algorithm>
 #include <deque>
 #include <vector>
 
@@ -142,6 +143,13 @@ struct hkv_pool {
     std::vector<Follower> followers;
     std::vector<uint32_t> mark;  // kv_pool_evict, kv_pool_copy_pages: pages marked in the present call (mark[id] == mark_now)
     uint32_t mark_now = 0;
+    void mark_anew() {
+        if (mark.empty()) mark.assign(d.num_pages, 0);
+        if (++mark_now == 0) {
+            std::fill(mark.begin(), mark.end(), 0u);
+            mark_now = 1;
+        }
+    }
     hkv_decode_plan *cached_decode = nullptr;
     hkv_prefill_plan *cached_prefill = nullptr;
 };
@@ -161,6 +169,11 @@ inline int fail_hip(hipError_t e, const char *what) {
         hipError_t e_ = (call);                        \
         if (e_ != hipSuccess) return fail_hip(e_, #call); \
     } while (0)
+
+inline bool is_capturing(hipStream_t s) {
+    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
+    return hipStreamIsCapturing(s, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone;
+}
 
 inline size_t align_up(size_t x, size_t a) { return (x + a - 1) / a * a; }
 

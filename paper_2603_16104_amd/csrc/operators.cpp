@@ -13,11 +13,6 @@ namespace {
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
 
-bool is_capturing(hipStream_t s) {
-    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-    return hipStreamIsCapturing(s, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone;
-}
-
 // The call's rows, checked, as the kernels take them.
 int projection_of(const hkv_pool *pool, int num_q_heads, const hkv_qkv *x, ProjectionLaunch &a, const char *who) {
     if (!x) return fail(HKV_EINVAL, "%s: null rows", who);
@@ -431,11 +426,7 @@ extern "C" int kv_pool_evict(hkv_pool *pool, int32_t n_seq, const int32_t *src_p
         if (src_pages[i] < 0 || src_pages[i] >= pool->d.num_pages)
             return fail(HKV_ERANGE, "%s: page id %d (entry %lld of src_pages) outside pool of %d pages", who, src_pages[i], (long long)i, pool->d.num_pages);
     // new places: pages of one owner, each once, none of those that are read
-    if (pool->mark.empty()) pool->mark.assign(pool->d.num_pages, 0);
-    if (++pool->mark_now == 0) {
-        std::fill(pool->mark.begin(), pool->mark.end(), 0u);
-        pool->mark_now = 1;
-    }
+    pool->mark_anew();
     for (int64_t i = 0; i < dst; ++i) {
         const int32_t id = dst_pages[i];
         if (id < 0 || id >= pool->d.num_pages)

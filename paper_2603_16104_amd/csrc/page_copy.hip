@@ -18,29 +18,28 @@ struct Entry {
     int32_t src, dst, tokens;
 };
 
-// Copies `bytes` (a multiple of 16) from piece `first` on, the threads of a workgroup U loads each.
-template <int U>
+constexpr int kPieces = 4;  // of 16 bytes, a thread's
+// n16 pieces from piece `first` on, as many as a workgroup copies.
 __device__ __forceinline__ void copy_pieces(const char *src, char *dst, int first, int n16) {
-    u32x4 w[U];
+    u32x4 w[kPieces];
 #pragma unroll
-    for (int j = 0; j < U; ++j) {
+    for (int j = 0; j < kPieces; ++j) {
         const int i = first + (int)threadIdx.x + 256 * j;
         if (i < n16) w[j] = ld16_stream(src + 16 * (size_t)i);
     }
 #pragma unroll
-    for (int j = 0; j < U; ++j) {
+    for (int j = 0; j < kPieces; ++j) {
         const int i = first + (int)threadIdx.x + 256 * j;
         if (i < n16) __builtin_nontemporal_store(w[j], reinterpret_cast<u32x4 *>(dst + 16 * (size_t)i));
     }
 }
 
-// Workgroup (entry, K or V, slice of 256 U pieces of the block's heads).
-template <int U>
+// Workgroup (entry, K or V, slice of 256 kPieces pieces of the block's heads).
 __device__ __forceinline__ void copy_block(const PageCopyLaunch &a, const Entry e, const int which, const int slice) {
     const int block_bytes = a.src.num_kv_heads * (kBlockElems / 8) * a.bits;
     const char *src = static_cast<const char *>(which ? a.src.v_pages : a.src.k_pages) + (size_t)e.src * block_bytes;
     char *dst = static_cast<char *>(const_cast<void *>(which ? a.dst.v_pages : a.dst.k_pages)) + (size_t)e.dst * block_bytes;
-    copy_pieces<U>(src, dst, slice * 256 * U, block_bytes / 16);
+    copy_pieces(src, dst, slice * 256 * kPieces, block_bytes / 16);
     if (a.scale_words > 0 && slice == 0) {  // of a block: fp8 a word per head, 4 bits 16
         const int n = a.scale_words * a.src.num_kv_heads;
         const uint32_t *s = reinterpret_cast<const uint32_t *>(which ? a.src.v_scale : a.src.k_scale) + (size_t)e.src * n;
@@ -180,13 +179,11 @@ __device__ __forceinline__ void convert_block(const PageCopyLaunch &a, const Ent
 
 __device__ __forceinline__ Entry entry_of(const int32_t *list, int i) { return Entry{list[3 * i], list[3 * i + 1], list[3 * i + 2]}; }
 
-template <int U>
 __global__ __launch_bounds__(256) void page_copy_kernel(PageCopyLaunch a) {
-    copy_block<U>(a, entry_of(a.list, blockIdx.x), blockIdx.y & 1, blockIdx.y >> 1);
+    copy_block(a, entry_of(a.list, blockIdx.x), blockIdx.y & 1, blockIdx.y >> 1);
 }
-template <int U>
 __global__ __launch_bounds__(256) void page_copy_inline_kernel(PageCopyInline a) {
-    copy_block<U>(a, entry_of(a.entries, blockIdx.x), blockIdx.y & 1, blockIdx.y >> 1);
+    copy_block(a, entry_of(a.entries, blockIdx.x), blockIdx.y & 1, blockIdx.y >> 1);
 }
 template <int SRC, int DST>
 __global__ __launch_bounds__(256) void page_convert_kernel(PageCopyLaunch a) {
@@ -226,15 +223,11 @@ hipError_t go(const A &launch, hipStream_t s) {
         a.bits = a.src.dtype == 0 ? 16 : a.src.dtype == 1 ? 8 : a.src.dtype == 2 ? 32 : 4;
         a.scale_words = a.src.dtype == 1 ? 1 : a.src.dtype == kDtypeFp4 ? four::kScaleBytes / 4 : 0;
         const int64_t bytes = (int64_t)a.src.num_kv_heads * (kBlockElems / 8) * a.bits;
-        auto launch_by = [&](auto u) {
-            constexpr int U = decltype(u)::value;
-            const dim3 grid(a.n, 2 * (unsigned)((bytes + 4096 * U - 1) / (4096 * U)));
-            if constexpr (std::is_same_v<A, PageCopyInline>)
-                hipLaunchKernelGGL(page_copy_inline_kernel<U>, grid, dim3(256), 0, s, a);
-            else
-                hipLaunchKernelGGL(page_copy_kernel<U>, grid, dim3(256), 0, s, a);
-        };
-        launch_by(std::integral_constant<int, 4>{});
+        const dim3 grid(a.n, 2 * (unsigned)((bytes + 4096 * kPieces - 1) / (4096 * kPieces)));
+        if constexpr (std::is_same_v<A, PageCopyInline>)
+            hipLaunchKernelGGL(page_copy_inline_kernel, grid, dim3(256), 0, s, a);
+        else
+            hipLaunchKernelGGL(page_copy_kernel, grid, dim3(256), 0, s, a);
         return hipGetLastError();
     }
     switch (a.src.dtype) {

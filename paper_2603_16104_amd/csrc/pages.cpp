@@ -11,20 +11,6 @@
 
 namespace {
 
-bool is_capturing(hipStream_t s) {
-    hipStreamCaptureStatus capture = hipStreamCaptureStatusNone;
-    return hipStreamIsCapturing(s, &capture) == hipSuccess && capture != hipStreamCaptureStatusNone;
-}
-
-// Pages listed from now on are looked up in pool->mark.
-void mark_anew(hkv_pool *pool) {
-    if (pool->mark.empty()) pool->mark.assign(pool->d.num_pages, 0);
-    if (++pool->mark_now == 0) {
-        std::fill(pool->mark.begin(), pool->mark.end(), 0u);
-        pool->mark_now = 1;
-    }
-}
-
 struct PagePair {
     int32_t src, dst, tokens;  // tokens: of the page
 };
@@ -128,7 +114,7 @@ extern "C" int kv_pool_copy_pages(hkv_pool *dst, const int32_t *dst_ids, hkv_poo
         return fail(HKV_ESHAPE, "%s: pages of %d tokens and %d KV heads into pages of %d and %d", who, src->d.page_size, src->d.num_kv_heads, dst->d.page_size,
                     dst->d.num_kv_heads);
     if (dst->d.num_kv_heads > 65535) return fail(HKV_ESHAPE, "%s: %d KV heads (65535 at most)", who, dst->d.num_kv_heads);
-    mark_anew(dst);
+    dst->mark_anew();
     std::vector<PagePair> pairs;
     pairs.reserve(n);
     for (int i = 0; i < n; ++i) {

@@ -79,3 +79,23 @@ def test_sums_of_unlike_products(kind, query, sign):
     check_rows(out, lse, tuple(np.stack([x[i] for x in refs]) for i in range(4)))
     hkv.hkv_decode_plan_destroy(plan)
     pool.close()
+
+
+@pytest.mark.parametrize("kind", list(KINDS))
+@pytest.mark.parametrize("q_by,k_by", [(-106, 110), (110, -115), (-60, -50), (60, 50)])
+def test_far_scales(kind, q_by, k_by):
+    """Queries and keys near the ends of their scales, whose scores are ordinary numbers of 32 bits."""
+    settings, rows = KINDS[kind]
+    n = rows // 8
+    f = Forest([(-1, 150)] + [(0, 5 + 3 * i) for i in range(n)], list(range(1, n + 1)), 16, seed=n)
+    pool = Pool(f.n_pages, 1, seed=n)
+    pool.k_scale += k_by % 256
+    q = queries(n, 8) * 2.0 ** q_by
+    k, v = pool.values()
+    scale = float(np.float32(12 / np.abs(f64(q) @ k.reshape(-1, 128).T).max()))
+    plan = hkv.hkv_decode_plan_create_ex(pool.handle, f.nodes, f.node_pages, f.leaves, 8, shared_chunk=0 if kind == "paths" else 2048, **settings)
+    out, lse = decode(plan, q, scale=scale)
+    refs = [reference(f64(q)[r], f.keys(k, leaf), f.keys(v, leaf), scale) for r, leaf in enumerate(f.leaves)]
+    check_rows(out, lse, tuple(np.stack([x[i] for x in refs]) for i in range(4)))
+    hkv.hkv_decode_plan_destroy(plan)
+    pool.close()
