@@ -92,7 +92,7 @@ enum {
  * dimension-major (d*16 + slot).
  * fp4 pools hold a token in 136 bytes per KV head (bf16 512, fp8 256): bf16 sources, q and out, as bf16 pools.  Attention over one
  * equals attention over a bf16 pool that holds the same values (code * scale is a bf16 number) up to the order of sums, but that decode loses
- * 2^-20 of the largest of 32 neighbouring elements of q (0 .. 31, 32 .. 63, ..) from those below 2^-12 of it.
+ * 2^-20 of the largest of 32 neighbouring elements of q (0 .. 31, 32 .. 63, ..) from those below 2^-12 of it (2^-129 where that is more).
  * Decode plans over fp4 pools run their nodes as items of up to 128 query rows (no tiles), small steps as whole paths; of the planner's settings
  * they know leaf_chunk, shared_chunk, max_rows, pack (1 and 3) and interleave (-1).  Prefill widens the batch's pages into workspace first, as over
  * fp8 pools. */

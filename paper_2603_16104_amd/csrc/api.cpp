@@ -1272,7 +1272,7 @@ static void estimate_paths(hkv_decode_plan &pl, RowsByLeaf &by) {
     const bool fp8 = pl.pool->d.dtype == HKV_FP8_E4M3;
     int xcds = 8;  // a KV head's workgroups lie Hkv apart
     for (int h = Hkv; h % 2 == 0 && xcds > 1; h /= 2) xcds /= 2;
-    const bool fp4 = pl.pool->d.dtype == HKV_FP4_E2M1;  // (11387 timings: 8 % rms; against items by both estimates 1.002 of the better one's time, items always 1.24)
+    const bool fp4 = pl.pool->d.dtype == HKV_FP4_E2M1;  // (of 1500 small steps, profiles/four_bit_path_timings.csv, 1382 run this way, as items they take 1.25 of the time; 38 of them are more than 3 % faster as items, 41 % at most: hundreds of short paths)
     unique *= 2.0 * HKV_HEAD_DIM * Hkv * (fp4 ? 0.53125 : fp8 ? 1 : 2) * xcds;
     const int waves = units <= n_cu ? 8 : 4;
     // in 1000 tokens: the longest path, and what a compute unit takes in beyond it (between the mean and that of whole workgroups)

@@ -11,9 +11,9 @@
 // A lane of a score tile t4 holds tokens 16 g + 4 i + t4 of its query row m: over the four tiles all 16 tokens of block g, which is what its
 // share of P^T is made of, so probabilities stay where they are.  Widened values are exact (two significant bits, a power of two).
 //
-// What bounds it: items of few rows memory (512 sequences of 1024 to 2048 tokens, 8 KV heads: 142 us, 6.0 TB/s), items of many rows their
-// instructions (16 x 8192 tokens under 256 rows of 8 KV heads: 141 us; matrix cores 49 % busy, vector units 53 %); both together, 512 requests on a
-// 70B-shaped layer, 250 us at the 1.9 GHz that the card keeps under them.  Small steps wait for their loads: item, page ids and rows, queries, codes.
+// What bounds it: items of few rows memory (512 sequences of 1024 to 2048 tokens, 8 KV heads: 143 us, 6.0 TB/s), items of many rows their
+// instructions (16 x 8192 tokens under 256 rows of 8 KV heads: 136 us; matrix cores 53 % busy, vector units 47 %); both together, 512 requests on a
+// 70B-shaped layer, 260 us at the 1.9 GHz that the card keeps under them.  Small steps wait for their loads: item, page ids and rows, queries, codes.
 #include <hip/hip_ext.h>
 
 #include <climits>
@@ -78,7 +78,7 @@ struct RowTile {
 
 // 32 dims of a query row as four e2m3 terms (three bits behind the point, at most 7.5, multiples of 1/8): the largest magnitude is brought into [4, 8) by a power of two, and
 // each term is what those in front leave, under scales 2^4, 2^10 and 2^15 below the first one's.  bf16 values down to 2^-12 of the largest of the 32 are exact, of smaller ones
-// 2^-20 of that is lost.  Products of e2m1 and e2m3 are added without loss inside the matrix instruction, and its sums are those of fp32; of products with e4m3 or e5m2 (two terms
+// 2^-20 of that is lost (2^-129 where that is more).  Products of e2m1 and e2m3 are added without loss inside the matrix instruction, and its sums are those of fp32; of products with e4m3 or e5m2 (two terms
 // in the same matrix time) it cuts off what lies below 2^-13 of the largest among eight neighbouring dims: lse off by 1e-3 for rows with an outlier.
 // A row that holds a NaN or an infinity gets a scale that is no number.  sign: -1 for a negative softmax scale.
 __device__ __forceinline__ void split_row(u32x4 (&w)[4], float sign, u32x6 (&q)[kTerms], uint32_t &q_scale) {
@@ -555,7 +555,7 @@ __device__ __forceinline__ void run_shared_tokens(const DecodeLaunch &a, const D
 }
 
 // Small steps: a workgroup of W wavefronts per KV head and leaf (and up to 16 of its rows) walks the whole path and writes the result itself: no items' partials
-// and no second launch (4 requests over 256 + 49 tokens 6.6 us, as items and merge 7.7).  What bounds it is the chain of record, codes and queries, and a
+// and no second launch (4 requests over 256 + 49 tokens 6.6 us, as items and merge 7.8).  What bounds it is the chain of record, codes and queries, and a
 // step's own length.  Blocks that are not full may lie anywhere on the path, at the end of every node; `gap` is how many of a block's last slots are nobody's.
 struct PathStep : Operands {
     int gap;  // of the lane's block of V, which is that of its scores too
@@ -1120,8 +1120,8 @@ __global__ __launch_bounds__(kWaves * 64, 2) void four_decode_kernel(DecodeLaunc
     if (at >= a.n_single) return;
     const DecodeItem it = a.items[at];
     const int rows = it.n_req * G;
-    // Measured on both sides (16 prompts of 2048 tokens, 8 KV heads): 32 rows with tokens shared 24.6 us, with 16 rows a wavefront 27.2; 48 rows
-    // with 16 a wavefront 29.8, with 32 a wavefront, two of them idle beside it, 37.  More than 64 rows only the last form takes.
+    // Measured on both sides (16 prompts of 2048 tokens in items of 1024, 8 KV heads): 32 rows with tokens shared 17.2 us, with 16 rows a wavefront 21.5; 48
+    // rows with 16 a wavefront 22.8, with 32 a wavefront, two of them idle beside it, 26.4.  More than 64 rows only the last form takes.
     if (rows <= 16)
         run_shared_tokens<1>(a, it, lds.s);
     else if (rows <= 32)

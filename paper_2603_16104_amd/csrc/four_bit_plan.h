@@ -32,9 +32,9 @@ struct Load {  // items of one kind
 };
 
 // A step's length: the items' costs over the chip's slots and part of the longest one, that one alone, or the bytes (512 sequences of 1024 to 2048 tokens:
-// 142 us with a wavefront each, 160 with a workgroup each); then the merge of the partials, of
-// which a row has `parts`.  6648 timings of 360 random plans of 8 to 340 us, cut in about 18 ways each: 7 % rms; the way that the estimate prefers takes
-// 1.02 of the best one's time in the mean over 300 others, 1.07 for one plan in ten, 1.21 at most.
+// 143 us with a wavefront each, 160 with a workgroup each); then the merge of the partials, of
+// which a row has `parts`.  Fitted to timings; of 700 random plans of 7 to 400 us (profiles/four_bit_plan_timings.csv) the cut that it prefers takes 1.02 of the time of
+// the best among that one and 14 random cuts in the mean, 1.08 for one plan in ten, 1.34 at most.
 inline double estimate_us(const Load (&load)[5], double bytes, int32_t parts, double partials, int n_cu) {
     double busy = 0, longest = 0;
     for (int k = 0; k < 5; ++k) {
@@ -136,7 +136,7 @@ std::vector<double> lengths(const std::vector<Proto> &items, size_t set, int gro
 // The order in which sets of two kinds go out to `slots` places: set i of the first kind as i, of the second as ~i.  Whenever a place is free, the kind
 // goes on whose remaining time over the places it would have, plus five times a set's, is longer: both share the chip all the while (one is bound by
 // its instructions, the other by memory), and neither is left alone with long sets at the end (512 requests over
-// 16 prompts of 8192 tokens: 239 us; with one set's time 254, with twenty 246, both kinds in even shares 284).  Of those that start at once the first kind's come
+// 16 prompts of 8192 tokens: 260 us; with one set's time 267, with twenty 262).  Of those that start at once the first kind's come
 // first: workgroups go to an XCD's compute units in turn, so each gets one of them before any gets two.
 inline std::vector<int32_t> dispatch_order(const std::array<std::vector<double>, 2> &us, int slots) {
     std::vector<int32_t> order;
